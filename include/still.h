@@ -257,6 +257,81 @@ still_status still_attend_biased_stack(still_ctx* ctx, int32_t n_layers, const v
                                        int64_t S, int32_t H, int32_t d, float scale,
                                        void* const* out, void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * A paged cache (App. B: a compact cache is installed into the slots of a serving engine's pages
+ * and decoding goes on behind it, positions running ahead of the slots by T - t). The keys and
+ * values of a layer live in a pool of pages that sequences own by a table, so that compact
+ * prefixes and what follows them grow in place. still_paged_append fills slots,
+ * still_paged_decode and still_paged_prefill attend over them; the three take the same
+ * still_paged_cache (memory) and still_paged_batch (who owns which slots).
+ *
+ * Slot j of a sequence lies in page table[b][j / page_size], at j mod page_size. */
+typedef struct {
+  void *K, *V;       /* bf16 pools: slot s of page p, KV-head h at p * s_page + s * s_slot +
+                        h * s_head (elements; d contiguous channels). Multiples of 8 elements and
+                        16-byte aligned, so pools may keep slots before heads or heads first. */
+  float* beta;       /* [n_pages][H][page_size] logit bias per slot, or NULL for none. Finite, or
+                        -inf: the slot is masked, whatever its K and V hold. */
+  int64_t s_page, s_slot, s_head;
+  int32_t n_pages;
+  int32_t page_size; /* slots, a power of two, 16 .. 65536 */
+  int32_t n_kv_heads; /* H */
+  int32_t head_dim;  /* d in {64, 128, 256} */
+} still_paged_cache;
+
+/* B sequences and the new tokens of a call: the last of each sequence's slots. Token i of the n_b
+ * new ones of sequence b has slot len[b] - n_b + i and position slot + pos_offset[b]. All arrays
+ * are device memory, read when the call executes (a captured call follows their values).
+ * Lengths below n_b are allowed: tokens whose slot would be negative are not appended and attend
+ * to nothing (an idle place of a batch has len 0). */
+typedef struct {
+  const int32_t* table;  /* [B][s_table], the first table_pages of a row are a sequence's pages */
+  int64_t s_table;
+  int32_t table_pages;
+  int32_t B;
+  const int32_t* len;        /* [B] slots in use, the new tokens included */
+  const int32_t* cu_new;     /* [B + 1] offsets of each sequence's new tokens in the packed rows,
+                                cu_new[B] = n; NULL: one token each, n = B */
+  const int64_t* pos_offset; /* [B], or NULL for 0 (App. B, "Logical vs. physical cache length") */
+} still_paged_batch;
+
+/* Puts n new tokens into their slots, keys rotated to their positions by the base model's RoPE
+ * (half-split pairs, base rope_theta, as it caches them), and rotates their queries on the way.
+ *   k, v    [n][H][d] bf16, token pitches k_stride, v_stride (elements, >= H d)
+ *   q       [n][Hq][d] bf16, token pitch q_stride, or NULL with Hq = 0
+ *   q_out   [n][Hq][d] bf16, contiguous (may be q itself when q_stride = Hq d)
+ *   beta    [n][H] fp32 biases, or NULL: 0 is written where the cache has biases. Refused
+ *           (STILL_ERR_INVALID_ARG) when the cache has none.
+ *   rope_theta  0: nothing is rotated and q must be NULL (the slots of a compact cache are at
+ *           their positions already: Ck, Cv and beta of the compaction calls go in as they are)
+ * Pointers 16-byte aligned, pitches multiples of 8. No two tokens of a call may share a slot.
+ * A table entry outside the pool, a length beyond the table or offsets outside 0 .. n are
+ * recorded (still_get_device_status: STILL_ERR_CUDA, detail code 2); such a token is skipped. */
+still_status still_paged_append(still_ctx* ctx, const still_paged_cache* cache,
+                                const still_paged_batch* batch, int32_t n, const void* k,
+                                int64_t k_stride, const void* v, int64_t v_stride,
+                                const void* q, int64_t q_stride, int32_t Hq, const float* beta,
+                                double rope_theta, void* q_out, void* stream);
+
+/* Attention of the new tokens over every slot up to their own, grouped query heads (query head i
+ * reads KV-head i / (Hq / H)): softmax over scale q K^T + beta applied to V. A token that sees
+ * nothing (no slots, or every bias -inf) gives zeros.
+ *   q    [n][Hq][d] bf16, token pitch q_stride (rotated already)
+ *   out  [n][Hq][d] bf16, contiguous
+ *   scale  0 means 1 / sqrt(d)
+ * still_paged_decode: one token per sequence (cu_new must be NULL, n = B).
+ * still_paged_prefill: any number of tokens per sequence, causal among them. A token's V is
+ * expected finite even where earlier tokens of its call do not see it.
+ * Device-side argument faults are recorded as by still_paged_append; slots of a page outside the
+ * pool count as masked. */
+still_status still_paged_decode(still_ctx* ctx, const still_paged_cache* cache,
+                                const still_paged_batch* batch, const void* q, int64_t q_stride,
+                                int32_t Hq, float scale, void* out, void* stream);
+still_status still_paged_prefill(still_ctx* ctx, const still_paged_cache* cache,
+                                 const still_paged_batch* batch, int32_t n, const void* q,
+                                 int64_t q_stride, int32_t Hq, float scale, void* out,
+                                 void* stream);
+
 /* Compacts layers 0..n_layers-1 (all loaded) over the same positions: the per-layer
  * compactors share nothing at forward time (App. M, "No inter-layer compactor channel"), so
  * this is one stream-ordered launch sequence over the layer stack. K[l], V[l], Ck[l], Cv[l] are device
@@ -461,6 +536,8 @@ typedef enum {
   STILL_K_BETA,         /* beta head: Z_out w_beta, shaped                  */
   STILL_K_DECODE,       /* biased decode attention (chunks + merge)         */
   STILL_K_REPAIR,       /* top-k repair of one-pass cross-attention scores  */
+  STILL_K_PAGED_APPEND, /* new tokens into a paged cache                    */
+  STILL_K_PAGED_ATTEND, /* attention over a paged cache                     */
   STILL_K_COUNT
 } still_kernel_class;
 

@@ -27,6 +27,7 @@
 #include "kernels.cuh"
 #include "ca_flash.cuh"
 #include "keyproj.cuh"
+#include "paged.cuh"
 
 using namespace still;
 
@@ -177,6 +178,9 @@ struct still_ctx {
   bool key_fold = true;  // fold W_K into the queries where the layer allows it
   Profiler prof;
   GemmChoice gemms[STILL_K_COUNT];  // the form last launched per kernel class
+  RopeTurns turns{};                // of still_paged_append, for turns_theta and turns_d
+  double turns_theta = 0;
+  int turns_d = 0;
 };
 
 namespace {
@@ -1716,6 +1720,150 @@ still_status still_attend_biased_stack(still_ctx* ctx, int32_t n_layers, const v
                             scale, out, stream);
 }
 
+}  // extern "C"
+
+namespace {
+
+// Host checks that the calls over a paged cache share; fills the kernels' view of it.
+still_status paged_args(still_ctx* ctx, const still_paged_cache* c, const still_paged_batch* b,
+                        int64_t n, PagedArgs& a) {
+  if (ctx == nullptr || c == nullptr || b == nullptr || c->K == nullptr || c->V == nullptr ||
+      b->table == nullptr || b->len == nullptr)
+    return STILL_ERR_INVALID_ARG;
+  if (c->n_pages < 1 || c->n_kv_heads < 1 || b->B < 1 || b->table_pages < 1 ||
+      b->s_table < b->table_pages || n < 0)
+    return STILL_ERR_INVALID_ARG;
+  const int d = c->head_dim;
+  if ((d != 64 && d != 128 && d != 256) || c->page_size < kMinPage || c->page_size > 65536 ||
+      (c->page_size & (c->page_size - 1)) != 0 || c->n_kv_heads > 1024)
+    return STILL_ERR_UNSUPPORTED;
+  if (c->s_page < 1 || c->s_slot < 1 || c->s_head < 1) return STILL_ERR_INVALID_ARG;
+  const uintptr_t al = reinterpret_cast<uintptr_t>(c->K) | reinterpret_cast<uintptr_t>(c->V);
+  const uintptr_t a4 = reinterpret_cast<uintptr_t>(c->beta) |
+                       reinterpret_cast<uintptr_t>(b->table) |
+                       reinterpret_cast<uintptr_t>(b->len) | reinterpret_cast<uintptr_t>(b->cu_new);
+  if ((al & 15) || (a4 & 3) || (reinterpret_cast<uintptr_t>(b->pos_offset) & 7) ||
+      ((c->s_page | c->s_slot | c->s_head) & 7))
+    return STILL_ERR_ALIGNMENT;
+  a.K = static_cast<bf16*>(c->K);
+  a.V = static_cast<bf16*>(c->V);
+  a.beta = c->beta;
+  a.s_page = c->s_page;
+  a.s_slot = c->s_slot;
+  a.s_head = c->s_head;
+  a.n_pages = c->n_pages;
+  a.page_shift = 0;
+  while ((1 << a.page_shift) < c->page_size) ++a.page_shift;
+  a.H = c->n_kv_heads;
+  a.d = d;
+  a.table = b->table;
+  a.s_table = b->s_table;
+  a.table_pages = b->table_pages;
+  a.B = b->B;
+  a.len = b->len;
+  a.cu_new = b->cu_new;
+  a.pos_offset = b->pos_offset;
+  a.n = (int32_t)n;
+  a.err = ctx->err;
+  return STILL_OK;
+}
+
+bool bad_rows(const void* p, int64_t pitch) {  // 16-byte aligned rows
+  return (reinterpret_cast<uintptr_t>(p) & 15) != 0 || (pitch & 7) != 0;
+}
+
+still_status paged_attend(still_ctx* ctx, const still_paged_cache* cache,
+                          const still_paged_batch* batch, int64_t n, const void* q,
+                          int64_t q_stride, int32_t Hq, float scale, void* out, void* stream) {
+  PagedArgs a;
+  TRY(paged_args(ctx, cache, batch, n, a));
+  if (Hq < a.H || Hq % a.H != 0 || q_stride < (int64_t)Hq * a.d || !(scale >= 0.f) ||
+      !std::isfinite(scale))
+    return STILL_ERR_INVALID_ARG;
+  if (Hq / a.H > 1024 || n * (Hq / a.H) > INT32_MAX / 2) return STILL_ERR_UNSUPPORTED;
+  if (n == 0) return STILL_OK;
+  if (q == nullptr || out == nullptr) return STILL_ERR_INVALID_ARG;
+  if (bad_rows(q, q_stride) || bad_rows(out, 0)) return STILL_ERR_ALIGNMENT;
+  PagedQuery p;
+  p.q = static_cast<const bf16*>(q);
+  p.s_q = q_stride;
+  p.out = static_cast<bf16*>(out);
+  p.Hq = Hq;
+  p.scale = scale > 0.f ? scale : 1.f / std::sqrt((float)a.d);
+  CK(cudaSetDevice(ctx->device));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  KLAUNCH(STILL_K_PAGED_ATTEND, launch_paged_rows(a, p, s));
+  return STILL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+still_status still_paged_append(still_ctx* ctx, const still_paged_cache* cache,
+                                const still_paged_batch* batch, int32_t n, const void* k,
+                                int64_t k_stride, const void* v, int64_t v_stride,
+                                const void* q, int64_t q_stride, int32_t Hq, const float* beta,
+                                double rope_theta, void* q_out, void* stream) {
+  PagedArgs a;
+  TRY(paged_args(ctx, cache, batch, n, a));
+  const int64_t row = (int64_t)a.H * a.d;
+  if (k_stride < row || v_stride < row || (a.cu_new == nullptr && n != a.B) ||
+      (beta != nullptr && a.beta == nullptr) || !std::isfinite(rope_theta) || rope_theta < 0 ||
+      Hq < 0 || (Hq > 0 && (rope_theta == 0 || q_stride < (int64_t)Hq * a.d)))
+    return STILL_ERR_INVALID_ARG;
+  if (Hq > 65536) return STILL_ERR_UNSUPPORTED;
+  if (n == 0) return STILL_OK;
+  if (k == nullptr || v == nullptr || (q == nullptr) != (Hq == 0) ||
+      (q != nullptr &&
+       (q_out == nullptr || (q == q_out && q_stride != (int64_t)Hq * a.d))))
+    return STILL_ERR_INVALID_ARG;
+  if (bad_rows(k, k_stride) || bad_rows(v, v_stride) ||
+      (q != nullptr && (bad_rows(q, q_stride) || bad_rows(q_out, 0))) ||
+      (reinterpret_cast<uintptr_t>(beta) & 3))
+    return STILL_ERR_ALIGNMENT;
+  PagedAppend p;
+  p.q = static_cast<const bf16*>(q);
+  p.k = static_cast<const bf16*>(k);
+  p.v = static_cast<const bf16*>(v);
+  p.s_q = q_stride;
+  p.s_k = k_stride;
+  p.s_v = v_stride;
+  p.beta = beta;
+  p.q_out = static_cast<bf16*>(q_out);
+  p.Hq = Hq;
+  p.rotate = rope_theta > 0;
+  if (p.rotate && (ctx->turns_theta != rope_theta || ctx->turns_d != a.d)) {
+    for (int m = 0; m < a.d / 2; ++m) {
+      // w_m / 2 pi in 64 fractional bits; w_0 = 1 and theta < 1 only raises the others
+      const double turn = std::pow(rope_theta, -2.0 * m / a.d) / 6.283185307179586476925;
+      ctx->turns.turns[m] = (unsigned long long)std::ldexp(turn - std::floor(turn), 64);
+    }
+    ctx->turns_theta = rope_theta;
+    ctx->turns_d = a.d;
+  }
+  CK(cudaSetDevice(ctx->device));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  KLAUNCH(STILL_K_PAGED_APPEND, launch_paged_append(a, p, ctx->turns, ctx->kernels.num_sms, s));
+  return STILL_OK;
+}
+
+still_status still_paged_decode(still_ctx* ctx, const still_paged_cache* cache,
+                                const still_paged_batch* batch, const void* q, int64_t q_stride,
+                                int32_t Hq, float scale, void* out, void* stream) {
+  if (batch != nullptr && batch->cu_new != nullptr) return STILL_ERR_INVALID_ARG;
+  return paged_attend(ctx, cache, batch, batch != nullptr ? batch->B : 0, q, q_stride, Hq, scale,
+                      out, stream);
+}
+
+still_status still_paged_prefill(still_ctx* ctx, const still_paged_cache* cache,
+                                 const still_paged_batch* batch, int32_t n, const void* q,
+                                 int64_t q_stride, int32_t Hq, float scale, void* out,
+                                 void* stream) {
+  if (batch != nullptr && batch->cu_new == nullptr && n != batch->B) return STILL_ERR_INVALID_ARG;
+  return paged_attend(ctx, cache, batch, n, q, q_stride, Hq, scale, out, stream);
+}
+
 still_status still_compact_layer_noalloc(still_ctx* ctx, int32_t layer, const void* K,
                                          const void* V, const int64_t strides_kv[3],
                                          const still_pos_segment* h_segments,
@@ -2073,7 +2221,8 @@ const char* still_kernel_class_name(int32_t cls) {
   static const char* names[STILL_K_COUNT] = {
       "strip", "rope_tables", "keyproj", "q_rope", "scores", "softmax", "px", "px_split",
       "vo", "rmsnorm", "sa_proj", "sa_v", "sa_scores", "sa_softmax", "sa_pv", "sa_out",
-      "ffn1", "ffn2", "heads", "norms", "load", "ca_fused", "beta", "decode", "repair"};
+      "ffn1", "ffn2", "heads", "norms", "load", "ca_fused", "beta", "decode", "repair",
+      "paged_append", "paged_attend"};
   return cls >= 0 && cls < STILL_K_COUNT ? names[cls] : "unknown";
 }
 

@@ -31,7 +31,8 @@ EXPORTS = [
     "still_selftest_wait_timeout", "still_compact_stack_masked", "still_lookahead_pass_info",
     "still_lookahead_totals", "still_lookahead_compact_layer", "still_lookahead_compact_stack",
     "still_set_beta_head", "still_compact_layer_beta", "still_attend_biased", "still_set_key_fold",
-    "still_attend_biased_stack",
+    "still_attend_biased_stack", "still_paged_append", "still_paged_decode",
+    "still_paged_prefill",
 ]
 
 NOALLOC_SCRATCH_MIB = 64  # STILL_NOALLOC_SCRATCH_MIB in include/still.h
@@ -39,7 +40,7 @@ NOALLOC_SCRATCH_MIB = 64  # STILL_NOALLOC_SCRATCH_MIB in include/still.h
 KERNEL_CLASSES = ["strip", "rope_tables", "keyproj", "q_rope", "scores", "softmax", "px",
                   "px_split", "vo", "rmsnorm", "sa_proj", "sa_v", "sa_scores", "sa_softmax",
                   "sa_pv", "sa_out", "ffn1", "ffn2", "heads", "norms", "load", "ca_fused",
-                  "beta", "decode", "repair"]
+                  "beta", "decode", "repair", "paged_append", "paged_attend"]
 
 
 class StillError(RuntimeError):
@@ -91,6 +92,21 @@ class LookaheadPass(ctypes.Structure):
 
 class PosSegment(ctypes.Structure):
     _fields_ = [("start", ctypes.c_double), ("step", ctypes.c_double), ("count", ctypes.c_int64)]
+
+
+class _PagedCache(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("beta", ctypes.c_void_p),
+                ("s_page", ctypes.c_int64), ("s_slot", ctypes.c_int64),
+                ("s_head", ctypes.c_int64), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
+class _PagedBatch(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("s_table", ctypes.c_int64),
+                ("table_pages", ctypes.c_int32), ("B", ctypes.c_int32),
+                ("len", ctypes.c_void_p), ("cu_new", ctypes.c_void_p),
+                ("pos_offset", ctypes.c_void_p)]
 
 
 _lib = None
@@ -161,6 +177,11 @@ def lib():
                                            ctypes.POINTER(P), I64, ctypes.POINTER(P),
                                            ctypes.POINTER(P), I64, I32, I32, ctypes.c_float,
                                            ctypes.POINTER(P), P], ctypes.c_int),
+            "still_paged_append": ([P, P, P, I32, P, I64, P, I64, P, I64, I32, P, D, P, P],
+                                   ctypes.c_int),
+            "still_paged_decode": ([P, P, P, P, I64, I32, ctypes.c_float, P, P], ctypes.c_int),
+            "still_paged_prefill": ([P, P, P, I32, P, I64, I32, ctypes.c_float, P, P],
+                                    ctypes.c_int),
             "still_lookahead_pass_info": ([I64, I64, I32, ctypes.POINTER(LookaheadPass)],
                                           ctypes.c_int),
             "still_lookahead_totals": ([I64, I64, I32, PI64, PI64], ctypes.c_int),
@@ -380,6 +401,103 @@ def still_attend_biased_stack(ctx, q, Ck, Cv, beta, Kfix, Vfix, out, scale=0.0, 
                                            arr(Cv, t > 0), betas, t, arr(Kfix, S > 0),
                                            arr(Vfix, S > 0), S, H, d, scale, arr(out),
                                            _stream(stream)), "still_attend_biased_stack")
+
+
+class PagedCache:
+    """A layer's pages (still_paged_cache): K, V [n_pages, page_size, H, d] bf16 CUDA tensors of
+    equal strides with contiguous channels (any order in memory, such as a transposed
+    [n_pages, H, page_size, d] pool), beta [n_pages, H, page_size] fp32 contiguous or None. Made
+    once; it keeps its tensors alive."""
+
+    def __init__(self, K, V, beta=None):
+        import torch
+        assert K.dtype == V.dtype == torch.bfloat16 and K.dim() == 4 and K.shape == V.shape
+        assert K.stride() == V.stride() and K.stride(3) == 1, "K and V must share strides"
+        n, page, H, d = K.shape
+        if beta is not None:
+            assert beta.dtype == torch.float32 and tuple(beta.shape) == (n, H, page)
+            assert beta.is_contiguous()
+        self.tensors = (K, V, beta)
+        self.struct = _PagedCache(K.data_ptr(), V.data_ptr(),
+                                  None if beta is None else beta.data_ptr(), K.stride(0),
+                                  K.stride(1), K.stride(2), n, page, H, d)
+        self.ref = ctypes.byref(self.struct)
+
+
+class PagedBatch:
+    """Who owns which slots (still_paged_batch): table [B, pages] int32, lens [B] int32 slots in
+    use with the call's new tokens, cu_new [B + 1] int32 or None (one new token each), pos_offset
+    [B] int64 or None (CUDA tensors, read when a call executes). It keeps its tensors alive."""
+
+    def __init__(self, table, lens, cu_new=None, pos_offset=None):
+        import torch
+        assert table.dtype == lens.dtype == torch.int32 and table.stride(1) == 1
+        assert lens.is_contiguous() and lens.shape[0] == table.shape[0]
+        assert cu_new is None or (cu_new.dtype == torch.int32 and cu_new.is_contiguous()
+                                  and cu_new.shape[0] == lens.shape[0] + 1)
+        assert pos_offset is None or (pos_offset.dtype == torch.int64
+                                      and pos_offset.is_contiguous()
+                                      and pos_offset.shape[0] == lens.shape[0])
+        self.tensors = (table, lens, cu_new, pos_offset)
+        self.struct = _PagedBatch(table.data_ptr(), max(table.stride(0), table.shape[1]),
+                                  table.shape[1], table.shape[0], lens.data_ptr(),
+                                  None if cu_new is None else cu_new.data_ptr(),
+                                  None if pos_offset is None else pos_offset.data_ptr())
+        self.ref = ctypes.byref(self.struct)
+
+
+def _rows(x, H, d):
+    """Data pointer and token pitch of [n, H, d] bf16 rows whose heads are contiguous."""
+    import torch
+    sn, sh, sd = x.stride()
+    assert x.dtype == torch.bfloat16 and x.shape[1:] == (H, d), "bf16 [n, H, d] rows"
+    assert sd == 1 and (sh == d or H == 1), "contiguous heads"
+    return x.data_ptr(), sn if x.shape[0] > 1 else H * d
+
+
+def still_paged_append(ctx, cache, batch, k, v, q=None, q_out=None, beta=None, rope_theta=0.0,
+                       stream=None):
+    """k, v [n, H, d] and q [n, Hq, d] bf16 (heads contiguous, any token pitch: slices of a fused
+    projection), q_out [n, Hq, d] contiguous; beta [n, H] fp32 or None."""
+    H, d = cache.struct.n_kv_heads, cache.struct.head_dim
+    kp, ks = _rows(k, H, d)
+    vp, vs = _rows(v, H, d)
+    n = k.shape[0]
+    qp, qs, Hq, qo = None, 0, 0, None
+    assert v.shape[0] == n
+    if beta is not None:
+        import torch
+        assert beta.dtype == torch.float32 and tuple(beta.shape) == (n, H)
+        assert beta.is_contiguous()
+    if q is not None:
+        Hq = q.shape[1]
+        qp, qs = _rows(q, Hq, d)
+        qo = q_out.data_ptr()
+        assert q_out.shape == q.shape and q.shape[0] == n and q_out.is_contiguous()
+        assert q_out.dtype == q.dtype
+    _check(lib().still_paged_append(ctx, cache.ref, batch.ref, n, kp, ks, vp, vs, qp, qs, Hq,
+                                    None if beta is None else beta.data_ptr(), rope_theta, qo,
+                                    _stream(stream)), "still_paged_append")
+
+
+def still_paged_decode(ctx, cache, batch, q, out, scale=0.0, stream=None):
+    """q [B, Hq, d] (heads contiguous, any token pitch), out [B, Hq, d] contiguous, bf16."""
+    n, Hq, d = q.shape
+    qp, qs = _rows(q, Hq, cache.struct.head_dim)
+    assert out.shape == q.shape and out.is_contiguous() and out.dtype == q.dtype
+    assert n == batch.struct.B
+    _check(lib().still_paged_decode(ctx, cache.ref, batch.ref, qp, qs, Hq, scale, out.data_ptr(),
+                                    _stream(stream)), "still_paged_decode")
+
+
+def still_paged_prefill(ctx, cache, batch, q, out, scale=0.0, stream=None):
+    """q [n, Hq, d] packed new tokens (heads contiguous, any token pitch), out [n, Hq, d]
+    contiguous, bf16."""
+    n, Hq, d = q.shape
+    qp, qs = _rows(q, Hq, cache.struct.head_dim)
+    assert out.shape == q.shape and out.is_contiguous() and out.dtype == q.dtype
+    _check(lib().still_paged_prefill(ctx, cache.ref, batch.ref, n, qp, qs, Hq, scale,
+                                     out.data_ptr(), _stream(stream)), "still_paged_prefill")
 
 
 def still_lookahead_pass_info(k: int, c: int, t: int) -> dict:
