@@ -52,6 +52,10 @@ struct PagedQuery {
   int32_t Hq = 0;
   float scale = 0.f;
 };
-cudaError_t launch_paged_rows(const PagedArgs& a, const PagedQuery& q, cudaStream_t s);
+// ws: paged_rows_workspace bytes; arrived: kPagedJoins counters, zero between calls.
+constexpr int kPagedJoins = 8192;
+size_t paged_rows_workspace(const PagedArgs& a, int Hq, int num_sms);
+cudaError_t launch_paged_rows(const PagedArgs& a, const PagedQuery& q, void* ws, int* arrived,
+                              int num_sms, cudaStream_t s);
 
 }  // namespace still

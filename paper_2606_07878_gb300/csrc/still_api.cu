@@ -170,6 +170,7 @@ struct still_ctx {
   int device = 0;
   KernelTable kernels;  // of this device
   int* err = nullptr;  // device error record [4]
+  int* arrived = nullptr;  // [kPagedJoins] of the attention over a paged cache
   std::vector<LayerW> layers;
   void* ws = nullptr;
   size_t ws_bytes = 0;
@@ -1486,7 +1487,11 @@ still_status still_create(int device, still_ctx** out) {
   int sms = 0;
   if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess ||
       cudaMalloc(&c->err, 4 * sizeof(int)) != cudaSuccess ||
-      cudaMemset(c->err, 0, 4 * sizeof(int)) != cudaSuccess) {
+      cudaMemset(c->err, 0, 4 * sizeof(int)) != cudaSuccess ||
+      cudaMalloc(&c->arrived, kPagedJoins * sizeof(int)) != cudaSuccess ||
+      cudaMemset(c->arrived, 0, kPagedJoins * sizeof(int)) != cudaSuccess) {
+    cudaFree(c->err);
+    cudaFree(c->arrived);
     delete c;
     return STILL_ERR_CUDA;
   }
@@ -1502,6 +1507,7 @@ still_status still_destroy(still_ctx* ctx) {
   for (auto& L : ctx->layers) free_layer(L);
   if (ctx->ws) cudaFree(ctx->ws);
   if (ctx->err) cudaFree(ctx->err);
+  if (ctx->arrived) cudaFree(ctx->arrived);
   delete ctx;
   return STILL_OK;
 }
@@ -1792,7 +1798,9 @@ still_status paged_attend(still_ctx* ctx, const still_paged_cache* cache,
   p.scale = scale > 0.f ? scale : 1.f / std::sqrt((float)a.d);
   CK(cudaSetDevice(ctx->device));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  KLAUNCH(STILL_K_PAGED_ATTEND, launch_paged_rows(a, p, s));
+  const int nsm = ctx->kernels.num_sms;
+  TRY(ensure_ws(ctx, paged_rows_workspace(a, Hq, nsm)));
+  KLAUNCH(STILL_K_PAGED_ATTEND, launch_paged_rows(a, p, ctx->ws, ctx->arrived, nsm, s));
   return STILL_OK;
 }
 
