@@ -1,48 +1,12 @@
 // The paged key-value cache: append (with the base model's RoPE) and attention of few rows.
-#include "paged.cuh"
-
 #include <algorithm>
 
 #include "launch.cuh"
-#include "ptx.cuh"
+#include "paged_dev.cuh"
 
 namespace still {
 
 namespace {
-
-// First new token, number of them and slots of sequence b, whatever the arrays hold: an offset
-// outside [0, n] or a length beyond the table is cut and recorded.
-struct Seq {
-  int first, count, len;
-};
-STILL_DEV Seq paged_seq(const PagedArgs& a, int b) {
-  Seq s;
-  int c0 = b, c1 = b + 1;
-  if (a.cu_new != nullptr) {
-    c0 = a.cu_new[b];
-    c1 = a.cu_new[b + 1];
-  }
-  const int cap = (int)min((int64_t)a.table_pages << a.page_shift, (int64_t)0x7fffff00);
-  s.len = a.len[b];
-  if (c0 < 0 || c1 < c0 || c1 > a.n || s.len < 0 || s.len > cap) {
-    dev_set_error(a.err, DEV_BAD_ARG, 600);
-    c0 = min(max(c0, 0), a.n);
-    c1 = min(max(c1, c0), a.n);
-    s.len = min(max(s.len, 0), cap);
-  }
-  s.first = c0;
-  s.count = c1 - c0;
-  return s;
-}
-
-// The page that holds slot j of the sequence whose pages `table` lists; -1 (and a record) when it
-// names none.
-STILL_DEV int paged_page(const PagedArgs& a, const int32_t* table, int j) {
-  const int p = table[j >> a.page_shift];
-  if ((unsigned)p < (unsigned)a.n_pages) return p;
-  dev_set_error(a.err, DEV_BAD_ARG, 601);
-  return -1;
-}
 
 // ----------------------------------------------------------------- append
 //
@@ -156,7 +120,6 @@ __global__ void __launch_bounds__(kAppendThreads)
 // that the kernel itself adds up. A set that lies in one range is written by its CTA; the parts of
 // another meet in the workspace, and the CTA that brings the last one joins them in their order, so
 // that the result does not depend on who that is. No CTA waits for another.
-constexpr float kLog2e = 1.44269504f;
 constexpr int kRowWarps = 4;
 constexpr int kRowThreads = 32 * kRowWarps;
 constexpr int kUnit = 16 * kRowWarps;  // slots
@@ -176,7 +139,6 @@ STILL_DEV uint32_t transpose8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
-STILL_DEV uint32_t bf16x2_bits(__nv_bfloat162 x) { return *reinterpret_cast<uint32_t*>(&x); }
 // Read-once data: past L1, first to leave L2.
 STILL_DEV uint4 ld_once(const __nv_bfloat16* p) {
   return __ldcs(reinterpret_cast<const uint4*>(p));

@@ -1,0 +1,872 @@
+// Attention of many new tokens over a paged cache, on the tensor cores (tcgen05).
+//
+// For a KV-head the rows (token i, query head h g + r) see slots j <= past + i:
+//   S = q K^T            128 x 128 tiles, operands from shared memory (TMA, one box per page and 64
+//                        channels), fp32 in TMEM
+//   P = e^(scale S + beta - m)   one row per thread, running m and sum; bf16, written over S
+//   O += P V             P from TMEM, V as the loaded rows (channels are its contiguous dimension)
+// An item is a sequence, KV-head and kTiles tiles of floor(128 / g) tokens x g heads, so that the
+// heads of a group share every K and V tile. For d <= 128 two tiles (256 rows) take turns: the
+// softmax of one lies under the products of the other. 256 channels leave TMEM for one tile (S
+// twice, O once): its two warpgroups take half of S's columns each, and the S of the next slots is
+// formed meanwhile.
+//
+// Order of the tensor pipe, i counting S tiles (kTiles = 2: both tiles of the same slots in turn):
+// S_0, S_1, PV_0, S_2, PV_1, S_3, ... PV_i waits for P_i alone; S_(i+2) overwrites P_i behind it.
+// The running maximum moves (and O is rescaled) only when a tile raises it by more than 2^8.
+//
+// Slots that do not count are zeroed in shared memory before their products (a weight of 0 times
+// a stale NaN would be NaN): those past the sequence's end, and those with a bias of -inf.
+//
+// CTA = 10 warps: 0 TMA producer, 1 MMA issuer and TMEM allocation, 2..9 softmax and output.
+// Every wait is bounded.
+#include <algorithm>
+
+#include "gemm_host.cuh"
+#include "paged_dev.cuh"
+
+namespace still {
+
+namespace {
+
+constexpr int kPfThreads = 320;
+constexpr int kPfKeys = 128;        // slots of a tile
+constexpr float kPfMoveLog2 = 8.f;  // P <= 2^8 needs no more of bf16's range
+constexpr int kPfGroups = 256;      // of sequences, for finding an item's
+
+struct PrefillParams {
+  PagedArgs a;
+  PagedQuery q;
+  int32_t tile_tokens = 0;  // floor(128 / g)
+  int32_t nsplit = 1;       // equal ranges of an item's slots
+  float* part_o = nullptr;  // [nsplit][n * Hq][d], when nsplit > 1
+  float2* part_ml = nullptr;  // [nsplit][n * Hq] (m, l), m in the kernel's units of a logit
+};
+
+template <int D, bool kBias>
+struct PfShape {
+  static constexpr int kTiles = D <= 128 ? 2 : 1;
+  static constexpr int kChan = D < 128 ? D : 128;   // channels of a ring slot
+  static constexpr int kHalves = D / kChan;          // ring slots of a K or V tile
+  static constexpr int kSlotBytes = kPfKeys * kChan * 2;
+  static constexpr int kChunkBytes = kPfKeys * 128;  // 64 channels of 128 rows
+  static constexpr int kQBytes = kTiles * (D / 64) * kChunkBytes;
+  static constexpr int kSlots = D == 64 ? 8 : D == 256 || kBias ? 4 : 5;
+  static constexpr int kCols = kTiles == 2 ? 128 : 64;  // S columns per softmax thread
+  static constexpr int kOCols = kTiles == 2 ? D : D / 2;  // O columns per softmax thread
+  static constexpr int kRing = kQBytes;
+  static constexpr int kBiasAt = kRing + kSlots * kSlotBytes;  // [8 warps][kCols]
+  static constexpr int kXchAt = kBiasAt + (kBias ? 8 * kCols * 4 : 0);  // [2][2][128], one tile only
+  static constexpr int kBarAt = kXchAt + (kTiles == 1 ? 2048 : 0);
+  static constexpr int kBytes = kBarAt + 256 + 1024;
+  static_assert(kBytes <= 232448, "shared memory budget");
+};
+
+// D[tmem] (+)= A[tmem, 128 lanes x 16] * B[smem, MN-major], kind::f16.
+STILL_DEV void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
+                      uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Shared-memory descriptor of an MN-major operand, 128-byte swizzle: rows (k) of 64 contiguous
+// elements, 8 rows an atom of 1024 bytes, atoms along k 1024 bytes apart, the next 64 elements
+// `chunk` bytes further.
+STILL_DEV uint64_t sdesc_mn_sw128(uint32_t saddr, int chunk) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(chunk >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+constexpr uint32_t kIdescBMn = 1u << 16;  // B is MN-major
+
+STILL_DEV void tma_load_3d(void* dst, const CUtensorMap* m, uint64_t* bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+STILL_DEV void tma_load_4d(void* dst, const CUtensorMap* m, uint64_t* bar, int x, int y, int z,
+                           int w) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
+      : "memory");
+}
+// 32 lanes x 32 columns of 32 bits from registers; complete after tmem_wait_st.
+STILL_DEV void tmem_st32_issue(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(
+          taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+      "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+      "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
+      "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+STILL_DEV void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+struct PfItem {
+  int b, h, qt, split;
+  int first, count, past, len;
+  int k0, k1;  // tiles of slots [k0, k1) of this split
+};
+
+// The numbers of items before each group of sequences, in shared memory.
+struct PfPlan {
+  int before[kPfGroups + 1];
+  int per;  // sequences of a group
+};
+
+STILL_DEV int pf_tiles(const Seq& s, int tokens) { return (s.count + tokens - 1) / tokens; }
+
+// Item x of the plan: sequences in order, the last tokens (which see most slots) first, then
+// KV-heads, then splits.
+STILL_DEV PfItem pf_item(const PrefillParams& f, const PfPlan& plan, int tokens, int x) {
+  PfItem r;
+  r.split = x % f.nsplit;
+  x /= f.nsplit;
+  int lo = 0, hi = kPfGroups;  // the last group that begins at or before x
+  while (lo + 1 < hi) {
+    const int mid = (lo + hi) / 2;
+    if (plan.before[mid] <= x)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  x -= plan.before[lo];
+  int b = lo * plan.per;
+  Seq s = paged_seq(f.a, b);
+  int n = pf_tiles(s, tokens);
+  while (x >= n * f.a.H) {
+    x -= n * f.a.H;
+    s = paged_seq(f.a, ++b);
+    n = pf_tiles(s, tokens);
+  }
+  r.b = b;
+  r.h = x % f.a.H;
+  r.qt = n - 1 - x / f.a.H;
+  r.first = s.first;
+  r.count = s.count;
+  r.len = s.len;
+  r.past = s.len - s.count;
+  const int most = r.past + min(s.count, (r.qt + 1) * tokens);
+  const int kt = most > 0 ? (most + kPfKeys - 1) / kPfKeys : 0;
+  r.k0 = (int)((int64_t)kt * r.split / f.nsplit);
+  r.k1 = (int)((int64_t)kt * (r.split + 1) / f.nsplit);
+  return r;
+}
+
+// The k-th item of CTA c of n: there and back, so that long items meet short ones.
+STILL_DEV int pf_turn(int k, int c, int n) { return k * n + ((k & 1) ? n - 1 - c : c); }
+
+// kC columns' biases of a warp, one tile of slots ahead: lane i holds those of columns
+// [kC / 32 i, + kC / 32).
+template <int kC>
+struct PfBias {
+  static constexpr int kPer = kC / 32;
+  float v[kPer];
+  STILL_DEV void load(const PagedArgs& a, const PfItem& it, int slot0, int lane) {
+    const int j = slot0 + kPer * lane;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) v[e] = 0.f;
+    if (j >= it.len) return;
+    const int pg = paged_page(a, a.table + (int64_t)it.b * a.s_table, j);
+    const int in = j & ((1 << a.page_shift) - 1);
+    const float* at = a.beta + ((((int64_t)max(pg, 0) * a.H + it.h) << a.page_shift) + in);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+      v[e] = pg < 0 ? -INFINITY : j + e < it.len ? at[e] : 0.f;
+  }
+};
+
+template <int D, bool kBias>
+__global__ void __launch_bounds__(kPfThreads, 1)
+    paged_prefill_kernel(const __grid_constant__ CUtensorMap tm_q,
+                         const __grid_constant__ CUtensorMap tm_k,
+                         const __grid_constant__ CUtensorMap tm_v,
+                         const __grid_constant__ PrefillParams f) {
+  using S = PfShape<D, kBias>;
+  constexpr int kTiles = S::kTiles, kSlots = S::kSlots, kHalves = S::kHalves;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ PfPlan plan;
+  __shared__ int warp_items[kPfThreads / 32];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kBarAt);  // ring slot loaded
+  uint64_t* empty = full + kSlots;   // ring slot consumed
+  uint64_t* qfull = empty + kSlots;  // the item's q loaded
+  uint64_t* qfree = qfull + 1;       // its last S complete
+  uint64_t* sfull = qfree + 1;       // [2] S_i complete
+  uint64_t* pfull = sfull + 2;       // [2] P_i written (and O rescaled where needed)
+  uint64_t* pvdone = pfull + 2;      // [2] O holds P_i V
+  uint64_t* ofree = pvdone + 2;      // O drained at the end of an item
+  uint64_t* xb = ofree + 1;          // [4] row-value exchange per lane quarter
+  uint64_t* drain = xb + 4;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  static_assert((2 * kSlots + 14) * 8 + 8 <= 256, "barriers");
+
+  const PagedArgs& a = f.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = f.q.Hq / a.H;
+  const int tokens = f.tile_tokens * kTiles;  // of an item
+  constexpr int kSCols = 128;                 // TMEM: S (P) at 128 i, O behind both
+  constexpr int kOAt = 2 * kSCols;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 1);
+    }
+    mbar_init(qfull, 1);
+    mbar_init(qfree, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sfull[i], 1);
+      mbar_init(&pfull[i], kTiles == 2 ? 4 : 8);
+      mbar_init(&pvdone[i], 1);
+    }
+    mbar_init(ofree, 8);
+    for (int i = 0; i < 4; ++i) mbar_init(&xb[i], 2);
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+    tma_prefetch_desc(&tm_q);
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
+  }
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  {  // the plan: thread t adds up group t
+    const int per = (a.B + kPfGroups - 1) / kPfGroups;
+    int mine = 0;
+    if (threadIdx.x < kPfGroups)
+      for (int b = threadIdx.x * per; b < min(a.B, ((int)threadIdx.x + 1) * per); ++b)
+        mine += pf_tiles(paged_seq(a, b), tokens) * a.H;
+    int sum = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += x;
+    }
+    if (lane == 31) warp_items[warp] = sum;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) sum += warp_items[w];
+    if (threadIdx.x < kPfGroups) plan.before[threadIdx.x + 1] = sum;
+    if (threadIdx.x == 0) {
+      plan.before[0] = 0;
+      plan.per = per;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const int items = plan.before[kPfGroups] * f.nsplit;
+  const int cta = blockIdx.x, nct = gridDim.x;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer
+    int slot = 0, n_items = 0;
+    uint32_t phase = 0;
+    uint32_t armed = 0, armed_par = 0;
+    bool q_armed = false, bad = false;
+    const int rows = min(1 << a.page_shift, kPfKeys);  // of a box
+    auto fail = [&](int where) {
+      if (lane == 0) {
+        dev_set_error(a.err, DEV_WAIT_TIMEOUT, where);
+        *abort_flag = 1;
+      }
+      bad = true;
+    };
+    // One half (kChan channels) of tile kt of K or V into the next ring slot.
+    auto load = [&](const CUtensorMap* tm, const PfItem& it, int kt, int half) {
+      if (!__all_sync(0xffffffffu, mbar_wait(&empty[slot], phase ^ 1))) return fail(610);
+      if (lane == 0) mbar_arrive_expect_tx(&full[slot], S::kSlotBytes);
+      armed |= 1u << slot;
+      armed_par = (armed_par & ~(1u << slot)) | (phase << slot);
+      __syncwarp();
+      const int boxes = kPfKeys / rows * (S::kChan / 64);
+      for (int x = lane; x < boxes; x += 32) {
+        const int c = x % (S::kChan / 64), r = x / (S::kChan / 64) * rows;
+        const int j = kt * kPfKeys + r;
+        // a box outside the pool (past the last page, or of an entry that names none) is zeros
+        int pg = j < it.len ? paged_page(a, a.table + (int64_t)it.b * a.s_table, j) : -1;
+        if (pg < 0) pg = a.n_pages;
+        tma_load_4d(smem + S::kRing + slot * S::kSlotBytes + c * S::kChunkBytes + r * 128, tm,
+                    &full[slot], half * S::kChan + c * 64, j & ((1 << a.page_shift) - 1), it.h, pg);
+      }
+      if (++slot == kSlots) {
+        slot = 0;
+        phase ^= 1;
+      }
+    };
+    auto load_tile = [&](const CUtensorMap* tm, const PfItem& it, int kt) {
+      for (int half = 0; half < kHalves && !bad; ++half) load(tm, it, kt, half);
+    };
+    for (int k = 0;; ++k) {
+      const int x = pf_turn(k, cta, nct);
+      if (k * nct >= items || bad || warp_flag(abort_flag)) break;
+      if (x >= items) continue;
+      const PfItem it = pf_item(f, plan, tokens, x);
+      if (it.k0 == it.k1) continue;
+      if (n_items > 0 && !__all_sync(0xffffffffu, mbar_wait(qfree, (n_items - 1) & 1))) {
+        fail(611);
+        break;
+      }
+      if (lane == 0) {
+        const uint32_t box = (uint32_t)f.tile_tokens * g * 128;
+        mbar_arrive_expect_tx(qfull, box * kTiles * (D / 64));
+        for (int t = 0; t < kTiles; ++t)
+          for (int c = 0; c < D / 64; ++c)
+            tma_load_3d(smem + (t * (D / 64) + c) * S::kChunkBytes, &tm_q, qfull, c * 64, it.h * g,
+                        it.first + it.qt * tokens + t * f.tile_tokens);
+      }
+      q_armed = true;
+      ++n_items;
+      // in the order in which the issuer takes them
+      constexpr int kAhead = kTiles == 2 ? 1 : 2;
+      for (int kt = it.k0; kt < min(it.k0 + kAhead, it.k1) && !bad; ++kt) load_tile(&tm_k, it, kt);
+      for (int kt = it.k0; kt < it.k1 && !bad; ++kt) {
+        load_tile(&tm_v, it, kt);
+        if (kt + kAhead < it.k1 && !bad) load_tile(&tm_k, it, kt + kAhead);
+      }
+    }
+    // The CTA may leave only when nothing is on its way into its shared memory: the last arrivals
+    // of the issuer's commits, or copies that nobody waited for.
+    for (int i = 0; i < kSlots && !bad && !warp_flag(abort_flag); ++i) {
+      if (!__all_sync(0xffffffffu, mbar_wait(&empty[slot], phase ^ 1))) fail(612);
+      if (++slot == kSlots) {
+        slot = 0;
+        phase ^= 1;
+      }
+    }
+    if (n_items > 0 && !bad && !warp_flag(abort_flag) &&
+        !__all_sync(0xffffffffu, mbar_wait(qfree, (n_items - 1) & 1)))
+      fail(613);
+    if (bad || warp_flag(abort_flag)) {
+      for (int s = 0; s < kSlots; ++s)
+        if (armed & (1u << s)) (void)mbar_wait(&full[s], (armed_par >> s) & 1);
+      if (q_armed) (void)mbar_wait(qfull, (n_items - 1) & 1);
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer
+    constexpr uint32_t idesc_s = idesc_f16(128, kPfKeys, 1);
+    constexpr uint32_t idesc_o = idesc_f16(128, S::kChan, 1) | kIdescBMn;
+    int slot = 0;
+    uint32_t phase = 0;
+    uint32_t n_i = 0, n_items = 0;  // S tiles and items so far
+    bool bad = false, issued = false;
+    PfBias<128> ahead;   // biases of the next tile of slots
+    // per lane: which of its 4 slots do not count, of the tile looked at last and the one before
+    uint32_t dead[2] = {0, 0};
+    auto fail = [&](int where) {
+      if (lane == 0) {
+        dev_set_error(a.err, DEV_WAIT_TIMEOUT, where);
+        *abort_flag = 1;
+      }
+      bad = true;
+    };
+    auto wait = [&](uint64_t* bar, uint32_t parity, int where) {
+      if (!__all_sync(0xffffffffu, mbar_wait(bar, parity))) fail(where);
+    };
+    // Zeroes the rows of a ring slot whose slots do not count.
+    auto scrub = [&](int s, uint32_t nib) {
+      if (!__any_sync(0xffffffffu, nib != 0)) return;
+      uint8_t* base = smem + S::kRing + s * S::kSlotBytes;
+      for (int r = 0; r < kPfKeys; r += 4) {
+        const uint32_t n4 = __shfl_sync(0xffffffffu, nib, r / 4);
+        if ((n4 >> (lane >> 3)) & 1)
+#pragma unroll
+          for (int c = 0; c < S::kChan / 64; ++c)
+            *reinterpret_cast<uint4*>(base + c * S::kChunkBytes + (r + (lane >> 3)) * 128 +
+                                      (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+    };
+    auto next_slot = [&]() {
+      if (++slot == kSlots) {
+        slot = 0;
+        phase ^= 1;
+      }
+    };
+    for (int k = 0;; ++k) {
+      const int x = pf_turn(k, cta, nct);
+      if (k * nct >= items || bad || warp_flag(abort_flag)) break;
+      if (x >= items) continue;
+      const PfItem it = pf_item(f, plan, tokens, x);
+      if (it.k0 == it.k1) continue;
+      const int n_k = it.k1 - it.k0;
+      if constexpr (kBias) ahead.load(a, it, it.k0 * kPfKeys, lane);
+      // which slots of tile kt count; tiles come in order
+      auto look = [&](int kt) {
+        uint32_t nib = 0;
+        const int j = kt * kPfKeys + 4 * lane;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (j + e >= it.len) nib |= 1u << e;
+          if (kBias && ahead.v[e] == -INFINITY) nib |= 1u << e;
+        }
+        if (kBias && kt + 1 < it.k1) ahead.load(a, it, (kt + 1) * kPfKeys, lane);
+        dead[1] = dead[0];
+        dead[0] = nib;
+      };
+      wait(qfull, n_items & 1, 620);
+      if (bad) break;
+      // S of tile t into buffer t, channels of one ring slot
+      auto mma_s = [&](int buf, int t, int half, int s) {
+        tc_fence_after();
+        if (lane == 0) {
+          const uint32_t q = smem_u32(smem + (t * (D / 64) + half * (S::kChan / 64)) * S::kChunkBytes);
+          const uint32_t kk = smem_u32(smem + S::kRing + s * S::kSlotBytes);
+#pragma unroll
+          for (int c = 0; c < S::kChan / 64; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              tc_mma_f16(tmem_base + buf * kSCols, sdesc_k_sw128(q + c * S::kChunkBytes) + 2 * e,
+                         sdesc_k_sw128(kk + c * S::kChunkBytes) + 2 * e, idesc_s,
+                         half + c + e > 0);
+        }
+        issued = true;
+      };
+      auto mma_o = [&](int buf, int t, int half, int s, bool first) {
+        tc_fence_after();
+        if (lane == 0) {
+          const uint32_t vv = smem_u32(smem + S::kRing + s * S::kSlotBytes);
+          const uint64_t vd = sdesc_mn_sw128(vv, S::kChunkBytes);
+#pragma unroll
+          for (int e = 0; e < kPfKeys / 16; ++e)
+            mma_ts(tmem_base + kOAt + t * D + half * S::kChan, tmem_base + buf * kSCols + 8 * e,
+                   vd + e * (2048 >> 4), idesc_o, !first || e > 0);
+        }
+      };
+      auto commit = [&](uint64_t* bar) {
+        if (lane == 0) tc_commit(bar);
+      };
+      if constexpr (kTiles == 2) {
+        int ks = 0, vs = 0;
+        auto take_k = [&](int kt) {  // K tile kt in a ring slot, ready for products
+          look(kt);
+          wait(&full[slot], phase, 621);
+          if (kBias) scrub(slot, dead[0]);
+          ks = slot;
+          next_slot();
+        };
+        take_k(it.k0);
+        if (bad) break;
+        for (int t = 0; t < 2; ++t) {
+          mma_s(t, t, 0, ks);
+          commit(&sfull[t]);
+        }
+        commit(&empty[ks]);
+        if (n_k == 1) commit(qfree);
+        for (int kt = it.k0; kt < it.k1 && !bad; ++kt) {
+          const bool more = kt + 1 < it.k1;
+          for (int t = 0; t < 2 && !bad; ++t, ++n_i) {
+            wait(&pfull[t], (n_i >> 1) & 1, 622);
+            if (kt == it.k0 && t == 0 && n_items > 0) wait(ofree, (n_items - 1) & 1, 623);
+            if (t == 0) {
+              wait(&full[slot], phase, 624);
+              scrub(slot, dead[0]);
+              vs = slot;
+              next_slot();
+            }
+            if (bad) break;
+            mma_o(t, t, 0, vs, kt == it.k0);
+            if (t == 1) commit(&empty[vs]);
+            commit(&pvdone[t]);
+            if (!more) continue;
+            if (t == 0) take_k(kt + 1);
+            if (bad) break;
+            mma_s(t, t, 0, ks);
+            commit(&sfull[t]);
+            if (t == 1) {
+              commit(&empty[ks]);
+              if (kt + 2 == it.k1) commit(qfree);
+            }
+          }
+        }
+      } else {
+        auto make_s = [&](int kt, uint32_t i) {
+          look(kt);
+          for (int half = 0; half < kHalves && !bad; ++half) {
+            wait(&full[slot], phase, 625);
+            if (bad) break;
+            if (kBias) scrub(slot, dead[0]);
+            mma_s(i & 1, 0, half, slot);
+            commit(&empty[slot]);
+            next_slot();
+          }
+          if (bad) return;
+          commit(&sfull[i & 1]);
+          if (kt + 1 == it.k1) commit(qfree);
+        };
+        make_s(it.k0, n_i);
+        if (n_k > 1 && !bad) make_s(it.k0 + 1, n_i + 1);
+        for (int kt = it.k0; kt < it.k1 && !bad; ++kt, ++n_i) {
+          wait(&pfull[n_i & 1], (n_i >> 1) & 1, 626);
+          if (kt == it.k0 && n_items > 0) wait(ofree, (n_items - 1) & 1, 627);
+          // tile kt + 1 was looked at last, if there is one
+          const uint32_t nib = kt + 1 < it.k1 ? dead[1] : dead[0];
+          for (int half = 0; half < kHalves && !bad; ++half) {
+            wait(&full[slot], phase, 628);
+            if (bad) break;
+            scrub(slot, nib);
+            mma_o(n_i & 1, 0, half, slot, kt == it.k0);
+            commit(&empty[slot]);
+            next_slot();
+          }
+          if (bad) break;
+          commit(&pvdone[n_i & 1]);
+          if (kt + 2 < it.k1) make_s(kt + 2, n_i + 2);
+        }
+      }
+      ++n_items;
+    }
+    if ((bad || warp_flag(abort_flag)) && issued) {
+      if (lane == 0) tc_commit(drain);
+      (void)mbar_wait(drain, 0);
+    }
+  } else {
+    // ------------------------------------------------------------ softmax and output
+    constexpr int kCols = S::kCols, kOCols = S::kOCols;
+    const int sw = warp - 2;
+    const int quarter = warp & 3;  // TMEM lanes [32 quarter, + 32)
+    const int wg = sw >> 2;        // its tile, or its half of the columns
+    const int row = quarter * 32 + lane;
+    const int col0 = kTiles == 2 ? 0 : kCols * wg;
+    const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16);
+    const uint32_t o_at = lanes + kOAt + (kTiles == 2 ? wg * D : wg * kOCols);
+    float* kw = reinterpret_cast<float*>(smem + S::kBiasAt) + sw * kCols;
+    float* xch = reinterpret_cast<float*>(smem + S::kXchAt);  // [2][2][128]
+    // exponents: with biases logits are natural (a bias of the lowest float must stay finite),
+    // without them S itself is kept and the scale joins the factor
+    const float to_log2 = kBias ? kLog2e : f.q.scale * kLog2e;
+    uint32_t n_i = kTiles == 2 ? wg : 0, n_x = 0;
+    bool bad = false;
+    auto wait_all = [&](uint64_t* bar, uint32_t parity, int where) -> bool {
+      const bool ok = __all_sync(0xffffffffu, mbar_wait(bar, parity));
+      if (!ok) {
+        if (lane == 0) {
+          dev_set_error(a.err, DEV_WAIT_TIMEOUT, where);
+          *abort_flag = 1;
+        }
+        bad = true;
+      }
+      return ok;
+    };
+    // One value per row for the other warp of this lane quarter; returns its value.
+    auto exchange = [&](float mine, int where) -> float {
+      float* at = xch + (n_x & 1) * 256;
+      at[wg * 128 + row] = mine;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&xb[quarter]);
+      const bool ok = wait_all(&xb[quarter], n_x & 1, where);
+      ++n_x;
+      return ok ? at[(1 - wg) * 128 + row] : mine;
+    };
+    for (int k = 0;; ++k) {
+      const int x = pf_turn(k, cta, nct);
+      if (k * nct >= items || bad || warp_flag(abort_flag)) break;
+      if (x >= items) continue;
+      const PfItem it = pf_item(f, plan, tokens, x);
+      const int tl = it.qt * tokens + (kTiles == 2 ? wg * f.tile_tokens : 0) + row / g;
+      const bool valid = row < f.tile_tokens * g && tl < it.count;
+      const int see = valid ? max(0, it.past + tl + 1) : 0;
+      const int64_t orow = (int64_t)(it.first + tl) * f.q.Hq + it.h * g + row % g;
+      float m_run = -INFINITY, l_run = 0.f;
+      PfBias<kCols> beta;
+      if (kBias && it.k0 < it.k1) beta.load(a, it, it.k0 * kPfKeys + col0, lane);
+      uint32_t last = 0;  // the S tile before
+      for (int kt = it.k0; kt < it.k1; ++kt, n_i += kTiles) {
+        const int buf = n_i & 1;
+        const uint32_t s_at = lanes + buf * kSCols;
+        if (!wait_all(&sfull[buf], (n_i >> 1) & 1, 630)) break;
+        tc_fence_after();
+        uint32_t v[kCols];
+#pragma unroll
+        for (int c = 0; c < kCols / 32; ++c) tmem_ld32_issue(s_at + col0 + 32 * c, v + 32 * c);
+        if constexpr (kBias) {
+#pragma unroll
+          for (int e = 0; e < beta.kPer; ++e) kw[beta.kPer * lane + e] = beta.v[e];
+          if (kt + 1 < it.k1) beta.load(a, it, (kt + 1) * kPfKeys + col0, lane);
+          __syncwarp();
+        }
+        tmem_wait_ld();
+#pragma unroll
+        for (int c = 0; c < kCols / 32; ++c) tmem_landed(v + 32 * c);
+        if constexpr (kBias) {
+          const uint64_t sc = pack2(f.q.scale, f.q.scale);
+#pragma unroll
+          for (int c = 0; c < kCols; c += 4) {
+            const float4 b4 = *reinterpret_cast<const float4*>(kw + c);
+            float u0, u1;
+            unpack2(fma2(pack2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), sc,
+                         pack2(b4.x, b4.y)), u0, u1);
+            v[c] = __float_as_uint(u0);
+            v[c + 1] = __float_as_uint(u1);
+            unpack2(fma2(pack2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), sc,
+                         pack2(b4.z, b4.w)), u0, u1);
+            v[c + 2] = __float_as_uint(u0);
+            v[c + 3] = __float_as_uint(u1);
+          }
+          __syncwarp();  // kw is written again
+        }
+        const int seen = see - kt * kPfKeys - col0;  // columns that this row sees
+        if (__any_sync(0xffffffffu, seen < kCols)) {
+#pragma unroll
+          for (int c = 0; c < kCols; ++c)
+            if (c >= seen) v[c] = 0xff800000u;
+        }
+        float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < kCols; c += 4) {
+          m0 = max3(m0, __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
+          m1 = max3(m1, __uint_as_float(v[c + 2]), __uint_as_float(v[c + 3]));
+        }
+        float mx = fmaxf(m0, m1);
+        if constexpr (kTiles == 1) {
+          mx = fmaxf(mx, exchange(mx, 631));
+          if (bad) break;
+        }
+        bool move = false;
+        float fac = 1.f;
+        if (m_run == -INFINITY) {
+          m_run = mx;  // O and l are 0 so far
+        } else if ((mx - m_run) * to_log2 > kPfMoveLog2) {
+          fac = ex2_ftz((m_run - mx) * to_log2);
+          m_run = mx;
+          l_run *= fac;
+          move = true;
+        }
+        // nothing seen yet: every weight is 2^-inf
+        const float by = m_run == -INFINITY ? 0.f : m_run;
+        const uint64_t by2 = pack2(-by, -by), k2 = pack2(to_log2, to_log2);
+        uint64_t s0 = 0ull, s1 = 0ull;
+#pragma unroll
+        for (int c = 0; c < kCols; c += 2) {
+          float u0, u1;
+          unpack2(mul2(add2(pack2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), by2), k2), u0,
+                  u1);
+          const uint32_t w = bf16x2_bits(__floats2bfloat162_rn(ex2_ftz(u0), ex2_ftz(u1)));
+          v[c / 2] = w;
+          if (c & 2)  // the weights as rounded
+            s1 = add2(s1, bf16_pair(w));
+          else
+            s0 = add2(s0, bf16_pair(w));
+        }
+        float l0, l1;
+        unpack2(add2(s0, s1), l0, l1);
+        l_run += l0 + l1;
+        // warp-collective: a warp rescales when any of its rows needs it
+        if (__any_sync(0xffffffffu, move) && kt > it.k0) {
+          if (!wait_all(&pvdone[last & 1], (last >> 1) & 1, 632)) break;
+          tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < kOCols; c += 32) {
+            float o[32];
+            tmem_ld32(o_at + c, o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] *= fac;
+            tmem_st32(o_at + c, o);
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < kCols / 64; ++c)
+          tmem_st32_issue(s_at + col0 / 2 + 32 * c, v + 32 * c);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&pfull[buf]);
+        last = n_i;
+      }
+      if (bad) break;
+      // ---- the item's rows
+      float l = l_run;
+      if (it.k0 < it.k1) {
+        if constexpr (kTiles == 1) {
+          l += exchange(l_run, 633);
+          if (bad) break;
+        }
+        if (!wait_all(&pvdone[last & 1], (last >> 1) & 1, 634)) break;
+        tc_fence_after();
+      }
+      const int oc = kTiles == 2 ? 0 : wg * kOCols;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll 1
+      for (int c = 0; c < kOCols; c += 32) {
+        float o[32];
+        if (it.k0 < it.k1) {
+          tmem_ld32(o_at + c, o);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0.f;
+        }
+        if (!valid) continue;
+        if (f.nsplit > 1) {
+          float4* dst = reinterpret_cast<float4*>(
+              f.part_o + ((int64_t)it.split * a.n * f.q.Hq + orow) * D + oc + c);
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)
+            dst[e / 4] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        } else {
+          uint4* dst = reinterpret_cast<uint4*>(f.q.out + orow * D + oc + c);
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              w[i] = bf16x2_bits(__floats2bfloat162_rn(o[e + 2 * i] * inv, o[e + 2 * i + 1] * inv));
+            dst[e / 8] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+      if (f.nsplit > 1 && valid && (kTiles == 2 || wg == 0))
+        f.part_ml[(int64_t)it.split * a.n * f.q.Hq + orow] = make_float2(m_run, l);
+      if (it.k0 < it.k1) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(ofree);
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, 512);
+  }
+}
+
+// The splits' parts of a row, in their order; a warp per row.
+__global__ void __launch_bounds__(256)
+    paged_join_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml,
+                      int64_t rows, int nsplit, int d, float to_log2,
+                      __nv_bfloat16* __restrict__ out) {
+  griddep_wait();
+  const int64_t row = blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (row >= rows) return;
+  float M = -INFINITY;
+  for (int s = 0; s < nsplit; ++s) M = fmaxf(M, part_ml[s * rows + row].x);
+  for (int c = 2 * lane; c < d; c += 64) {
+    float L = 0.f;
+    float2 O = make_float2(0.f, 0.f);
+#pragma unroll 4
+    for (int s = 0; s < nsplit; ++s) {
+      const float2 ml = part_ml[s * rows + row];
+      const float2 o = *reinterpret_cast<const float2*>(part_o + (s * rows + row) * d + c);
+      const float w = ml.x == M ? 1.f : exp2f((ml.x - M) * to_log2);
+      L += w * ml.y;
+      O.x += w * o.x;
+      O.y += w * o.y;
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    *reinterpret_cast<__nv_bfloat162*>(out + row * d + c) =
+        __floats2bfloat162_rn(O.x * inv, O.y * inv);
+  }
+}
+
+// dims {channels, slots, KV-heads, pages}; boxes of 64 channels of the slots of a page
+bool pool_tmap(CUtensorMap* m, const PagedArgs& a, const void* ptr) {
+  auto enc = tensor_map_encoder();
+  if (enc == nullptr) return false;
+  const cuuint64_t page = (cuuint64_t)1 << a.page_shift;
+  cuuint64_t dims[4] = {(cuuint64_t)a.d, page, (cuuint64_t)a.H, (cuuint64_t)a.n_pages};
+  cuuint64_t strides[3] = {(cuuint64_t)a.s_slot * 2, (cuuint64_t)a.s_head * 2,
+                           (cuuint64_t)a.s_page * 2};
+  cuuint32_t box[4] = {64, (cuuint32_t)std::min<cuuint64_t>(page, kPfKeys), 1, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box,
+             estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool query_tmap(CUtensorMap* m, const PagedArgs& a, const PagedQuery& q, int tokens) {
+  auto enc = tensor_map_encoder();
+  if (enc == nullptr) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)a.d, (cuuint64_t)q.Hq, (cuuint64_t)a.n};
+  cuuint64_t strides[2] = {(cuuint64_t)a.d * 2, (cuuint64_t)q.s_q * 2};
+  cuuint32_t box[3] = {64, (cuuint32_t)(q.Hq / a.H), (cuuint32_t)tokens};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16*>(q.q), dims,
+             strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, bool kBias>
+cudaError_t launch_prefill(const PagedArgs& a, const PagedQuery& q, void* ws, int nsplit,
+                           const KernelTable& dev, cudaStream_t s) {
+  using S = PfShape<D, kBias>;
+  using Id = KernelId<paged_prefill_kernel<D, kBias>, kPfThreads, S::kBytes>;
+  if (dev.of<Id>().status != cudaSuccess) return dev.of<Id>().status;
+  PrefillParams f;
+  f.a = a;
+  f.q = q;
+  f.tile_tokens = 128 / (q.Hq / a.H);
+  f.nsplit = nsplit;
+  const int64_t rows = (int64_t)a.n * q.Hq;
+  f.part_o = static_cast<float*>(ws);
+  f.part_ml = reinterpret_cast<float2*>(f.part_o + (nsplit > 1 ? nsplit * rows * a.d : 0));
+  CUtensorMap tq, tk, tv;
+  if (!query_tmap(&tq, a, q, f.tile_tokens) || !pool_tmap(&tk, a, a.K) || !pool_tmap(&tv, a, a.V))
+    return cudaErrorInvalidValue;
+  paged_prefill_kernel<D, kBias><<<dev.num_sms, kPfThreads, S::kBytes, s>>>(tq, tk, tv, f);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess || nsplit == 1) return e;
+  return launch_chained(paged_join_kernel, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, s, 1,
+                        f.part_o, f.part_ml, rows, nsplit, a.d, (kBias ? 1.f : q.scale) * kLog2e,
+                        q.out);
+}
+
+}  // namespace
+
+bool paged_prefill_fits(const PagedArgs& a, int Hq) { return Hq / a.H <= 128; }
+
+int paged_prefill_splits(const PagedArgs& a, int Hq, int num_sms) {
+  const int tokens = 128 / (Hq / a.H) * (a.d <= 128 ? 2 : 1);
+  // items, exact for one sequence and at most
+  const int64_t items = a.H * ((int64_t)a.n / tokens + (a.B > 1 ? a.B : a.n % tokens != 0));
+  const int64_t tiles = (((int64_t)a.table_pages << a.page_shift) + kPfKeys - 1) / kPfKeys;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({num_sms / std::max<int64_t>(1, items),
+                                                      tiles / 2, 32}));
+}
+
+size_t paged_prefill_workspace(const PagedArgs& a, int Hq, int nsplit) {
+  return nsplit > 1 ? (size_t)nsplit * a.n * Hq * (a.d * 4 + 8) : 0;
+}
+
+cudaError_t launch_paged_prefill(const PagedArgs& a, const PagedQuery& q, void* ws, int nsplit,
+                                 const KernelTable& dev, cudaStream_t s) {
+  const bool bias = a.beta != nullptr;
+  switch (a.d) {
+    case 64:
+      return bias ? launch_prefill<64, true>(a, q, ws, nsplit, dev, s)
+                  : launch_prefill<64, false>(a, q, ws, nsplit, dev, s);
+    case 128:
+      return bias ? launch_prefill<128, true>(a, q, ws, nsplit, dev, s)
+                  : launch_prefill<128, false>(a, q, ws, nsplit, dev, s);
+    case 256:
+      return bias ? launch_prefill<256, true>(a, q, ws, nsplit, dev, s)
+                  : launch_prefill<256, false>(a, q, ws, nsplit, dev, s);
+  }
+  return cudaErrorInvalidValue;
+}
+
+}  // namespace still

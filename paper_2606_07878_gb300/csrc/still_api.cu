@@ -1799,6 +1799,15 @@ still_status paged_attend(still_ctx* ctx, const still_paged_cache* cache,
   CK(cudaSetDevice(ctx->device));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const int nsm = ctx->kernels.num_sms;
+  // more than a block of 16 rows per sequence: tiles on the tensor cores
+  if (n * (Hq / a.H) > 16 * (int64_t)a.B && a.cu_new != nullptr && paged_prefill_fits(a, Hq)) {
+    const int nsplit = paged_prefill_splits(a, Hq, nsm);
+    TRY(ensure_ws(ctx, paged_prefill_workspace(a, Hq, nsplit)));
+    KLAUNCH(STILL_K_PAGED_ATTEND,
+            launch_paged_prefill(a, p, ctx->ws, nsplit, ctx->kernels, s));
+    ctx->prof.launches[STILL_K_PAGED_ATTEND] += nsplit > 1;  // the join
+    return STILL_OK;
+  }
   TRY(ensure_ws(ctx, paged_rows_workspace(a, Hq, nsm)));
   KLAUNCH(STILL_K_PAGED_ATTEND, launch_paged_rows(a, p, ctx->ws, ctx->arrived, nsm, s));
   return STILL_OK;
