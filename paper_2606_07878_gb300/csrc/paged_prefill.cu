@@ -18,9 +18,10 @@
 // Slots that do not count are zeroed in shared memory before their products (a weight of 0 times
 // a stale NaN would be NaN): those past the sequence's end, and those with a bias of -inf.
 //
-// CTA = 10 warps: 0 TMA producer, 1 MMA issuer and TMEM allocation, 2..9 softmax and output.
-// Every wait is bounded.
+// CTA = 12 warps: 0 TMA producer, 1 MMA issuer and TMEM allocation, 4..11 softmax and output, which
+// take over registers of the first four (128 x 104 + 256 x 200 = 384 x 168). Every wait is bounded.
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm_host.cuh"
 #include "paged_dev.cuh"
@@ -29,7 +30,8 @@ namespace still {
 
 namespace {
 
-constexpr int kPfThreads = 320;
+constexpr int kPfThreads = 384;
+constexpr int kPfFewRegs = 104, kPfManyRegs = 200;
 constexpr int kPfKeys = 128;        // slots of a tile
 constexpr float kPfMoveLog2 = 8.f;  // P <= 2^8 needs no more of bf16's range
 constexpr int kPfGroups = 256;      // of sequences, for finding an item's
@@ -114,6 +116,14 @@ STILL_DEV void tmem_st32_issue(uint32_t taddr, const uint32_t* r) {
       "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
       "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
+}
+template <int kRegs>
+STILL_DEV void fewer_regs() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs));
+}
+template <int kRegs>
+STILL_DEV void more_regs() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs));
 }
 STILL_DEV void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -280,6 +290,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
+    fewer_regs<kPfFewRegs>();
     int slot = 0, n_items = 0;
     uint32_t phase = 0;
     uint32_t armed = 0, armed_par = 0;
@@ -364,6 +375,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer
+    fewer_regs<kPfFewRegs>();
     constexpr uint32_t idesc_s = idesc_f16(128, kPfKeys, 1);
     constexpr uint32_t idesc_o = idesc_f16(128, S::kChan, 1) | kIdescBMn;
     int slot = 0;
@@ -541,10 +553,11 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       if (lane == 0) tc_commit(drain);
       (void)mbar_wait(drain, 0);
     }
-  } else {
+  } else if (warp >= 4) {
     // ------------------------------------------------------------ softmax and output
+    more_regs<kPfManyRegs>();
     constexpr int kCols = S::kCols, kOCols = S::kOCols;
-    const int sw = warp - 2;
+    const int sw = warp - 4;
     const int quarter = warp & 3;  // TMEM lanes [32 quarter, + 32)
     const int wg = sw >> 2;        // its tile, or its half of the columns
     const int row = quarter * 32 + lane;
@@ -592,10 +605,13 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       PfBias<kCols> beta;
       if (kBias && it.k0 < it.k1) beta.load(a, it, it.k0 * kPfKeys + col0, lane);
       uint32_t last = 0;  // the S tile before
-      for (int kt = it.k0; kt < it.k1; ++kt, n_i += kTiles) {
+      // One tile of slots; kMask: some row of the warp does not see all of its columns. (A branch
+      // around the selects alone costs 500 bytes of spilled registers.)
+      auto tile = [&](auto mask, int kt) {
+        constexpr bool kMask = decltype(mask)::value;
         const int buf = n_i & 1;
         const uint32_t s_at = lanes + buf * kSCols;
-        if (!wait_all(&sfull[buf], (n_i >> 1) & 1, 630)) break;
+        if (!wait_all(&sfull[buf], (n_i >> 1) & 1, 630)) return;
         tc_fence_after();
         uint32_t v[kCols];
 #pragma unroll
@@ -626,11 +642,10 @@ __global__ void __launch_bounds__(kPfThreads, 1)
           }
           __syncwarp();  // kw is written again
         }
-        const int seen = see - kt * kPfKeys - col0;  // columns that this row sees
-        if (__any_sync(0xffffffffu, seen < kCols)) {
+        if constexpr (kMask) {
+          const int seen = see - kt * kPfKeys - col0;  // columns that this row sees
 #pragma unroll
-          for (int c = 0; c < kCols; ++c)
-            if (c >= seen) v[c] = 0xff800000u;
+          for (int c = 0; c < kCols; ++c) v[c] = c < seen ? v[c] : 0xff800000u;
         }
         float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll
@@ -641,7 +656,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         float mx = fmaxf(m0, m1);
         if constexpr (kTiles == 1) {
           mx = fmaxf(mx, exchange(mx, 631));
-          if (bad) break;
+          if (bad) return;
         }
         bool move = false;
         float fac = 1.f;
@@ -655,13 +670,14 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         }
         // nothing seen yet: every weight is 2^-inf
         const float by = m_run == -INFINITY ? 0.f : m_run;
-        const uint64_t by2 = pack2(-by, -by), k2 = pack2(to_log2, to_log2);
+        const float shift = kBias ? -by : -by * to_log2;
+        const uint64_t by2 = pack2(shift, shift), k2 = pack2(to_log2, to_log2);
         uint64_t s0 = 0ull, s1 = 0ull;
 #pragma unroll
         for (int c = 0; c < kCols; c += 2) {
           float u0, u1;
-          unpack2(mul2(add2(pack2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), by2), k2), u0,
-                  u1);
+          const uint64_t x = pack2(__uint_as_float(v[c]), __uint_as_float(v[c + 1]));
+          unpack2(kBias ? mul2(add2(x, by2), k2) : fma2(x, k2, by2), u0, u1);
           const uint32_t w = bf16x2_bits(__floats2bfloat162_rn(ex2_ftz(u0), ex2_ftz(u1)));
           v[c / 2] = w;
           if (c & 2)  // the weights as rounded
@@ -674,7 +690,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         l_run += l0 + l1;
         // warp-collective: a warp rescales when any of its rows needs it
         if (__any_sync(0xffffffffu, move) && kt > it.k0) {
-          if (!wait_all(&pvdone[last & 1], (last >> 1) & 1, 632)) break;
+          if (!wait_all(&pvdone[last & 1], (last >> 1) & 1, 632)) return;
           tc_fence_after();
 #pragma unroll 1
           for (int c = 0; c < kOCols; c += 32) {
@@ -693,6 +709,12 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(&pfull[buf]);
         last = n_i;
+      };
+      for (int kt = it.k0; kt < it.k1 && !bad; ++kt, n_i += kTiles) {
+        if (__any_sync(0xffffffffu, see - kt * kPfKeys - col0 < kCols))
+          tile(std::true_type{}, kt);
+        else
+          tile(std::false_type{}, kt);
       }
       if (bad) break;
       // ---- the item's rows
@@ -743,6 +765,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         if (lane == 0) mbar_arrive(ofree);
       }
     }
+  } else {
+    fewer_regs<kPfFewRegs>();
   }
   tc_fence_before();
   __syncthreads();

@@ -94,22 +94,20 @@ def attention64(p, q, new, scale=None):
     for b, n in enumerate(new):
         L = p.lens[b]
         k, v = p.rows(p.K, b).double(), p.rows(p.V, b).double()
-        for i in range(n):
-            see = min(L, max(0, L - n + i + 1))
-            for h in range(p.H):
-                bias = p.rows(p.beta, b)[:see, h].double() if p.beta is not None else None
-                keep = torch.ones(see, dtype=torch.bool, device=DEV)
-                if bias is not None:
-                    keep = bias != -math.inf
-                if not keep.any():
-                    continue
-                x = q[at + i, h * g:(h + 1) * g].double() @ k[:see, h][keep].T
-                x = x * (scale or 1 / math.sqrt(d))
-                if bias is not None:
-                    x = x + bias[keep]
-                w = torch.softmax(x, -1)
-                out[at + i, h * g:(h + 1) * g] = w @ v[:see, h][keep]
-                size[at + i, h * g:(h + 1) * g] = w @ v[:see, h][keep].abs()
+        see = torch.arange(L - n, L, device=DEV) + 1  # slots that each new token sees
+        late = torch.arange(L, device=DEV) >= see[:, None]
+        for h in range(p.H if n and L else 0):
+            bias = p.rows(p.beta, b)[:, h].double() if p.beta is not None else torch.zeros(
+                L, dtype=torch.float64, device=DEV)
+            hidden = late | (bias == -math.inf)
+            kh = torch.where((bias == -math.inf)[:, None], 0.0, k[:, h])
+            vh = torch.where((bias == -math.inf)[:, None], 0.0, v[:, h])
+            x = torch.einsum("nid,jd->nij", q[at:at + n, h * g:(h + 1) * g].double(), kh)
+            x = (x * (scale or 1 / math.sqrt(d)) + bias).masked_fill(hidden[:, None], -math.inf)
+            w = torch.softmax(x, -1)
+            w = torch.where(hidden.all(-1)[:, None, None], 0.0, w)
+            out[at:at + n, h * g:(h + 1) * g] = w @ vh
+            size[at:at + n, h * g:(h + 1) * g] = w @ vh.abs()
         at += n
     return out, size
 
@@ -160,6 +158,16 @@ def test_decode_matches_64_bits(ctx, d, H, Hq, page, lens, beta, heads_first):
     (256, 1, 2, 16, [129, 65], [0, 31], True, False),
     (256, 2, 10, 32, [30], [99], False, True),
     (128, 1, 4, 16, [3, 70], [2000, 1500], True, False),
+    # several items per CTA, slots split over CTAs, every table of pages
+    (128, 8, 32, 64, [700, 513, 1], [900, 3, 128], False, False),
+    (128, 8, 24, 32, [600, 1, 999], [0, 77, 1500], True, True),
+    (128, 1, 4, 64, [40], [9000], False, False),
+    (128, 1, 4, 256, [64], [9000], True, True),
+    (64, 8, 8, 16, [1500, 900], [0, 700], False, True),
+    (64, 1, 48, 128, [31, 5], [3000, 0], True, False),
+    (256, 8, 16, 16, [700, 90, 350], [0, 1000, 64], False, False),
+    (256, 2, 4, 64, [100], [5000], True, False),
+    (256, 1, 128, 32, [3], [700], True, False),
 ])
 def test_prefill_matches_64_bits(ctx, d, H, Hq, page, new, past, beta, heads_first):
     p = Pages(3, [a + b for a, b in zip(new, past)], H, d, page, beta, heads_first)
