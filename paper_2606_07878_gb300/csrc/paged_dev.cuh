@@ -10,10 +10,11 @@ constexpr float kLog2e = 1.44269504f;
 STILL_DEV uint32_t bf16x2_bits(__nv_bfloat162 x) { return *reinterpret_cast<uint32_t*>(&x); }
 
 // First new token, number of them and slots of sequence b, whatever the arrays hold: an offset
-// outside [0, n] or a length beyond the table is cut and recorded.
+// outside [0, n] or a length beyond the table is cut, and recorded (by one of those who look).
 struct Seq {
   int first, count, len;
 };
+template <bool kRecord = true>
 STILL_DEV Seq paged_seq(const PagedArgs& a, int b) {
   Seq s;
   int c0 = b, c1 = b + 1;
@@ -24,7 +25,7 @@ STILL_DEV Seq paged_seq(const PagedArgs& a, int b) {
   const int cap = (int)min((int64_t)a.table_pages << a.page_shift, (int64_t)0x7fffff00);
   s.len = a.len[b];
   if (c0 < 0 || c1 < c0 || c1 > a.n || s.len < 0 || s.len > cap) {
-    dev_set_error(a.err, DEV_BAD_ARG, 600);
+    if (kRecord) dev_set_error(a.err, DEV_BAD_ARG, 600);
     c0 = min(max(c0, 0), a.n);
     c1 = min(max(c1, c0), a.n);
     s.len = min(max(s.len, 0), cap);
@@ -36,10 +37,11 @@ STILL_DEV Seq paged_seq(const PagedArgs& a, int b) {
 
 // The page that holds slot j of the sequence whose pages `table` lists; -1 (and a record) when it
 // names none.
+template <bool kRecord = true>
 STILL_DEV int paged_page(const PagedArgs& a, const int32_t* table, int j) {
   const int p = table[j >> a.page_shift];
   if ((unsigned)p < (unsigned)a.n_pages) return p;
-  dev_set_error(a.err, DEV_BAD_ARG, 601);
+  if (kRecord) dev_set_error(a.err, DEV_BAD_ARG, 601);
   return -1;
 }
 

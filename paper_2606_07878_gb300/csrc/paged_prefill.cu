@@ -18,10 +18,9 @@
 // Slots that do not count are zeroed in shared memory before their products (a weight of 0 times
 // a stale NaN would be NaN): those past the sequence's end, and those with a bias of -inf.
 //
-// CTA = 12 warps: 0 TMA producer, 1 MMA issuer and TMEM allocation, 4..11 softmax and output, which
-// take over registers of the first four (128 x 104 + 256 x 200 = 384 x 168). Every wait is bounded.
+// CTA = 10 warps: 0 TMA producer, 1 MMA issuer and TMEM allocation, 2..9 softmax and output.
+// Every wait is bounded.
 #include <algorithm>
-#include <type_traits>
 
 #include "gemm_host.cuh"
 #include "paged_dev.cuh"
@@ -30,8 +29,7 @@ namespace still {
 
 namespace {
 
-constexpr int kPfThreads = 384;
-constexpr int kPfFewRegs = 104, kPfManyRegs = 200;
+constexpr int kPfThreads = 320;
 constexpr int kPfKeys = 128;        // slots of a tile
 constexpr float kPfMoveLog2 = 8.f;  // P <= 2^8 needs no more of bf16's range
 constexpr int kPfGroups = 256;      // of sequences, for finding an item's
@@ -59,7 +57,8 @@ struct PfShape {
   static constexpr int kRing = kQBytes;
   static constexpr int kBiasAt = kRing + kSlots * kSlotBytes;  // [8 warps][kCols]
   static constexpr int kXchAt = kBiasAt + (kBias ? 8 * kCols * 4 : 0);  // [2][2][128], one tile only
-  static constexpr int kBarAt = kXchAt + (kTiles == 1 ? 2048 : 0);
+  static constexpr int kMarkAt = kXchAt + (kTiles == 1 ? 2048 : 0);  // [slots][32] bytes, [slots] ints
+  static constexpr int kBarAt = kMarkAt + kSlots * 36 + (kSlots & 1) * 4;
   static constexpr int kBytes = kBarAt + 256 + 1024;
   static_assert(kBytes <= 232448, "shared memory budget");
 };
@@ -117,21 +116,40 @@ STILL_DEV void tmem_st32_issue(uint32_t taddr, const uint32_t* r) {
       "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
-template <int kRegs>
-STILL_DEV void fewer_regs() {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs));
-}
-template <int kRegs>
-STILL_DEV void more_regs() {
-  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs));
-}
 STILL_DEV void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Zeroes the rows of a ring slot that lane i marks in its bits for rows [4 i, 4 i + 4).
+STILL_DEV void zero_rows(uint8_t* slot, int chunks, uint32_t marks) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int r = 0; r < kPfKeys; r += 4) {
+    const uint32_t n4 = __shfl_sync(0xffffffffu, marks, r / 4);
+    if ((n4 >> (lane >> 3)) & 1)
+#pragma unroll 1
+      for (int c = 0; c < chunks; ++c)
+        *reinterpret_cast<uint4*>(slot + c * (kPfKeys * 128) + (r + (lane >> 3)) * 128 +
+                                  (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
+  }
+  fence_proxy_async_smem();
+  __syncwarp();
+}
 
 struct PfItem {
   int b, h, qt, split;
   int first, count, past, len;
   int k0, k1;  // tiles of slots [k0, k1) of this split
 };
+
+// A whole warp waits for a phase; false (and a record, and the flag for the others) at the limit.
+STILL_DEV bool pf_wait(uint64_t* bar, uint32_t parity, int* err, volatile int* abort_flag,
+                       int where) {
+  const bool ok = __all_sync(0xffffffffu, mbar_wait(bar, parity));
+  if (!ok && (threadIdx.x & 31) == 0) {
+    dev_set_error(err, DEV_WAIT_TIMEOUT, where);
+    *abort_flag = 1;
+  }
+  return ok;
+}
 
 // The numbers of items before each group of sequences, in shared memory.
 struct PfPlan {
@@ -157,11 +175,11 @@ STILL_DEV PfItem pf_item(const PrefillParams& f, const PfPlan& plan, int tokens,
   }
   x -= plan.before[lo];
   int b = lo * plan.per;
-  Seq s = paged_seq(f.a, b);
+  Seq s = paged_seq<false>(f.a, b);
   int n = pf_tiles(s, tokens);
   while (x >= n * f.a.H) {
     x -= n * f.a.H;
-    s = paged_seq(f.a, ++b);
+    s = paged_seq<false>(f.a, ++b);
     n = pf_tiles(s, tokens);
   }
   r.b = b;
@@ -192,7 +210,7 @@ struct PfBias {
 #pragma unroll
     for (int e = 0; e < kPer; ++e) v[e] = 0.f;
     if (j >= it.len) return;
-    const int pg = paged_page(a, a.table + (int64_t)it.b * a.s_table, j);
+    const int pg = paged_page<false>(a, a.table + (int64_t)it.b * a.s_table, j);
     const int in = j & ((1 << a.page_shift) - 1);
     const float* at = a.beta + ((((int64_t)max(pg, 0) * a.H + it.h) << a.page_shift) + in);
 #pragma unroll
@@ -214,6 +232,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   __shared__ int warp_items[kPfThreads / 32];
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* marks = smem + S::kMarkAt;  // per ring slot and lane: which of 4 rows do not count
+  volatile int* marked = reinterpret_cast<volatile int*>(marks + kSlots * 32);  // any of them
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kBarAt);  // ring slot loaded
   uint64_t* empty = full + kSlots;   // ring slot consumed
   uint64_t* qfull = empty + kSlots;  // the item's q loaded
@@ -290,22 +310,22 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
-    fewer_regs<kPfFewRegs>();
     int slot = 0, n_items = 0;
     uint32_t phase = 0;
     uint32_t armed = 0, armed_par = 0;
     bool q_armed = false, bad = false;
     const int rows = min(1 << a.page_shift, kPfKeys);  // of a box
-    auto fail = [&](int where) {
-      if (lane == 0) {
-        dev_set_error(a.err, DEV_WAIT_TIMEOUT, where);
-        *abort_flag = 1;
-      }
-      bad = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity, int where) {
+      if (!pf_wait(bar, parity, a.err, abort_flag, where)) bad = true;
+      return !bad;
     };
     // One half (kChan channels) of tile kt of K or V into the next ring slot.
-    auto load = [&](const CUtensorMap* tm, const PfItem& it, int kt, int half) {
-      if (!__all_sync(0xffffffffu, mbar_wait(&empty[slot], phase ^ 1))) return fail(610);
+    auto load = [&](const CUtensorMap* tm, const PfItem& it, int kt, int half, uint32_t mark) {
+      if (!wait(&empty[slot], phase ^ 1, 610)) return;
+      const bool any = __any_sync(0xffffffffu, mark != 0);
+      if (any) marks[slot * 32 + lane] = (uint8_t)mark;
+      if (lane == 0) marked[slot] = any;
+      __syncwarp();  // behind lane 0's arrival
       if (lane == 0) mbar_arrive_expect_tx(&full[slot], S::kSlotBytes);
       armed |= 1u << slot;
       armed_par = (armed_par & ~(1u << slot)) | (phase << slot);
@@ -325,8 +345,21 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         phase ^= 1;
       }
     };
-    auto load_tile = [&](const CUtensorMap* tm, const PfItem& it, int kt) {
-      for (int half = 0; half < kHalves && !bad; ++half) load(tm, it, kt, half);
+    PfBias<128> beta;  // of the next tile of K
+    uint32_t mark[2] = {0, 0};  // of the tile of K loaded last and of the one before
+    // K of tile kt, tiles in order: which of its slots count is found out here
+    auto load_k = [&](const PfItem& it, int kt) {
+      uint32_t m = 0;
+      const int j = kt * kPfKeys + 4 * lane;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (j + e >= it.len || (kBias && beta.v[e] == -INFINITY)) m |= 1u << e;
+      if (kBias && kt + 1 < it.k1) beta.load(a, it, (kt + 1) * kPfKeys, lane);
+      mark[1] = mark[0];
+      mark[0] = m;
+      // without biases the row limits mask what K holds past the end
+#pragma unroll 1
+      for (int half = 0; half < kHalves && !bad; ++half) load(&tm_k, it, kt, half, kBias ? m : 0u);
     };
     for (int k = 0;; ++k) {
       const int x = pf_turn(k, cta, nct);
@@ -334,10 +367,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       if (x >= items) continue;
       const PfItem it = pf_item(f, plan, tokens, x);
       if (it.k0 == it.k1) continue;
-      if (n_items > 0 && !__all_sync(0xffffffffu, mbar_wait(qfree, (n_items - 1) & 1))) {
-        fail(611);
-        break;
-      }
+      if (n_items > 0 && !wait(qfree, (n_items - 1) & 1, 611)) break;
       if (lane == 0) {
         const uint32_t box = (uint32_t)f.tile_tokens * g * 128;
         mbar_arrive_expect_tx(qfull, box * kTiles * (D / 64));
@@ -348,26 +378,29 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       }
       q_armed = true;
       ++n_items;
-      // in the order in which the issuer takes them
+      // in the order in which the issuer takes them: K up to kAhead tiles before V
       constexpr int kAhead = kTiles == 2 ? 1 : 2;
-      for (int kt = it.k0; kt < min(it.k0 + kAhead, it.k1) && !bad; ++kt) load_tile(&tm_k, it, kt);
-      for (int kt = it.k0; kt < it.k1 && !bad; ++kt) {
-        load_tile(&tm_v, it, kt);
-        if (kt + kAhead < it.k1 && !bad) load_tile(&tm_k, it, kt + kAhead);
+      if constexpr (kBias) beta.load(a, it, it.k0 * kPfKeys, lane);
+#pragma unroll 1
+      for (int kt = it.k0 - kAhead; kt < it.k1 && !bad; ++kt) {
+        if (kt >= it.k0) {
+          const uint32_t m = kAhead == 2 && kt + 1 < it.k1 ? mark[1] : mark[0];
+#pragma unroll 1
+          for (int half = 0; half < kHalves && !bad; ++half) load(&tm_v, it, kt, half, m);
+        }
+        if (kt + kAhead < it.k1 && !bad) load_k(it, kt + kAhead);
       }
     }
     // The CTA may leave only when nothing is on its way into its shared memory: the last arrivals
     // of the issuer's commits, or copies that nobody waited for.
     for (int i = 0; i < kSlots && !bad && !warp_flag(abort_flag); ++i) {
-      if (!__all_sync(0xffffffffu, mbar_wait(&empty[slot], phase ^ 1))) fail(612);
+      wait(&empty[slot], phase ^ 1, 612);
       if (++slot == kSlots) {
         slot = 0;
         phase ^= 1;
       }
     }
-    if (n_items > 0 && !bad && !warp_flag(abort_flag) &&
-        !__all_sync(0xffffffffu, mbar_wait(qfree, (n_items - 1) & 1)))
-      fail(613);
+    if (n_items > 0 && !bad && !warp_flag(abort_flag)) wait(qfree, (n_items - 1) & 1, 613);
     if (bad || warp_flag(abort_flag)) {
       for (int s = 0; s < kSlots; ++s)
         if (armed & (1u << s)) (void)mbar_wait(&full[s], (armed_par >> s) & 1);
@@ -375,46 +408,57 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer
-    fewer_regs<kPfFewRegs>();
     constexpr uint32_t idesc_s = idesc_f16(128, kPfKeys, 1);
     constexpr uint32_t idesc_o = idesc_f16(128, S::kChan, 1) | kIdescBMn;
     int slot = 0;
     uint32_t phase = 0;
     uint32_t n_i = 0, n_items = 0;  // S tiles and items so far
     bool bad = false, issued = false;
-    PfBias<128> ahead;   // biases of the next tile of slots
-    // per lane: which of its 4 slots do not count, of the tile looked at last and the one before
-    uint32_t dead[2] = {0, 0};
-    auto fail = [&](int where) {
-      if (lane == 0) {
-        dev_set_error(a.err, DEV_WAIT_TIMEOUT, where);
-        *abort_flag = 1;
-      }
-      bad = true;
-    };
     auto wait = [&](uint64_t* bar, uint32_t parity, int where) {
-      if (!__all_sync(0xffffffffu, mbar_wait(bar, parity))) fail(where);
+      if (!pf_wait(bar, parity, a.err, abort_flag, where)) bad = true;
+      return !bad;
     };
-    // Zeroes the rows of a ring slot whose slots do not count.
-    auto scrub = [&](int s, uint32_t nib) {
-      if (!__any_sync(0xffffffffu, nib != 0)) return;
-      uint8_t* base = smem + S::kRing + s * S::kSlotBytes;
-      for (int r = 0; r < kPfKeys; r += 4) {
-        const uint32_t n4 = __shfl_sync(0xffffffffu, nib, r / 4);
-        if ((n4 >> (lane >> 3)) & 1)
-#pragma unroll
-          for (int c = 0; c < S::kChan / 64; ++c)
-            *reinterpret_cast<uint4*>(base + c * S::kChunkBytes + (r + (lane >> 3)) * 128 +
-                                      (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-    };
-    auto next_slot = [&]() {
+    // The next ring slot, loaded and with its marked rows zeroed; -1 at a time-out.
+    auto take = [&]() -> int {
+      if (!wait(&full[slot], phase, 620)) return -1;
+      if (warp_flag(&marked[slot]))
+        zero_rows(smem + S::kRing + slot * S::kSlotBytes, S::kChan / 64, marks[slot * 32 + lane]);
+      tc_fence_after();
+      const int s = slot;
       if (++slot == kSlots) {
         slot = 0;
         phase ^= 1;
       }
+      return s;
+    };
+    const uint64_t q_desc = sdesc_k_sw128(smem_u32(smem));
+    const uint64_t k_desc = sdesc_k_sw128(smem_u32(smem + S::kRing));
+    const uint64_t v_desc = sdesc_mn_sw128(smem_u32(smem + S::kRing), S::kChunkBytes);
+    constexpr uint64_t kChunkStep = S::kChunkBytes >> 4, kSlotStep = S::kSlotBytes >> 4;
+    // S of tile t into buffer buf, over the channels of one ring slot
+    auto mma_s = [&](int buf, int t, int half, int s) {
+      issued = true;
+      if (lane != 0) return;
+      const uint64_t q = q_desc + (t * (D / 64) + half * (S::kChan / 64)) * kChunkStep;
+      const uint64_t k = k_desc + s * kSlotStep;
+#pragma unroll
+      for (int c = 0; c < S::kChan / 64; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          tc_mma_f16(tmem_base + buf * kSCols, q + c * kChunkStep + 2 * e, k + c * kChunkStep + 2 * e,
+                     idesc_s, half + c + e > 0);
+    };
+    // O of tile t, the channels of one ring slot, += P in buffer buf times V
+    auto mma_o = [&](int buf, int t, int half, int s, bool first) {
+      if (lane != 0) return;
+      const uint64_t v = v_desc + s * kSlotStep;
+#pragma unroll
+      for (int e = 0; e < kPfKeys / 16; ++e)
+        mma_ts(tmem_base + kOAt + t * D + half * S::kChan, tmem_base + buf * kSCols + 8 * e,
+               v + e * (2048 >> 4), idesc_o, !first || e > 0);
+    };
+    auto commit = [&](uint64_t* bar) {
+      if (lane == 0) tc_commit(bar);
     };
     for (int k = 0;; ++k) {
       const int x = pf_turn(k, cta, nct);
@@ -422,129 +466,64 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       if (x >= items) continue;
       const PfItem it = pf_item(f, plan, tokens, x);
       if (it.k0 == it.k1) continue;
-      const int n_k = it.k1 - it.k0;
-      if constexpr (kBias) ahead.load(a, it, it.k0 * kPfKeys, lane);
-      // which slots of tile kt count; tiles come in order
-      auto look = [&](int kt) {
-        uint32_t nib = 0;
-        const int j = kt * kPfKeys + 4 * lane;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (j + e >= it.len) nib |= 1u << e;
-          if (kBias && ahead.v[e] == -INFINITY) nib |= 1u << e;
-        }
-        if (kBias && kt + 1 < it.k1) ahead.load(a, it, (kt + 1) * kPfKeys, lane);
-        dead[1] = dead[0];
-        dead[0] = nib;
-      };
-      wait(qfull, n_items & 1, 620);
-      if (bad) break;
-      // S of tile t into buffer t, channels of one ring slot
-      auto mma_s = [&](int buf, int t, int half, int s) {
-        tc_fence_after();
-        if (lane == 0) {
-          const uint32_t q = smem_u32(smem + (t * (D / 64) + half * (S::kChan / 64)) * S::kChunkBytes);
-          const uint32_t kk = smem_u32(smem + S::kRing + s * S::kSlotBytes);
-#pragma unroll
-          for (int c = 0; c < S::kChan / 64; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              tc_mma_f16(tmem_base + buf * kSCols, sdesc_k_sw128(q + c * S::kChunkBytes) + 2 * e,
-                         sdesc_k_sw128(kk + c * S::kChunkBytes) + 2 * e, idesc_s,
-                         half + c + e > 0);
-        }
-        issued = true;
-      };
-      auto mma_o = [&](int buf, int t, int half, int s, bool first) {
-        tc_fence_after();
-        if (lane == 0) {
-          const uint32_t vv = smem_u32(smem + S::kRing + s * S::kSlotBytes);
-          const uint64_t vd = sdesc_mn_sw128(vv, S::kChunkBytes);
-#pragma unroll
-          for (int e = 0; e < kPfKeys / 16; ++e)
-            mma_ts(tmem_base + kOAt + t * D + half * S::kChan, tmem_base + buf * kSCols + 8 * e,
-                   vd + e * (2048 >> 4), idesc_o, !first || e > 0);
-        }
-      };
-      auto commit = [&](uint64_t* bar) {
-        if (lane == 0) tc_commit(bar);
-      };
+      if (!wait(qfull, n_items & 1, 621)) break;
       if constexpr (kTiles == 2) {
+        // step i: P_i V, then S_(i+2); i = -2, -1 are the first two S
+        const int steps = 2 * (it.k1 - it.k0);
         int ks = 0, vs = 0;
-        auto take_k = [&](int kt) {  // K tile kt in a ring slot, ready for products
-          look(kt);
-          wait(&full[slot], phase, 621);
-          if (kBias) scrub(slot, dead[0]);
-          ks = slot;
-          next_slot();
-        };
-        take_k(it.k0);
-        if (bad) break;
-        for (int t = 0; t < 2; ++t) {
-          mma_s(t, t, 0, ks);
-          commit(&sfull[t]);
-        }
-        commit(&empty[ks]);
-        if (n_k == 1) commit(qfree);
-        for (int kt = it.k0; kt < it.k1 && !bad; ++kt) {
-          const bool more = kt + 1 < it.k1;
-          for (int t = 0; t < 2 && !bad; ++t, ++n_i) {
-            wait(&pfull[t], (n_i >> 1) & 1, 622);
-            if (kt == it.k0 && t == 0 && n_items > 0) wait(ofree, (n_items - 1) & 1, 623);
-            if (t == 0) {
-              wait(&full[slot], phase, 624);
-              scrub(slot, dead[0]);
-              vs = slot;
-              next_slot();
-            }
-            if (bad) break;
-            mma_o(t, t, 0, vs, kt == it.k0);
+#pragma unroll 1
+        for (int i = -2; i < steps && !bad; ++i) {
+          const int t = i & 1;
+          if (i >= 0) {
+            if (!wait(&pfull[t], (n_i >> 1) & 1, 622)) break;
+            if (i == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 623)) break;
+            if (t == 0 && (vs = take()) < 0) break;
+            tc_fence_after();
+            mma_o(t, t, 0, vs, i < 2);
             if (t == 1) commit(&empty[vs]);
             commit(&pvdone[t]);
-            if (!more) continue;
-            if (t == 0) take_k(kt + 1);
-            if (bad) break;
+            ++n_i;
+          }
+          if (i + 2 < steps) {
+            if (t == 0 && (ks = take()) < 0) break;
             mma_s(t, t, 0, ks);
+            if (t == 1) commit(&empty[ks]);
             commit(&sfull[t]);
-            if (t == 1) {
-              commit(&empty[ks]);
-              if (kt + 2 == it.k1) commit(qfree);
-            }
+            if (i + 3 == steps) commit(qfree);
           }
         }
       } else {
-        auto make_s = [&](int kt, uint32_t i) {
-          look(kt);
-          for (int half = 0; half < kHalves && !bad; ++half) {
-            wait(&full[slot], phase, 625);
+        const int steps = it.k1 - it.k0;
+#pragma unroll 1
+        for (int i = -2; i < steps && !bad; ++i) {
+          const int buf = (n_i + (i < 0 ? i + 2 : 0)) & 1;
+          if (i >= 0) {
+            if (!wait(&pfull[buf], (n_i >> 1) & 1, 624)) break;
+            if (i == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 625)) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int half = 0; half < kHalves; ++half) {
+              const int s = take();
+              if (s < 0) break;
+              mma_o(buf, 0, half, s, i == 0);
+              commit(&empty[s]);
+            }
             if (bad) break;
-            if (kBias) scrub(slot, dead[0]);
-            mma_s(i & 1, 0, half, slot);
-            commit(&empty[slot]);
-            next_slot();
+            commit(&pvdone[buf]);
+            ++n_i;
           }
-          if (bad) return;
-          commit(&sfull[i & 1]);
-          if (kt + 1 == it.k1) commit(qfree);
-        };
-        make_s(it.k0, n_i);
-        if (n_k > 1 && !bad) make_s(it.k0 + 1, n_i + 1);
-        for (int kt = it.k0; kt < it.k1 && !bad; ++kt, ++n_i) {
-          wait(&pfull[n_i & 1], (n_i >> 1) & 1, 626);
-          if (kt == it.k0 && n_items > 0) wait(ofree, (n_items - 1) & 1, 627);
-          // tile kt + 1 was looked at last, if there is one
-          const uint32_t nib = kt + 1 < it.k1 ? dead[1] : dead[0];
-          for (int half = 0; half < kHalves && !bad; ++half) {
-            wait(&full[slot], phase, 628);
+          if (i + 2 < steps) {
+#pragma unroll 1
+            for (int half = 0; half < kHalves; ++half) {
+              const int s = take();
+              if (s < 0) break;
+              mma_s(buf, 0, half, s);
+              commit(&empty[s]);
+            }
             if (bad) break;
-            scrub(slot, nib);
-            mma_o(n_i & 1, 0, half, slot, kt == it.k0);
-            commit(&empty[slot]);
-            next_slot();
+            commit(&sfull[buf]);
+            if (i + 3 == steps) commit(qfree);
           }
-          if (bad) break;
-          commit(&pvdone[n_i & 1]);
-          if (kt + 2 < it.k1) make_s(kt + 2, n_i + 2);
         }
       }
       ++n_items;
@@ -553,11 +532,10 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       if (lane == 0) tc_commit(drain);
       (void)mbar_wait(drain, 0);
     }
-  } else if (warp >= 4) {
+  } else {
     // ------------------------------------------------------------ softmax and output
-    more_regs<kPfManyRegs>();
     constexpr int kCols = S::kCols, kOCols = S::kOCols;
-    const int sw = warp - 4;
+    const int sw = warp - 2;
     const int quarter = warp & 3;  // TMEM lanes [32 quarter, + 32)
     const int wg = sw >> 2;        // its tile, or its half of the columns
     const int row = quarter * 32 + lane;
@@ -572,15 +550,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     uint32_t n_i = kTiles == 2 ? wg : 0, n_x = 0;
     bool bad = false;
     auto wait_all = [&](uint64_t* bar, uint32_t parity, int where) -> bool {
-      const bool ok = __all_sync(0xffffffffu, mbar_wait(bar, parity));
-      if (!ok) {
-        if (lane == 0) {
-          dev_set_error(a.err, DEV_WAIT_TIMEOUT, where);
-          *abort_flag = 1;
-        }
-        bad = true;
-      }
-      return ok;
+      if (!pf_wait(bar, parity, a.err, abort_flag, where)) bad = true;
+      return !bad;
     };
     // One value per row for the other warp of this lane quarter; returns its value.
     auto exchange = [&](float mine, int where) -> float {
@@ -605,58 +576,64 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       PfBias<kCols> beta;
       if (kBias && it.k0 < it.k1) beta.load(a, it, it.k0 * kPfKeys + col0, lane);
       uint32_t last = 0;  // the S tile before
-      // One tile of slots; kMask: some row of the warp does not see all of its columns. (A branch
-      // around the selects alone costs 500 bytes of spilled registers.)
-      auto tile = [&](auto mask, int kt) {
-        constexpr bool kMask = decltype(mask)::value;
+      const int least = __reduce_min_sync(0xffffffffu, see);  // slots that every row sees
+#pragma unroll 1
+      for (int kt = it.k0; kt < it.k1; ++kt, n_i += kTiles) {
         const int buf = n_i & 1;
-        const uint32_t s_at = lanes + buf * kSCols;
-        if (!wait_all(&sfull[buf], (n_i >> 1) & 1, 630)) return;
-        tc_fence_after();
-        uint32_t v[kCols];
-#pragma unroll
-        for (int c = 0; c < kCols / 32; ++c) tmem_ld32_issue(s_at + col0 + 32 * c, v + 32 * c);
+        const uint32_t s_at = lanes + buf * kSCols + col0;
+        const int slot0 = kt * kPfKeys + col0;
         if constexpr (kBias) {
 #pragma unroll
           for (int e = 0; e < beta.kPer; ++e) kw[beta.kPer * lane + e] = beta.v[e];
-          if (kt + 1 < it.k1) beta.load(a, it, (kt + 1) * kPfKeys + col0, lane);
+          if (kt + 1 < it.k1) beta.load(a, it, slot0 + kPfKeys, lane);
           __syncwarp();
         }
-        tmem_wait_ld();
+        if (!wait_all(&sfull[buf], (n_i >> 1) & 1, 630)) break;
+        tc_fence_after();
+        uint32_t v[64];
+        // Columns [c, c + 64) as logits, -inf where the row does not see the slot.
+        auto logits = [&](int c) {
+          tmem_ld32_issue(s_at + c, v);
+          tmem_ld32_issue(s_at + c + 32, v + 32);
+          tmem_wait_ld();
+          tmem_landed(v);
+          tmem_landed(v + 32);
+          if constexpr (kBias) {
+            const uint64_t sc = pack2(f.q.scale, f.q.scale);
 #pragma unroll
-        for (int c = 0; c < kCols / 32; ++c) tmem_landed(v + 32 * c);
-        if constexpr (kBias) {
-          const uint64_t sc = pack2(f.q.scale, f.q.scale);
-#pragma unroll
-          for (int c = 0; c < kCols; c += 4) {
-            const float4 b4 = *reinterpret_cast<const float4*>(kw + c);
-            float u0, u1;
-            unpack2(fma2(pack2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), sc,
-                         pack2(b4.x, b4.y)), u0, u1);
-            v[c] = __float_as_uint(u0);
-            v[c + 1] = __float_as_uint(u1);
-            unpack2(fma2(pack2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), sc,
-                         pack2(b4.z, b4.w)), u0, u1);
-            v[c + 2] = __float_as_uint(u0);
-            v[c + 3] = __float_as_uint(u1);
+            for (int e = 0; e < 64; e += 4) {
+              const float4 b4 = *reinterpret_cast<const float4*>(kw + c + e);
+              float u0, u1;
+              unpack2(fma2(pack2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), sc,
+                           pack2(b4.x, b4.y)), u0, u1);
+              v[e] = __float_as_uint(u0);
+              v[e + 1] = __float_as_uint(u1);
+              unpack2(fma2(pack2(__uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])), sc,
+                           pack2(b4.z, b4.w)), u0, u1);
+              v[e + 2] = __float_as_uint(u0);
+              v[e + 3] = __float_as_uint(u1);
+            }
           }
-          __syncwarp();  // kw is written again
-        }
-        if constexpr (kMask) {
-          const int seen = see - kt * kPfKeys - col0;  // columns that this row sees
+          if (least < slot0 + c + 64) {
+            const int seen = see - slot0 - c;  // columns that this row sees
 #pragma unroll
-          for (int c = 0; c < kCols; ++c) v[c] = c < seen ? v[c] : 0xff800000u;
-        }
+            for (int e = 0; e < 64; ++e) v[e] = e < seen ? v[e] : 0xff800000u;
+          }
+        };
         float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll 1
+        for (int c = 0; c < kCols; c += 64) {
+          logits(c);
 #pragma unroll
-        for (int c = 0; c < kCols; c += 4) {
-          m0 = max3(m0, __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
-          m1 = max3(m1, __uint_as_float(v[c + 2]), __uint_as_float(v[c + 3]));
+          for (int e = 0; e < 64; e += 4) {
+            m0 = max3(m0, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
+            m1 = max3(m1, __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
+          }
         }
         float mx = fmaxf(m0, m1);
         if constexpr (kTiles == 1) {
           mx = fmaxf(mx, exchange(mx, 631));
-          if (bad) return;
+          if (bad) break;
         }
         bool move = false;
         float fac = 1.f;
@@ -668,29 +645,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
           l_run *= fac;
           move = true;
         }
-        // nothing seen yet: every weight is 2^-inf
-        const float by = m_run == -INFINITY ? 0.f : m_run;
-        const float shift = kBias ? -by : -by * to_log2;
-        const uint64_t by2 = pack2(shift, shift), k2 = pack2(to_log2, to_log2);
-        uint64_t s0 = 0ull, s1 = 0ull;
-#pragma unroll
-        for (int c = 0; c < kCols; c += 2) {
-          float u0, u1;
-          const uint64_t x = pack2(__uint_as_float(v[c]), __uint_as_float(v[c + 1]));
-          unpack2(kBias ? mul2(add2(x, by2), k2) : fma2(x, k2, by2), u0, u1);
-          const uint32_t w = bf16x2_bits(__floats2bfloat162_rn(ex2_ftz(u0), ex2_ftz(u1)));
-          v[c / 2] = w;
-          if (c & 2)  // the weights as rounded
-            s1 = add2(s1, bf16_pair(w));
-          else
-            s0 = add2(s0, bf16_pair(w));
-        }
-        float l0, l1;
-        unpack2(add2(s0, s1), l0, l1);
-        l_run += l0 + l1;
-        // warp-collective: a warp rescales when any of its rows needs it
+        // warp-collective: a warp rescales O when any of its rows needs it
         if (__any_sync(0xffffffffu, move) && kt > it.k0) {
-          if (!wait_all(&pvdone[last & 1], (last >> 1) & 1, 632)) return;
+          if (!wait_all(&pvdone[last & 1], (last >> 1) & 1, 632)) break;
           tc_fence_after();
 #pragma unroll 1
           for (int c = 0; c < kOCols; c += 32) {
@@ -701,20 +658,36 @@ __global__ void __launch_bounds__(kPfThreads, 1)
             tmem_st32(o_at + c, o);
           }
         }
+        // nothing seen yet: every weight is 2^-inf
+        const float by = m_run == -INFINITY ? 0.f : m_run;
+        const float shift = kBias ? -by : -by * to_log2;
+        const uint64_t by2 = pack2(shift, shift), k2 = pack2(to_log2, to_log2);
+        uint64_t s0 = 0ull, s1 = 0ull;
+#pragma unroll 1
+        for (int c = 0; c < kCols; c += 64) {
+          if (kCols > 64) logits(c);
 #pragma unroll
-        for (int c = 0; c < kCols / 64; ++c)
-          tmem_st32_issue(s_at + col0 / 2 + 32 * c, v + 32 * c);
+          for (int e = 0; e < 64; e += 2) {
+            float u0, u1;
+            const uint64_t x = pack2(__uint_as_float(v[e]), __uint_as_float(v[e + 1]));
+            unpack2(kBias ? mul2(add2(x, by2), k2) : fma2(x, k2, by2), u0, u1);
+            const uint32_t w = bf16x2_bits(__floats2bfloat162_rn(ex2_ftz(u0), ex2_ftz(u1)));
+            v[e / 2] = w;
+            if (e & 2)  // the weights as rounded
+              s1 = add2(s1, bf16_pair(w));
+            else
+              s0 = add2(s0, bf16_pair(w));
+          }
+          tmem_st32_issue(s_at - col0 + (col0 + c) / 2, v);
+        }
+        float l0, l1;
+        unpack2(add2(s0, s1), l0, l1);
+        l_run += l0 + l1;
         tmem_wait_st();
         tc_fence_before();
-        __syncwarp();
+        __syncwarp();  // and kw is written again
         if (lane == 0) mbar_arrive(&pfull[buf]);
         last = n_i;
-      };
-      for (int kt = it.k0; kt < it.k1 && !bad; ++kt, n_i += kTiles) {
-        if (__any_sync(0xffffffffu, see - kt * kPfKeys - col0 < kCols))
-          tile(std::true_type{}, kt);
-        else
-          tile(std::false_type{}, kt);
       }
       if (bad) break;
       // ---- the item's rows
@@ -765,8 +738,6 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         if (lane == 0) mbar_arrive(ofree);
       }
     }
-  } else {
-    fewer_regs<kPfFewRegs>();
   }
   tc_fence_before();
   __syncthreads();
