@@ -57,8 +57,7 @@ struct PfShape {
   static constexpr int kRing = kQBytes;
   static constexpr int kBiasAt = kRing + kSlots * kSlotBytes;  // [8 warps][kCols]
   static constexpr int kXchAt = kBiasAt + (kBias ? 8 * kCols * 4 : 0);  // [2][2][128], one tile only
-  static constexpr int kMarkAt = kXchAt + (kTiles == 1 ? 2048 : 0);  // [slots][32] bytes, [slots] ints
-  static constexpr int kBarAt = kMarkAt + kSlots * 36 + (kSlots & 1) * 4;
+  static constexpr int kBarAt = kXchAt + (kTiles == 1 ? 2048 : 0);
   static constexpr int kBytes = kBarAt + 256 + 1024;
   static_assert(kBytes <= 232448, "shared memory budget");
 };
@@ -72,6 +71,16 @@ STILL_DEV void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
       "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
+}
+// One lane of a converged warp, as the compiler knows: behind it operands stay uniform.
+STILL_DEV bool elect_one() {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "elect.sync _|q, 0xffffffff;\n\t"
+      "selp.b32 %0, 1, 0, q;\n}\n"
+      : "=r"(r));
+  return r != 0;
 }
 // Shared-memory descriptor of an MN-major operand, 128-byte swizzle: rows (k) of 64 contiguous
 // elements, 8 rows an atom of 1024 bytes, atoms along k 1024 bytes apart, the next 64 elements
@@ -232,8 +241,6 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   __shared__ int warp_items[kPfThreads / 32];
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* marks = smem + S::kMarkAt;  // per ring slot and lane: which of 4 rows do not count
-  volatile int* marked = reinterpret_cast<volatile int*>(marks + kSlots * 32);  // any of them
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kBarAt);  // ring slot loaded
   uint64_t* empty = full + kSlots;   // ring slot consumed
   uint64_t* qfull = empty + kSlots;  // the item's q loaded
@@ -243,10 +250,11 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   uint64_t* pvdone = pfull + 2;      // [2] O holds P_i V
   uint64_t* ofree = pvdone + 2;      // O drained at the end of an item
   uint64_t* xb = ofree + 1;          // [4] row-value exchange per lane quarter
-  uint64_t* drain = xb + 4;
+  uint64_t* landed = xb + 4;         // the copies into a ring slot that has rows to be zeroed
+  uint64_t* drain = landed + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((2 * kSlots + 14) * 8 + 8 <= 256, "barriers");
+  static_assert((2 * kSlots + 15) * 8 + 8 <= 256, "barriers");
 
   const PagedArgs& a = f.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -269,6 +277,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     }
     mbar_init(ofree, 8);
     for (int i = 0; i < 4; ++i) mbar_init(&xb[i], 2);
+    mbar_init(landed, 1);
     mbar_init(drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
@@ -312,7 +321,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     // ------------------------------------------------------------ TMA producer
     int slot = 0, n_items = 0;
     uint32_t phase = 0;
-    uint32_t armed = 0, armed_par = 0;
+    uint32_t armed = 0, armed_par = 0, n_landed = 0;
     bool q_armed = false, bad = false;
     const int rows = min(1 << a.page_shift, kPfKeys);  // of a box
     auto wait = [&](uint64_t* bar, uint32_t parity, int where) {
@@ -322,13 +331,14 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     // One half (kChan channels) of tile kt of K or V into the next ring slot.
     auto load = [&](const CUtensorMap* tm, const PfItem& it, int kt, int half, uint32_t mark) {
       if (!wait(&empty[slot], phase ^ 1, 610)) return;
+      // A slot with rows to be zeroed is full when that is done, a moment after its copies.
       const bool any = __any_sync(0xffffffffu, mark != 0);
-      if (any) marks[slot * 32 + lane] = (uint8_t)mark;
-      if (lane == 0) marked[slot] = any;
-      __syncwarp();  // behind lane 0's arrival
-      if (lane == 0) mbar_arrive_expect_tx(&full[slot], S::kSlotBytes);
-      armed |= 1u << slot;
-      armed_par = (armed_par & ~(1u << slot)) | (phase << slot);
+      uint64_t* bar = any ? landed : &full[slot];
+      if (lane == 0) mbar_arrive_expect_tx(bar, S::kSlotBytes);
+      if (!any) {
+        armed |= 1u << slot;
+        armed_par = (armed_par & ~(1u << slot)) | (phase << slot);
+      }
       __syncwarp();
       const int boxes = kPfKeys / rows * (S::kChan / 64);
       for (int x = lane; x < boxes; x += 32) {
@@ -338,7 +348,12 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         int pg = j < it.len ? paged_page(a, a.table + (int64_t)it.b * a.s_table, j) : -1;
         if (pg < 0) pg = a.n_pages;
         tma_load_4d(smem + S::kRing + slot * S::kSlotBytes + c * S::kChunkBytes + r * 128, tm,
-                    &full[slot], half * S::kChan + c * 64, j & ((1 << a.page_shift) - 1), it.h, pg);
+                    bar, half * S::kChan + c * 64, j & ((1 << a.page_shift) - 1), it.h, pg);
+      }
+      if (any) {
+        if (!wait(landed, n_landed++ & 1, 614)) return;
+        zero_rows(smem + S::kRing + slot * S::kSlotBytes, S::kChan / 64, mark);
+        if (lane == 0) mbar_arrive(&full[slot]);
       }
       if (++slot == kSlots) {
         slot = 0;
@@ -406,7 +421,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         if (armed & (1u << s)) (void)mbar_wait(&full[s], (armed_par >> s) & 1);
       if (q_armed) (void)mbar_wait(qfull, (n_items - 1) & 1);
     }
-  } else if (warp == 1) {
+  } else if (warp == 1 && elect_one()) {
     // ------------------------------------------------------------ MMA issuer
     constexpr uint32_t idesc_s = idesc_f16(128, kPfKeys, 1);
     constexpr uint32_t idesc_o = idesc_f16(128, S::kChan, 1) | kIdescBMn;
@@ -415,15 +430,15 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     uint32_t n_i = 0, n_items = 0;  // S tiles and items so far
     bool bad = false, issued = false;
     auto wait = [&](uint64_t* bar, uint32_t parity, int where) {
-      if (!pf_wait(bar, parity, a.err, abort_flag, where)) bad = true;
-      return !bad;
+      if (mbar_wait(bar, parity)) return true;
+      dev_set_error(a.err, DEV_WAIT_TIMEOUT, where);
+      *abort_flag = 1;
+      bad = true;
+      return false;
     };
-    // The next ring slot, loaded and with its marked rows zeroed; -1 at a time-out.
+    // The next ring slot, loaded; -1 at a time-out.
     auto take = [&]() -> int {
       if (!wait(&full[slot], phase, 620)) return -1;
-      if (warp_flag(&marked[slot]))
-        zero_rows(smem + S::kRing + slot * S::kSlotBytes, S::kChan / 64, marks[slot * 32 + lane]);
-      tc_fence_after();
       const int s = slot;
       if (++slot == kSlots) {
         slot = 0;
@@ -437,8 +452,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     constexpr uint64_t kChunkStep = S::kChunkBytes >> 4, kSlotStep = S::kSlotBytes >> 4;
     // S of tile t into buffer buf, over the channels of one ring slot
     auto mma_s = [&](int buf, int t, int half, int s) {
-      issued = true;
-      if (lane != 0) return;
+      tc_fence_after();
       const uint64_t q = q_desc + (t * (D / 64) + half * (S::kChan / 64)) * kChunkStep;
       const uint64_t k = k_desc + s * kSlotStep;
 #pragma unroll
@@ -447,92 +461,99 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         for (int e = 0; e < 4; ++e)
           tc_mma_f16(tmem_base + buf * kSCols, q + c * kChunkStep + 2 * e, k + c * kChunkStep + 2 * e,
                      idesc_s, half + c + e > 0);
+      issued = true;
     };
     // O of tile t, the channels of one ring slot, += P in buffer buf times V
     auto mma_o = [&](int buf, int t, int half, int s, bool first) {
-      if (lane != 0) return;
+      tc_fence_after();
       const uint64_t v = v_desc + s * kSlotStep;
 #pragma unroll
       for (int e = 0; e < kPfKeys / 16; ++e)
         mma_ts(tmem_base + kOAt + t * D + half * S::kChan, tmem_base + buf * kSCols + 8 * e,
                v + e * (2048 >> 4), idesc_o, !first || e > 0);
     };
-    auto commit = [&](uint64_t* bar) {
-      if (lane == 0) tc_commit(bar);
-    };
     for (int k = 0;; ++k) {
       const int x = pf_turn(k, cta, nct);
-      if (k * nct >= items || bad || warp_flag(abort_flag)) break;
+      if (k * nct >= items || bad || *abort_flag) break;
       if (x >= items) continue;
       const PfItem it = pf_item(f, plan, tokens, x);
       if (it.k0 == it.k1) continue;
       if (!wait(qfull, n_items & 1, 621)) break;
+      const int n_k = it.k1 - it.k0;
       if constexpr (kTiles == 2) {
-        // step i: P_i V, then S_(i+2); i = -2, -1 are the first two S
-        const int steps = 2 * (it.k1 - it.k0);
-        int ks = 0, vs = 0;
+        int ks = take();
+        if (ks < 0) break;
+        mma_s(0, 0, 0, ks);
+        tc_commit(&sfull[0]);
+        mma_s(1, 1, 0, ks);
+        tc_commit(&sfull[1]);
+        tc_commit(&empty[ks]);
+        if (n_k == 1) tc_commit(qfree);
 #pragma unroll 1
-        for (int i = -2; i < steps && !bad; ++i) {
-          const int t = i & 1;
-          if (i >= 0) {
-            if (!wait(&pfull[t], (n_i >> 1) & 1, 622)) break;
-            if (i == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 623)) break;
-            if (t == 0 && (vs = take()) < 0) break;
-            tc_fence_after();
-            mma_o(t, t, 0, vs, i < 2);
-            if (t == 1) commit(&empty[vs]);
-            commit(&pvdone[t]);
-            ++n_i;
+        for (int j = 0; j < n_k; ++j, ++n_i) {  // n_i: pairs of S tiles
+          const bool more = j + 1 < n_k;
+          if (!wait(&pfull[0], n_i & 1, 622)) break;
+          if (j == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 623)) break;
+          const int vs = take();
+          if (vs < 0) break;
+          mma_o(0, 0, 0, vs, j == 0);
+          tc_commit(&pvdone[0]);
+          if (more) {
+            if ((ks = take()) < 0) break;
+            mma_s(0, 0, 0, ks);
+            tc_commit(&sfull[0]);
           }
-          if (i + 2 < steps) {
-            if (t == 0 && (ks = take()) < 0) break;
-            mma_s(t, t, 0, ks);
-            if (t == 1) commit(&empty[ks]);
-            commit(&sfull[t]);
-            if (i + 3 == steps) commit(qfree);
+          if (!wait(&pfull[1], n_i & 1, 624)) break;
+          mma_o(1, 1, 0, vs, j == 0);
+          tc_commit(&pvdone[1]);
+          tc_commit(&empty[vs]);
+          if (more) {
+            mma_s(1, 1, 0, ks);
+            tc_commit(&sfull[1]);
+            tc_commit(&empty[ks]);
+            if (j + 2 == n_k) tc_commit(qfree);
           }
         }
       } else {
-        const int steps = it.k1 - it.k0;
+        // step i: P_i V, then S_(i+2); i = -2, -1 are the first two S
 #pragma unroll 1
-        for (int i = -2; i < steps && !bad; ++i) {
+        for (int i = -2; i < n_k && !bad; ++i) {
           const int buf = (n_i + (i < 0 ? i + 2 : 0)) & 1;
           if (i >= 0) {
-            if (!wait(&pfull[buf], (n_i >> 1) & 1, 624)) break;
-            if (i == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 625)) break;
-            tc_fence_after();
+            if (!wait(&pfull[buf], (n_i >> 1) & 1, 625)) break;
+            if (i == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 626)) break;
 #pragma unroll 1
             for (int half = 0; half < kHalves; ++half) {
               const int s = take();
               if (s < 0) break;
               mma_o(buf, 0, half, s, i == 0);
-              commit(&empty[s]);
+              tc_commit(&empty[s]);
             }
             if (bad) break;
-            commit(&pvdone[buf]);
+            tc_commit(&pvdone[buf]);
             ++n_i;
           }
-          if (i + 2 < steps) {
+          if (i + 2 < n_k) {
 #pragma unroll 1
             for (int half = 0; half < kHalves; ++half) {
               const int s = take();
               if (s < 0) break;
               mma_s(buf, 0, half, s);
-              commit(&empty[s]);
+              tc_commit(&empty[s]);
             }
             if (bad) break;
-            commit(&sfull[buf]);
-            if (i + 3 == steps) commit(qfree);
+            tc_commit(&sfull[buf]);
+            if (i + 3 == n_k) tc_commit(qfree);
           }
         }
       }
       ++n_items;
     }
-    if ((bad || warp_flag(abort_flag)) && issued) {
-      if (lane == 0) tc_commit(drain);
+    if ((bad || *abort_flag) && issued) {
+      tc_commit(drain);
       (void)mbar_wait(drain, 0);
     }
-  } else {
+  } else if (warp >= 2) {
     // ------------------------------------------------------------ softmax and output
     constexpr int kCols = S::kCols, kOCols = S::kOCols;
     const int sw = warp - 2;
