@@ -591,7 +591,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       const PfItem it = pf_item(f, plan, tokens, x);
       const int tl = it.qt * tokens + (kTiles == 2 ? wg * f.tile_tokens : 0) + row / g;
       const bool valid = row < f.tile_tokens * g && tl < it.count;
-      const int see = valid ? max(0, it.past + tl + 1) : 0;
+      // (rows of no token are not stored: they need no masks)
+      const int see = valid ? max(0, it.past + tl + 1) : INT32_MAX;
       const int64_t orow = (int64_t)(it.first + tl) * f.q.Hq + it.h * g + row % g;
       float m_run = -INFINITY, l_run = 0.f;
       PfBias<kCols> beta;
@@ -664,7 +665,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
           fac = ex2_ftz((m_run - mx) * to_log2);
           m_run = mx;
           l_run *= fac;
-          move = true;
+          move = valid;
         }
         // warp-collective: a warp rescales O when any of its rows needs it
         if (__any_sync(0xffffffffu, move) && kt > it.k0) {
