@@ -492,10 +492,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 #pragma unroll 1
         for (int j = 0; j < n_k; ++j, ++n_i) {  // n_i: pairs of S tiles
           const bool more = j + 1 < n_k;
-          if (!wait(&pfull[0], n_i & 1, 622)) break;
-          if (j == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 623)) break;
           const int vs = take();
-          if (vs < 0) break;
+          if (vs < 0 || !wait(&pfull[0], n_i & 1, 622)) break;
+          if (j == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 623)) break;
           mma_o(0, 0, 0, vs, j == 0);
           tc_commit(&pvdone[0]);
           if (more) {
@@ -693,12 +692,12 @@ __global__ void __launch_bounds__(kPfThreads, 1)
             float u0, u1;
             const uint64_t x = pack2(__uint_as_float(v[e]), __uint_as_float(v[e + 1]));
             unpack2(kBias ? mul2(add2(x, by2), k2) : fma2(x, k2, by2), u0, u1);
-            const uint32_t w = bf16x2_bits(__floats2bfloat162_rn(ex2_ftz(u0), ex2_ftz(u1)));
-            v[e / 2] = w;
-            if (e & 2)  // the weights as rounded
-              s1 = add2(s1, bf16_pair(w));
+            const float p0 = ex2_ftz(u0), p1 = ex2_ftz(u1);
+            if (e & 2)
+              s1 = add2(s1, pack2(p0, p1));
             else
-              s0 = add2(s0, bf16_pair(w));
+              s0 = add2(s0, pack2(p0, p1));
+            v[e / 2] = bf16x2_bits(__floats2bfloat162_rn(p0, p1));
           }
           tmem_st32_issue(s_at - col0 + (col0 + c) / 2, v);
         }
