@@ -58,7 +58,7 @@ struct PfShape {
   static constexpr int kBiasAt = kRing + kSlots * kSlotBytes;  // [8 warps][kCols]
   static constexpr int kXchAt = kBiasAt + (kBias ? 8 * kCols * 4 : 0);  // [2][2][128], one tile only
   static constexpr int kBarAt = kXchAt + (kTiles == 1 ? 2048 : 0);
-  static constexpr int kBytes = kBarAt + 256 + 1024;
+  static constexpr int kBytes = kBarAt + 320 + 1024;
   static_assert(kBytes <= 232448, "shared memory budget");
 };
 
@@ -251,10 +251,11 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   uint64_t* ofree = pvdone + 2;      // O drained at the end of an item
   uint64_t* xb = ofree + 1;          // [4] row-value exchange per lane quarter
   uint64_t* landed = xb + 4;         // the copies into a ring slot that has rows to be zeroed
-  uint64_t* drain = landed + 1;
+  uint64_t* phalf = landed + 1;      // [2] the first 64 slots of P_i written (two tiles only)
+  uint64_t* drain = phalf + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((2 * kSlots + 15) * 8 + 8 <= 256, "barriers");
+  static_assert((2 * kSlots + 17) * 8 + 8 <= 320, "barriers");
 
   const PagedArgs& a = f.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -273,6 +274,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sfull[i], 1);
       mbar_init(&pfull[i], kTiles == 2 ? 4 : 8);
+      mbar_init(&phalf[i], 4);
       mbar_init(&pvdone[i], 1);
     }
     mbar_init(ofree, 8);
@@ -464,11 +466,11 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       issued = true;
     };
     // O of tile t, the channels of one ring slot, += P in buffer buf times V
-    auto mma_o = [&](int buf, int t, int half, int s, bool first) {
+    auto mma_o = [&](int buf, int t, int half, int s, bool first, int e0 = 0, int e1 = kPfKeys / 16) {
       tc_fence_after();
       const uint64_t v = v_desc + s * kSlotStep;
 #pragma unroll
-      for (int e = 0; e < kPfKeys / 16; ++e)
+      for (int e = e0; e < e1; ++e)
         mma_ts(tmem_base + kOAt + t * D + half * S::kChan, tmem_base + buf * kSCols + 8 * e,
                v + e * (2048 >> 4), idesc_o, !first || e > 0);
     };
@@ -493,17 +495,21 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         for (int j = 0; j < n_k; ++j, ++n_i) {  // n_i: pairs of S tiles
           const bool more = j + 1 < n_k;
           const int vs = take();
-          if (vs < 0 || !wait(&pfull[0], n_i & 1, 622)) break;
+          if (vs < 0 || !wait(&phalf[0], n_i & 1, 622)) break;
           if (j == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 623)) break;
-          mma_o(0, 0, 0, vs, j == 0);
+          mma_o(0, 0, 0, vs, j == 0, 0, 4);
+          if (!wait(&pfull[0], n_i & 1, 627)) break;
+          mma_o(0, 0, 0, vs, j == 0, 4, 8);
           tc_commit(&pvdone[0]);
           if (more) {
             if ((ks = take()) < 0) break;
             mma_s(0, 0, 0, ks);
             tc_commit(&sfull[0]);
           }
-          if (!wait(&pfull[1], n_i & 1, 624)) break;
-          mma_o(1, 1, 0, vs, j == 0);
+          if (!wait(&phalf[1], n_i & 1, 624)) break;
+          mma_o(1, 1, 0, vs, j == 0, 0, 4);
+          if (!wait(&pfull[1], n_i & 1, 628)) break;
+          mma_o(1, 1, 0, vs, j == 0, 4, 8);
           tc_commit(&pvdone[1]);
           tc_commit(&empty[vs]);
           if (more) {
@@ -700,6 +706,12 @@ __global__ void __launch_bounds__(kPfThreads, 1)
             v[e / 2] = bf16x2_bits(__floats2bfloat162_rn(p0, p1));
           }
           tmem_st32_issue(s_at - col0 + (col0 + c) / 2, v);
+          if (kTiles == 2 && c == 0) {
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&phalf[buf]);
+          }
         }
         float l0, l1;
         unpack2(add2(s0, s1), l0, l1);
