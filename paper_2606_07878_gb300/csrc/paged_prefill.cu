@@ -18,8 +18,9 @@
 // Slots that do not count are zeroed in shared memory before their products (a weight of 0 times
 // a stale NaN would be NaN): those past the sequence's end, and those with a bias of -inf.
 //
-// CTA = 10 warps: 0 TMA producer, 1 MMA issuer and TMEM allocation, 2..9 softmax and output.
-// Every wait is bounded.
+// CTA = 12 warps: 0, 10 and 11 TMA producers (a copy takes about 60 clocks to issue, and pages of
+// 16 slots are 128 copies a tile of 256 channels: 352 us with one, 0 and the others share them out),
+// 1 MMA issuer and TMEM allocation, 2..9 softmax and output. Every wait is bounded.
 #include <algorithm>
 
 #include "gemm_host.cuh"
@@ -29,7 +30,8 @@ namespace still {
 
 namespace {
 
-constexpr int kPfThreads = 320;
+constexpr int kPfThreads = 384;
+constexpr int kPfProducers = 3;     // warps
 constexpr int kPfKeys = 128;        // slots of a tile
 constexpr float kPfMoveLog2 = 8.f;  // P <= 2^8 needs no more of bf16's range
 constexpr int kPfGroups = 256;      // of sequences, for finding an item's
@@ -58,7 +60,7 @@ struct PfShape {
   static constexpr int kBiasAt = kRing + kSlots * kSlotBytes;  // [8 warps][kCols]
   static constexpr int kXchAt = kBiasAt + (kBias ? 8 * kCols * 4 : 0);  // [2][2][128], one tile only
   static constexpr int kBarAt = kXchAt + (kTiles == 1 ? 2048 : 0);
-  static constexpr int kBytes = kBarAt + 320 + 1024;
+  static constexpr int kBytes = kBarAt + 352 + 1024;
   static_assert(kBytes <= 232448, "shared memory budget");
 };
 
@@ -251,11 +253,11 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   uint64_t* ofree = pvdone + 2;      // O drained at the end of an item
   uint64_t* xb = ofree + 1;          // [4] row-value exchange per lane quarter
   uint64_t* landed = xb + 4;         // the copies into a ring slot that has rows to be zeroed
-  uint64_t* phalf = landed + 1;      // [2] the first 64 slots of P_i written (two tiles only)
+  uint64_t* phalf = landed + kSlots;      // [2] the first 64 slots of P_i written (two tiles only)
   uint64_t* drain = phalf + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((2 * kSlots + 17) * 8 + 8 <= 320, "barriers");
+  static_assert((3 * kSlots + 16) * 8 + 8 <= 352, "barriers");
 
   const PagedArgs& a = f.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -268,6 +270,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(&full[s], 1);
       mbar_init(&empty[s], 1);
+      mbar_init(&landed[s], 1);
     }
     mbar_init(qfull, 1);
     mbar_init(qfree, 1);
@@ -279,7 +282,6 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     }
     mbar_init(ofree, 8);
     for (int i = 0; i < 4; ++i) mbar_init(&xb[i], 2);
-    mbar_init(landed, 1);
     mbar_init(drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
@@ -319,11 +321,12 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   const int items = plan.before[kPfGroups] * f.nsplit;
   const int cta = blockIdx.x, nct = gridDim.x;
 
-  if (warp == 0) {
-    // ------------------------------------------------------------ TMA producer
+  if (warp == 0 || warp >= 10) {
+    // ------------------------------------------------------------ TMA producers
+    const int me = warp == 0 ? 0 : warp - 9;  // 0 also loads q, arms the barriers and zeroes rows
     int slot = 0, n_items = 0;
     uint32_t phase = 0;
-    uint32_t armed = 0, armed_par = 0, n_landed = 0;
+    uint32_t armed = 0, armed_par = 0, land_par = 0;
     bool q_armed = false, bad = false;
     const int rows = min(1 << a.page_shift, kPfKeys);  // of a box
     auto wait = [&](uint64_t* bar, uint32_t parity, int where) {
@@ -335,15 +338,15 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       if (!wait(&empty[slot], phase ^ 1, 610)) return;
       // A slot with rows to be zeroed is full when that is done, a moment after its copies.
       const bool any = __any_sync(0xffffffffu, mark != 0);
-      uint64_t* bar = any ? landed : &full[slot];
-      if (lane == 0) mbar_arrive_expect_tx(bar, S::kSlotBytes);
+      uint64_t* bar = any ? &landed[slot] : &full[slot];
+      if (me == 0 && lane == 0) mbar_arrive_expect_tx(bar, S::kSlotBytes);
       if (!any) {
         armed |= 1u << slot;
         armed_par = (armed_par & ~(1u << slot)) | (phase << slot);
       }
       __syncwarp();
       const int boxes = kPfKeys / rows * (S::kChan / 64);
-      for (int x = lane; x < boxes; x += 32) {
+      for (int x = me + kPfProducers * lane; x < boxes; x += 32 * kPfProducers) {
         const int c = x % (S::kChan / 64), r = x / (S::kChan / 64) * rows;
         const int j = kt * kPfKeys + r;
         // a box outside the pool (past the last page, or of an entry that names none) is zeros
@@ -352,8 +355,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         tma_load_4d(smem + S::kRing + slot * S::kSlotBytes + c * S::kChunkBytes + r * 128, tm,
                     bar, half * S::kChan + c * 64, j & ((1 << a.page_shift) - 1), it.h, pg);
       }
-      if (any) {
-        if (!wait(landed, n_landed++ & 1, 614)) return;
+      if (any && me == 0) {
+        if (!wait(&landed[slot], (land_par >> slot) & 1, 614)) return;
+        land_par ^= 1u << slot;
         zero_rows(smem + S::kRing + slot * S::kSlotBytes, S::kChan / 64, mark);
         if (lane == 0) mbar_arrive(&full[slot]);
       }
@@ -384,8 +388,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       if (x >= items) continue;
       const PfItem it = pf_item(f, plan, tokens, x);
       if (it.k0 == it.k1) continue;
-      if (n_items > 0 && !wait(qfree, (n_items - 1) & 1, 611)) break;
-      if (lane == 0) {
+      if (me == 0 && n_items > 0 && !wait(qfree, (n_items - 1) & 1, 611)) break;
+      if (me == 0 && lane == 0) {
         const uint32_t box = (uint32_t)f.tile_tokens * g * 128;
         mbar_arrive_expect_tx(qfull, box * kTiles * (D / 64));
         for (int t = 0; t < kTiles; ++t)
@@ -410,15 +414,15 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     }
     // The CTA may leave only when nothing is on its way into its shared memory: the last arrivals
     // of the issuer's commits, or copies that nobody waited for.
-    for (int i = 0; i < kSlots && !bad && !warp_flag(abort_flag); ++i) {
+    for (int i = 0; i < kSlots && me == 0 && !bad && !warp_flag(abort_flag); ++i) {
       wait(&empty[slot], phase ^ 1, 612);
       if (++slot == kSlots) {
         slot = 0;
         phase ^= 1;
       }
     }
-    if (n_items > 0 && !bad && !warp_flag(abort_flag)) wait(qfree, (n_items - 1) & 1, 613);
-    if (bad || warp_flag(abort_flag)) {
+    if (me == 0 && n_items > 0 && !bad && !warp_flag(abort_flag)) wait(qfree, (n_items - 1) & 1, 613);
+    if (me == 0 && (bad || warp_flag(abort_flag))) {
       for (int s = 0; s < kSlots; ++s)
         if (armed & (1u << s)) (void)mbar_wait(&full[s], (armed_par >> s) & 1);
       if (q_armed) (void)mbar_wait(qfull, (n_items - 1) & 1);
