@@ -58,12 +58,11 @@ size_t paged_rows_workspace(const PagedArgs& a, int Hq, int num_sms);
 cudaError_t launch_paged_rows(const PagedArgs& a, const PagedQuery& q, void* ws, int* arrived,
                               int num_sms, cudaStream_t s);
 
-// Many rows, on the tensor cores (paged_prefill.cu). Groups of more than 128 query heads do not
-// fit a tile. nsplit: ranges that an item's slots are cut into, joined by a second launch.
+// Many rows, on the tensor cores (paged_prefill.cu), and the join of what several CTAs share: two
+// launches. Groups of more than 128 query heads do not fit a tile.
 bool paged_prefill_fits(const PagedArgs& a, int Hq);
-int paged_prefill_splits(const PagedArgs& a, int Hq, int num_sms);
-size_t paged_prefill_workspace(const PagedArgs& a, int Hq, int nsplit);
-cudaError_t launch_paged_prefill(const PagedArgs& a, const PagedQuery& q, void* ws, int nsplit,
+size_t paged_prefill_workspace(const PagedArgs& a, int num_sms);
+cudaError_t launch_paged_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
                                  const KernelTable& dev, cudaStream_t s);
 
 }  // namespace still

@@ -34,15 +34,22 @@ constexpr int kPfThreads = 384;
 constexpr int kPfProducers = 3;     // warps
 constexpr int kPfKeys = 128;        // slots of a tile
 constexpr float kPfMoveLog2 = 8.f;  // P <= 2^8 needs no more of bf16's range
-constexpr int kPfGroups = 256;      // of sequences, for finding an item's
+constexpr int kPfItemCost = 2;      // of an item's beginning and end, in tiles of slots
 
 struct PrefillParams {
   PagedArgs a;
   PagedQuery q;
   int32_t tile_tokens = 0;  // floor(128 / g)
-  int32_t nsplit = 1;       // equal ranges of an item's slots
-  float* part_o = nullptr;  // [nsplit][n * Hq][d], when nsplit > 1
-  float2* part_ml = nullptr;  // [nsplit][n * Hq] (m, l), m in the kernel's units of a logit
+  // parts of items that lie in several CTAs' ranges: what CTA c continues (2 c), begins (2 c + 1)
+  float4* part_o = nullptr;   // [2 x CTAs][d / 4][rows of an item]
+  float2* part_ml = nullptr;  // [2 x CTAs][rows of an item] (m, l), m in the kernel's units
+  struct PfSplit* split = nullptr;  // [CTAs]
+};
+
+// The item that CTA c begins and does not end.
+struct PfSplit {
+  int32_t last;    // the CTA that ends it; c: there is none
+  int32_t token0, tokens, h;
 };
 
 template <int D, bool kBias>
@@ -145,10 +152,22 @@ STILL_DEV void zero_rows(uint8_t* slot, int chunks, uint32_t marks) {
   __syncwarp();
 }
 
+// What a CTA does of an item.
 struct PfItem {
-  int b, h, qt, split;
-  int first, count, past, len;
-  int k0, k1;  // tiles of slots [k0, k1) of this split
+  int b, h, len;
+  int token0, tokens;  // its tokens, packed rows
+  int see;             // slots that the first of them sees (below 1: none)
+  int k0, k1;          // tiles of slots [k0, k1)
+  int part;            // 0: all of the item, else where the part goes: 1 + (it is the first)
+  int last;            // the CTA that ends an item which this one begins
+};
+
+// Where a CTA's range begins, in shared memory.
+struct PfStart {
+  int64_t base;  // cost of all items before this one
+  int64_t total, left;  // of all items, of this CTA's range
+  int b, qt, h, off;    // off: cost of this item that lies before the range
+  int nct;              // CTAs that have a range
 };
 
 // A whole warp waits for a phase; false (and a record, and the flag for the others) at the limit.
@@ -162,53 +181,64 @@ STILL_DEV bool pf_wait(uint64_t* bar, uint32_t parity, int* err, volatile int* a
   return ok;
 }
 
-// The numbers of items before each group of sequences, in shared memory.
-struct PfPlan {
-  int before[kPfGroups + 1];
-  int per;  // sequences of a group
-};
-
 STILL_DEV int pf_tiles(const Seq& s, int tokens) { return (s.count + tokens - 1) / tokens; }
-
-// Item x of the plan: sequences in order, the last tokens (which see most slots) first, then
-// KV-heads, then splits.
-STILL_DEV PfItem pf_item(const PrefillParams& f, const PfPlan& plan, int tokens, int x) {
-  PfItem r;
-  r.split = x % f.nsplit;
-  x /= f.nsplit;
-  int lo = 0, hi = kPfGroups;  // the last group that begins at or before x
-  while (lo + 1 < hi) {
-    const int mid = (lo + hi) / 2;
-    if (plan.before[mid] <= x)
-      lo = mid;
-    else
-      hi = mid;
-  }
-  x -= plan.before[lo];
-  int b = lo * plan.per;
-  Seq s = paged_seq<false>(f.a, b);
-  int n = pf_tiles(s, tokens);
-  while (x >= n * f.a.H) {
-    x -= n * f.a.H;
-    s = paged_seq<false>(f.a, ++b);
-    n = pf_tiles(s, tokens);
-  }
-  r.b = b;
-  r.h = x % f.a.H;
-  r.qt = n - 1 - x / f.a.H;
-  r.first = s.first;
-  r.count = s.count;
-  r.len = s.len;
-  r.past = s.len - s.count;
-  const int most = r.past + min(s.count, (r.qt + 1) * tokens);
-  const int kt = most > 0 ? (most + kPfKeys - 1) / kPfKeys : 0;
-  r.k0 = (int)((int64_t)kt * r.split / f.nsplit);
-  r.k1 = (int)((int64_t)kt * (r.split + 1) / f.nsplit);
-  return r;
+// Tiles of slots that item qt of a sequence sees.
+STILL_DEV int pf_slots(const Seq& s, int tokens, int qt) {
+  const int most = s.len - s.count + min(s.count, (qt + 1) * tokens);
+  return most > 0 ? (most + kPfKeys - 1) / kPfKeys : 0;
 }
 
-// The k-th item of CTA c of n: there and back, so that long items meet short ones.
-STILL_DEV int pf_turn(int k, int c, int n) { return k * n + ((k & 1) ? n - 1 - c : c); }
+// The items of a CTA's range, in order: sequences, tokens, KV-heads. An item's cost is its tiles of
+// slots, then kPfItemCost for its beginning and end.
+struct PfWalk {
+  const PagedArgs& a;
+  int tokens;  // of an item
+  int64_t base, left, total;
+  int b, qt, h, off, nq, nct;
+  Seq s;
+  STILL_DEV PfWalk(const PagedArgs& args, int item_tokens, const PfStart& p)
+      : a(args), tokens(item_tokens), base(p.base), left(p.left), total(p.total), b(p.b), qt(p.qt),
+        h(p.h), off(p.off), nct(p.nct) {
+    if (left > 0) {
+      s = paged_seq<false>(a, b);
+      nq = pf_tiles(s, tokens);
+    }
+  }
+  STILL_DEV bool next(PfItem& it) {
+    while (left > 0) {
+      const int kt = pf_slots(s, tokens, qt), cost = kt + kPfItemCost;
+      const int end = (int)min((int64_t)cost, off + left);
+      const bool begins = off == 0;
+      it.b = b;
+      it.h = h;
+      it.len = s.len;
+      it.token0 = s.first + qt * tokens;
+      it.tokens = min(tokens, s.count - qt * tokens);
+      it.see = s.len - s.count + qt * tokens + 1;
+      it.k0 = min(off, kt);
+      it.k1 = min(end, kt);
+      it.part = begins && end >= kt ? 0 : begins ? 2 : 1;
+      if (it.part == 2) it.last = (int)(((base + kt) * nct - 1) / total);
+      left -= end - off;
+      off = 0;
+      if (end == cost) {
+        base += cost;
+        if (++h == a.H) {
+          h = 0;
+          if (++qt == nq) {
+            qt = nq = 0;
+            while (left > 0 && nq == 0) {
+              s = paged_seq<false>(a, ++b);
+              nq = pf_tiles(s, tokens);
+            }
+          }
+        }
+      }
+      if (it.k0 < it.k1 || (begins && kt == 0)) return true;
+    }
+    return false;
+  }
+};
 
 // kC columns' biases of a warp, one tile of slots ahead: lane i holds those of columns
 // [kC / 32 i, + kC / 32).
@@ -239,14 +269,17 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   using S = PfShape<D, kBias>;
   constexpr int kTiles = S::kTiles, kSlots = S::kSlots, kHalves = S::kHalves;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ PfPlan plan;
-  __shared__ int warp_items[kPfThreads / 32];
+  __shared__ PfStart start;
+  __shared__ PfItem shown[2];  // items n & 1 as the producer shows them to the others
+  __shared__ int64_t warp_cost[kPfThreads / 32];
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kBarAt);  // ring slot loaded
   uint64_t* empty = full + kSlots;   // ring slot consumed
-  uint64_t* qfull = empty + kSlots;  // the item's q loaded
-  uint64_t* qfree = qfull + 1;       // its last S complete
+  // [2] q of item n loaded and the item shown, n & 1. (The softmax of an item of one tile of slots
+  // may wait for it only when the next one's q has come as well.)
+  uint64_t* qfull = empty + kSlots;
+  uint64_t* qfree = qfull + 2;       // an item's last S complete
   uint64_t* sfull = qfree + 1;       // [2] S_i complete
   uint64_t* pfull = sfull + 2;       // [2] P_i written (and O rescaled where needed)
   uint64_t* pvdone = pfull + 2;      // [2] O holds P_i V
@@ -257,7 +290,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   uint64_t* drain = phalf + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((3 * kSlots + 16) * 8 + 8 <= 352, "barriers");
+  static_assert((3 * kSlots + 17) * 8 + 8 <= 352, "barriers");
 
   const PagedArgs& a = f.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -272,7 +305,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       mbar_init(&empty[s], 1);
       mbar_init(&landed[s], 1);
     }
-    mbar_init(qfull, 1);
+    mbar_init(&qfull[0], 1);
+    mbar_init(&qfull[1], 1);
     mbar_init(qfree, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sfull[i], 1);
@@ -293,33 +327,66 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     tmem_alloc(tmem_slot, 512);
     tmem_relinquish();
   }
-  {  // the plan: thread t adds up group t
-    const int per = (a.B + kPfGroups - 1) / kPfGroups;
-    int mine = 0;
-    if (threadIdx.x < kPfGroups)
-      for (int b = threadIdx.x * per; b < min(a.B, ((int)threadIdx.x + 1) * per); ++b)
-        mine += pf_tiles(paged_seq(a, b), tokens) * a.H;
-    int sum = mine;
+  const int cta = blockIdx.x;
+  {  // equal ranges of the cost of all items: a thread adds up some sequences, or a share of one's
+    const int per = (a.B + kPfThreads - 1) / kPfThreads, shares = max(1, kPfThreads / a.B);
+    const int share = threadIdx.x % shares;
+    const int sb0 = min(a.B, (int)threadIdx.x / shares * per), sb1 = min(a.B, sb0 + per);
+    auto first_item = [&](int nq, int x) { return (int)((int64_t)nq * x / shares); };
+    int64_t mine = 0;
+    for (int b = sb0; b < sb1; ++b) {
+      const Seq s = paged_seq(a, b);
+      const int nq = pf_tiles(s, tokens);
+      int sum = 0;
+      for (int qt = first_item(nq, share); qt < first_item(nq, share + 1); ++qt)
+        sum += pf_slots(s, tokens, qt) + kPfItemCost;
+      mine += (int64_t)sum * a.H;
+    }
+    int64_t before = mine, total = 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += x;
+      const int64_t x = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += x;
     }
-    if (lane == 31) warp_items[warp] = sum;
+    if (lane == 31) warp_cost[warp] = before;
+    if (threadIdx.x == 0) start.left = 0;
+    if (threadIdx.x == 0) f.split[cta].last = cta;
     __syncthreads();
-    for (int w = 0; w < warp; ++w) sum += warp_items[w];
-    if (threadIdx.x < kPfGroups) plan.before[threadIdx.x + 1] = sum;
-    if (threadIdx.x == 0) {
-      plan.before[0] = 0;
-      plan.per = per;
+    for (int w = 0; w < kPfThreads / 32; ++w) {
+      if (w < warp) before += warp_cost[w];
+      total += warp_cost[w];
+    }
+    before -= mine;
+    // no range is shorter than an item's beginning and a tile
+    const int nct = (int)max((int64_t)1, min((int64_t)gridDim.x, total / (kPfItemCost + 1)));
+    const int64_t u0 = cta < nct ? total * cta / nct : total;
+    if (u0 >= before && u0 < before + mine) {
+      PfStart p;
+      p.total = total;
+      p.left = total * (cta + 1) / nct - u0;
+      p.nct = nct;
+      for (p.b = sb0;; ++p.b) {
+        const Seq s = paged_seq(a, p.b);
+        const int nq = first_item(pf_tiles(s, tokens), share + 1);
+        for (p.qt = first_item(pf_tiles(s, tokens), share); p.qt < nq; ++p.qt) {
+          const int cost = pf_slots(s, tokens, p.qt) + kPfItemCost;
+          if (u0 < before + (int64_t)cost * a.H) {
+            p.h = (int)((u0 - before) / cost);
+            p.base = before + (int64_t)cost * p.h;
+            p.off = (int)(u0 - p.base);
+            break;
+          }
+          before += (int64_t)cost * a.H;
+        }
+        if (p.qt < nq) break;
+      }
+      start = p;
     }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  const int items = plan.before[kPfGroups] * f.nsplit;
-  const int cta = blockIdx.x, nct = gridDim.x;
 
   if (warp == 0 || warp >= 10) {
     // ------------------------------------------------------------ TMA producers
@@ -382,20 +449,28 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 #pragma unroll 1
       for (int half = 0; half < kHalves && !bad; ++half) load(&tm_k, it, kt, half, kBias ? m : 0u);
     };
-    for (int k = 0;; ++k) {
-      const int x = pf_turn(k, cta, nct);
-      if (k * nct >= items || bad || warp_flag(abort_flag)) break;
-      if (x >= items) continue;
-      const PfItem it = pf_item(f, plan, tokens, x);
-      if (it.k0 == it.k1) continue;
+    PfWalk walk(a, tokens, start);
+    PfItem it;
+    while (!bad && !warp_flag(abort_flag) && walk.next(it)) {
+      if (it.k0 == it.k1) {  // its rows see nothing
+        if (me == 1)
+          for (int x = lane; x < it.tokens * g * (D / 8); x += 32) {
+            const int t = x / (g * (D / 8));
+            reinterpret_cast<uint4*>(f.q.out + ((int64_t)(it.token0 + t) * f.q.Hq + it.h * g) *
+                                                   D)[x % (g * (D / 8))] = make_uint4(0, 0, 0, 0);
+          }
+        continue;
+      }
       if (me == 0 && n_items > 0 && !wait(qfree, (n_items - 1) & 1, 611)) break;
       if (me == 0 && lane == 0) {
+        shown[n_items & 1] = it;
+        if (it.part == 2) f.split[cta] = PfSplit{it.last, it.token0, it.tokens, it.h};
         const uint32_t box = (uint32_t)f.tile_tokens * g * 128;
-        mbar_arrive_expect_tx(qfull, box * kTiles * (D / 64));
+        mbar_arrive_expect_tx(&qfull[n_items & 1], box * kTiles * (D / 64));
         for (int t = 0; t < kTiles; ++t)
           for (int c = 0; c < D / 64; ++c)
-            tma_load_3d(smem + (t * (D / 64) + c) * S::kChunkBytes, &tm_q, qfull, c * 64, it.h * g,
-                        it.first + it.qt * tokens + t * f.tile_tokens);
+            tma_load_3d(smem + (t * (D / 64) + c) * S::kChunkBytes, &tm_q, &qfull[n_items & 1], c * 64, it.h * g,
+                        it.token0 + t * f.tile_tokens);
       }
       q_armed = true;
       ++n_items;
@@ -422,10 +497,14 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       }
     }
     if (me == 0 && n_items > 0 && !bad && !warp_flag(abort_flag)) wait(qfree, (n_items - 1) & 1, 613);
+    if (me == 0 && lane == 0 && !bad && !*abort_flag) {  // no more items
+      shown[n_items & 1].k0 = shown[n_items & 1].k1 = 0;
+      mbar_arrive(&qfull[n_items & 1]);
+    }
     if (me == 0 && (bad || warp_flag(abort_flag))) {
       for (int s = 0; s < kSlots; ++s)
         if (armed & (1u << s)) (void)mbar_wait(&full[s], (armed_par >> s) & 1);
-      if (q_armed) (void)mbar_wait(qfull, (n_items - 1) & 1);
+      if (q_armed) (void)mbar_wait(&qfull[(n_items - 1) & 1], ((n_items - 1) >> 1) & 1);
     }
   } else if (warp == 1 && elect_one()) {
     // ------------------------------------------------------------ MMA issuer
@@ -478,14 +557,10 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         mma_ts(tmem_base + kOAt + t * D + half * S::kChan, tmem_base + buf * kSCols + 8 * e,
                v + e * (2048 >> 4), idesc_o, !first || e > 0);
     };
-    for (int k = 0;; ++k) {
-      const int x = pf_turn(k, cta, nct);
-      if (k * nct >= items || bad || *abort_flag) break;
-      if (x >= items) continue;
-      const PfItem it = pf_item(f, plan, tokens, x);
-      if (it.k0 == it.k1) continue;
-      if (!wait(qfull, n_items & 1, 621)) break;
-      const int n_k = it.k1 - it.k0;
+    while (!bad && !*abort_flag) {
+      if (!wait(&qfull[n_items & 1], (n_items >> 1) & 1, 621)) break;
+      const int n_k = shown[n_items & 1].k1 - shown[n_items & 1].k0;
+      if (n_k < 1) break;
       if constexpr (kTiles == 2) {
         int ks = take();
         if (ks < 0) break;
@@ -593,19 +668,17 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       ++n_x;
       return ok ? at[(1 - wg) * 128 + row] : mine;
     };
-    for (int k = 0;; ++k) {
-      const int x = pf_turn(k, cta, nct);
-      if (k * nct >= items || bad || warp_flag(abort_flag)) break;
-      if (x >= items) continue;
-      const PfItem it = pf_item(f, plan, tokens, x);
-      const int tl = it.qt * tokens + (kTiles == 2 ? wg * f.tile_tokens : 0) + row / g;
-      const bool valid = row < f.tile_tokens * g && tl < it.count;
+    const int token = (kTiles == 2 ? wg * f.tile_tokens : 0) + row / g;  // of an item
+    for (uint32_t n_items = 0; !bad && !warp_flag(abort_flag); ++n_items) {
+      if (!wait_all(&qfull[n_items & 1], (n_items >> 1) & 1, 629)) break;
+      const PfItem it = shown[n_items & 1];
+      if (it.k1 <= it.k0) break;
+      const bool valid = row < f.tile_tokens * g && token < it.tokens;
       // (rows of no token are not stored: they need no masks)
-      const int see = valid ? max(0, it.past + tl + 1) : INT32_MAX;
-      const int64_t orow = (int64_t)(it.first + tl) * f.q.Hq + it.h * g + row % g;
+      const int see = valid ? max(0, it.see + token) : INT32_MAX;
       float m_run = -INFINITY, l_run = 0.f;
       PfBias<kCols> beta;
-      if (kBias && it.k0 < it.k1) beta.load(a, it, it.k0 * kPfKeys + col0, lane);
+      if (kBias) beta.load(a, it, it.k0 * kPfKeys + col0, lane);
       uint32_t last = 0;  // the S tile before
       const int least = __reduce_min_sync(0xffffffffu, see);  // slots that every row sees
 #pragma unroll 1
@@ -729,51 +802,71 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       if (bad) break;
       // ---- the item's rows
       float l = l_run;
-      if (it.k0 < it.k1) {
-        if constexpr (kTiles == 1) {
-          l += exchange(l_run, 633);
-          if (bad) break;
-        }
-        if (!wait_all(&pvdone[last & 1], (last >> 1) & 1, 634)) break;
-        tc_fence_after();
+      if constexpr (kTiles == 1) {
+        l += exchange(l_run, 633);
+        if (bad) break;
       }
+      if (!wait_all(&pvdone[last & 1], (last >> 1) & 1, 634)) break;
+      tc_fence_after();
       const int oc = kTiles == 2 ? 0 : wg * kOCols;
-      const float inv = l == 0.f ? 0.f : 1.f / l;
+      if (it.part != 0) {  // columns apart, so that a warp's rows lie side by side
+        const int64_t part = 2 * cta + it.part - 1;
+        const int prow = (kTiles == 2 ? 128 * wg : 0) + row;
+        float4* dst = f.part_o + (part * (D / 4) + oc / 4) * (128 * kTiles) + prow;
 #pragma unroll 1
-      for (int c = 0; c < kOCols; c += 32) {
-        float o[32];
-        if (it.k0 < it.k1) {
+        for (int c = 0; c < kOCols; c += 32) {
+          float o[32];
           tmem_ld32(o_at + c, o);
-        } else {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0.f;
+          for (int e = 0; e < 8; ++e)
+            dst[(c / 4 + e) * (128 * kTiles)] =
+                make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
         }
-        if (!valid) continue;
-        if (f.nsplit > 1) {
-          float4* dst = reinterpret_cast<float4*>(
-              f.part_o + ((int64_t)it.split * a.n * f.q.Hq + orow) * D + oc + c);
+        if (kTiles == 2 || wg == 0) f.part_ml[part * (128 * kTiles) + prow] = make_float2(m_run, l);
+      } else {
+        // Four lanes exchange pieces of 16 bytes, so that they store 64 bytes of one row at a time:
+        // a row per lane takes four times as many passes of the store unit.
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const int64_t orow =
+            valid ? (int64_t)(it.token0 + token) * f.q.Hq + it.h * g + row % g : -1;
+        int64_t at[4];
 #pragma unroll
-          for (int e = 0; e < 32; e += 4)
-            dst[e / 4] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-        } else {
-          uint4* dst = reinterpret_cast<uint4*>(f.q.out + orow * D + oc + c);
+        for (int i = 0; i < 4; ++i) at[i] = __shfl_sync(0xffffffffu, orow, (lane & ~3) + i);
+        const bool odd = lane & 1, high = lane & 2;
+#pragma unroll 1
+        for (int c = 0; c < kOCols; c += 32) {
+          float o[32];
+          tmem_ld32(o_at + c, o);
+          uint32_t w[4][4];
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {
-            uint32_t w[4];
+          for (int e = 0; e < 16; ++e)
+            w[e / 4][e % 4] =
+                bf16x2_bits(__floats2bfloat162_rn(o[2 * e] * inv, o[2 * e + 1] * inv));
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              w[i] = bf16x2_bits(__floats2bfloat162_rn(o[e + 2 * i] * inv, o[e + 2 * i + 1] * inv));
-            dst[e / 8] = make_uint4(w[0], w[1], w[2], w[3]);
-          }
+          for (int m = 0; m < 4; m += 2)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t x = __shfl_xor_sync(0xffffffffu, odd ? w[m][i] : w[m + 1][i], 1);
+              (odd ? w[m][i] : w[m + 1][i]) = x;
+            }
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t x = __shfl_xor_sync(0xffffffffu, high ? w[m][i] : w[m + 2][i], 2);
+              (high ? w[m][i] : w[m + 2][i]) = x;
+            }
+          // piece lane & 3 of four rows
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (at[i] >= 0)
+              *reinterpret_cast<uint4*>(f.q.out + at[i] * D + oc + c + 8 * (lane & 3)) =
+                  make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
         }
       }
-      if (f.nsplit > 1 && valid && (kTiles == 2 || wg == 0))
-        f.part_ml[(int64_t)it.split * a.n * f.q.Hq + orow] = make_float2(m_run, l);
-      if (it.k0 < it.k1) {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(ofree);
-      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(ofree);
     }
   }
   tc_fence_before();
@@ -784,32 +877,49 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   }
 }
 
-// The splits' parts of a row, in their order; a warp per row.
+// Rows of the items that lie in several CTAs' ranges: block (c, x) joins rows [32 x, + 32) of the item
+// that CTA c begins, its parts in the order of their slots; a lane takes a row, a warp d / 8 channels.
+template <int D>
 __global__ void __launch_bounds__(256)
-    paged_join_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml,
-                      int64_t rows, int nsplit, int d, float to_log2,
-                      __nv_bfloat16* __restrict__ out) {
+    paged_join_kernel(const __grid_constant__ PrefillParams f, int item_rows, float to_log2) {
   griddep_wait();
-  const int64_t row = blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (row >= rows) return;
-  float M = -INFINITY;
-  for (int s = 0; s < nsplit; ++s) M = fmaxf(M, part_ml[s * rows + row].x);
-  for (int c = 2 * lane; c < d; c += 64) {
-    float L = 0.f;
-    float2 O = make_float2(0.f, 0.f);
-#pragma unroll 4
-    for (int s = 0; s < nsplit; ++s) {
-      const float2 ml = part_ml[s * rows + row];
-      const float2 o = *reinterpret_cast<const float2*>(part_o + (s * rows + row) * d + c);
-      const float w = ml.x == M ? 1.f : exp2f((ml.x - M) * to_log2);
-      L += w * ml.y;
-      O.x += w * o.x;
-      O.y += w * o.y;
+  const int c = blockIdx.x;
+  const PfSplit sp = f.split[c];
+  if (sp.last <= c) return;
+  const int g = f.q.Hq / f.a.H;
+  const int r = 32 * blockIdx.y + (threadIdx.x & 31), x0 = (threadIdx.x >> 5) * (D / 8);
+  const int in = r & 127, token = (r >> 7) * f.tile_tokens + in / g;
+  if (in >= f.tile_tokens * g || token >= sp.tokens) return;
+  auto part = [&](int p) { return (int64_t)(p == c ? 2 * c + 1 : 2 * p); };
+  float M = -INFINITY, L = 0.f, O[D / 8];
+#pragma unroll
+  for (int e = 0; e < D / 8; ++e) O[e] = 0.f;
+  for (int p = c; p <= sp.last; ++p) M = fmaxf(M, f.part_ml[part(p) * item_rows + r].x);
+  for (int p = c; p <= sp.last; ++p) {
+    const float2 ml = f.part_ml[part(p) * item_rows + r];
+    const float w = ml.x == M ? 1.f : exp2f((ml.x - M) * to_log2);
+    const float4* src = f.part_o + (part(p) * (D / 4) + x0 / 4) * item_rows + r;
+    L += w * ml.y;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) {
+      const float4 o = src[e * item_rows];
+      O[4 * e] += w * o.x;
+      O[4 * e + 1] += w * o.y;
+      O[4 * e + 2] += w * o.z;
+      O[4 * e + 3] += w * o.w;
     }
-    const float inv = L == 0.f ? 0.f : 1.f / L;
-    *reinterpret_cast<__nv_bfloat162*>(out + row * d + c) =
-        __floats2bfloat162_rn(O.x * inv, O.y * inv);
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  uint4* dst = reinterpret_cast<uint4*>(
+      f.q.out + ((int64_t)(sp.token0 + token) * f.q.Hq + sp.h * g + in % g) * D + x0);
+#pragma unroll
+  for (int e = 0; e < D / 64; ++e) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = bf16x2_bits(
+          __floats2bfloat162_rn(O[8 * e + 2 * i] * inv, O[8 * e + 2 * i + 1] * inv));
+    dst[e] = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
@@ -843,60 +953,51 @@ bool query_tmap(CUtensorMap* m, const PagedArgs& a, const PagedQuery& q, int tok
 }
 
 template <int D, bool kBias>
-cudaError_t launch_prefill(const PagedArgs& a, const PagedQuery& q, void* ws, int nsplit,
+cudaError_t launch_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
                            const KernelTable& dev, cudaStream_t s) {
   using S = PfShape<D, kBias>;
   using Id = KernelId<paged_prefill_kernel<D, kBias>, kPfThreads, S::kBytes>;
   if (dev.of<Id>().status != cudaSuccess) return dev.of<Id>().status;
+  constexpr int rows = 128 * S::kTiles;
   PrefillParams f;
   f.a = a;
   f.q = q;
   f.tile_tokens = 128 / (q.Hq / a.H);
-  f.nsplit = nsplit;
-  const int64_t rows = (int64_t)a.n * q.Hq;
-  f.part_o = static_cast<float*>(ws);
-  f.part_ml = reinterpret_cast<float2*>(f.part_o + (nsplit > 1 ? nsplit * rows * a.d : 0));
+  f.part_o = static_cast<float4*>(ws);
+  f.part_ml = reinterpret_cast<float2*>(f.part_o + (int64_t)2 * dev.num_sms * rows * (D / 4));
+  f.split = reinterpret_cast<PfSplit*>(f.part_ml + (int64_t)2 * dev.num_sms * rows);
   CUtensorMap tq, tk, tv;
   if (!query_tmap(&tq, a, q, f.tile_tokens) || !pool_tmap(&tk, a, a.K) || !pool_tmap(&tv, a, a.V))
     return cudaErrorInvalidValue;
   paged_prefill_kernel<D, kBias><<<dev.num_sms, kPfThreads, S::kBytes, s>>>(tq, tk, tv, f);
   cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess || nsplit == 1) return e;
-  return launch_chained(paged_join_kernel, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, s, 1,
-                        f.part_o, f.part_ml, rows, nsplit, a.d, (kBias ? 1.f : q.scale) * kLog2e,
-                        q.out);
+  if (e != cudaSuccess) return e;
+  return launch_chained(paged_join_kernel<D>, dim3(dev.num_sms, rows / 32), dim3(256), 0, s, 1, f, rows,
+                        (kBias ? 1.f : q.scale) * kLog2e);
 }
 
 }  // namespace
 
 bool paged_prefill_fits(const PagedArgs& a, int Hq) { return Hq / a.H <= 128; }
 
-int paged_prefill_splits(const PagedArgs& a, int Hq, int num_sms) {
-  const int tokens = 128 / (Hq / a.H) * (a.d <= 128 ? 2 : 1);
-  // items, exact for one sequence and at most
-  const int64_t items = a.H * ((int64_t)a.n / tokens + (a.B > 1 ? a.B : a.n % tokens != 0));
-  const int64_t tiles = (((int64_t)a.table_pages << a.page_shift) + kPfKeys - 1) / kPfKeys;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({num_sms / std::max<int64_t>(1, items),
-                                                      tiles / 2, 32}));
+size_t paged_prefill_workspace(const PagedArgs& a, int num_sms) {
+  const size_t rows = a.d <= 128 ? 256 : 128;
+  return (size_t)num_sms * (2 * rows * (a.d * 4 + 8) + sizeof(PfSplit));
 }
 
-size_t paged_prefill_workspace(const PagedArgs& a, int Hq, int nsplit) {
-  return nsplit > 1 ? (size_t)nsplit * a.n * Hq * (a.d * 4 + 8) : 0;
-}
-
-cudaError_t launch_paged_prefill(const PagedArgs& a, const PagedQuery& q, void* ws, int nsplit,
+cudaError_t launch_paged_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
                                  const KernelTable& dev, cudaStream_t s) {
   const bool bias = a.beta != nullptr;
   switch (a.d) {
     case 64:
-      return bias ? launch_prefill<64, true>(a, q, ws, nsplit, dev, s)
-                  : launch_prefill<64, false>(a, q, ws, nsplit, dev, s);
+      return bias ? launch_prefill<64, true>(a, q, ws, dev, s)
+                  : launch_prefill<64, false>(a, q, ws, dev, s);
     case 128:
-      return bias ? launch_prefill<128, true>(a, q, ws, nsplit, dev, s)
-                  : launch_prefill<128, false>(a, q, ws, nsplit, dev, s);
+      return bias ? launch_prefill<128, true>(a, q, ws, dev, s)
+                  : launch_prefill<128, false>(a, q, ws, dev, s);
     case 256:
-      return bias ? launch_prefill<256, true>(a, q, ws, nsplit, dev, s)
-                  : launch_prefill<256, false>(a, q, ws, nsplit, dev, s);
+      return bias ? launch_prefill<256, true>(a, q, ws, dev, s)
+                  : launch_prefill<256, false>(a, q, ws, dev, s);
   }
   return cudaErrorInvalidValue;
 }

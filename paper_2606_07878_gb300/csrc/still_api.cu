@@ -1801,11 +1801,9 @@ still_status paged_attend(still_ctx* ctx, const still_paged_cache* cache,
   const int nsm = ctx->kernels.num_sms;
   // more than a block of 16 rows per sequence: tiles on the tensor cores
   if (n * (Hq / a.H) > 16 * (int64_t)a.B && a.cu_new != nullptr && paged_prefill_fits(a, Hq)) {
-    const int nsplit = paged_prefill_splits(a, Hq, nsm);
-    TRY(ensure_ws(ctx, paged_prefill_workspace(a, Hq, nsplit)));
-    KLAUNCH(STILL_K_PAGED_ATTEND,
-            launch_paged_prefill(a, p, ctx->ws, nsplit, ctx->kernels, s));
-    ctx->prof.launches[STILL_K_PAGED_ATTEND] += nsplit > 1;  // the join
+    TRY(ensure_ws(ctx, paged_prefill_workspace(a, nsm)));
+    KLAUNCH(STILL_K_PAGED_ATTEND, launch_paged_prefill(a, p, ctx->ws, ctx->kernels, s));
+    ctx->prof.launches[STILL_K_PAGED_ATTEND] += 1;  // the join
     return STILL_OK;
   }
   TRY(ensure_ws(ctx, paged_rows_workspace(a, Hq, nsm)));
