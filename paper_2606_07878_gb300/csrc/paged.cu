@@ -115,14 +115,16 @@ __global__ void __launch_bounds__(kAppendThreads)
 // K, V and O never touch shared memory. Logits stay in natural units up to the subtraction of the
 // maximum: in units of log 2 a bias of the lowest float would become -inf, which masks.
 //
-// Work: a set is a sequence's KV-head and block of 8 or 16 rows; its slots are cut into units of
-// 64, and all units of all sets, one after another, into equal ranges, one per CTA, from lengths
-// that the kernel itself adds up. A set that lies in one range is written by its CTA; the parts of
-// another meet in the workspace, and the CTA that brings the last one joins them in their order, so
-// that the result does not depend on who that is. No CTA waits for another.
-constexpr int kRowWarps = 4;
+// Work: a set is a sequence's KV-head and block of 8 or 16 rows; its slots are cut into batches of
+// 16, and all batches of all sets, one after another, into equal ranges, one per warp, from lengths
+// that the kernel itself adds up. A warp streams through its range without meeting another: K and V
+// of the next batch are on their way while it computes one, across the ends of sets too. A set that
+// lies in one range is written by its warp; the parts of another meet in the workspace, and a second
+// launch joins them in their order.
+constexpr int kRowWarps = 4;  // of a CTA
 constexpr int kRowThreads = 32 * kRowWarps;
-constexpr int kUnit = 16 * kRowWarps;  // slots
+constexpr int kBatch = 16;      // slots
+constexpr int kLeastBatches = 2;  // of a range, where there are fewer ranges than warps
 
 // c (16 x 8) += a (16 x 16 bf16) b (16 x 8 bf16)
 STILL_DEV void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
@@ -151,17 +153,24 @@ STILL_DEV uint32_t word(const uint4& v, int i) {
 template <int D, int NB>
 struct Rows {
   static constexpr int kRows = 8 * NB;
-  static constexpr int kPart = kRows * (D + 2);  // floats of a part: O rows, then m, l
-  static constexpr int kMinCtas = D == 64 ? (NB == 1 ? 5 : 4) : D == 128 ? (NB == 1 ? 3 : 2) : 2;
+  static constexpr int kMinCtas = D == 64 ? (NB == 1 ? 4 : 3) : D == 128 ? (NB == 1 ? 3 : 2) : 2;
+  static constexpr bool kQShared = D == 256;  // no registers left for q beside K, V and O
 };
 
+// The set that warp w begins and does not end.
+struct RowsSplit {
+  int32_t last;  // the warp that ends it; w: there is none
+  int32_t token0, row0, rows;  // the sequence's first new token, the set's rows
+  int32_t h;
+};
 struct RowsJoin {
-  float* parts = nullptr;  // [2 x CTAs][Rows::kPart]: what CTA c continues (2 c), begins (2 c + 1)
-  int* arrived = nullptr;  // [CTAs], zero between calls
+  // parts of the sets that several warps share: what warp w continues (2 w), begins (2 w + 1)
+  float* part_o = nullptr;     // [2 x warps][kRows][d]
+  float2* part_ml = nullptr;   // [2 x warps][kRows] (m, l)
+  RowsSplit* split = nullptr;  // [warps]
 };
 
-// Units of a sequence's sets, and their number per KV-head.
-STILL_DEV int seq_units(const Seq& s) { return s.count > 0 ? (s.len + kUnit - 1) / kUnit : 0; }
+STILL_DEV int seq_batches(const Seq& s) { return s.count > 0 ? (s.len + kBatch - 1) / kBatch : 0; }
 template <int kRows>
 STILL_DEV int seq_blocks(const Seq& s, int g) {
   return (int)(((int64_t)s.count * g + kRows - 1) / kRows);
@@ -171,22 +180,24 @@ template <int D, int NB>
 __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
     paged_rows_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedQuery p,
                       const RowsJoin join) {
-  using R = Rows<D, NB>;
-  constexpr int kRows = R::kRows;
-  __shared__ __align__(16) float red[kRowWarps][8][D + 4];  // O rows of a block, m and l behind
+  constexpr int kRows = Rows<D, NB>::kRows;
   __shared__ int64_t warp_sum[kRowWarps];
-  __shared__ int64_t at_unit;  // units before sequence at_seq
-  __shared__ int at_seq, is_last;
+  __shared__ int64_t at_batch[kRowWarps];  // batches before sequence at_seq
+  __shared__ int at_seq[kRowWarps];
+  constexpr bool kQShared = Rows<D, NB>::kQShared;
+  __shared__ uint4 q_shared[kQShared ? kRowWarps : 1][kQShared ? NB * (D / 32) : 1][32];
   const int g = p.Hq / a.H;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int lg = lane >> 2, lj = lane & 3;
-  // ---- this CTA's range [u0, u1) of all units, and the sequence in which it begins
+  // ---- this warp's range [u0, u1) of all batches, and the sequence in which it begins
   const int per = (a.B + kRowThreads - 1) / kRowThreads;  // consecutive sequences of a thread
   const int sb0 = min(a.B, (int)threadIdx.x * per), sb1 = min(a.B, sb0 + per);
   int64_t mine = 0;
+  bool none = false;  // a sequence without slots
   for (int b = sb0; b < sb1; ++b) {
     const Seq s = paged_seq(a, b);
-    mine += (int64_t)seq_units(s) * seq_blocks<kRows>(s, g) * a.H;
+    none |= seq_batches(s) == 0;
+    mine += (int64_t)seq_batches(s) * seq_blocks<kRows>(s, g) * a.H;
   }
   int64_t before = mine;
 #pragma unroll
@@ -195,7 +206,7 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
     if (lane >= o) before += x;
   }
   if (lane == 31) warp_sum[warp] = before;
-  __syncthreads();
+  none = __syncthreads_or(none);
   int64_t total = 0;
 #pragma unroll
   for (int w = 0; w < kRowWarps; ++w) {
@@ -203,337 +214,484 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
     total += warp_sum[w];
   }
   before -= mine;
-  const int nct = (int)min((int64_t)gridDim.x, total);
-  // sequences without slots: zeros
-  for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+  const int nw = (int)max((int64_t)1, min((int64_t)gridDim.x * kRowWarps, total / kLeastBatches));
+  // The warps of a CTA are neighbours in the order of ranges where every warp has one, else spread.
+  const int ctas = gridDim.x;
+  auto range_of = [&](int w) { return ctas * kRowWarps == nw ? blockIdx.x * kRowWarps + w
+                                                             : w * ctas + blockIdx.x; };
+  for (int w = 0; w < kRowWarps; ++w) {
+    const int64_t u = total * min(range_of(w), nw) / nw;
+    if (u < before || u >= before + mine) continue;
+    int64_t at = before;
+    int b = sb0;
+    for (;; ++b) {
+      const Seq s = paged_seq(a, b);
+      const int64_t n = (int64_t)seq_batches(s) * seq_blocks<kRows>(s, g) * a.H;
+      if (u < at + n) break;
+      at += n;
+    }
+    at_seq[w] = b;
+    at_batch[w] = at;
+  }
+  for (int b = blockIdx.x; none && b < a.B; b += gridDim.x) {  // their rows are zeros
     const Seq s = paged_seq(a, b);
-    if (seq_units(s) > 0) continue;
+    if (seq_batches(s) > 0) continue;
     uint4* o = reinterpret_cast<uint4*>(p.out + (int64_t)s.first * p.Hq * D);
     for (int64_t i = threadIdx.x; i < (int64_t)s.count * p.Hq * D / 8; i += kRowThreads)
       o[i] = make_uint4(0, 0, 0, 0);
   }
-  if ((int)blockIdx.x >= nct) return;
-  const int64_t u0 = total * blockIdx.x / nct, u1 = total * (blockIdx.x + 1) / nct;
-  if (u0 >= before && u0 < before + mine) {
-    int b = sb0;
-    for (;; ++b) {
-      const Seq s = paged_seq(a, b);
-      const int64_t n = (int64_t)seq_units(s) * seq_blocks<kRows>(s, g) * a.H;
-      if (u0 < before + n) break;
-      before += n;
-    }
-    at_seq = b;
-    at_unit = before;
-  }
   __syncthreads();
-  int b = at_seq;
-  int64_t seq_u = at_unit;  // first unit of sequence b
+  const int me = range_of(warp);
+  if (lane == 0) join.split[me].last = me;
+  if (me >= nw || total == 0) return;
+  const int64_t u0 = total * me / nw, u1 = total * (me + 1) / nw;
   const int mask = (1 << a.page_shift) - 1;
   const int64_t beta_page = (int64_t)a.H << a.page_shift;
 
-  for (int64_t u = u0; u < u1;) {
-    // ---- the set of unit u: sequence b, KV-head h, block rb; its units [su, su + nu)
-    Seq s = paged_seq(a, b);
-    int nu = seq_units(s), nblk = seq_blocks<kRows>(s, g);
-    while (u >= seq_u + (int64_t)nu * nblk * a.H) {
-      seq_u += (int64_t)nu * nblk * a.H;
-      s = paged_seq(a, ++b);
-      nu = seq_units(s);
-      nblk = seq_blocks<kRows>(s, g);
+  // ---- where the loads are: a set, its slots from e0 up to `end`
+  struct {
+    Seq s;
+    int b, h, r0;       // the set
+    int nrows, most;    // its rows, the slots that any of them sees
+    int batch, nb;      // batch of the set, batches of the set
+    int64_t set0;       // batches before the set
+  } at{};
+  int64_t left = u1 - u0;  // batches of the range that are not loaded yet
+  auto enter = [&]() {     // the set's sizes
+    at.nrows = min(kRows, at.s.count * g - at.r0);
+    at.most = max(0, at.s.len - at.s.count + (at.r0 + at.nrows - 1) / g + 1);
+  };
+  at.b = at_seq[warp];
+  at.s = paged_seq(a, at.b);
+  at.nb = seq_batches(at.s);
+  {
+    const int64_t in = u0 - at_batch[warp];
+    const int nblk = seq_blocks<kRows>(at.s, g);
+    const int64_t set = in / at.nb;
+    at.h = (int)(set / nblk);
+    at.r0 = (int)(set % nblk) * kRows;
+    at.batch = (int)(in - set * at.nb);
+    at.set0 = u0 - at.batch;
+    enter();
+  }
+  // On to the next batch; true if it is another set's.
+  auto advance = [&]() -> bool {
+    if (--left == 0 || ++at.batch < at.nb) return false;
+    at.set0 += at.nb;
+    at.batch = 0;
+    at.r0 += kRows;
+    if (at.r0 >= at.s.count * g) {
+      at.r0 = 0;
+      if (++at.h == a.H) {
+        at.h = 0;
+        do {
+          at.s = paged_seq(a, ++at.b);
+          at.nb = seq_batches(at.s);
+        } while (at.nb == 0);
+      }
     }
-    const int64_t set = (u - seq_u) / nu;
-    const int h = (int)(set / nblk), r0 = (int)(set % nblk) * kRows;
-    const int64_t su = seq_u + set * nu;
-    const int ua = (int)(u - su), ub = (int)(min(u1, su + nu) - su);
-    const int nrows = min(kRows, s.count * g - r0);
-    const int past = s.len - s.count;  // token i sees slots up to past + i
-    const int most = max(0, past + (r0 + nrows - 1) / g + 1);
-    const int end = min(ub * kUnit, most);
-    const int32_t* table = a.table + (int64_t)b * a.s_table;
-    const __nv_bfloat16* Kh = a.K + (int64_t)h * a.s_head + 8 * lj;
-    const __nv_bfloat16* Vh = a.V + (int64_t)h * a.s_head + 8 * lg;
-    const float* Bh = a.beta != nullptr ? a.beta + ((int64_t)h << a.page_shift) : nullptr;
-    int see[NB][2];
+    enter();
+    return true;
+  };
+
+  uint4 kx[2][D / 32], vx[4][D / 64];
+  float bias[2];
+  // K, V and biases of slots [e0, min(e0 + 16, end)) of a KV-head; slots past the end repeat the
+  // last one (their weight is 0, their V zeroed). A batch past what its set's rows see is not loaded.
+  auto load_k = [&](int h, int pg, int e0, int end) {
+    const int in = e0 & mask, most = end - e0 - 1;
+    const int64_t page = max(pg, 0);
+    const __nv_bfloat16* base = a.K + page * a.s_page + (int64_t)h * a.s_head + 8 * lj;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = in + min(lg + 8 * i, most);
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) kx[i][c] = ld_once(base + r * a.s_slot + 32 * c);
+      bias[i] = pg < 0               ? -INFINITY
+                : a.beta != nullptr ? a.beta[page * beta_page + ((int64_t)h << a.page_shift) + r]
+                                    : 0.f;
+    }
+  };
+  auto load_v = [&](int h, int pg, int e0, int end) {
+    const int in = e0 & mask, most = end - e0 - 1;
+    const __nv_bfloat16* base =
+        a.V + (int64_t)max(pg, 0) * a.s_page + (int64_t)h * a.s_head + 8 * lg;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const int r = in + min(2 * lj + (v & 1) + 8 * (v >> 1), most);
+#pragma unroll
+      for (int x = 0; x < D / 64; ++x) vx[v][x] = ld_once(base + r * a.s_slot + 64 * x);
+    }
+  };
+  auto page_at = [&](int b, int e0) { return paged_page(a, a.table + (int64_t)b * a.s_table, e0); };
+
+  float m[NB][2], l[NB][2];   // rows 2 lj, 2 lj + 1 of a block; l: this lane's share
+  float o[NB][D / 64][4][4];  // O^T: channels 64 x + 8 lg + 2 w (+1), rows 2 lj (+1)
+  uint4 qf[NB][kQShared ? 1 : D / 32];
+  int see[NB][2];  // slots that a row sees
+  auto begin_set = [&](const Seq& s, int h, int r0, int nrows) {
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      const int r = 8 * k + lg;
+      const bool ok = r < nrows;
+      const int tok = s.first + (r0 + r) / g, qh = h * g + (r0 + r) % g;
+      const __nv_bfloat16* qp = p.q + (ok ? (int64_t)tok * p.s_q + (int64_t)qh * D : 0) + 8 * lj;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c)
+        (kQShared ? q_shared[warp][k * (D / 32) + c][lane] : qf[k][kQShared ? 0 : c]) =
+            ok ? *reinterpret_cast<const uint4*>(qp + 32 * c) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int rr = 8 * k + 2 * lj + e;
+        see[k][e] = rr < nrows ? s.len - s.count + (r0 + rr) / g + 1 : 0;
+      }
+    }
+  };
+  auto clear = [&]() {
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      m[k][0] = m[k][1] = -INFINITY;
+      l[k][0] = l[k][1] = 0.f;
+#pragma unroll
+      for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[k][x][w][e] = 0.f;
+    }
+  };
+  // The batch of slots [e0, end) that kx, vx and bias hold. `then_k` and `then_v` may overwrite them
+  // where they are done with; rests: with P's rounding rests.
+  auto compute = [&](int e0, int end, bool rests, auto then_k, auto then_v) {
+    float c[NB][4];
+    const float b0 = bias[0], b1 = bias[1];
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      float c2[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[k][e] = 0.f;
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x) {
+        const uint4 q = kQShared ? q_shared[warp][k * (D / 32) + x][lane] : qf[k][kQShared ? 0 : x];
+        mma_bf16(c[k], kx[0][x].x, kx[1][x].x, kx[0][x].y, kx[1][x].y, q.x, q.y);
+        mma_bf16(c2, kx[0][x].z, kx[1][x].z, kx[0][x].w, kx[1][x].w, q.z, q.w);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[k][e] += c2[e];
+    }
+    then_k();
+    // slots whose value does not count: 0 * inf would be NaN
+    const int n = end - e0;
+    const unsigned dead0 = __ballot_sync(0xffffffffu, b0 == -INFINITY || lg >= n);
+    const unsigned dead1 = __ballot_sync(0xffffffffu, b1 == -INFINITY || lg + 8 >= n);
+    if (dead0 | dead1) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        if (((v >> 1 ? dead1 : dead0) >> (4 * (2 * lj + (v & 1)))) & 1)
+#pragma unroll
+          for (int x = 0; x < D / 64; ++x) vx[v][x] = make_uint4(0, 0, 0, 0);
+    }
+    uint32_t hi[NB][2], lo[NB][2];
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      float top[2];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {  // slot lg + 8 (e / 2), row 2 lj + e % 2
+        const float be = e >> 1 ? b1 : b0;
+        const bool ok = e0 + lg + 8 * (e >> 1) < see[k][e & 1] && be != -INFINITY;
+        c[k][e] = ok ? c[k][e] * p.scale + be : -INFINITY;
+      }
+      bool moved = false;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        top[e] = fmaxf(c[k][e], c[k][e + 2]);
+#pragma unroll
+        for (int x = 4; x <= 16; x <<= 1)
+          top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], x));
+        moved |= top[e] > m[k][e];
+      }
+      if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float n = fmaxf(m[k][e], top[e]);
+          const float f = n == m[k][e] ? 1.f : exp2f((m[k][e] - n) * kLog2e);
+          m[k][e] = n;
+          l[k][e] *= f;
+#pragma unroll
+          for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              o[k][x][w][e] *= f;
+              o[k][x][w][e + 2] *= f;
+            }
+        }
+      }
+      // nothing seen yet: every weight is 2^-inf
+      const float by0 = m[k][0] == -INFINITY ? 0.f : m[k][0];
+      const float by1 = m[k][1] == -INFINITY ? 0.f : m[k][1];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float w0 = exp2f((c[k][2 * i] - by0) * kLog2e);
+        const float w1 = exp2f((c[k][2 * i + 1] - by1) * kLog2e);
+        l[k][0] += w0;
+        l[k][1] += w1;
+        const __nv_bfloat162 ph = __floats2bfloat162_rn(w0, w1);
+        const float2 r = __bfloat1622float2(ph);
+        hi[k][i] = transpose8(bf16x2_bits(ph));
+        lo[k][i] = transpose8(bf16x2_bits(__floats2bfloat162_rn(w0 - r.x, w1 - r.y)));
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t v0 = word(vx[0][x], w), v1 = word(vx[1][x], w);
+        const uint32_t v2 = word(vx[2][x], w), v3 = word(vx[3][x], w);
+        const uint32_t a0 = __byte_perm(v0, v1, 0x5410), a1 = __byte_perm(v0, v1, 0x7632);
+        const uint32_t a2 = __byte_perm(v2, v3, 0x5410), a3 = __byte_perm(v2, v3, 0x7632);
+#pragma unroll
+        for (int k = 0; k < NB; ++k) {
+          mma_bf16(o[k][x][w], a0, a1, a2, a3, hi[k][0], hi[k][1]);
+          if (rests) mma_bf16(o[k][x][w], a0, a1, a2, a3, lo[k][0], lo[k][1]);
+        }
+      }
+    then_v();
+  };
+
+  int pg = page_at(at.b, kBatch * at.batch);
+  if (kBatch * at.batch < at.most) {
+    load_k(at.h, pg, kBatch * at.batch, at.most);
+    load_v(at.h, pg, kBatch * at.batch, at.most);
+  }
+  while (left > 0) {
+    // ---- a set, or this warp's part of it
+    const Seq s = at.s;
+    const int b = at.b, h = at.h, r0 = at.r0, nrows = at.nrows, most = at.most;
+    const int first = at.batch, nb = at.nb;
+    const int64_t set0 = at.set0;
+    begin_set(s, h, r0, nrows);
+    clear();
+    int batch = first;
+    for (bool other = false; !other && left > 0; ++batch) {
+      other = advance();
+      const bool more = left > 0 && kBatch * at.batch < at.most;
+      if (left > 0) pg = page_at(at.b, kBatch * at.batch);
+      auto then_k = [&]() {
+        if (more) load_k(at.h, pg, kBatch * at.batch, at.most);
+      };
+      auto then_v = [&]() {
+        if (more) load_v(at.h, pg, kBatch * at.batch, at.most);
+      };
+      if (kBatch * batch < most) {
+        compute(kBatch * batch, most, true, then_k, then_v);
+      } else {
+        then_k();
+        then_v();
+      }
+    }
+    // An infinite value times a rest of 0 (or below 0) is no infinity any more: once more without
+    // the rests, where a sum came out as NaN.
+    bool nan = false;
+#pragma unroll
+    for (int k = 0; k < NB; ++k)
+#pragma unroll
+      for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) nan |= o[k][x][w][e] != o[k][x][w][e];
+    if (__any_sync(0xffffffffu, nan)) {
+      clear();
+#pragma unroll 1
+      for (int x = first; x < batch && kBatch * x < most; ++x) {
+        const int page = page_at(b, kBatch * x);
+        load_k(h, page, kBatch * x, most);
+        load_v(h, page, kBatch * x, most);
+        compute(kBatch * x, most, false, [] {}, [] {});
+      }
+      if (left > 0 && kBatch * at.batch < at.most) {
+        load_k(at.h, pg, kBatch * at.batch, at.most);
+        load_v(at.h, pg, kBatch * at.batch, at.most);
+      }
+    }
+    // ---- its rows
+    const bool begins = first == 0, ends = batch == nb;
+    const int64_t part = 2 * (int64_t)me + (begins ? 1 : 0);
 #pragma unroll
     for (int k = 0; k < NB; ++k)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int r = 8 * k + 2 * lj + e;
-        see[k][e] = r < nrows ? past + (r0 + r) / g + 1 : 0;
-      }
-    uint4 kx[2][D / 32], vx[4][D / 64];
-    float bias[2];
-    int kpage = 0;  // page of the slots in kx
-    auto page_of = [&](int e0) { return e0 < end ? paged_page(a, table, e0) : -1; };
-    // Slots past the end repeat the last one (their weight is 0, their V zeroed).
-    auto load_k = [&](int e0, int pg) {
-      const int64_t at = (int64_t)max(pg, 0);
-      const int in = e0 & mask, left = end - e0;
-      const __nv_bfloat16* base = Kh + at * a.s_page;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int r = in + min(lg + 8 * i, left - 1);
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) kx[i][c] = ld_once(base + r * a.s_slot + 32 * c);
-        bias[i] = pg < 0 ? -INFINITY : Bh != nullptr ? Bh[at * beta_page + r] : 0.f;
-      }
-    };
-    auto load_v = [&](int e0, int pg) {
-      const int in = e0 & mask, left = end - e0;
-      const __nv_bfloat16* base = Vh + (int64_t)max(pg, 0) * a.s_page;
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int r = in + min(2 * lj + (v & 1) + 8 * (v >> 1), left - 1);
-#pragma unroll
-        for (int x = 0; x < D / 64; ++x) vx[v][x] = ld_once(base + r * a.s_slot + 64 * x);
-      }
-    };
-    float m[NB][2], l[NB][2];       // rows 2 lj, 2 lj + 1 of a block; l: this lane's share
-    float o[NB][D / 64][4][4];      // O^T: channels 64 x + 8 lg + 2 u (+1), rows 2 lj (+1)
-    uint4 qf[NB][D / 32];
-    bool rests = true;  // the product with P's rounding rests
-    for (;;) {
-      const int e_first = ua * kUnit + 16 * warp;
-      kpage = page_of(e_first);
-      int next = page_of(e_first + kUnit);  // page of the following slots, one step ahead
-      if (e_first < end) {
-        load_k(e_first, kpage);
-        load_v(e_first, kpage);
-      }
-#pragma unroll
-      for (int k = 0; k < NB; ++k) {
-        const int r = 8 * k + lg;
-        const bool ok = r < nrows;
-        const int tok = s.first + (r0 + r) / g, qh = h * g + (r0 + r) % g;
-        const __nv_bfloat16* qp = p.q + (ok ? (int64_t)tok * p.s_q + (int64_t)qh * D : 0) + 8 * lj;
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c)
-          qf[k][c] = ok ? *reinterpret_cast<const uint4*>(qp + 32 * c) : make_uint4(0, 0, 0, 0);
-        m[k][0] = m[k][1] = -INFINITY;
-        l[k][0] = l[k][1] = 0.f;
-#pragma unroll
-        for (int x = 0; x < D / 64; ++x)
-#pragma unroll
-          for (int w = 0; w < 4; ++w)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[k][x][w][e] = 0.f;
-      }
-#pragma unroll 1
-      for (int e0 = e_first; e0 < end; e0 += kUnit) {
-        const int left = end - e0;
-        float c[NB][4];
-        const float b0 = bias[0], b1 = bias[1];
-#pragma unroll
-        for (int k = 0; k < NB; ++k) {
-          float c2[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) c[k][e] = 0.f;
-#pragma unroll
-          for (int x = 0; x < D / 32; ++x) {
-            mma_bf16(c[k], kx[0][x].x, kx[1][x].x, kx[0][x].y, kx[1][x].y, qf[k][x].x, qf[k][x].y);
-            mma_bf16(c2, kx[0][x].z, kx[1][x].z, kx[0][x].w, kx[1][x].w, qf[k][x].z, qf[k][x].w);
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) c[k][e] += c2[e];
-        }
-        // the next slots' K
-        if (e0 + kUnit < end) load_k(e0 + kUnit, next);
-        kpage = next;
-        next = page_of(e0 + 2 * kUnit);
-        // slots whose value does not count: 0 * inf would be NaN
-        const unsigned dead0 = __ballot_sync(0xffffffffu, b0 == -INFINITY || lg >= left);
-        const unsigned dead1 = __ballot_sync(0xffffffffu, b1 == -INFINITY || lg + 8 >= left);
-        if (dead0 | dead1) {
-#pragma unroll
-          for (int v = 0; v < 4; ++v)
-            if (((v >> 1 ? dead1 : dead0) >> (4 * (2 * lj + (v & 1)))) & 1)
-#pragma unroll
-              for (int x = 0; x < D / 64; ++x) vx[v][x] = make_uint4(0, 0, 0, 0);
-        }
-        uint32_t hi[NB][2], lo[NB][2];
-#pragma unroll
-        for (int k = 0; k < NB; ++k) {
-          float top[2];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {  // slot lg + 8 (e / 2), row 2 lj + e % 2
-            const float be = e >> 1 ? b1 : b0;
-            const bool ok = e0 + lg + 8 * (e >> 1) < see[k][e & 1] && be != -INFINITY;
-            c[k][e] = ok ? c[k][e] * p.scale + be : -INFINITY;
-          }
-          bool moved = false;
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            top[e] = fmaxf(c[k][e], c[k][e + 2]);
-#pragma unroll
-            for (int x = 4; x <= 16; x <<= 1)
-              top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], x));
-            moved |= top[e] > m[k][e];
-          }
-          if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const float n = fmaxf(m[k][e], top[e]);
-              const float f = n == m[k][e] ? 1.f : exp2f((m[k][e] - n) * kLog2e);
-              m[k][e] = n;
-              l[k][e] *= f;
-#pragma unroll
-              for (int x = 0; x < D / 64; ++x)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                  o[k][x][w][e] *= f;
-                  o[k][x][w][e + 2] *= f;
-                }
-            }
-          }
-          // nothing seen yet: every weight is 2^-inf
-          const float by0 = m[k][0] == -INFINITY ? 0.f : m[k][0];
-          const float by1 = m[k][1] == -INFINITY ? 0.f : m[k][1];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float w0 = exp2f((c[k][2 * i] - by0) * kLog2e);
-            const float w1 = exp2f((c[k][2 * i + 1] - by1) * kLog2e);
-            l[k][0] += w0;
-            l[k][1] += w1;
-            const __nv_bfloat162 ph = __floats2bfloat162_rn(w0, w1);
-            const float2 r = __bfloat1622float2(ph);
-            hi[k][i] = transpose8(bf16x2_bits(ph));
-            lo[k][i] = transpose8(bf16x2_bits(__floats2bfloat162_rn(w0 - r.x, w1 - r.y)));
-          }
-        }
-#pragma unroll
-        for (int x = 0; x < D / 64; ++x)
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const uint32_t v0 = word(vx[0][x], w), v1 = word(vx[1][x], w);
-            const uint32_t v2 = word(vx[2][x], w), v3 = word(vx[3][x], w);
-            const uint32_t a0 = __byte_perm(v0, v1, 0x5410), a1 = __byte_perm(v0, v1, 0x7632);
-            const uint32_t a2 = __byte_perm(v2, v3, 0x5410), a3 = __byte_perm(v2, v3, 0x7632);
-#pragma unroll
-            for (int k = 0; k < NB; ++k) {
-              mma_bf16(o[k][x][w], a0, a1, a2, a3, hi[k][0], hi[k][1]);
-              if (rests) mma_bf16(o[k][x][w], a0, a1, a2, a3, lo[k][0], lo[k][1]);
-            }
-          }
-        if (e0 + kUnit < end) load_v(e0 + kUnit, kpage);
-      }
-      // An infinite value times a rest of 0 (or below 0) is no infinity any more: once more
-      // without the rests, where a sum came out as NaN.
-      bool nan = false;
-      if (rests) {
-#pragma unroll
-        for (int k = 0; k < NB; ++k)
-#pragma unroll
-          for (int x = 0; x < D / 64; ++x)
-#pragma unroll
-            for (int w = 0; w < 4; ++w)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) nan |= o[k][x][w][e] != o[k][x][w][e];
-      }
-      if (!__any_sync(0xffffffffu, nan)) break;
-      rests = false;
-    }
-    // ---- the warps' states, a block of 8 rows at a time
-    const bool begins = ua == 0, ends = ub == nu;
-    float* part = join.parts + (int64_t)(2 * blockIdx.x + (begins ? 1 : 0)) * R::kPart;
-#pragma unroll
-    for (int k = 0; k < NB; ++k) {
-      if (8 * k >= nrows) break;
-      if (k > 0) __syncthreads();
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float* row = red[warp][2 * lj + e];
 #pragma unroll
         for (int x = 4; x <= 16; x <<= 1) l[k][e] += __shfl_xor_sync(0xffffffffu, l[k][e], x);
-#pragma unroll
-        for (int x = 0; x < D / 64; ++x) {
-          float* at = row + 64 * x + 8 * lg;
-          *reinterpret_cast<float4*>(at) =
-              make_float4(o[k][x][0][e], o[k][x][0][e + 2], o[k][x][1][e], o[k][x][1][e + 2]);
-          *reinterpret_cast<float4*>(at + 4) =
-              make_float4(o[k][x][2][e], o[k][x][2][e + 2], o[k][x][3][e], o[k][x][3][e + 2]);
-        }
-        if (lg == 0) {
-          row[D] = m[k][e];
-          row[D + 1] = l[k][e];
-        }
-      }
-      __syncthreads();
-      const int nr = min(8, nrows - 8 * k);
-      for (int it = threadIdx.x; it < nr * D; it += kRowThreads) {
-        const int r = it / D, col = it % D;
-        float M = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < kRowWarps; ++w) M = fmaxf(M, red[w][r][D]);
-        float L = 0.f, O = 0.f;
-#pragma unroll
-        for (int w = 0; w < kRowWarps; ++w) {
-          // a warp that saw nothing has sums of 0, or of NaN
-          const float f = red[w][r][D] == M ? 1.f : exp2f((red[w][r][D] - M) * kLog2e);
-          L += f * red[w][r][D + 1];
-          O += f * red[w][r][col];
-        }
-        const int row = r0 + 8 * k + r;
+        const int r = 8 * k + 2 * lj + e;
+        if (r >= nrows) continue;
         if (begins && ends) {
-          p.out[((int64_t)(s.first + row / g) * p.Hq + h * g + row % g) * D + col] =
-              __float2bfloat16_rn(L == 0.f ? 0.f : O / L);
-        } else {
-          part[(8 * k + r) * D + col] = O;
-          if (col == 0)
-            *reinterpret_cast<float2*>(part + kRows * D + 2 * (8 * k + r)) = make_float2(M, L);
-        }
-      }
-    }
-    if (!(begins && ends)) {
-      // the CTAs that hold the set's first and last unit
-      const int c0 = (int)(((su + 1) * nct - 1) / total);
-      const int c1 = (int)(((su + nu) * nct - 1) / total);
-      __threadfence();
-      __syncthreads();
-      if (threadIdx.x == 0) is_last = atomicAdd(&join.arrived[c0], 1) == c1 - c0;
-      __syncthreads();
-      if (is_last) {
-        __threadfence();
-        for (int it = threadIdx.x; it < nrows * D; it += kRowThreads) {
-          const int r = it / D, col = it % D;
-          const float* first = join.parts + (int64_t)(2 * c0 + 1) * R::kPart;
-          float M = -INFINITY, L = 0.f, O = 0.f;
-#pragma unroll 4
-          for (int c = c0; c <= c1; ++c) {
-            const float* x = c == c0 ? first : join.parts + (int64_t)(2 * c) * R::kPart;
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(x + kRows * D + 2 * r));
-            const float xo = __ldcg(x + r * D + col);
-            const float n = fmaxf(M, ml.x);
-            const float f = M == n ? 1.f : exp2f((M - n) * kLog2e);
-            const float w = ml.x == n ? 1.f : exp2f((ml.x - n) * kLog2e);
-            L = L * f + ml.y * w;
-            O = O * f + xo * w;
-            M = n;
+          const float inv = l[k][e] == 0.f ? 0.f : 1.f / l[k][e];
+          __nv_bfloat16* dst = p.out + ((int64_t)(s.first + (r0 + r) / g) * p.Hq + h * g +
+                                        (r0 + r) % g) * D + 8 * lg;
+#pragma unroll
+          for (int x = 0; x < D / 64; ++x) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              w[i] = bf16x2_bits(__floats2bfloat162_rn(o[k][x][i][e] * inv, o[k][x][i][e + 2] * inv));
+            *reinterpret_cast<uint4*>(dst + 64 * x) = make_uint4(w[0], w[1], w[2], w[3]);
           }
-          const int row = r0 + r;
-          p.out[((int64_t)(s.first + row / g) * p.Hq + h * g + row % g) * D + col] =
-              __float2bfloat16_rn(L == 0.f ? 0.f : O / L);
+        } else {
+          float* dst = join.part_o + (part * kRows + r) * D + 8 * lg;
+#pragma unroll
+          for (int x = 0; x < D / 64; ++x) {
+            *reinterpret_cast<float4*>(dst + 64 * x) = make_float4(
+                o[k][x][0][e], o[k][x][0][e + 2], o[k][x][1][e], o[k][x][1][e + 2]);
+            *reinterpret_cast<float4*>(dst + 64 * x + 4) = make_float4(
+                o[k][x][2][e], o[k][x][2][e + 2], o[k][x][3][e], o[k][x][3][e + 2]);
+          }
+          if (lg == 0) join.part_ml[part * kRows + r] = make_float2(m[k][e], l[k][e]);
         }
-        if (threadIdx.x == 0) join.arrived[c0] = 0;
+      }
+    if (begins && !ends && lane == 0)
+      join.split[me] = RowsSplit{(int)(((set0 + nb) * nw - 1) / total), s.first, r0, nrows, h};
+  }
+}
+
+// The sets that several warps share. A block looks at kJoinSets warps' sets: those of few parts are
+// joined row by row, a warp a row; one of many (there is at most one: it begins once in as many
+// warps) by all warps, which share its rows and parts out.
+constexpr int kJoinWarps = 16;
+constexpr int kJoinSets = 4;
+constexpr int kJoinFew = 16;
+
+template <int D>
+__global__ void __launch_bounds__(32 * kJoinWarps)
+    paged_rows_join_kernel(const RowsJoin join, int warps, int kRows, int g, int Hq,
+                           __nv_bfloat16* __restrict__ out) {
+  griddep_wait();
+  constexpr int kPer = D / 32;  // channels of a lane
+  __shared__ float red[kJoinWarps][D + 2];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  float M, L, O[kPer];
+  // parts i, i + step, ... of row r of the set that warp `from` begins, in order
+  auto add_up = [&](int from, int last, int r, int i, int step) {
+    M = -INFINITY;
+    L = 0.f;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) O[e] = 0.f;
+    for (int w0 = from + i; w0 <= last; w0 += 32 * step) {
+      const int n = min(32, (last - w0) / step + 1);
+      const int w = w0 + lane * step;
+      auto slot = [&](int x) { return (int64_t)(x == from ? 2 * x + 1 : 2 * x) * kRows + r; };
+      const float2 ml =
+          lane < n ? join.part_ml[slot(w)] : make_float2(-INFINITY, 0.f);  // a lane a part
+      float m = fmaxf(M, ml.x);
+#pragma unroll
+      for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+      const float f = M == m ? 1.f : exp2f((M - m) * kLog2e);
+      const float weight = ml.x == m ? 1.f : exp2f((ml.x - m) * kLog2e);
+      float sum = lane < n ? weight * ml.y : 0.f;
+#pragma unroll
+      for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+      M = m;
+      L = L * f + sum;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) O[e] *= f;
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) {
+        const float v = __shfl_sync(0xffffffffu, weight, j);
+        const float* src = join.part_o + slot(w0 + j * step) * D + kPer * lane;
+#pragma unroll
+        for (int e = 0; e < kPer; e += 2) {
+          const float2 x = *reinterpret_cast<const float2*>(src + e);
+          O[e] += v * x.x;
+          O[e + 1] += v * x.y;
+        }
       }
     }
-    u = su + ub;
-    if (u < u1) __syncthreads();  // red and is_last are written again
+  };
+  auto write = [&](const RowsSplit& q, int r) {
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    const int row = q.row0 + r;
+    __nv_bfloat162* dst = reinterpret_cast<__nv_bfloat162*>(
+        out + ((int64_t)(q.token0 + row / g) * Hq + q.h * g + row % g) * D + kPer * lane);
+#pragma unroll
+    for (int e = 0; e < kPer; e += 2) dst[e / 2] = __floats2bfloat162_rn(O[e] * inv, O[e + 1] * inv);
+  };
+  RowsSplit sets[kJoinSets];
+#pragma unroll
+  for (int k = 0; k < kJoinSets; ++k) {
+    const int w = blockIdx.x * kJoinSets + k;
+    sets[k].last = -1;
+    if (w < warps) sets[k] = join.split[w];
   }
+  int task = warp, large = -1;
+#pragma unroll
+  for (int k = 0; k < kJoinSets; ++k) {
+    const int from = blockIdx.x * kJoinSets + k, parts = sets[k].last - from + 1;
+    if (parts < 2) continue;
+    if (parts > kJoinFew) {
+      large = k;
+      continue;
+    }
+    for (; task < sets[k].rows; task += kJoinWarps) {
+      add_up(from, sets[k].last, task, 0, 1);
+      write(sets[k], task);
+    }
+    task -= sets[k].rows;
+  }
+  if (large < 0) return;
+  const int from = blockIdx.x * kJoinSets + large;
+  RowsSplit q = sets[0];
+#pragma unroll
+  for (int k = 1; k < kJoinSets; ++k)
+    if (k == large) q = sets[k];
+  const int shares = max(1, kJoinWarps / q.rows);  // of a row's parts
+  if (warp < q.rows * shares) {
+    add_up(from, q.last, warp / shares, warp % shares, shares);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) red[warp][kPer * lane + e] = O[e];
+    if (lane == 0) {
+      red[warp][D] = M;
+      red[warp][D + 1] = L;
+    }
+  }
+  __syncthreads();
+  if (warp >= q.rows) return;
+  const float* sums = red[warp * shares];
+  M = -INFINITY;
+  for (int i = 0; i < shares; ++i) M = fmaxf(M, sums[i * (D + 2) + D]);
+  L = 0.f;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) O[e] = 0.f;
+  for (int i = 0; i < shares; ++i) {
+    const float* x = sums + i * (D + 2);
+    const float v = x[D] == M ? 1.f : exp2f((x[D] - M) * kLog2e);
+    L += v * x[D + 1];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) O[e] += v * x[kPer * lane + e];
+  }
+  write(q, warp);
 }
 
 template <int D, int NB>
 struct RowsLaunch {
   static int ctas(int num_sms) { return num_sms * Rows<D, NB>::kMinCtas; }
-  static cudaError_t run(const PagedArgs& a, const PagedQuery& p, void* ws, int* arrived,
-                         int num_sms, cudaStream_t s) {
-    RowsJoin join;
-    join.parts = static_cast<float*>(ws);
-    join.arrived = arrived;
-    paged_rows_kernel<D, NB><<<ctas(num_sms), kRowThreads, 0, s>>>(a, p, join);
-    return cudaGetLastError();
-  }
   static size_t bytes(int num_sms) {
-    return (size_t)2 * ctas(num_sms) * Rows<D, NB>::kPart * sizeof(float);
+    const size_t parts = (size_t)2 * ctas(num_sms) * kRowWarps * Rows<D, NB>::kRows;
+    return parts * (D * sizeof(float) + sizeof(float2)) +
+           (size_t)ctas(num_sms) * kRowWarps * sizeof(RowsSplit);
+  }
+  static cudaError_t run(const PagedArgs& a, const PagedQuery& p, void* ws, int num_sms,
+                         cudaStream_t s) {
+    const int warps = ctas(num_sms) * kRowWarps, rows = Rows<D, NB>::kRows;
+    RowsJoin join;
+    join.part_o = static_cast<float*>(ws);
+    join.part_ml = reinterpret_cast<float2*>(join.part_o + (int64_t)2 * warps * rows * D);
+    join.split = reinterpret_cast<RowsSplit*>(join.part_ml + (int64_t)2 * warps * rows);
+    paged_rows_kernel<D, NB><<<ctas(num_sms), kRowThreads, 0, s>>>(a, p, join);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    return launch_chained(paged_rows_join_kernel<D>, dim3((warps + kJoinSets - 1) / kJoinSets),
+                          dim3(32 * kJoinWarps), 0, s, 1, join, warps, rows, p.Hq / a.H, p.Hq,
+                          p.out);
   }
 };
 
@@ -561,10 +719,9 @@ size_t paged_rows_workspace(const PagedArgs& a, int Hq, int num_sms) {
   return rows_form(a.d, Hq / a.H, [&](auto form) { return form.bytes(num_sms); });
 }
 
-cudaError_t launch_paged_rows(const PagedArgs& a, const PagedQuery& p, void* ws, int* arrived,
-                              int num_sms, cudaStream_t s) {
-  return rows_form(a.d, p.Hq / a.H,
-                   [&](auto form) { return form.run(a, p, ws, arrived, num_sms, s); });
+cudaError_t launch_paged_rows(const PagedArgs& a, const PagedQuery& p, void* ws, int num_sms,
+                              cudaStream_t s) {
+  return rows_form(a.d, p.Hq / a.H, [&](auto form) { return form.run(a, p, ws, num_sms, s); });
 }
 
 }  // namespace still

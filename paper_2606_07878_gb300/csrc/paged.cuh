@@ -52,11 +52,11 @@ struct PagedQuery {
   int32_t Hq = 0;
   float scale = 0.f;
 };
-// ws: paged_rows_workspace bytes; arrived: kPagedJoins counters, zero between calls.
-constexpr int kPagedJoins = 8192;
+// Few rows (paged.cu), and the join of what several warps share: two launches. ws:
+// paged_rows_workspace bytes.
 size_t paged_rows_workspace(const PagedArgs& a, int Hq, int num_sms);
-cudaError_t launch_paged_rows(const PagedArgs& a, const PagedQuery& q, void* ws, int* arrived,
-                              int num_sms, cudaStream_t s);
+cudaError_t launch_paged_rows(const PagedArgs& a, const PagedQuery& q, void* ws, int num_sms,
+                              cudaStream_t s);
 
 // Many rows, on the tensor cores (paged_prefill.cu), and the join of what several CTAs share: two
 // launches. Groups of more than 128 query heads do not fit a tile.

@@ -170,7 +170,6 @@ struct still_ctx {
   int device = 0;
   KernelTable kernels;  // of this device
   int* err = nullptr;  // device error record [4]
-  int* arrived = nullptr;  // [kPagedJoins] of the attention over a paged cache
   std::vector<LayerW> layers;
   void* ws = nullptr;
   size_t ws_bytes = 0;
@@ -1487,11 +1486,7 @@ still_status still_create(int device, still_ctx** out) {
   int sms = 0;
   if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess ||
       cudaMalloc(&c->err, 4 * sizeof(int)) != cudaSuccess ||
-      cudaMemset(c->err, 0, 4 * sizeof(int)) != cudaSuccess ||
-      cudaMalloc(&c->arrived, kPagedJoins * sizeof(int)) != cudaSuccess ||
-      cudaMemset(c->arrived, 0, kPagedJoins * sizeof(int)) != cudaSuccess) {
-    cudaFree(c->err);
-    cudaFree(c->arrived);
+      cudaMemset(c->err, 0, 4 * sizeof(int)) != cudaSuccess) {
     delete c;
     return STILL_ERR_CUDA;
   }
@@ -1507,7 +1502,6 @@ still_status still_destroy(still_ctx* ctx) {
   for (auto& L : ctx->layers) free_layer(L);
   if (ctx->ws) cudaFree(ctx->ws);
   if (ctx->err) cudaFree(ctx->err);
-  if (ctx->arrived) cudaFree(ctx->arrived);
   delete ctx;
   return STILL_OK;
 }
@@ -1807,7 +1801,8 @@ still_status paged_attend(still_ctx* ctx, const still_paged_cache* cache,
     return STILL_OK;
   }
   TRY(ensure_ws(ctx, paged_rows_workspace(a, Hq, nsm)));
-  KLAUNCH(STILL_K_PAGED_ATTEND, launch_paged_rows(a, p, ctx->ws, ctx->arrived, nsm, s));
+  KLAUNCH(STILL_K_PAGED_ATTEND, launch_paged_rows(a, p, ctx->ws, nsm, s));
+  ctx->prof.launches[STILL_K_PAGED_ATTEND] += 1;  // the join
   return STILL_OK;
 }
 
