@@ -162,9 +162,11 @@ struct RowsSplit {
   int32_t last;  // the warp that ends it; w: there is none
   int32_t token0, row0, rows;  // the sequence's first new token, the set's rows
   int32_t h;
+  int32_t cta0, cta1;  // CTAs [cta0, cta1) whose warps have nothing but this set: one part each
 };
 struct RowsJoin {
-  // parts of the sets that several warps share: what warp w continues (2 w), begins (2 w + 1)
+  // parts of the sets that several warps share: what warp w continues (2 w), begins (2 w + 1); a
+  // CTA's common part is its first warp's
   float* part_o = nullptr;     // [2 x warps][kRows][d]
   float2* part_ml = nullptr;   // [2 x warps][kRows] (m, l)
   RowsSplit* split = nullptr;  // [warps]
@@ -184,6 +186,7 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
   __shared__ int64_t warp_sum[kRowWarps];
   __shared__ int64_t at_batch[kRowWarps];  // batches before sequence at_seq
   __shared__ int at_seq[kRowWarps];
+  __shared__ __align__(16) float red[kRowWarps][4][D + 4];  // four rows of each warp, m and l behind
   constexpr bool kQShared = Rows<D, NB>::kQShared;
   __shared__ uint4 q_shared[kQShared ? kRowWarps : 1][kQShared ? NB * (D / 32) : 1][32];
   const int g = p.Hq / a.H;
@@ -515,20 +518,88 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
       }
     }
     // ---- its rows
+#pragma unroll
+    for (int k = 0; k < NB; ++k)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int x = 4; x <= 16; x <<= 1) l[k][e] += __shfl_xor_sync(0xffffffffu, l[k][e], x);
+    auto out_row = [&](int r) {
+      return p.out + ((int64_t)(s.first + (r0 + r) / g) * p.Hq + h * g + (r0 + r) % g) * D;
+    };
+    // CTAs [cta0, cta1) lie in this set whole
+    int cta0 = 0, cta1 = 0;
+    if (ctas * kRowWarps == nw) {
+      cta0 = (int)((set0 * ctas + total - 1) / total);
+      cta1 = (int)((set0 + nb) * ctas / total);
+    }
+    if ((int)blockIdx.x >= cta0 && (int)blockIdx.x < cta1) {
+      // ---- one part of this CTA: its warps' states, four rows at a time
+      const bool begins = total * blockIdx.x / ctas == set0;
+      const bool ends = total * (blockIdx.x + 1) / ctas == set0 + nb;
+      const int64_t part = 2 * (int64_t)kRowWarps * blockIdx.x + (begins ? 1 : 0);
+#pragma unroll
+      for (int q = 0; q < 2 * NB; ++q) {
+        if (4 * q >= nrows) break;
+        if (q > 0) __syncthreads();
+        if (lj >> 1 == (q & 1)) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float* row = red[warp][2 * (lj & 1) + e];
+#pragma unroll
+            for (int x = 0; x < D / 64; ++x) {
+              float* dst = row + 64 * x + 8 * lg;
+              *reinterpret_cast<float4*>(dst) =
+                  make_float4(o[q / 2][x][0][e], o[q / 2][x][0][e + 2], o[q / 2][x][1][e],
+                              o[q / 2][x][1][e + 2]);
+              *reinterpret_cast<float4*>(dst + 4) =
+                  make_float4(o[q / 2][x][2][e], o[q / 2][x][2][e + 2], o[q / 2][x][3][e],
+                              o[q / 2][x][3][e + 2]);
+            }
+            if (lg == 0) {
+              row[D] = m[q / 2][e];
+              row[D + 1] = l[q / 2][e];
+            }
+          }
+        }
+        __syncthreads();
+        const int nr = min(4, nrows - 4 * q);
+        for (int it = threadIdx.x; it < nr * D; it += kRowThreads) {
+          const int r = it / D, col = it % D;
+          float M = -INFINITY, L = 0.f, O = 0.f;
+#pragma unroll
+          for (int w = 0; w < kRowWarps; ++w) M = fmaxf(M, red[w][r][D]);
+#pragma unroll
+          for (int w = 0; w < kRowWarps; ++w) {
+            // a warp that saw nothing has sums of 0, or of NaN
+            const float f = red[w][r][D] == M ? 1.f : exp2f((red[w][r][D] - M) * kLog2e);
+            L += f * red[w][r][D + 1];
+            O += f * red[w][r][col];
+          }
+          if (begins && ends) {
+            out_row(4 * q + r)[col] = __float2bfloat16_rn(L == 0.f ? 0.f : O / L);
+          } else {
+            join.part_o[(part * kRows + 4 * q + r) * D + col] = O;
+            if (col == 0) join.part_ml[part * kRows + 4 * q + r] = make_float2(M, L);
+          }
+        }
+      }
+      if (begins && !ends && threadIdx.x == 0)
+        join.split[me] =
+            RowsSplit{(int)(((set0 + nb) * nw - 1) / total), s.first, r0, nrows, h, cta0, cta1};
+      return;  // it was all of this CTA's range
+    }
     const bool begins = first == 0, ends = batch == nb;
     const int64_t part = 2 * (int64_t)me + (begins ? 1 : 0);
 #pragma unroll
     for (int k = 0; k < NB; ++k)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-#pragma unroll
-        for (int x = 4; x <= 16; x <<= 1) l[k][e] += __shfl_xor_sync(0xffffffffu, l[k][e], x);
         const int r = 8 * k + 2 * lj + e;
         if (r >= nrows) continue;
         if (begins && ends) {
           const float inv = l[k][e] == 0.f ? 0.f : 1.f / l[k][e];
-          __nv_bfloat16* dst = p.out + ((int64_t)(s.first + (r0 + r) / g) * p.Hq + h * g +
-                                        (r0 + r) % g) * D + 8 * lg;
+          __nv_bfloat16* dst = out_row(r) + 8 * lg;
 #pragma unroll
           for (int x = 0; x < D / 64; ++x) {
             uint32_t w[4];
@@ -550,16 +621,18 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
         }
       }
     if (begins && !ends && lane == 0)
-      join.split[me] = RowsSplit{(int)(((set0 + nb) * nw - 1) / total), s.first, r0, nrows, h};
+      join.split[me] =
+          RowsSplit{(int)(((set0 + nb) * nw - 1) / total), s.first, r0, nrows, h, cta0, cta1};
   }
 }
 
 // The sets that several warps share. A block looks at kJoinSets warps' sets: those of few parts are
 // joined row by row, a warp a row; one of many (there is at most one: it begins once in as many
-// warps) by all warps, which share its rows and parts out.
+// warps) by all warps, which share its rows and parts out. What bounds it is one dependent read of
+// memory after another, of a microsecond each: the set, m and l of its parts, O.
 constexpr int kJoinWarps = 16;
 constexpr int kJoinSets = 4;
-constexpr int kJoinFew = 16;
+constexpr int kJoinFew = 8;
 
 template <int D>
 __global__ void __launch_bounds__(32 * kJoinWarps)
@@ -570,39 +643,54 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
   __shared__ float red[kJoinWarps][D + 2];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   float M, L, O[kPer];
-  // parts i, i + step, ... of row r of the set that warp `from` begins, in order
-  auto add_up = [&](int from, int last, int r, int i, int step) {
+  // Parts of a set: its first warps', then those of its whole CTAs, then its last warps'.
+  auto parts_of = [](const RowsSplit& q, int from) {
+    return q.last - from + 1 - (kRowWarps - 1) * max(0, q.cta1 - q.cta0);
+  };
+  auto slot_of = [](const RowsSplit& q, int from, int i) -> int64_t {
+    int w = from + i;
+    if (q.cta1 > q.cta0 && w > kRowWarps * q.cta0) {
+      const int c = w - kRowWarps * q.cta0;  // CTAs, then single warps
+      w = kRowWarps * q.cta0 + kRowWarps * min(c, q.cta1 - q.cta0) + max(0, c - (q.cta1 - q.cta0));
+    }
+    return i == 0 ? 2 * w + 1 : 2 * w;
+  };
+  // parts i, i + step, ... of n of row r of the set that warp `from` begins, in order
+  auto add_up = [&](const RowsSplit& q, int from, int n, int r, int i, int step) {
     M = -INFINITY;
     L = 0.f;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) O[e] = 0.f;
-    for (int w0 = from + i; w0 <= last; w0 += 32 * step) {
-      const int n = min(32, (last - w0) / step + 1);
-      const int w = w0 + lane * step;
-      auto slot = [&](int x) { return (int64_t)(x == from ? 2 * x + 1 : 2 * x) * kRows + r; };
-      const float2 ml =
-          lane < n ? join.part_ml[slot(w)] : make_float2(-INFINITY, 0.f);  // a lane a part
+    for (int i0 = i; i0 < n; i0 += 32 * step) {
+      const int here = min(32, (n - i0 - 1) / step + 1);
+      // a lane a part
+      const int64_t mine = slot_of(q, from, min(i0 + lane * step, n - 1)) * kRows + r;
+      const float2 ml = lane < here ? join.part_ml[mine] : make_float2(-INFINITY, 0.f);
       float m = fmaxf(M, ml.x);
 #pragma unroll
       for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
       const float f = M == m ? 1.f : exp2f((M - m) * kLog2e);
       const float weight = ml.x == m ? 1.f : exp2f((ml.x - m) * kLog2e);
-      float sum = lane < n ? weight * ml.y : 0.f;
+      float sum = lane < here ? weight * ml.y : 0.f;
 #pragma unroll
       for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
       M = m;
       L = L * f + sum;
 #pragma unroll
       for (int e = 0; e < kPer; ++e) O[e] *= f;
-#pragma unroll 8
-      for (int j = 0; j < n; ++j) {
+#pragma unroll 4
+      for (int j = 0; j < here; ++j) {
         const float v = __shfl_sync(0xffffffffu, weight, j);
-        const float* src = join.part_o + slot(w0 + j * step) * D + kPer * lane;
+        const float* src = join.part_o + __shfl_sync(0xffffffffu, mine, j) * D + kPer * lane;
 #pragma unroll
-        for (int e = 0; e < kPer; e += 2) {
-          const float2 x = *reinterpret_cast<const float2*>(src + e);
-          O[e] += v * x.x;
-          O[e + 1] += v * x.y;
+        for (int e = 0; e < kPer; e += kPer < 4 ? 2 : 4) {
+          float x[4];
+          if constexpr (kPer < 4)
+            *reinterpret_cast<float2*>(x) = *reinterpret_cast<const float2*>(src + e);
+          else
+            *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(src + e);
+#pragma unroll
+          for (int y = 0; y < (kPer < 4 ? 2 : 4); ++y) O[e + y] += v * x[y];
         }
       }
     }
@@ -625,27 +713,25 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
   int task = warp, large = -1;
 #pragma unroll
   for (int k = 0; k < kJoinSets; ++k) {
-    const int from = blockIdx.x * kJoinSets + k, parts = sets[k].last - from + 1;
-    if (parts < 2) continue;
+    const int from = blockIdx.x * kJoinSets + k;
+    if (sets[k].last <= from) continue;
+    const int parts = parts_of(sets[k], from);
     if (parts > kJoinFew) {
       large = k;
       continue;
     }
     for (; task < sets[k].rows; task += kJoinWarps) {
-      add_up(from, sets[k].last, task, 0, 1);
+      add_up(sets[k], from, parts, task, 0, 1);
       write(sets[k], task);
     }
     task -= sets[k].rows;
   }
   if (large < 0) return;
   const int from = blockIdx.x * kJoinSets + large;
-  RowsSplit q = sets[0];
-#pragma unroll
-  for (int k = 1; k < kJoinSets; ++k)
-    if (k == large) q = sets[k];
+  const RowsSplit q = join.split[from];
   const int shares = max(1, kJoinWarps / q.rows);  // of a row's parts
   if (warp < q.rows * shares) {
-    add_up(from, q.last, warp / shares, warp % shares, shares);
+    add_up(q, from, parts_of(q, from), warp / shares, warp % shares, shares);
 #pragma unroll
     for (int e = 0; e < kPer; ++e) red[warp][kPer * lane + e] = O[e];
     if (lane == 0) {
