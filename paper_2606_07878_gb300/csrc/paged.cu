@@ -222,8 +222,16 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
   const int ctas = gridDim.x;
   auto range_of = [&](int w) { return ctas * kRowWarps == nw ? blockIdx.x * kRowWarps + w
                                                              : w * ctas + blockIdx.x; };
+  // the first `wider` ranges have one batch more than `width`
+  const int64_t width = total / nw;
+  const int wider = (int)(total - width * nw);
+  auto range_at = [&](int w) { return width * w + min(w, wider); };
+  auto warp_at = [&](int64_t u) {  // whose range holds batch u; nw at the end
+    const int64_t x = (width + 1) * wider;
+    return (int)(u < x ? u / (width + 1) : width > 0 ? wider + (u - x) / width : wider);
+  };
   for (int w = 0; w < kRowWarps; ++w) {
-    const int64_t u = total * min(range_of(w), nw) / nw;
+    const int64_t u = range_at(min(range_of(w), nw));
     if (u < before || u >= before + mine) continue;
     int64_t at = before;
     int b = sb0;
@@ -247,7 +255,7 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
   const int me = range_of(warp);
   if (lane == 0) join.split[me].last = me;
   if (me >= nw || total == 0) return;
-  const int64_t u0 = total * me / nw, u1 = total * (me + 1) / nw;
+  const int64_t u0 = range_at(me), u1 = range_at(me + 1);
   const int mask = (1 << a.page_shift) - 1;
   const int64_t beta_page = (int64_t)a.H << a.page_shift;
 
@@ -270,7 +278,7 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
   {
     const int64_t in = u0 - at_batch[warp];
     const int nblk = seq_blocks<kRows>(at.s, g);
-    const int64_t set = in / at.nb;
+    const int64_t set = in < (int64_t)INT32_MAX ? (int)in / at.nb : in / at.nb;
     at.h = (int)(set / nblk);
     at.r0 = (int)(set % nblk) * kRows;
     at.batch = (int)(in - set * at.nb);
@@ -530,13 +538,14 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
     // CTAs [cta0, cta1) lie in this set whole
     int cta0 = 0, cta1 = 0;
     if (ctas * kRowWarps == nw) {
-      cta0 = (int)((set0 * ctas + total - 1) / total);
-      cta1 = (int)((set0 + nb) * ctas / total);
+      const int w0 = warp_at(set0);
+      cta0 = (w0 + (range_at(w0) < set0) + kRowWarps - 1) / kRowWarps;
+      cta1 = warp_at(set0 + nb) / kRowWarps;
     }
     if ((int)blockIdx.x >= cta0 && (int)blockIdx.x < cta1) {
       // ---- one part of this CTA: its warps' states, four rows at a time
-      const bool begins = total * blockIdx.x / ctas == set0;
-      const bool ends = total * (blockIdx.x + 1) / ctas == set0 + nb;
+      const bool begins = range_at(kRowWarps * blockIdx.x) == set0;
+      const bool ends = range_at(kRowWarps * (blockIdx.x + 1)) == set0 + nb;
       const int64_t part = 2 * (int64_t)kRowWarps * blockIdx.x + (begins ? 1 : 0);
 #pragma unroll
       for (int q = 0; q < 2 * NB; ++q) {
@@ -586,7 +595,7 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
       }
       if (begins && !ends && threadIdx.x == 0)
         join.split[me] =
-            RowsSplit{(int)(((set0 + nb) * nw - 1) / total), s.first, r0, nrows, h, cta0, cta1};
+            RowsSplit{warp_at(set0 + nb - 1), s.first, r0, nrows, h, cta0, cta1};
       return;  // it was all of this CTA's range
     }
     const bool begins = first == 0, ends = batch == nb;
@@ -622,7 +631,7 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
       }
     if (begins && !ends && lane == 0)
       join.split[me] =
-          RowsSplit{(int)(((set0 + nb) * nw - 1) / total), s.first, r0, nrows, h, cta0, cta1};
+          RowsSplit{warp_at(set0 + nb - 1), s.first, r0, nrows, h, cta0, cta1};
   }
 }
 
