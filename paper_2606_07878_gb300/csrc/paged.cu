@@ -163,6 +163,7 @@ struct RowsSplit {
   int32_t token0, row0, rows;  // the sequence's first new token, the set's rows
   int32_t h;
   int32_t cta0, cta1;  // CTAs [cta0, cta1) whose warps have nothing but this set: one part each
+  int32_t unused;
 };
 struct RowsJoin {
   // parts of the sets that several warps share: what warp w continues (2 w), begins (2 w + 1); a
@@ -595,7 +596,7 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
       }
       if (begins && !ends && threadIdx.x == 0)
         join.split[me] =
-            RowsSplit{warp_at(set0 + nb - 1), s.first, r0, nrows, h, cta0, cta1};
+            RowsSplit{warp_at(set0 + nb - 1), s.first, r0, nrows, h, cta0, cta1, 0};
       return;  // it was all of this CTA's range
     }
     const bool begins = first == 0, ends = batch == nb;
@@ -631,7 +632,7 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
       }
     if (begins && !ends && lane == 0)
       join.split[me] =
-          RowsSplit{warp_at(set0 + nb - 1), s.first, r0, nrows, h, cta0, cta1};
+          RowsSplit{warp_at(set0 + nb - 1), s.first, r0, nrows, h, cta0, cta1, 0};
   }
 }
 
@@ -712,50 +713,58 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
 #pragma unroll
     for (int e = 0; e < kPer; e += 2) dst[e / 2] = __floats2bfloat162_rn(O[e] * inv, O[e + 1] * inv);
   };
-  RowsSplit sets[kJoinSets];
-#pragma unroll
-  for (int k = 0; k < kJoinSets; ++k) {
-    const int w = blockIdx.x * kJoinSets + k;
-    sets[k].last = -1;
-    if (w < warps) sets[k] = join.split[w];
-  }
+  // lanes 0 .. 3 hold the sets of the block's warps
+  const int first = blockIdx.x * kJoinSets;
+  RowsSplit mine{-1, 0, 0, 0, 0, 0, 0, 0};
+  if (lane < kJoinSets && first + lane < warps) mine = join.split[first + lane];
+  unsigned todo = __ballot_sync(0xffffffffu, mine.last > first + lane);
   int task = warp, large = -1;
+  RowsSplit q;
+#pragma unroll 1
+  while (todo != 0) {  // (one loop for all of it: the code is fetched anew at every launch)
+    const int k = __ffs(todo) - 1, from = first + k;
+    todo &= todo - 1;
+    q.last = __shfl_sync(0xffffffffu, mine.last, k);
+    q.token0 = __shfl_sync(0xffffffffu, mine.token0, k);
+    q.row0 = __shfl_sync(0xffffffffu, mine.row0, k);
+    q.rows = __shfl_sync(0xffffffffu, mine.rows, k);
+    q.h = __shfl_sync(0xffffffffu, mine.h, k);
+    q.cta0 = __shfl_sync(0xffffffffu, mine.cta0, k);
+    q.cta1 = __shfl_sync(0xffffffffu, mine.cta1, k);
+    const int parts = parts_of(q, from);
+    const int shares = parts > kJoinFew ? max(1, kJoinWarps / q.rows) : 1;  // of a row's parts
+    for (; task < q.rows * shares; task += kJoinWarps) {
+      add_up(q, from, parts, task / shares, task % shares, shares);
+      if (shares == 1) {
+        write(q, task);
+      } else {
 #pragma unroll
-  for (int k = 0; k < kJoinSets; ++k) {
-    const int from = blockIdx.x * kJoinSets + k;
-    if (sets[k].last <= from) continue;
-    const int parts = parts_of(sets[k], from);
-    if (parts > kJoinFew) {
-      large = k;
-      continue;
+        for (int e = 0; e < kPer; ++e) red[task][kPer * lane + e] = O[e];
+        if (lane == 0) {
+          red[task][D] = M;
+          red[task][D + 1] = L;
+        }
+      }
     }
-    for (; task < sets[k].rows; task += kJoinWarps) {
-      add_up(sets[k], from, parts, task, 0, 1);
-      write(sets[k], task);
-    }
-    task -= sets[k].rows;
+    task -= q.rows * shares;
+    if (shares > 1) large = k;
   }
   if (large < 0) return;
-  const int from = blockIdx.x * kJoinSets + large;
-  const RowsSplit q = join.split[from];
-  const int shares = max(1, kJoinWarps / q.rows);  // of a row's parts
-  if (warp < q.rows * shares) {
-    add_up(q, from, parts_of(q, from), warp / shares, warp % shares, shares);
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) red[warp][kPer * lane + e] = O[e];
-    if (lane == 0) {
-      red[warp][D] = M;
-      red[warp][D + 1] = L;
-    }
-  }
   __syncthreads();
+  q.rows = __shfl_sync(0xffffffffu, mine.rows, large);
   if (warp >= q.rows) return;
+  q.token0 = __shfl_sync(0xffffffffu, mine.token0, large);
+  q.row0 = __shfl_sync(0xffffffffu, mine.row0, large);
+  q.h = __shfl_sync(0xffffffffu, mine.h, large);
+  const int shares = kJoinWarps / q.rows;
   const float* sums = red[warp * shares];
   M = -INFINITY;
+#pragma unroll 1
   for (int i = 0; i < shares; ++i) M = fmaxf(M, sums[i * (D + 2) + D]);
   L = 0.f;
 #pragma unroll
   for (int e = 0; e < kPer; ++e) O[e] = 0.f;
+#pragma unroll 2
   for (int i = 0; i < shares; ++i) {
     const float* x = sums + i * (D + 2);
     const float v = x[D] == M ? 1.f : exp2f((x[D] - M) * kLog2e);
