@@ -57,14 +57,14 @@ struct PfShape {
   static constexpr int kTiles = D <= 128 ? 2 : 1;
   static constexpr int kChan = D < 128 ? D : 128;   // channels of a ring slot
   static constexpr int kHalves = D / kChan;          // ring slots of a K or V tile
-  static constexpr int kSlotBytes = kPfKeys * kChan * 2;
+  static constexpr int kStageBytes = kPfKeys * kChan * 2;
   static constexpr int kChunkBytes = kPfKeys * 128;  // 64 channels of 128 rows
   static constexpr int kQBytes = kTiles * (D / 64) * kChunkBytes;
-  static constexpr int kSlots = D == 64 ? 8 : D == 256 || kBias ? 4 : 5;
+  static constexpr int kStages = D == 64 ? 8 : D == 256 || kBias ? 4 : 5;
   static constexpr int kCols = kTiles == 2 ? 128 : 64;  // S columns per softmax thread
   static constexpr int kOCols = kTiles == 2 ? D : D / 2;  // O columns per softmax thread
   static constexpr int kRing = kQBytes;
-  static constexpr int kBiasAt = kRing + kSlots * kSlotBytes;  // [8 warps][kCols]
+  static constexpr int kBiasAt = kRing + kStages * kStageBytes;  // [8 warps][kCols]
   static constexpr int kXchAt = kBiasAt + (kBias ? 8 * kCols * 4 : 0);  // [2][2][128], one tile only
   static constexpr int kBarAt = kXchAt + (kTiles == 1 ? 2048 : 0);
   static constexpr int kBytes = kBarAt + 352 + 1024;
@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
                          const __grid_constant__ CUtensorMap tm_v,
                          const __grid_constant__ PrefillParams f) {
   using S = PfShape<D, kBias>;
-  constexpr int kTiles = S::kTiles, kSlots = S::kSlots, kHalves = S::kHalves;
+  constexpr int kTiles = S::kTiles, kStages = S::kStages, kHalves = S::kHalves;
   extern __shared__ uint8_t smem_raw[];
   __shared__ PfStart start;
   __shared__ PfItem shown[2];  // items n & 1 as the producer shows them to the others
@@ -275,10 +275,10 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kBarAt);  // ring slot loaded
-  uint64_t* empty = full + kSlots;   // ring slot consumed
+  uint64_t* empty = full + kStages;   // ring slot consumed
   // [2] q of item n loaded and the item shown, n & 1. (The softmax of an item of one tile of slots
   // may wait for it only when the next one's q has come as well.)
-  uint64_t* qfull = empty + kSlots;
+  uint64_t* qfull = empty + kStages;
   uint64_t* qfree = qfull + 2;       // an item's last S complete
   uint64_t* sfull = qfree + 1;       // [2] S_i complete
   uint64_t* pfull = sfull + 2;       // [2] P_i written (and O rescaled where needed)
@@ -286,11 +286,11 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   uint64_t* ofree = pvdone + 2;      // O drained at the end of an item
   uint64_t* xb = ofree + 1;          // [4] row-value exchange per lane quarter
   uint64_t* landed = xb + 4;         // the copies into a ring slot that has rows to be zeroed
-  uint64_t* phalf = landed + kSlots;      // [2] the first 64 slots of P_i written (two tiles only)
+  uint64_t* phalf = landed + kStages;      // [2] the first 64 slots of P_i written (two tiles only)
   uint64_t* drain = phalf + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((3 * kSlots + 17) * 8 + 8 <= 352, "barriers");
+  static_assert((3 * kStages + 17) * 8 + 8 <= 352, "barriers");
 
   const PagedArgs& a = f.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   constexpr int kOAt = 2 * kSCols;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kSlots; ++s) {
+    for (int s = 0; s < kStages; ++s) {
       mbar_init(&full[s], 1);
       mbar_init(&empty[s], 1);
       mbar_init(&landed[s], 1);
@@ -391,9 +391,10 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   if (warp == 0 || warp >= 10) {
     // ------------------------------------------------------------ TMA producers
     const int me = warp == 0 ? 0 : warp - 9;  // 0 also loads q, arms the barriers and zeroes rows
-    int slot = 0, n_items = 0;
+    int stage = 0, n_items = 0;
     uint32_t phase = 0;
-    uint32_t armed = 0, armed_par = 0, land_par = 0;
+    uint32_t armed = 0, armed_par = 0;  // stages whose copies were asked for, and their phases
+    uint32_t marked = 0, land_par = 0;  // the same of `landed`, the phase after
     bool q_armed = false, bad = false;
     const int rows = min(1 << a.page_shift, kPfKeys);  // of a box
     auto wait = [&](uint64_t* bar, uint32_t parity, int where) {
@@ -402,14 +403,17 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     };
     // One half (kChan channels) of tile kt of K or V into the next ring slot.
     auto load = [&](const CUtensorMap* tm, const PfItem& it, int kt, int half, uint32_t mark) {
-      if (!wait(&empty[slot], phase ^ 1, 610)) return;
+      if (!wait(&empty[stage], phase ^ 1, 610)) return;
       // A slot with rows to be zeroed is full when that is done, a moment after its copies.
       const bool any = __any_sync(0xffffffffu, mark != 0);
-      uint64_t* bar = any ? &landed[slot] : &full[slot];
-      if (me == 0 && lane == 0) mbar_arrive_expect_tx(bar, S::kSlotBytes);
+      uint64_t* bar = any ? &landed[stage] : &full[stage];
+      if (me == 0 && lane == 0) mbar_arrive_expect_tx(bar, S::kStageBytes);
       if (!any) {
-        armed |= 1u << slot;
-        armed_par = (armed_par & ~(1u << slot)) | (phase << slot);
+        armed |= 1u << stage;
+        armed_par = (armed_par & ~(1u << stage)) | (phase << stage);
+      } else {
+        marked |= 1u << stage;
+        land_par ^= 1u << stage;
       }
       __syncwarp();
       const int boxes = kPfKeys / rows * (S::kChan / 64);
@@ -419,17 +423,16 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         // a box outside the pool (past the last page, or of an entry that names none) is zeros
         int pg = j < it.len ? paged_page(a, a.table + (int64_t)it.b * a.s_table, j) : -1;
         if (pg < 0) pg = a.n_pages;
-        tma_load_4d(smem + S::kRing + slot * S::kSlotBytes + c * S::kChunkBytes + r * 128, tm,
+        tma_load_4d(smem + S::kRing + stage * S::kStageBytes + c * S::kChunkBytes + r * 128, tm,
                     bar, half * S::kChan + c * 64, j & ((1 << a.page_shift) - 1), it.h, pg);
       }
       if (any && me == 0) {
-        if (!wait(&landed[slot], (land_par >> slot) & 1, 614)) return;
-        land_par ^= 1u << slot;
-        zero_rows(smem + S::kRing + slot * S::kSlotBytes, S::kChan / 64, mark);
-        if (lane == 0) mbar_arrive(&full[slot]);
+        if (!wait(&landed[stage], ((land_par >> stage) & 1) ^ 1, 614)) return;
+        zero_rows(smem + S::kRing + stage * S::kStageBytes, S::kChan / 64, mark);
+        if (lane == 0) mbar_arrive(&full[stage]);
       }
-      if (++slot == kSlots) {
-        slot = 0;
+      if (++stage == kStages) {
+        stage = 0;
         phase ^= 1;
       }
     };
@@ -489,28 +492,41 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     }
     // The CTA may leave only when nothing is on its way into its shared memory: the last arrivals
     // of the issuer's commits, or copies that nobody waited for.
-    for (int i = 0; i < kSlots && me == 0 && !bad && !warp_flag(abort_flag); ++i) {
-      wait(&empty[slot], phase ^ 1, 612);
-      if (++slot == kSlots) {
-        slot = 0;
-        phase ^= 1;
+    if (me == 0 && lane == 0 && !bad) {
+      for (int i = 0; i < kStages && !bad && !*abort_flag; ++i) {
+        if (!mbar_wait(&empty[stage], phase ^ 1)) {
+          dev_set_error(a.err, DEV_WAIT_TIMEOUT, 612);
+          *abort_flag = 1;
+          bad = true;
+        }
+        if (++stage == kStages) {
+          stage = 0;
+          phase ^= 1;
+        }
+      }
+      if (!bad && !*abort_flag && n_items > 0 && !mbar_wait(qfree, (n_items - 1) & 1)) {
+        dev_set_error(a.err, DEV_WAIT_TIMEOUT, 613);
+        *abort_flag = 1;
+      }
+      if (!*abort_flag) {  // no more items
+        shown[n_items & 1].k0 = shown[n_items & 1].k1 = 0;
+        mbar_arrive(&qfull[n_items & 1]);
       }
     }
-    if (me == 0 && n_items > 0 && !bad && !warp_flag(abort_flag)) wait(qfree, (n_items - 1) & 1, 613);
-    if (me == 0 && lane == 0 && !bad && !*abort_flag) {  // no more items
-      shown[n_items & 1].k0 = shown[n_items & 1].k1 = 0;
-      mbar_arrive(&qfull[n_items & 1]);
-    }
-    if (me == 0 && (bad || warp_flag(abort_flag))) {
-      for (int s = 0; s < kSlots; ++s)
-        if (armed & (1u << s)) (void)mbar_wait(&full[s], (armed_par >> s) & 1);
-      if (q_armed) (void)mbar_wait(&qfull[(n_items - 1) & 1], ((n_items - 1) >> 1) & 1);
+    if (lane == 0) {
+      if (bad || *abort_flag) {
+        for (int s = 0; s < kStages; ++s) {
+          if (armed & (1u << s)) (void)mbar_wait(&full[s], (armed_par >> s) & 1);
+          if (marked & (1u << s)) (void)mbar_wait(&landed[s], ((land_par >> s) & 1) ^ 1);
+        }
+        if (q_armed) (void)mbar_wait(&qfull[(n_items - 1) & 1], ((n_items - 1) >> 1) & 1);
+      }
     }
   } else if (warp == 1 && elect_one()) {
     // ------------------------------------------------------------ MMA issuer
     constexpr uint32_t idesc_s = idesc_f16(128, kPfKeys, 1);
     constexpr uint32_t idesc_o = idesc_f16(128, S::kChan, 1) | kIdescBMn;
-    int slot = 0;
+    int stage = 0;
     uint32_t phase = 0;
     uint32_t n_i = 0, n_items = 0;  // S tiles and items so far
     bool bad = false, issued = false;
@@ -523,10 +539,10 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     };
     // The next ring slot, loaded; -1 at a time-out.
     auto take = [&]() -> int {
-      if (!wait(&full[slot], phase, 620)) return -1;
-      const int s = slot;
-      if (++slot == kSlots) {
-        slot = 0;
+      if (!wait(&full[stage], phase, 620)) return -1;
+      const int s = stage;
+      if (++stage == kStages) {
+        stage = 0;
         phase ^= 1;
       }
       return s;
@@ -534,12 +550,12 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     const uint64_t q_desc = sdesc_k_sw128(smem_u32(smem));
     const uint64_t k_desc = sdesc_k_sw128(smem_u32(smem + S::kRing));
     const uint64_t v_desc = sdesc_mn_sw128(smem_u32(smem + S::kRing), S::kChunkBytes);
-    constexpr uint64_t kChunkStep = S::kChunkBytes >> 4, kSlotStep = S::kSlotBytes >> 4;
+    constexpr uint64_t kChunkStep = S::kChunkBytes >> 4, kStageStep = S::kStageBytes >> 4;
     // S of tile t into buffer buf, over the channels of one ring slot
     auto mma_s = [&](int buf, int t, int half, int s) {
       tc_fence_after();
       const uint64_t q = q_desc + (t * (D / 64) + half * (S::kChan / 64)) * kChunkStep;
-      const uint64_t k = k_desc + s * kSlotStep;
+      const uint64_t k = k_desc + s * kStageStep;
 #pragma unroll
       for (int c = 0; c < S::kChan / 64; ++c)
 #pragma unroll
@@ -551,7 +567,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     // O of tile t, the channels of one ring slot, += P in buffer buf times V
     auto mma_o = [&](int buf, int t, int half, int s, bool first, int e0 = 0, int e1 = kPfKeys / 16) {
       tc_fence_after();
-      const uint64_t v = v_desc + s * kSlotStep;
+      const uint64_t v = v_desc + s * kStageStep;
 #pragma unroll
       for (int e = e0; e < e1; ++e)
         mma_ts(tmem_base + kOAt + t * D + half * S::kChan, tmem_base + buf * kSCols + 8 * e,

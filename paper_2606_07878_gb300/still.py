@@ -214,6 +214,10 @@ def _ptr(x):
 def _stream(stream):
     if stream is None:
         import torch
+        # the handle alone, where torch gives it: a Stream object around it takes 3 us a call
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return ctypes.c_void_p(raw(torch.cuda.current_device()))
         return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
@@ -449,10 +453,10 @@ class PagedBatch:
 def _rows(x, H, d):
     """Data pointer and token pitch of [n, H, d] bf16 rows whose heads are contiguous."""
     import torch
-    sn, sh, sd = x.stride()
-    assert x.dtype == torch.bfloat16 and x.shape[1:] == (H, d), "bf16 [n, H, d] rows"
+    (n, heads, channels), (sn, sh, sd) = x.shape, x.stride()
+    assert x.dtype == torch.bfloat16 and heads == H and channels == d, "bf16 [n, H, d] rows"
     assert sd == 1 and (sh == d or H == 1), "contiguous heads"
-    return x.data_ptr(), sn if x.shape[0] > 1 else H * d
+    return x.data_ptr(), sn if n > 1 else H * d
 
 
 def still_paged_append(ctx, cache, batch, k, v, q=None, q_out=None, beta=None, rope_theta=0.0,
