@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   uint64_t* ofree = pvdone + 2;      // O drained at the end of an item
   uint64_t* xb = ofree + 1;          // [4] row-value exchange per lane quarter
   uint64_t* landed = xb + 4;         // the copies into a ring slot that has rows to be zeroed
-  uint64_t* phalf = landed + kStages;      // [2] the first 64 slots of P_i written (two tiles only)
+  uint64_t* phalf = landed + kStages;      // [2] the last 64 slots of P_i written (two tiles only)
   uint64_t* drain = phalf + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -296,8 +296,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = f.q.Hq / a.H;
   const int tokens = f.tile_tokens * kTiles;  // of an item
-  constexpr int kSCols = 128;                 // TMEM: S (P) at 128 i, O behind both
-  constexpr int kOAt = 2 * kSCols;
+  // TMEM: S at 128 i, P over those of its columns that are read first, O behind both
+  constexpr int kSCols = 128, kOAt = 2 * kSCols;
+  constexpr int kPAt = kTiles == 2 ? 64 : 0;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -570,8 +571,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       const uint64_t v = v_desc + s * kStageStep;
 #pragma unroll
       for (int e = e0; e < e1; ++e)
-        mma_ts(tmem_base + kOAt + t * D + half * S::kChan, tmem_base + buf * kSCols + 8 * e,
-               v + e * (2048 >> 4), idesc_o, !first || e > 0);
+        mma_ts(tmem_base + kOAt + t * D + half * S::kChan, tmem_base + buf * kSCols + kPAt + 8 * e,
+               v + e * (2048 >> 4), idesc_o, !first || e > e0);
     };
     while (!bad && !*abort_flag) {
       if (!wait(&qfull[n_items & 1], (n_items >> 1) & 1, 621)) break;
@@ -592,9 +593,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
           const int vs = take();
           if (vs < 0 || !wait(&phalf[0], n_i & 1, 622)) break;
           if (j == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 623)) break;
-          mma_o(0, 0, 0, vs, j == 0, 0, 4);
-          if (!wait(&pfull[0], n_i & 1, 627)) break;
           mma_o(0, 0, 0, vs, j == 0, 4, 8);
+          if (!wait(&pfull[0], n_i & 1, 627)) break;
+          mma_o(0, 0, 0, vs, false, 0, 4);
           tc_commit(&pvdone[0]);
           if (more) {
             if ((ks = take()) < 0) break;
@@ -602,9 +603,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
             tc_commit(&sfull[0]);
           }
           if (!wait(&phalf[1], n_i & 1, 624)) break;
-          mma_o(1, 1, 0, vs, j == 0, 0, 4);
-          if (!wait(&pfull[1], n_i & 1, 628)) break;
           mma_o(1, 1, 0, vs, j == 0, 4, 8);
+          if (!wait(&pfull[1], n_i & 1, 628)) break;
+          mma_o(1, 1, 0, vs, false, 0, 4);
           tc_commit(&pvdone[1]);
           tc_commit(&empty[vs]);
           if (more) {
@@ -783,9 +784,10 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         const float shift = kBias ? -by : -by * to_log2;
         const uint64_t by2 = pack2(shift, shift), k2 = pack2(to_log2, to_log2);
         uint64_t s0 = 0ull, s1 = 0ull;
+        // the last columns first: v still holds them
 #pragma unroll 1
-        for (int c = 0; c < kCols; c += 64) {
-          if (kCols > 64) logits(c);
+        for (int c = kCols - 64; c >= 0; c -= 64) {
+          if (c < kCols - 64) logits(c);
 #pragma unroll
           for (int e = 0; e < 64; e += 2) {
             float u0, u1;
@@ -798,8 +800,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
               s0 = add2(s0, pack2(p0, p1));
             v[e / 2] = bf16x2_bits(__floats2bfloat162_rn(p0, p1));
           }
-          tmem_st32_issue(s_at - col0 + (col0 + c) / 2, v);
-          if (kTiles == 2 && c == 0) {
+          tmem_st32_issue(s_at - col0 + kPAt + (col0 + c) / 2, v);
+          if (kTiles == 2 && c > 0) {
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
