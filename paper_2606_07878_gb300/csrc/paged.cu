@@ -226,11 +226,9 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
     total += warp_sum[w];
   }
   before -= mine;
-  const int nw = (int)max((int64_t)1, min((int64_t)gridDim.x * kRowWarps, total / kLeastBatches));
-  // The warps of a CTA are neighbours in the order of ranges where every warp has one, else spread.
-  const int ctas = gridDim.x;
-  auto range_of = [&](int w) { return ctas * kRowWarps == nw ? blockIdx.x * kRowWarps + w
-                                                             : w * ctas + blockIdx.x; };
+  // CTAs and warps that have a range: every warp of these CTAs, if there are batches for it
+  const int ctas = (int)max((int64_t)1, min((int64_t)gridDim.x, total / (kRowWarps * kLeastBatches)));
+  const int nw = (int)max((int64_t)1, min((int64_t)ctas * kRowWarps, total));
   // the first `wider` ranges have one batch more than `width`
   const int64_t width = total / nw;
   const int wider = (int)(total - width * nw);
@@ -240,7 +238,7 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
     return (int)(u < x ? u / (width + 1) : width > 0 ? wider + (u - x) / width : wider);
   };
   for (int w = 0; w < kRowWarps; ++w) {
-    const int64_t u = range_at(min(range_of(w), nw));
+    const int64_t u = range_at(min((int)blockIdx.x * kRowWarps + w, nw));
     if (u < before || u >= before + mine) continue;
     int64_t at = before;
     int b = sb0;
@@ -261,7 +259,7 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
       o[i] = make_uint4(0, 0, 0, 0);
   }
   __syncthreads();
-  const int me = range_of(warp);
+  const int me = blockIdx.x * kRowWarps + warp;
   if (lane == 0) join.split[me].last = me;
   if (me >= nw || total == 0) return;
   const int64_t u0 = range_at(me), u1 = range_at(me + 1);
@@ -807,11 +805,13 @@ struct RowsLaunch {
   }
 };
 
-// Calls f with the form that serves d channels and groups of g heads. 16 rows of 256 channels do
-// not fit a thread's registers beside their K and V: larger groups take several blocks of 8.
+// Calls f with the form that serves d channels and so many rows per sequence and KV-head: a block of
+// 16 that is half empty costs 15% (4 x 60,000 slots of 128 channels: 51 us against 41 to 45), two
+// blocks of 8 read everything twice. 16 rows of 256 channels do not fit a thread's registers beside
+// their K and V.
 template <class F>
-auto rows_form(int d, int g, F f) {
-  const bool two = g > 8;
+auto rows_form(int d, int rows, F f) {
+  const bool two = rows > 8;
   if (d == 64) return two ? f(RowsLaunch<64, 2>()) : f(RowsLaunch<64, 1>());
   if (d == 128) return two ? f(RowsLaunch<128, 2>()) : f(RowsLaunch<128, 1>());
   return f(RowsLaunch<256, 1>());
@@ -832,13 +832,18 @@ cudaError_t launch_paged_append(const PagedArgs& a, const PagedAppend& p, const 
   return cudaGetLastError();
 }
 
+int paged_mean_rows(const PagedArgs& a, int Hq) {
+  return (int)(((int64_t)a.n * (Hq / a.H) + a.B - 1) / a.B);
+}
+
 size_t paged_rows_workspace(const PagedArgs& a, int Hq, int num_sms) {
-  return rows_form(a.d, Hq / a.H, [&](auto form) { return form.bytes(num_sms); });
+  return rows_form(a.d, paged_mean_rows(a, Hq), [&](auto form) { return form.bytes(num_sms); });
 }
 
 cudaError_t launch_paged_rows(const PagedArgs& a, const PagedQuery& p, void* ws, int num_sms,
                               cudaStream_t s) {
-  return rows_form(a.d, p.Hq / a.H, [&](auto form) { return form.run(a, p, ws, num_sms, s); });
+  return rows_form(a.d, paged_mean_rows(a, p.Hq),
+                   [&](auto form) { return form.run(a, p, ws, num_sms, s); });
 }
 
 }  // namespace still

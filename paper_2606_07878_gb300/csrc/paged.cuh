@@ -54,13 +54,14 @@ struct PagedQuery {
 };
 // Few rows (paged.cu), and the join of what several warps share: two launches. ws:
 // paged_rows_workspace bytes.
+int paged_mean_rows(const PagedArgs& a, int Hq);  // of a sequence and KV-head, rounded up
 size_t paged_rows_workspace(const PagedArgs& a, int Hq, int num_sms);
 cudaError_t launch_paged_rows(const PagedArgs& a, const PagedQuery& q, void* ws, int num_sms,
                               cudaStream_t s);
 
 // Many rows, on the tensor cores (paged_prefill.cu), and the join of what several CTAs share: two
-// launches. Groups of more than 128 query heads do not fit a tile.
-bool paged_prefill_fits(const PagedArgs& a, int Hq);
+// launches. paged_prefill_serves: whether a call takes this kernel.
+bool paged_prefill_serves(const PagedArgs& a, int Hq);
 size_t paged_prefill_workspace(const PagedArgs& a, int num_sms);
 cudaError_t launch_paged_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
                                  const KernelTable& dev, cudaStream_t s);

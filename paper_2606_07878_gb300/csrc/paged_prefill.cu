@@ -912,7 +912,9 @@ __global__ void __launch_bounds__(256)
   float M = -INFINITY, L = 0.f, O[D / 8];
 #pragma unroll
   for (int e = 0; e < D / 8; ++e) O[e] = 0.f;
+#pragma unroll 8
   for (int p = c; p <= sp.last; ++p) M = fmaxf(M, f.part_ml[part(p) * item_rows + r].x);
+#pragma unroll 4
   for (int p = c; p <= sp.last; ++p) {
     const float2 ml = f.part_ml[part(p) * item_rows + r];
     const float w = ml.x == M ? 1.f : exp2f((ml.x - M) * to_log2);
@@ -996,7 +998,13 @@ cudaError_t launch_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
 
 }  // namespace
 
-bool paged_prefill_fits(const PagedArgs& a, int Hq) { return Hq / a.H <= 128; }
+bool paged_prefill_serves(const PagedArgs& a, int Hq) {
+  // Measured, us, few rows' kernel / this one, 16 sequences of 5,000 slots and 4 KV-heads (256
+  // channels: 2): 8 rows 28 / 39, 39 / 48, 42 / 49 for 64, 128, 256 channels; 16 rows 33 / 39,
+  // 49 / 48, 64 / 49; 32 rows 49 / 39, 80 / 49, 96 / 49. Groups of more than 128 query heads do not
+  // fit a tile.
+  return Hq / a.H <= 128 && paged_mean_rows(a, Hq) > (a.d == 256 ? 8 : 16);
+}
 
 size_t paged_prefill_workspace(const PagedArgs& a, int num_sms) {
   const size_t rows = a.d <= 128 ? 256 : 128;

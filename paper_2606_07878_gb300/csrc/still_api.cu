@@ -1793,8 +1793,7 @@ still_status paged_attend(still_ctx* ctx, const still_paged_cache* cache,
   CK(cudaSetDevice(ctx->device));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const int nsm = ctx->kernels.num_sms;
-  // more than a block of 16 rows per sequence: tiles on the tensor cores
-  if (n * (Hq / a.H) > 16 * (int64_t)a.B && a.cu_new != nullptr && paged_prefill_fits(a, Hq)) {
+  if (paged_prefill_serves(a, Hq)) {
     TRY(ensure_ws(ctx, paged_prefill_workspace(a, nsm)));
     KLAUNCH(STILL_K_PAGED_ATTEND, launch_paged_prefill(a, p, ctx->ws, ctx->kernels, s));
     ctx->prof.launches[STILL_K_PAGED_ATTEND] += 1;  // the join
