@@ -139,6 +139,12 @@ WEIGHTS = 2.0 ** -8 + 2.0 ** -11
     (256, 1, 3, 16, [1, 16, 47, 129], True, True),
     (256, 2, 18, 64, [65, 500], False, False),
     (256, 1, 33, 32, [100], False, False),
+    # slots of one set in many warps, groups that fit no tile, ranges shorter than a CTA
+    (256, 2, 4, 64, [30000], True, False),
+    (128, 1, 7, 16, [20000, 40, 12000], False, True),
+    (64, 1, 1, 256, [70000], False, False),
+    (64, 1, 160, 32, [200, 31], True, False),
+    (128, 1, 4, 16, [16], False, False),
 ])
 def test_decode_matches_64_bits(ctx, d, H, Hq, page, lens, beta, heads_first):
     p = Pages(1, lens, H, d, page, beta, heads_first)
@@ -168,6 +174,9 @@ def test_decode_matches_64_bits(ctx, d, H, Hq, page, lens, beta, heads_first):
     (256, 8, 16, 16, [700, 90, 350], [0, 1000, 64], False, False),
     (256, 2, 4, 64, [100], [5000], True, False),
     (256, 1, 128, 32, [3], [700], True, False),
+    (64, 1, 200, 16, [3, 1], [70, 0], False, False),
+    (128, 1, 2, 16, [(7 * i) % 23 for i in range(500)], [(11 * i) % 50 for i in range(500)], True,
+     False),
 ])
 def test_prefill_matches_64_bits(ctx, d, H, Hq, page, new, past, beta, heads_first):
     p = Pages(3, [a + b for a, b in zip(new, past)], H, d, page, beta, heads_first)
@@ -229,6 +238,23 @@ def test_values_of_the_lowest_size_and_infinities(ctx, d):
     out = torch.empty_like(q)
     still.still_paged_decode(ctx, p.cache(), batch_of(p), q, out)
     assert torch.isnan(out[0, 2]).all() and torch.isfinite(out[0, [0, 1, 3]]).all()
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_infinite_values_of_a_long_sequence(ctx, d):
+    """Infinite values among slots that many warps share stay in their channels; two of opposite
+    signs in one channel are NaN there."""
+    p = Pages(40, [4000, 300], 1, d, 16)
+    for j, c, x in ((17, 3, math.inf), (2500, 5, -math.inf), (3999, 9, math.inf),
+                    (100, 9, -math.inf)):
+        p.V[int(p.table[0, j // 16]), j % 16, 0, c] = x
+    q, = fused_rows(41, 2, [4], d)
+    out = torch.empty_like(q)
+    still.still_paged_decode(ctx, p.cache(), batch_of(p), q, out)
+    assert torch.isposinf(out[0, :, 3]).all() and torch.isneginf(out[0, :, 5]).all()
+    assert torch.isnan(out[0, :, 9]).all()
+    rest = [c for c in range(d) if c not in (3, 5, 9)]
+    assert torch.isfinite(out[0][:, rest]).all() and torch.isfinite(out[1]).all()
 
 
 def test_more_new_tokens_than_slots(ctx):
@@ -431,20 +457,25 @@ def test_device_side_faults_are_recorded():
         out = torch.empty(1, 1, 64, device=DEV, dtype=torch.bfloat16)
         good = p.table.clone()
         for bad in (-1, p.K.shape[0], 2 ** 31 - 1):
-            for call in ("append", "decode", "prefill"):
+            for call in ("append", "decode", "prefill", "prefill of many"):
                 p.table[0, 2] = bad
                 batch = batch_of(p)
                 if call == "append":
                     still.still_paged_append(c, p.cache(), batch, k, v)
                 elif call == "decode":
                     still.still_paged_decode(c, p.cache(), batch, q, out)
+                elif call == "prefill of many":
+                    many, = fused_rows(34, 40, [1], 64)
+                    still.still_paged_prefill(c, p.cache(), batch_of(p, [40]), many,
+                                              torch.empty_like(many))
                 else:
                     still.still_paged_prefill(c, p.cache(), batch, q, out)
                 assert recorded(), (bad, call)
         p.table.copy_(good)
         cap = p.table.shape[1] * 16
         p.table[0, 3:] = p.table[0, 0]
-        for lens, cu in (([cap + 1], None), ([-1], None), ([20], [0, 2]), ([20], [-1, 1])):
+        for lens, cu in (([cap + 1], None), ([-1], None), ([20], [0, 2]), ([20], [-1, 1]),
+                         ([20], [1, 0])):
             b = still.PagedBatch(p.table, i32(lens), None if cu is None else i32(cu))
             still.still_paged_prefill(c, p.cache(), b, q, out)
             assert recorded(), (lens, cu)
