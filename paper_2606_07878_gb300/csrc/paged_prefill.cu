@@ -52,25 +52,6 @@ struct PfSplit {
   int32_t token0, tokens, h;
 };
 
-template <int D, bool kBias>
-struct PfShape {
-  static constexpr int kTiles = D <= 128 ? 2 : 1;
-  static constexpr int kChan = D < 128 ? D : 128;   // channels of a ring slot
-  static constexpr int kHalves = D / kChan;          // ring slots of a K or V tile
-  static constexpr int kStageBytes = kPfKeys * kChan * 2;
-  static constexpr int kChunkBytes = kPfKeys * 128;  // 64 channels of 128 rows
-  static constexpr int kQBytes = kTiles * (D / 64) * kChunkBytes;
-  static constexpr int kStages = D == 64 ? 8 : D == 256 || kBias ? 4 : 5;
-  static constexpr int kCols = kTiles == 2 ? 128 : 64;  // S columns per softmax thread
-  static constexpr int kOCols = kTiles == 2 ? D : D / 2;  // O columns per softmax thread
-  static constexpr int kRing = kQBytes;
-  static constexpr int kBiasAt = kRing + kStages * kStageBytes;  // [8 warps][kCols]
-  static constexpr int kXchAt = kBiasAt + (kBias ? 8 * kCols * 4 : 0);  // [2][2][128], one tile only
-  static constexpr int kBarAt = kXchAt + (kTiles == 1 ? 2048 : 0);
-  static constexpr int kBytes = kBarAt + 352 + 1024;
-  static_assert(kBytes <= 232448, "shared memory budget");
-};
-
 // D[tmem] (+)= A[tmem, 128 lanes x 16] * B[smem, MN-major], kind::f16.
 STILL_DEV void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
                       uint32_t accumulate) {
@@ -181,6 +162,32 @@ STILL_DEV bool pf_wait(uint64_t* bar, uint32_t parity, int* err, volatile int* a
   return ok;
 }
 
+struct PfPlan {  // in shared memory
+  PfStart start;
+  PfItem shown[2];  // items n & 1 as the producer shows them to the others
+  int64_t warp_cost[kPfThreads / 32];
+};
+
+template <int D, bool kBias>
+struct PfShape {
+  static constexpr int kTiles = D <= 128 ? 2 : 1;
+  static constexpr int kChan = D < 128 ? D : 128;   // channels of a ring slot
+  static constexpr int kHalves = D / kChan;          // ring slots of a K or V tile
+  static constexpr int kStageBytes = kPfKeys * kChan * 2;
+  static constexpr int kChunkBytes = kPfKeys * 128;  // 64 channels of 128 rows
+  static constexpr int kQBytes = kTiles * (D / 64) * kChunkBytes;
+  static constexpr int kStages = D == 64 ? 8 : kBias ? 4 : 5;
+  static constexpr int kCols = kTiles == 2 ? 128 : 64;  // S columns per softmax thread
+  static constexpr int kOCols = kTiles == 2 ? D : D / 2;  // O columns per softmax thread
+  static constexpr int kRing = kQBytes;
+  static constexpr int kBiasAt = kRing + kStages * kStageBytes;  // [8 warps][kCols]
+  static constexpr int kXchAt = kBiasAt + (kBias ? 8 * kCols * 4 : 0);  // [2][2][128], one tile only
+  static constexpr int kBarAt = kXchAt + (kTiles == 1 ? 2048 : 0);
+  static constexpr int kPlanAt = kBarAt + 352;
+  static constexpr int kBytes = kPlanAt + sizeof(PfPlan);
+  static_assert(kBytes <= 232448, "shared memory budget");
+};
+
 STILL_DEV int pf_tiles(const Seq& s, int tokens) { return (s.count + tokens - 1) / tokens; }
 // Tiles of slots that item qt of a sequence sees.
 STILL_DEV int pf_slots(const Seq& s, int tokens, int qt) {
@@ -268,12 +275,17 @@ __global__ void __launch_bounds__(kPfThreads, 1)
                          const __grid_constant__ PrefillParams f) {
   using S = PfShape<D, kBias>;
   constexpr int kTiles = S::kTiles, kStages = S::kStages, kHalves = S::kHalves;
-  extern __shared__ uint8_t smem_raw[];
-  __shared__ PfStart start;
-  __shared__ PfItem shown[2];  // items n & 1 as the producer shows them to the others
-  __shared__ int64_t warp_cost[kPfThreads / 32];
-  uint8_t* smem = reinterpret_cast<uint8_t*>(
-      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  // All of it: no byte is left beside five stages of 256 channels, so the base has to be aligned as
+  // it is.
+  extern __shared__ __align__(1024) uint8_t smem[];
+  if ((smem_u32(smem) & 1023) != 0) {
+    dev_set_error(f.a.err, DEV_BAD_ARG, 602);
+    return;
+  }
+  PfPlan& plan = *reinterpret_cast<PfPlan*>(smem + S::kPlanAt);
+  PfStart& start = plan.start;
+  PfItem* shown = plan.shown;
+  int64_t* warp_cost = plan.warp_cost;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kBarAt);  // ring slot loaded
   uint64_t* empty = full + kStages;   // ring slot consumed
   // [2] q of item n loaded and the item shown, n & 1. (The softmax of an item of one tile of slots
