@@ -22,6 +22,7 @@
 // 16 slots are 128 copies a tile of 256 channels: 352 us with one, 0 and the others share them out),
 // 1 MMA issuer and TMEM allocation, 2..9 softmax and output. Every wait is bounded.
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm_host.cuh"
 #include "paged_dev.cuh"
@@ -541,7 +542,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     constexpr uint32_t idesc_o = idesc_f16(128, S::kChan, 1) | kIdescBMn;
     int stage = 0;
     uint32_t phase = 0;
-    uint32_t n_i = 0, n_items = 0;  // S tiles and items so far
+    uint32_t n_i = 0, n_odd = 0;  // uses of buffer 0 (two tiles: of both), of buffer 1
+    uint32_t n_items = 0;
     bool bad = false, issued = false;
     auto wait = [&](uint64_t* bar, uint32_t parity, int where) {
       if (mbar_wait(bar, parity)) return true;
@@ -600,7 +602,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         tc_commit(&empty[ks]);
         if (n_k == 1) tc_commit(qfree);
 #pragma unroll 1
-        for (int j = 0; j < n_k; ++j, ++n_i) {  // n_i: pairs of S tiles
+        for (int j = 0; j < n_k; ++j, ++n_i) {
           const bool more = j + 1 < n_k;
           const int vs = take();
           if (vs < 0 || !wait(&phalf[0], n_i & 1, 622)) break;
@@ -628,36 +630,43 @@ __global__ void __launch_bounds__(kPfThreads, 1)
           }
         }
       } else {
-        // step i: P_i V, then S_(i+2); i = -2, -1 are the first two S
-#pragma unroll 1
-        for (int i = -2; i < n_k && !bad; ++i) {
-          const int buf = (n_i + (i < 0 ? i + 2 : 0)) & 1;
-          if (i >= 0) {
-            if (!wait(&pfull[buf], (n_i >> 1) & 1, 625)) break;
-            if (i == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 626)) break;
-#pragma unroll 1
-            for (int half = 0; half < kHalves; ++half) {
-              const int s = take();
-              if (s < 0) break;
-              mma_o(buf, 0, half, s, i == 0);
-              tc_commit(&empty[s]);
-            }
-            if (bad) break;
-            tc_commit(&pvdone[buf]);
-            ++n_i;
+        // S and P take buffers 0 and 1 in turn, from 0 on in every item (constants: with a buffer and
+        // a half that the loop counts, issuing takes longer than the products)
+        auto make_s = [&](auto buf, int i) {
+#pragma unroll
+          for (int half = 0; half < kHalves; ++half) {
+            const int s = take();
+            if (s < 0) return;
+            mma_s(buf, 0, half, s);
+            tc_commit(&empty[s]);
           }
-          if (i + 2 < n_k) {
-#pragma unroll 1
-            for (int half = 0; half < kHalves; ++half) {
-              const int s = take();
-              if (s < 0) break;
-              mma_s(buf, 0, half, s);
-              tc_commit(&empty[s]);
-            }
-            if (bad) break;
-            tc_commit(&sfull[buf]);
-            if (i + 3 == n_k) tc_commit(qfree);
+          tc_commit(&sfull[buf]);
+          if (i + 1 == n_k) tc_commit(qfree);
+        };
+        auto add_pv = [&](auto buf, uint32_t& uses, int i) {
+          if (!wait(&pfull[buf], uses & 1, 625)) return;
+          if (i == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 626)) return;
+#pragma unroll
+          for (int half = 0; half < kHalves; ++half) {
+            const int s = take();
+            if (s < 0) return;
+            mma_o(buf, 0, half, s, i == 0);
+            tc_commit(&empty[s]);
           }
+          tc_commit(&pvdone[buf]);
+          ++uses;
+        };
+        constexpr std::integral_constant<int, 0> b0;
+        constexpr std::integral_constant<int, 1> b1;
+        make_s(b0, 0);
+        if (n_k > 1 && !bad) make_s(b1, 1);
+#pragma unroll 1
+        for (int i = 0; i < n_k && !bad; i += 2) {
+          add_pv(b0, n_i, i);
+          if (i + 2 < n_k && !bad) make_s(b0, i + 2);
+          if (i + 1 == n_k || bad) break;
+          add_pv(b1, n_odd, i + 1);
+          if (i + 3 < n_k && !bad) make_s(b1, i + 3);
         }
       }
       ++n_items;
@@ -681,7 +690,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     // exponents: with biases logits are natural (a bias of the lowest float must stay finite),
     // without them S itself is kept and the scale joins the factor
     const float to_log2 = kBias ? kLog2e : f.q.scale * kLog2e;
-    uint32_t n_i = kTiles == 2 ? wg : 0, n_x = 0;
+    uint32_t uses[2] = {0, 0}, n_x = 0;  // of the buffers of S so far
     bool bad = false;
     auto wait_all = [&](uint64_t* bar, uint32_t parity, int where) -> bool {
       if (!pf_wait(bar, parity, a.err, abort_flag, where)) bad = true;
@@ -708,11 +717,11 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       float m_run = -INFINITY, l_run = 0.f;
       PfBias<kCols> beta;
       if (kBias) beta.load(a, it, it.k0 * kPfKeys + col0, lane);
-      uint32_t last = 0;  // the S tile before
+      int buf = 0;
       const int least = __reduce_min_sync(0xffffffffu, see);  // slots that every row sees
 #pragma unroll 1
-      for (int kt = it.k0; kt < it.k1; ++kt, n_i += kTiles) {
-        const int buf = n_i & 1;
+      for (int kt = it.k0; kt < it.k1; ++kt) {
+        buf = kTiles == 2 ? wg : (kt - it.k0) & 1;
         const uint32_t s_at = lanes + buf * kSCols + col0;
         const int slot0 = kt * kPfKeys + col0;
         if constexpr (kBias) {
@@ -721,7 +730,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
           if (kt + 1 < it.k1) beta.load(a, it, slot0 + kPfKeys, lane);
           __syncwarp();
         }
-        if (!wait_all(&sfull[buf], (n_i >> 1) & 1, 630)) break;
+        if (!wait_all(&sfull[buf], (buf ? uses[1] : uses[0]) & 1, 630)) break;
         tc_fence_after();
         uint32_t v[64];
         // Columns [c, c + 64) as logits, -inf where the row does not see the slot.
@@ -780,7 +789,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         }
         // warp-collective: a warp rescales O when any of its rows needs it
         if (__any_sync(0xffffffffu, move) && kt > it.k0) {
-          if (!wait_all(&pvdone[last & 1], (last >> 1) & 1, 632)) break;
+          const int before = kTiles == 2 ? buf : buf ^ 1;  // where P of the tile before was
+          if (!wait_all(&pvdone[before], ((before ? uses[1] : uses[0]) - 1) & 1, 632)) break;
           tc_fence_after();
 #pragma unroll 1
           for (int c = 0; c < kOCols; c += 32) {
@@ -827,7 +837,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         tc_fence_before();
         __syncwarp();  // and kw is written again
         if (lane == 0) mbar_arrive(&pfull[buf]);
-        last = n_i;
+        ++(buf ? uses[1] : uses[0]);
       }
       if (bad) break;
       // ---- the item's rows
@@ -836,7 +846,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         l += exchange(l_run, 633);
         if (bad) break;
       }
-      if (!wait_all(&pvdone[last & 1], (last >> 1) & 1, 634)) break;
+      if (!wait_all(&pvdone[buf], ((buf ? uses[1] : uses[0]) - 1) & 1, 634)) break;
       tc_fence_after();
       const int oc = kTiles == 2 ? 0 : wg * kOCols;
       if (it.part != 0) {  // columns apart, so that a warp's rows lie side by side
