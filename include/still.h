@@ -322,8 +322,11 @@ still_status still_paged_append(still_ctx* ctx, const still_paged_cache* cache,
  * still_paged_decode: one token per sequence (cu_new must be NULL, n = B).
  * still_paged_prefill: any number of tokens per sequence, causal among them. A token's V is
  * expected finite even where earlier tokens of its call do not see it.
- * Device-side argument faults are recorded as by still_paged_append; slots of a page outside the
- * pool count as masked. */
+ * out must not overlap q or the pools. Device-side argument faults are recorded as by
+ * still_paged_append; what rows that would read a page outside the pool come out as is unspecified.
+ * Partial results lie in the context's workspace, whose size depends on head_dim alone (at most 41
+ * MB). The first call of a kind allocates it, so it belongs before a capture, and calls that share
+ * a context must be ordered on one stream or otherwise serialised. */
 still_status still_paged_decode(still_ctx* ctx, const still_paged_cache* cache,
                                 const still_paged_batch* batch, const void* q, int64_t q_stride,
                                 int32_t Hq, float scale, void* out, void* stream);

@@ -16,9 +16,10 @@ namespace {
 // turns. The sines and cosines of a token are formed once, in shared memory, and serve all its
 // heads.
 //
-// Memory bounds it: rows are read and written once. Two tokens a CTA: 8,192 tokens of 32 + 8 + 8 heads
-// of 128 channels in 37 us, against 39 with four or one and 41 with eight, whose chain of look-ups
-// and angles fewer other CTAs cover. Asking for the rows before the look-ups: 39 to 41.
+// Memory bounds it: rows are read and written once. Two tokens a CTA: 8,192 tokens of 32 + 8 + 8
+// heads of 128 channels in 37 us (201 MB: 5.5 TB/s, 0.81 of a copy), against 39 with four or one
+// and 41 with eight, whose chain of look-ups and angles fewer other CTAs cover. Asking for the
+// rows before the look-ups: 39 to 41.
 constexpr int kAppendThreads = 256;  // at most
 constexpr int kAppendTokens = 2;  // most tokens of a CTA
 
@@ -127,12 +128,20 @@ __global__ void __launch_bounds__(kAppendThreads)
 // 16, and all batches of all sets, one after another, into equal ranges, one per warp, from lengths
 // that the kernel itself adds up. A warp streams through its range without meeting another: K and V
 // of the next batch are on their way while it computes one, across the ends of sets too. A set that
-// lies in one range is written by its warp; the parts of another meet in the workspace, and a second
-// launch joins them in their order.
+// lies in one range is written by its warp; the parts of another meet in the workspace, and a
+// second launch joins them in their order. Ranges of CTAs instead, whose warps join after every
+// set, with the last CTA of a set joining its parts: 36 / 109 / 170 / 193 us where this takes 32 /
+// 90 / 169 / 178 (8 sequences of 1,311 to 1,600 slots; 256 of up to 1,024; 24 of 8,192 to 32,768;
+// one of 131,072 with 256 channels); the last warp joining in this kernel: 40 / 93 / 181 / 186.
+//
+// Memory bounds the large calls: the 24 sequences are 1.0 GB, 5.95 TB/s and 0.88 of a copy, with
+// the mma.sync pipe at 12%, so the tensor cores of tcgen05 would have nothing to gain. Small calls
+// are the latency of a chain of reads (lengths, table, K and V) and of the second launch: 32 us
+// for 8 sequences, of which 16 are memory.
 constexpr int kRowWarps = 4;  // of a CTA
 constexpr int kRowThreads = 32 * kRowWarps;
 constexpr int kBatch = 16;      // slots
-constexpr int kLeastBatches = 2;  // of a range, where there are fewer ranges than warps
+constexpr int kLeastBatches = 2;  // of a range, on average, where a call has few batches
 
 // c (16 x 8) += a (16 x 16 bf16) b (16 x 8 bf16)
 STILL_DEV void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
@@ -143,7 +152,8 @@ STILL_DEV void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, ui
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// The transpose of an 8 x 8 matrix of 16-bit values: lane i holds row i / 4, columns 2 (i % 4), + 1.
+// The transpose of an 8 x 8 matrix of 16-bit values: lane i holds row i / 4, columns 2 (i % 4) and
+// 2 (i % 4) + 1.
 STILL_DEV uint32_t transpose8(uint32_t x) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
@@ -195,7 +205,8 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
   __shared__ int64_t warp_sum[kRowWarps];
   __shared__ int64_t at_batch[kRowWarps];  // batches before sequence at_seq
   __shared__ int at_seq[kRowWarps];
-  __shared__ __align__(16) float red[kRowWarps][4][D + 4];  // four rows of each warp, m and l behind
+  // four rows of each warp, m and l behind
+  __shared__ __align__(16) float red[kRowWarps][4][D + 4];
   constexpr bool kQShared = Rows<D, NB>::kQShared;
   __shared__ uint4 q_shared[kQShared ? kRowWarps : 1][kQShared ? NB * (D / 32) : 1][32];
   const int g = p.Hq / a.H;
@@ -227,7 +238,8 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
   }
   before -= mine;
   // CTAs and warps that have a range: every warp of these CTAs, if there are batches for it
-  const int ctas = (int)max((int64_t)1, min((int64_t)gridDim.x, total / (kRowWarps * kLeastBatches)));
+  const int ctas =
+      (int)max((int64_t)1, min((int64_t)gridDim.x, total / (kRowWarps * kLeastBatches)));
   const int nw = (int)max((int64_t)1, min((int64_t)ctas * kRowWarps, total));
   // the first `wider` ranges have one batch more than `width`
   const int64_t width = total / nw;
@@ -315,7 +327,8 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
   uint4 kx[2][D / 32], vx[4][D / 64];
   float bias[2];
   // K, V and biases of slots [e0, min(e0 + 16, end)) of a KV-head; slots past the end repeat the
-  // last one (their weight is 0, their V zeroed). A batch past what its set's rows see is not loaded.
+  // last one (their weight is 0, their V zeroed). A batch past what its set's rows see is not
+  // loaded.
   auto load_k = [&](int h, int pg, int e0, int end) {
     const int in = e0 & mask, most = end - e0 - 1;
     const int64_t page = max(pg, 0);
@@ -378,8 +391,8 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
           for (int e = 0; e < 4; ++e) o[k][x][w][e] = 0.f;
     }
   };
-  // The batch of slots [e0, end) that kx, vx and bias hold. `then_k` and `then_v` may overwrite them
-  // where they are done with; rests: with P's rounding rests.
+  // The batch of slots [e0, end) that kx, vx and bias hold. `then_k` and `then_v` may overwrite
+  // them where they are done with; rests: with P's rounding rests.
   auto compute = [&](int e0, int end, bool rests, auto then_k, auto then_v) {
     float c[NB][4];
     const float b0 = bias[0], b1 = bias[1];
@@ -621,7 +634,8 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB>::kMinCtas)
             uint32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              w[i] = bf16x2_bits(__floats2bfloat162_rn(o[k][x][i][e] * inv, o[k][x][i][e + 2] * inv));
+              w[i] = bf16x2_bits(
+                  __floats2bfloat162_rn(o[k][x][i][e] * inv, o[k][x][i][e + 2] * inv));
             *reinterpret_cast<uint4*>(dst + 64 * x) = make_uint4(w[0], w[1], w[2], w[3]);
           }
         } else {
@@ -717,7 +731,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps)
     __nv_bfloat162* dst = reinterpret_cast<__nv_bfloat162*>(
         out + ((int64_t)(q.token0 + row / g) * Hq + q.h * g + row % g) * D + kPer * lane);
 #pragma unroll
-    for (int e = 0; e < kPer; e += 2) dst[e / 2] = __floats2bfloat162_rn(O[e] * inv, O[e + 1] * inv);
+    for (int e = 0; e < kPer; e += 2)
+      dst[e / 2] = __floats2bfloat162_rn(O[e] * inv, O[e + 1] * inv);
   };
   // lanes 0 .. 3 hold the sets of the block's warps
   const int first = blockIdx.x * kJoinSets;
@@ -805,10 +820,10 @@ struct RowsLaunch {
   }
 };
 
-// Calls f with the form that serves d channels and so many rows per sequence and KV-head: a block of
-// 16 that is half empty costs 15% (4 x 60,000 slots of 128 channels: 51 us against 41 to 45), two
-// blocks of 8 read everything twice. 16 rows of 256 channels do not fit a thread's registers beside
-// their K and V.
+// Calls f with the form that serves d channels and so many rows per sequence and KV-head: a block
+// of 16 that is half empty costs 15% (4 x 60,000 slots of 128 channels: 51 us against 41 to 45),
+// two blocks of 8 read everything twice. 16 rows of 256 channels do not fit a thread's registers
+// beside their K and V.
 template <class F>
 auto rows_form(int d, int rows, F f) {
   const bool two = rows > 8;
@@ -824,11 +839,11 @@ cudaError_t launch_paged_append(const PagedArgs& a, const PagedAppend& p, const 
   const int tokens = std::max(1, std::min(kAppendTokens, a.n / (4 * num_sms)));
   const size_t smem = p.rotate ? (size_t)tokens * (a.d / 2) * sizeof(float2) : 0;
   // Half the threads where two tokens have no more than 256 pieces (16 channels each): the compact
-  // slots of 8 KV-heads of 128 channels, 8 x 1,311 of them, take 19.1 us against 20.5 with twice the
-  // threads; 32 query heads beside them, 8,192 tokens, 37.2 against 36.8.
+  // slots of 8 KV-heads of 128 channels, 8 x 1,311 of them, take 19.1 us against 20.5 with twice
+  // the threads; 32 query heads beside them, 8,192 tokens, 37.2 against 36.8.
   const int pieces = kAppendTokens * (p.Hq + 2 * a.H) * (a.d / 16);
-  paged_append_kernel<<<(a.n + tokens - 1) / tokens, pieces <= kAppendThreads ? 128 : kAppendThreads,
-                        smem, s>>>(a, p, turns, tokens);
+  const int threads = pieces <= kAppendThreads ? 128 : kAppendThreads;
+  paged_append_kernel<<<(a.n + tokens - 1) / tokens, threads, smem, s>>>(a, p, turns, tokens);
   return cudaGetLastError();
 }
 

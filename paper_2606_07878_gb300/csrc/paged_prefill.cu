@@ -13,14 +13,29 @@
 //
 // Order of the tensor pipe, i counting S tiles (kTiles = 2: both tiles of the same slots in turn):
 // S_0, S_1, PV_0, S_2, PV_1, S_3, ... PV_i waits for P_i alone; S_(i+2) overwrites P_i behind it.
-// The running maximum moves (and O is rescaled) only when a tile raises it by more than 2^8.
+// With two tiles P_i comes in halves, the last 64 slots first: they are the ones whose S the
+// maximum left in registers, and their product starts under the others' exponentials. The running
+// maximum moves (and O is rescaled) only when a tile raises it by more than 2^8.
+//
+// P is bf16: its rounding, 2^-9 of a weight at most, averages out over the slots, and outputs lie
+// 0.0023 of their root mean square from 64-bit ones where the rounding of the outputs alone leaves
+// 0.0017. A second product for the rest, as few rows have it, would double PV.
 //
 // Slots that do not count are zeroed in shared memory before their products (a weight of 0 times
 // a stale NaN would be NaN): those past the sequence's end, and those with a bias of -inf.
 //
-// CTA = 12 warps: 0, 10 and 11 TMA producers (a copy takes about 60 clocks to issue, and pages of
-// 16 slots are 128 copies a tile of 256 channels: 352 us with one, 0 and the others share them out),
-// 1 MMA issuer and TMEM allocation, 2..9 softmax and output. Every wait is bounded.
+// CTA = 12 warps: 0, 10 and 11 TMA producers (a copy takes about 40 clocks to issue, and pages of
+// 16 slots are 64 copies for K and V of 128 slots and 256 channels: 352 us with one producer, 235
+// with three), 1 MMA issuer and TMEM allocation, 2..9 softmax and output. Every wait is bounded.
+//
+// Work: a CTA an SM, equal ranges of the cost of all items; what several CTAs share of an item goes
+// to the workspace and a second launch joins it.
+//
+// 8,192 tokens over themselves, 28 query and 4 KV-heads of 128 channels (481 GFLOP): 337 us, 1.43
+// PFLOP/s, 0.75 of the library's matrix product. The tensor pipe is busy 70% of the kernel; the
+// rest is S -> maximum -> exponentials -> P, 128 columns a thread, twice from TMEM. (Held in
+// registers in between: 375 us at the same stage as 352 this way, for the spills.) Biases cost a
+// read of shared memory and two packed operations per two logits: 1.2 PFLOP/s.
 #include <algorithm>
 #include <type_traits>
 
@@ -35,7 +50,9 @@ constexpr int kPfThreads = 384;
 constexpr int kPfProducers = 3;     // warps
 constexpr int kPfKeys = 128;        // slots of a tile
 constexpr float kPfMoveLog2 = 8.f;  // P <= 2^8 needs no more of bf16's range
-constexpr int kPfItemCost = 2;      // of an item's beginning and end, in tiles of slots
+// of an item's beginning and end, in tiles of slots (1: 379 and 249 us for 8,192 tokens and for
+// three short prompts of 256 channels; 2: 345 and 240; 4: 350 and 247)
+constexpr int kPfItemCost = 2;
 
 struct PrefillParams {
   PagedArgs a;
@@ -182,7 +199,8 @@ struct PfShape {
   static constexpr int kOCols = kTiles == 2 ? D : D / 2;  // O columns per softmax thread
   static constexpr int kRing = kQBytes;
   static constexpr int kBiasAt = kRing + kStages * kStageBytes;  // [8 warps][kCols]
-  static constexpr int kXchAt = kBiasAt + (kBias ? 8 * kCols * 4 : 0);  // [2][2][128], one tile only
+  // [2][2][128], one tile only
+  static constexpr int kXchAt = kBiasAt + (kBias ? 8 * kCols * 4 : 0);
   static constexpr int kBarAt = kXchAt + (kTiles == 1 ? 2048 : 0);
   static constexpr int kPlanAt = kBarAt + 352;
   static constexpr int kBytes = kPlanAt + sizeof(PfPlan);
@@ -486,8 +504,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         mbar_arrive_expect_tx(&qfull[n_items & 1], box * kTiles * (D / 64));
         for (int t = 0; t < kTiles; ++t)
           for (int c = 0; c < D / 64; ++c)
-            tma_load_3d(smem + (t * (D / 64) + c) * S::kChunkBytes, &tm_q, &qfull[n_items & 1], c * 64, it.h * g,
-                        it.token0 + t * f.tile_tokens);
+            tma_load_3d(smem + (t * (D / 64) + c) * S::kChunkBytes, &tm_q, &qfull[n_items & 1],
+                        c * 64, it.h * g, it.token0 + t * f.tile_tokens);
       }
       q_armed = true;
       ++n_items;
@@ -575,12 +593,14 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       for (int c = 0; c < S::kChan / 64; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          tc_mma_f16(tmem_base + buf * kSCols, q + c * kChunkStep + 2 * e, k + c * kChunkStep + 2 * e,
-                     idesc_s, half + c + e > 0);
+          tc_mma_f16(tmem_base + buf * kSCols, q + c * kChunkStep + 2 * e,
+                     k + c * kChunkStep + 2 * e, idesc_s, half + c + e > 0);
       issued = true;
     };
     // O of tile t, the channels of one ring slot, += P in buffer buf times V
-    auto mma_o = [&](int buf, int t, int half, int s, bool first, int e0 = 0, int e1 = kPfKeys / 16) {
+    // (slots [16 e0, 16 e1) of the tile)
+    auto mma_o = [&](int buf, int t, int half, int s, bool first, int e0 = 0,
+                     int e1 = kPfKeys / 16) {
       tc_fence_after();
       const uint64_t v = v_desc + s * kStageStep;
 #pragma unroll
@@ -630,8 +650,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
           }
         }
       } else {
-        // S and P take buffers 0 and 1 in turn, from 0 on in every item (constants: with a buffer and
-        // a half that the loop counts, issuing takes longer than the products)
+        // S and P take buffers 0 and 1 in turn, from 0 on in every item (constants: with a buffer
+        // and a half that the loop counts, issuing takes longer than the products)
         auto make_s = [&](auto buf, int i) {
 #pragma unroll
           for (int half = 0; half < kHalves; ++half) {
@@ -917,8 +937,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   }
 }
 
-// Rows of the items that lie in several CTAs' ranges: block (c, x) joins rows [32 x, + 32) of the item
-// that CTA c begins, its parts in the order of their slots; a lane takes a row, a warp d / 8 channels.
+// Rows of the items that lie in several CTAs' ranges: block (c, x) joins rows [32 x, + 32) of the
+// item that CTA c begins, its parts in the order of their slots; a lane takes a row, a warp d / 8
+// channels.
 template <int D>
 __global__ void __launch_bounds__(256)
     paged_join_kernel(const __grid_constant__ PrefillParams f, int item_rows, float to_log2) {
@@ -1014,8 +1035,8 @@ cudaError_t launch_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
   paged_prefill_kernel<D, kBias><<<dev.num_sms, kPfThreads, S::kBytes, s>>>(tq, tk, tv, f);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  return launch_chained(paged_join_kernel<D>, dim3(dev.num_sms, rows / 32), dim3(256), 0, s, 1, f, rows,
-                        (kBias ? 1.f : q.scale) * kLog2e);
+  return launch_chained(paged_join_kernel<D>, dim3(dev.num_sms, rows / 32), dim3(256), 0, s, 1, f,
+                        rows, (kBias ? 1.f : q.scale) * kLog2e);
 }
 
 }  // namespace

@@ -4,11 +4,11 @@ compaction"; App. B): one layer's part of it, with synthetic rows in place of a 
     python -m paper_2606_07878_gb300.paged_serving
 
 The document comes in chunks of c * t tokens. A pass appends a chunk to the cache (keys rotated to
-their positions), attends from its tokens to [compact chunks | raw chunk | the chunk itself], compacts
-the oldest raw chunk to t slots and puts those into pages of their own. The raw chunk's pages then
-leave the sequence's table and the compact ones take their place: nothing else moves, and positions
-run ahead of slots by what the compactions took out. A question of some tokens and an answer, token by
-token, follow.
+their positions), attends from its tokens to [compact chunks | raw chunk | the chunk itself],
+compacts the oldest raw chunk to t slots and puts those into pages of their own. The raw chunk's
+pages then leave the sequence's table and the compact ones take their place: nothing else moves, and
+positions run ahead of slots by what the compactions took out. A question of some tokens and an
+answer, token by token, follow.
 """
 from __future__ import annotations
 
