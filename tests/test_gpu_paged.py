@@ -174,6 +174,10 @@ def test_decode_matches_64_bits(ctx, d, H, Hq, page, lens, beta, heads_first):
     (256, 8, 16, 16, [700, 90, 350], [0, 1000, 64], False, False),
     (256, 2, 4, 64, [100], [5000], True, False),
     (256, 1, 128, 32, [3], [700], True, False),
+    (256, 2, 4, 128, [400, 30], [0, 1000], True, True),
+    (256, 4, 8, 256, [900, 0, 65], [300, 5, 0], False, False),
+    (256, 1, 1, 16, [130, 257, 1], [0, 128, 77], True, False),
+    (256, 8, 24, 32, [333, 40, 700, 2], [0, 1500, 77, 0], True, True),
     (64, 1, 200, 16, [3, 1], [70, 0], False, False),
     (128, 1, 2, 16, [(7 * i) % 23 for i in range(500)], [(11 * i) % 50 for i in range(500)], True,
      False),
