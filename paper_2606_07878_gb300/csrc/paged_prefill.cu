@@ -5,19 +5,19 @@
 //                        channels), fp32 in TMEM
 //   P = e^(scale S + beta - m)   one row per thread, running m and sum; bf16, written over S
 //   O += P V             P from TMEM, V as the loaded rows (channels are its contiguous dimension)
-// An item is a sequence, KV-head and kTiles tiles of floor(128 / g) tokens x g heads, so that the
-// heads of a group share every K and V tile. For d <= 128 two tiles (256 rows) take turns: the
-// softmax of one lies under the products of the other. 256 channels leave TMEM for one tile (S
-// twice, O once): its two warpgroups take half of S's columns each, and the S of the next slots is
-// formed meanwhile. There a pair of CTAs (a cluster) takes the two tiles of an item, and each loads
-// half of every K and V tile into both (TMA multicast): half the copies to issue, half the reads of
-// L2.
+// An item is a sequence, KV-head and two tiles of floor(128 / g) tokens x g heads (one, for 256
+// channels and few rows), so that the heads of a group share every K and V tile. For d <= 128 the
+// two tiles take turns on one SM: the softmax of one lies under the products of the other. 256
+// channels leave TMEM for one tile (S twice, O once): its two softmax warpgroups take tiles of
+// slots in turn, handing the running maximum on, and a pair of CTAs (a cluster) takes the two
+// tiles, each loading half of every K and V tile into both (TMA multicast): half the copies to
+// issue, half the reads of L2.
 //
 // Order of the tensor pipe, i counting S tiles (kTiles = 2: both tiles of the same slots in turn):
 // S_0, S_1, PV_0, S_2, PV_1, S_3, ... PV_i waits for P_i alone; S_(i+2) overwrites P_i behind it.
-// With two tiles P_i comes in halves, the last 64 slots first: they are the ones whose S the
-// maximum left in registers, and their product starts under the others' exponentials. The running
-// maximum moves (and O is rescaled) only when a tile raises it by more than 2^8.
+// P_i comes in halves, the last 64 slots first: they are the ones whose S the maximum left in
+// registers, and their product starts under the others' exponentials. The running maximum moves
+// (and O is rescaled) only when a tile raises it by more than 2^8.
 //
 // P is bf16: its rounding, 2^-9 of a weight at most, averages out over the slots, and outputs lie
 // 0.0023 of their root mean square from 64-bit ones where the rounding of the outputs alone leaves
@@ -34,10 +34,15 @@
 // to the workspace and a second launch joins it.
 //
 // 8,192 tokens over themselves, 28 query and 4 KV-heads of 128 channels (481 GFLOP): 337 us, 1.43
-// PFLOP/s, 0.75 of the library's matrix product. The tensor pipe is busy 70% of the kernel; the
-// rest is S -> maximum -> exponentials -> P, 128 columns a thread, twice from TMEM. (Held in
-// registers in between: 375 us at the same stage as 352 this way, for the spills.) Biases cost a
-// read of shared memory and two packed operations per two logits: 1.2 PFLOP/s.
+// PFLOP/s, 0.75 of the library's matrix product; the tensor pipe is busy 70%. Shared memory bounds
+// it: per 128 slots and two tiles the products take 2,048 clocks, their operands (q and K for S, V
+// for P V) 1,536 at 128 bytes a clock and the loads of K and V another 512; and the softmax, 128
+// columns a thread, twice from TMEM, has no time to spare either. (S held in registers in between:
+// 375 us at a stage of this kernel that took 352 otherwise, for the spills.) Biases cost a read of
+// shared memory and two packed operations per two logits: 1.2 PFLOP/s. With 256 channels a tile has
+// K and V to itself, 2,560 clocks of shared memory for 2,048 of products: 432 us for 8,192 tokens
+// of 8 KV- and 16 query heads, 1.27 PFLOP/s, with a ring of four slots as with five; 490 in pages
+// of 16, for the copies.
 #include <algorithm>
 #include <type_traits>
 
@@ -215,14 +220,13 @@ struct PfShape {
   static constexpr int kChunkBytes = kPfKeys * 128;  // 64 channels of 128 rows
   static constexpr int kQBytes = kTiles * (D / 64) * kChunkBytes;
   static constexpr int kStages = D == 64 ? 8 : kBias ? 4 : 5;
-  static constexpr int kCols = kTiles == 2 ? 128 : 64;  // S columns per softmax thread
   static constexpr int kOCols = kTiles == 2 ? D : D / 2;  // O columns per softmax thread
   static constexpr int kRing = kQBytes;
-  static constexpr int kBiasAt = kRing + kStages * kStageBytes;  // [8 warps][kCols]
-  // [2][2][128], one tile only
-  static constexpr int kXchAt = kBiasAt + (kBias ? 8 * kCols * 4 : 0);
+  static constexpr int kBiasAt = kRing + kStages * kStageBytes;  // [8 warps][128]
+  // one tile only: running maxima and sums, [2][128] each
+  static constexpr int kXchAt = kBiasAt + (kBias ? 8 * kPfKeys * 4 : 0);
   static constexpr int kBarAt = kXchAt + (kTiles == 1 ? 2048 : 0);
-  static constexpr int kPlanAt = kBarAt + 352;
+  static constexpr int kPlanAt = kBarAt + (3 * kStages + 26) * 8;
   static constexpr int kBytes = kPlanAt + sizeof(PfPlan);
   static_assert(kBytes <= 232448, "shared memory budget");
 };
@@ -286,11 +290,9 @@ struct PfWalk {
   }
 };
 
-// kC columns' biases of a warp, one tile of slots ahead: lane i holds those of columns
-// [kC / 32 i, + kC / 32).
-template <int kC>
+// Biases of a tile of slots, loaded ahead by a warp: lane i holds those of slots [4 i, 4 i + 4).
 struct PfBias {
-  static constexpr int kPer = kC / 32;
+  static constexpr int kPer = kPfKeys / 32;
   float v[kPer];
   STILL_DEV void load(const PagedArgs& a, const PfItem& it, int slot0, int lane) {
     const int j = slot0 + kPer * lane;
@@ -335,13 +337,16 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   uint64_t* pfull = sfull + 2;       // [2] P_i written (and O rescaled where needed)
   uint64_t* pvdone = pfull + 2;      // [2] O holds P_i V
   uint64_t* ofree = pvdone + 2;      // O drained at the end of an item
-  uint64_t* xb = ofree + 1;          // [4] row-value exchange per lane quarter
-  uint64_t* landed = xb + 4;         // the copies into a ring slot that has rows to be zeroed
-  uint64_t* phalf = landed + kStages;      // [2] the last 64 slots of P_i written (two tiles only)
+  // one tile only, per lane quarter: the running maximum behind S_i (of buffer 0, of buffer 1), and
+  // both warps' sums at the end of an item
+  uint64_t* mb = ofree + 1;          // [2][4]
+  uint64_t* lb = mb + 8;             // [4]
+  uint64_t* landed = lb + 4;         // the copies into a ring slot that has rows to be zeroed
+  uint64_t* phalf = landed + kStages;  // [2] the last 64 slots of P_i written
   uint64_t* drain = phalf + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((3 * kStages + 17) * 8 + 8 <= 352, "barriers");
+  static_assert((3 * kStages + 25) * 8 + 8 == S::kPlanAt - S::kBarAt, "barriers");
 
   const PagedArgs& a = f.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -352,7 +357,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   const int rank = kPair ? (int)cluster_ctarank() : 0;  // this CTA's tile of a pair's item
   // TMEM: S at 128 i, P over those of its columns that are read first, O behind both
   constexpr int kSCols = 128, kOAt = 2 * kSCols;
-  constexpr int kPAt = kTiles == 2 ? 64 : 0;
+  constexpr int kPAt = 64;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -365,12 +370,13 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     mbar_init(qfree, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sfull[i], 1);
-      mbar_init(&pfull[i], kTiles == 2 ? 4 : 8);
+      mbar_init(&pfull[i], 4);
       mbar_init(&phalf[i], 4);
       mbar_init(&pvdone[i], 1);
     }
     mbar_init(ofree, 8);
-    for (int i = 0; i < 4; ++i) mbar_init(&xb[i], 2);
+    for (int i = 0; i < 8; ++i) mbar_init(&mb[i], 1);
+    for (int i = 0; i < 4; ++i) mbar_init(&lb[i], 2);
     mbar_init(drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
@@ -413,7 +419,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     }
     before -= mine;
     // no range is shorter than an item's beginning and a tile
-    const int nct = (int)max((int64_t)1, min((int64_t)(kPair ? gridDim.x / 2 : gridDim.x), total / (kPfItemCost + 1)));
+    const int64_t most = kPair ? gridDim.x / 2 : gridDim.x;
+    const int nct = (int)max((int64_t)1, min(most, total / (kPfItemCost + 1)));
     const int64_t u0 = cta < nct ? total * cta / nct : total;
     if (u0 >= before && u0 < before + mine) {
       PfStart p;
@@ -498,7 +505,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         phase ^= 1;
       }
     };
-    PfBias<128> beta;  // of the next tile of K
+    PfBias beta;  // of the next tile of K
     uint32_t mark[2] = {0, 0};  // of the tile of K loaded last and of the one before
     // K of tile kt, tiles in order: which of its slots count is found out here
     auto load_k = [&](const PfItem& it, int kt) {
@@ -696,14 +703,19 @@ __global__ void __launch_bounds__(kPfThreads, 1)
           if (i + 1 == n_k) tc_commit(qfree);
         };
         auto add_pv = [&](auto buf, uint32_t& uses, int i) {
-          if (!wait(&pfull[buf], uses & 1, 625)) return;
+          if (!wait(&phalf[buf], uses & 1, 625)) return;
           if (i == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 626)) return;
+          int vs[kHalves];
 #pragma unroll
           for (int half = 0; half < kHalves; ++half) {
-            const int s = take();
-            if (s < 0) return;
-            mma_o(buf, 0, half, s, i == 0);
-            give(s);
+            if ((vs[half] = take()) < 0) return;
+            mma_o(buf, 0, half, vs[half], i == 0, 4, 8);
+          }
+          if (!wait(&pfull[buf], uses & 1, 635)) return;
+#pragma unroll
+          for (int half = 0; half < kHalves; ++half) {
+            mma_o(buf, 0, half, vs[half], false, 0, 4);
+            give(vs[half]);
           }
           tc_commit(&pvdone[buf]);
           ++uses;
@@ -729,34 +741,33 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     }
   } else if (warp >= 2) {
     // ------------------------------------------------------------ softmax and output
-    constexpr int kCols = S::kCols, kOCols = S::kOCols;
+    constexpr int kOCols = S::kOCols;
     const int sw = warp - 2;
     const int quarter = warp & 3;  // TMEM lanes [32 quarter, + 32)
-    const int wg = sw >> 2;        // its tile, or its half of the columns
+    const int wg = sw >> 2;        // its buffer of S: its tile, or every other tile of slots
     const int row = quarter * 32 + lane;
-    const int col0 = kTiles == 2 ? 0 : kCols * wg;
     const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16);
-    const uint32_t o_at = lanes + kOAt + (kTiles == 2 ? wg * D : wg * kOCols);
-    float* kw = reinterpret_cast<float*>(smem + S::kBiasAt) + sw * kCols;
-    float* xch = reinterpret_cast<float*>(smem + S::kXchAt);  // [2][2][128]
+    const uint32_t o_at = lanes + kOAt + (kTiles == 2 ? wg * D : 0);
+    const uint32_t s_at = lanes + wg * kSCols;
+    float* kw = reinterpret_cast<float*>(smem + S::kBiasAt) + sw * kPfKeys;
+    float* xm = reinterpret_cast<float*>(smem + S::kXchAt) + row;  // [2][128]
+    float* xl = xm + 256;                                          // [2][128]
     // exponents: with biases logits are natural (a bias of the lowest float must stay finite),
     // without them S itself is kept and the scale joins the factor
     const float to_log2 = kBias ? kLog2e : f.q.scale * kLog2e;
-    uint32_t uses[2] = {0, 0}, n_x = 0;  // of the buffers of S so far
+    uint32_t mine = 0, other = 0;  // uses of this warp's buffer of S before this item, of the other
     bool bad = false;
     auto wait_all = [&](uint64_t* bar, uint32_t parity, int where) -> bool {
       if (!pf_wait(bar, parity, a.err, abort_flag, where)) bad = true;
       return !bad;
     };
-    // One value per row for the other warp of this lane quarter; returns its value.
-    auto exchange = [&](float mine, int where) -> float {
-      float* at = xch + (n_x & 1) * 256;
-      at[wg * 128 + row] = mine;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&xb[quarter]);
-      const bool ok = wait_all(&xb[quarter], n_x & 1, where);
-      ++n_x;
-      return ok ? at[(1 - wg) * 128 + row] : mine;
+    // The running maximum that the other warp of this lane quarter left behind its use n of its
+    // buffer (from 1 on); this warp's sum is brought to it.
+    auto follow = [&](uint32_t n, float& m, float& l) {
+      if (!wait_all(&mb[4 * (wg ^ 1) + quarter], (n - 1) & 1, 631)) return;
+      const float theirs = xm[128 * (wg ^ 1)];
+      if (theirs != m) l *= ex2_ftz((m - theirs) * to_log2);
+      m = theirs;
     };
     const int tile = kTiles == 2 ? wg : rank;                  // of an item
     const int token = tile * f.tile_tokens + row / g;  // of an item
@@ -768,22 +779,22 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       // (rows of no token are not stored: they need no masks)
       const int see = valid ? max(0, it.see + token) : INT32_MAX;
       float m_run = -INFINITY, l_run = 0.f;
-      PfBias<kCols> beta;
-      if (kBias) beta.load(a, it, it.k0 * kPfKeys + col0, lane);
-      int buf = 0;
+      PfBias beta;
+      const int first = it.k0 + (kTiles == 2 ? 0 : wg);
+      constexpr int kStep = 3 - kTiles;  // tiles of slots from one of this warp's to the next
+      if (kBias && first < it.k1) beta.load(a, it, first * kPfKeys, lane);
+      uint32_t n = mine;  // uses of the buffer
       const int least = __reduce_min_sync(0xffffffffu, see);  // slots that every row sees
 #pragma unroll 1
-      for (int kt = it.k0; kt < it.k1; ++kt) {
-        buf = kTiles == 2 ? wg : (kt - it.k0) & 1;
-        const uint32_t s_at = lanes + buf * kSCols + col0;
-        const int slot0 = kt * kPfKeys + col0;
+      for (int kt = first; kt < it.k1; kt += kStep, ++n) {
+        const int slot0 = kt * kPfKeys;
         if constexpr (kBias) {
 #pragma unroll
           for (int e = 0; e < beta.kPer; ++e) kw[beta.kPer * lane + e] = beta.v[e];
-          if (kt + 1 < it.k1) beta.load(a, it, slot0 + kPfKeys, lane);
+          if (kt + kStep < it.k1) beta.load(a, it, slot0 + kStep * kPfKeys, lane);
           __syncwarp();
         }
-        if (!wait_all(&sfull[buf], (buf ? uses[1] : uses[0]) & 1, 630)) break;
+        if (!wait_all(&sfull[wg], n & 1, 630)) break;
         tc_fence_after();
         uint32_t v[64];
         // Columns [c, c + 64) as logits, -inf where the row does not see the slot.
@@ -817,7 +828,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         };
         float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll 1
-        for (int c = 0; c < kCols; c += 64) {
+        for (int c = 0; c < kPfKeys; c += 64) {
           logits(c);
 #pragma unroll
           for (int e = 0; e < 64; e += 4) {
@@ -825,9 +836,11 @@ __global__ void __launch_bounds__(kPfThreads, 1)
             m1 = max3(m1, __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
           }
         }
-        float mx = fmaxf(m0, m1);
-        if constexpr (kTiles == 1) {
-          mx = fmaxf(mx, exchange(mx, 631));
+        const float mx = fmaxf(m0, m1);
+        // uses of the buffer that the tile before was in
+        const uint32_t before = kTiles == 2 ? n : other + (kt - it.k0 + 1) / 2;
+        if (kTiles == 1 && kt > it.k0) {
+          follow(before, m_run, l_run);
           if (bad) break;
         }
         bool move = false;
@@ -840,13 +853,17 @@ __global__ void __launch_bounds__(kPfThreads, 1)
           l_run *= fac;
           move = valid;
         }
+        if constexpr (kTiles == 1) {
+          xm[128 * wg] = m_run;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&mb[4 * wg + quarter]);
+        }
         // warp-collective: a warp rescales O when any of its rows needs it
         if (__any_sync(0xffffffffu, move) && kt > it.k0) {
-          const int before = kTiles == 2 ? buf : buf ^ 1;  // where P of the tile before was
-          if (!wait_all(&pvdone[before], ((before ? uses[1] : uses[0]) - 1) & 1, 632)) break;
+          if (!wait_all(&pvdone[kTiles == 2 ? wg : wg ^ 1], (before - 1) & 1, 632)) break;
           tc_fence_after();
 #pragma unroll 1
-          for (int c = 0; c < kOCols; c += 32) {
+          for (int c = 0; c < D; c += 32) {
             float o[32];
             tmem_ld32(o_at + c, o);
 #pragma unroll
@@ -861,8 +878,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         uint64_t s0 = 0ull, s1 = 0ull;
         // the last columns first: v still holds them
 #pragma unroll 1
-        for (int c = kCols - 64; c >= 0; c -= 64) {
-          if (c < kCols - 64) logits(c);
+        for (int c = kPfKeys - 64; c >= 0; c -= 64) {
+          if (c < kPfKeys - 64) logits(c);
 #pragma unroll
           for (int e = 0; e < 64; e += 2) {
             float u0, u1;
@@ -875,12 +892,12 @@ __global__ void __launch_bounds__(kPfThreads, 1)
               s0 = add2(s0, pack2(p0, p1));
             v[e / 2] = bf16x2_bits(__floats2bfloat162_rn(p0, p1));
           }
-          tmem_st32_issue(s_at - col0 + kPAt + (col0 + c) / 2, v);
-          if (kTiles == 2 && c > 0) {
+          tmem_st32_issue(s_at + kPAt + c / 2, v);
+          if (c > 0) {
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&phalf[buf]);
+            if (lane == 0) mbar_arrive(&phalf[wg]);
           }
         }
         float l0, l1;
@@ -889,19 +906,31 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();  // and kw is written again
-        if (lane == 0) mbar_arrive(&pfull[buf]);
-        ++(buf ? uses[1] : uses[0]);
+        if (lane == 0) mbar_arrive(&pfull[wg]);
       }
       if (bad) break;
       // ---- the item's rows
       float l = l_run;
-      if constexpr (kTiles == 1) {
-        l += exchange(l_run, 633);
-        if (bad) break;
+      const int oc = kTiles == 2 ? 0 : wg * kOCols;  // the columns that this warp writes
+      if constexpr (kTiles == 2) {
+        mine = n;
+        if (!wait_all(&pvdone[wg], (n - 1) & 1, 634)) break;
+      } else {
+        const int tiles = it.k1 - it.k0;
+        const bool last_mine = ((tiles - 1) & 1) == wg;
+        mine += (tiles + 1 - wg) / 2;
+        other += (tiles + wg) / 2;
+        if (!last_mine) follow(other, m_run, l);
+        if (bad || !wait_all(&pvdone[(tiles - 1) & 1], ((last_mine ? mine : other) - 1) & 1, 634))
+          break;
+        // (behind that wait nobody reads the sums of the item before any more)
+        xl[128 * wg] = l;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&lb[quarter]);
+        if (!wait_all(&lb[quarter], n_items & 1, 633)) break;
+        l += xl[128 * (wg ^ 1)];
       }
-      if (!wait_all(&pvdone[buf], ((buf ? uses[1] : uses[0]) - 1) & 1, 634)) break;
       tc_fence_after();
-      const int oc = kTiles == 2 ? 0 : wg * kOCols;
       if (it.part != 0) {  // columns apart, so that a warp's rows lie side by side
         const int64_t part = 2 * cta + it.part - 1;
         const int prow = 128 * tile + row;
@@ -909,7 +938,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 #pragma unroll 1
         for (int c = 0; c < kOCols; c += 32) {
           float o[32];
-          tmem_ld32(o_at + c, o);
+          tmem_ld32(o_at + oc + c, o);
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             dst[(c / 4 + e) * kRows] =
@@ -929,7 +958,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 #pragma unroll 1
         for (int c = 0; c < kOCols; c += 32) {
           float o[32];
-          tmem_ld32(o_at + c, o);
+          tmem_ld32(o_at + oc + c, o);
           uint32_t w[4][4];
 #pragma unroll
           for (int e = 0; e < 16; ++e)
@@ -1106,9 +1135,11 @@ size_t paged_prefill_workspace(const PagedArgs& a, int num_sms) {
 
 cudaError_t launch_paged_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
                                  const KernelTable& dev, cudaStream_t s) {
-  // 256 channels in pairs of CTAs where sequences have rows for two tiles. Three prompts of
-  // 900 to 2,300 tokens, 8 KV-heads with 2 query heads each, pages of 16: 216 us against 243; 8,192
-  // tokens: 504 against 577 in pages of 16, 439 against 444 in pages of 128.
+  // 256 channels in pairs of CTAs where sequences have rows for two tiles. Three prompts of 900 to
+  // 2,300 tokens, 8 KV-heads with 2 query heads each, pages of 16: 216 us against 243; 8,192
+  // tokens: 504 against 577 in pages of 16, 439 against 444 in pages of 128. Where the second tile
+  // has two rows (65 tokens of 2 heads over 2,000 slots, 4 KV-heads): 57 us against 62 for 16
+  // sequences; for 4 sequences of 100 tokens 35 against 33.
   const bool bias = a.beta != nullptr, pair = paged_mean_rows(a, q.Hq) > 128;
   switch (a.d) {
     case 64:
