@@ -34,15 +34,14 @@
 // to the workspace and a second launch joins it.
 //
 // 8,192 tokens over themselves, 28 query and 4 KV-heads of 128 channels (481 GFLOP): 337 us, 1.43
-// PFLOP/s, 0.75 of the library's matrix product; the tensor pipe is busy 70%. Shared memory bounds
-// it: per 128 slots and two tiles the products take 2,048 clocks, their operands (q and K for S, V
-// for P V) 1,536 at 128 bytes a clock and the loads of K and V another 512; and the softmax, 128
-// columns a thread, twice from TMEM, has no time to spare either. (S held in registers in between:
-// 375 us at a stage of this kernel that took 352 otherwise, for the spills.) Biases cost a read of
-// shared memory and two packed operations per two logits: 1.2 PFLOP/s. With 256 channels a tile has
-// K and V to itself, 2,560 clocks of shared memory for 2,048 of products: 432 us for 8,192 tokens
-// of 8 KV- and 16 query heads, 1.27 PFLOP/s, with a ring of four slots as with five; 490 in pages
-// of 16, for the copies.
+// PFLOP/s, 0.75 of the library's matrix product. The tensor pipe is busy 71% of the kernel, tensor
+// memory 75%, issue slots 48%: what is left is the chain S, maximum, exponentials, P of two tiles
+// that take turns, with S read from TMEM twice. (Held in registers in between: 375 us at a stage of
+// this kernel that took 352 otherwise, for the spills.) Biases cost a read of shared memory and two
+// packed operations per two logits: 1.2 PFLOP/s. With 256 channels a tile has K and V to itself, so
+// an SM takes in 128 KB for 2,048 clocks of products, what its port to L2 can give in that time:
+// 432 us for 8,192 tokens of 8 KV- and 16 query heads, 1.27 PFLOP/s, the tensor pipe busy 50%; 490
+// in pages of 16, for the copies.
 #include <algorithm>
 #include <type_traits>
 
