@@ -10,8 +10,8 @@
 // two tiles take turns on one SM: the softmax of one lies under the products of the other. 256
 // channels leave TMEM for one tile (S twice, O once): its two softmax warpgroups take tiles of
 // slots in turn, handing the running maximum on, and a pair of CTAs (a cluster) takes the two
-// tiles, each loading half of every K and V tile into both (TMA multicast): half the copies to
-// issue, half the reads of L2.
+// tiles in 2-SM products (cta_group::2, M = 256): each CTA loads half of K (64 slots) and half of V
+// (128 channels), where one of its own would take in 128 KB for 2,048 clocks of products.
 //
 // Order of the tensor pipe, i counting S tiles (kTiles = 2: both tiles of the same slots in turn):
 // S_0, S_1, PV_0, S_2, PV_1, S_3, ... PV_i waits for P_i alone; S_(i+2) overwrites P_i behind it.
@@ -38,10 +38,10 @@
 // memory 75%, issue slots 48%: what is left is the chain S, maximum, exponentials, P of two tiles
 // that take turns, with S read from TMEM twice. (Held in registers in between: 375 us at a stage of
 // this kernel that took 352 otherwise, for the spills.) Biases cost a read of shared memory and two
-// packed operations per two logits: 1.2 PFLOP/s. With 256 channels a tile has K and V to itself, so
-// an SM takes in 128 KB for 2,048 clocks of products, what its port to L2 can give in that time:
-// 432 us for 8,192 tokens of 8 KV- and 16 query heads, 1.27 PFLOP/s, the tensor pipe busy 50%; 490
-// in pages of 16, for the copies.
+// packed operations per two logits: 1.2 PFLOP/s. 8,192 tokens of 8 KV- and 16 query heads of 256
+// channels (half the softmax for the same products): 350 us, 1.57 PFLOP/s; 412 in pages of 16, for
+// the copies. There each CTA with a tile and all of K and V: 444 and 577; the pair with copies of
+// all of K and V in both, loaded once by multicast: 432 and 490.
 #include <algorithm>
 #include <type_traits>
 
@@ -86,6 +86,17 @@ STILL_DEV void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t
       "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+// The same on a CTA pair, issued by the even CTA: A's rows [0, 128) from its TMEM, [128, 256) from
+// the odd CTA's, and half of B's columns from each one's shared memory.
+STILL_DEV void mma_ts_2sm(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
+                          uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
 // One lane of a converged warp, as the compiler knows: behind it operands stay uniform.
 STILL_DEV bool elect_one() {
   uint32_t r;
@@ -125,22 +136,13 @@ STILL_DEV void tma_load_4d(void* dst, const CUtensorMap* m, uint64_t* bar, int x
       "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
       : "memory");
 }
-// The same box into the same place of both CTAs of a cluster, each on its own barrier.
-STILL_DEV void tma_load_4d_both(void* dst, const CUtensorMap* m, uint64_t* bar, int x, int y,
-                                int z, int w) {
+// The same, its completion on an mbarrier of either CTA of the pair (a shared::cluster address).
+STILL_DEV void tma_load_4d_2sm(void* dst, const CUtensorMap* m, uint32_t bar_cluster, int x, int y,
+                               int z, int w) {
   asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
-      ".multicast::cluster [%0], [%1, {%3, %4, %5, %6}], [%2], %7;" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w),
-      "h"((uint16_t)3)
-      : "memory");
-}
-// Arrive on `bar` of both CTAs when all previously issued tcgen05.mma of this thread complete.
-STILL_DEV void tc_commit_both(uint64_t* bar) {
-  asm volatile(
-      "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64"
-      " [%0], %1;" ::"r"(smem_u32(bar)),
-      "h"((uint16_t)3)
+      "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(bar_cluster), "r"(x), "r"(y), "r"(z), "r"(w)
       : "memory");
 }
 // 32 lanes x 32 columns of 32 bits from registers; complete after tmem_wait_st.
@@ -159,17 +161,18 @@ STILL_DEV void tmem_st32_issue(uint32_t taddr, const uint32_t* r) {
 }
 STILL_DEV void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Zeroes the rows of a ring slot that lane i marks in its bits for rows [4 i, 4 i + 4).
-STILL_DEV void zero_rows(uint8_t* slot, int chunks, uint32_t marks) {
+// Zeroes rows of a ring slot whose chunks have `rows` rows, slots [first, first + rows) of a tile:
+// those that lane i marks in its bits for slots [4 i, 4 i + 4).
+STILL_DEV void zero_rows(uint8_t* slot, int chunks, int rows, int first, uint32_t marks) {
   const int lane = threadIdx.x & 31;
 #pragma unroll 1
-  for (int r = 0; r < kPfKeys; r += 4) {
-    const uint32_t n4 = __shfl_sync(0xffffffffu, marks, r / 4);
+  for (int r = 0; r < rows; r += 4) {
+    const uint32_t n4 = __shfl_sync(0xffffffffu, marks, (first + r) / 4);
     if ((n4 >> (lane >> 3)) & 1)
 #pragma unroll 1
       for (int c = 0; c < chunks; ++c)
-        *reinterpret_cast<uint4*>(slot + c * (kPfKeys * 128) + (r + (lane >> 3)) * 128 +
-                                  (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(slot + (c * rows + r + (lane >> 3)) * 128 + (lane & 7) * 16) =
+            make_uint4(0, 0, 0, 0);
   }
   fence_proxy_async_smem();
   __syncwarp();
@@ -210,12 +213,17 @@ struct PfPlan {  // in shared memory
   int64_t warp_cost[kPfThreads / 32];
 };
 
-template <int D, bool kBias>
+template <int D, bool kBias, bool kPair>
 struct PfShape {
-  static constexpr int kTiles = D <= 128 ? 2 : 1;
-  static constexpr int kChan = D < 128 ? D : 128;   // channels of a ring slot
-  static constexpr int kHalves = D / kChan;          // ring slots of a K or V tile
-  static constexpr int kStageBytes = kPfKeys * kChan * 2;
+  static constexpr int kTiles = D <= 128 ? 2 : 1;  // of an item on an SM
+  // A ring slot holds 128 slots of kChan channels; a pair's CTA has one with its half of a tile: of
+  // K all channels of 64 slots (kKRows), of V kChan channels of all.
+  static constexpr int kChan = D < 128 ? D : 128;
+  static constexpr int kHalves = kPair ? 1 : D / kChan;  // ring slots of a K or V tile
+  static constexpr int kKRows = kPair ? kPfKeys / 2 : kPfKeys;
+  static constexpr int kStageBits = kChan == 64 ? 14 : 15;
+  static constexpr int kStageBytes = 1 << kStageBits;
+  static_assert(kStageBytes == kPfKeys * kChan * 2, "a ring slot");
   static constexpr int kChunkBytes = kPfKeys * 128;  // 64 channels of 128 rows
   static constexpr int kQBytes = kTiles * (D / 64) * kChunkBytes;
   static constexpr int kStages = D == 64 ? 8 : kBias ? 4 : 5;
@@ -225,7 +233,7 @@ struct PfShape {
   // one tile only: running maxima and sums, [2][128] each
   static constexpr int kXchAt = kBiasAt + (kBias ? 8 * kPfKeys * 4 : 0);
   static constexpr int kBarAt = kXchAt + (kTiles == 1 ? 2048 : 0);
-  static constexpr int kPlanAt = kBarAt + (3 * kStages + 26) * 8;
+  static constexpr int kPlanAt = kBarAt + (3 * kStages + 28) * 8;
   static constexpr int kBytes = kPlanAt + sizeof(PfPlan);
   static_assert(kBytes <= 232448, "shared memory budget");
 };
@@ -313,7 +321,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
                          const __grid_constant__ CUtensorMap tm_k,
                          const __grid_constant__ CUtensorMap tm_v,
                          const __grid_constant__ PrefillParams f) {
-  using S = PfShape<D, kBias>;
+  using S = PfShape<D, kBias, kPair>;
   constexpr int kTiles = S::kTiles, kStages = S::kStages, kHalves = S::kHalves;
   // All of it: no byte is left beside five stages of 256 channels, so the base has to be aligned as
   // it is.
@@ -342,16 +350,20 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   uint64_t* lb = mb + 8;             // [4]
   uint64_t* landed = lb + 4;         // the copies into a ring slot that has rows to be zeroed
   uint64_t* phalf = landed + kStages;  // [2] the last 64 slots of P_i written
-  uint64_t* drain = phalf + 2;
+  uint64_t* qpeer = phalf + 2;  // the other CTA's q loaded
+  uint64_t* drain = qpeer + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((3 * kStages + 25) * 8 + 8 == S::kPlanAt - S::kBarAt, "barriers");
+  static_assert((3 * kStages + 26) * 8 + 16 == S::kPlanAt - S::kBarAt, "barriers");
 
   const PagedArgs& a = f.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = f.q.Hq / a.H;
   static_assert(kTiles == 1 || !kPair, "a pair's CTAs have a tile each");
-  constexpr int kRows = 128 * (kPair ? 2 : kTiles);  // of an item
+  // A pair's products are 2-SM ones: its even CTA (0) issues them for both, and the barriers that
+  // its issuer waits for are the even CTA's.
+  constexpr int kSides = kPair ? 2 : 1;
+  constexpr int kRows = 128 * kSides * kTiles;  // of an item
   const int tokens = f.tile_tokens * (kRows / 128);  // of an item
   const int rank = kPair ? (int)cluster_ctarank() : 0;  // this CTA's tile of a pair's item
   // TMEM: S at 128 i, P over those of its columns that are read first, O behind both
@@ -360,8 +372,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(&full[s], 1);
-      mbar_init(&empty[s], kPair ? 2 : 1);
+      mbar_init(&full[s], kSides);
+      mbar_init(&empty[s], 1);
       mbar_init(&landed[s], 1);
     }
     mbar_init(&qfull[0], 1);
@@ -369,11 +381,12 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     mbar_init(qfree, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sfull[i], 1);
-      mbar_init(&pfull[i], 4);
-      mbar_init(&phalf[i], 4);
+      mbar_init(&pfull[i], 4 * kSides);
+      mbar_init(&phalf[i], 4 * kSides);
       mbar_init(&pvdone[i], 1);
     }
-    mbar_init(ofree, 8);
+    mbar_init(ofree, 8 * kSides);
+    mbar_init(qpeer, 1);
     for (int i = 0; i < 8; ++i) mbar_init(&mb[i], 1);
     for (int i = 0; i < 4; ++i) mbar_init(&lb[i], 2);
     mbar_init(drain, 1);
@@ -384,8 +397,13 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     tma_prefetch_desc(&tm_v);
   }
   if (warp == 1) {
-    tmem_alloc(tmem_slot, 512);
-    tmem_relinquish();
+    if constexpr (kPair) {
+      tmem_alloc_2sm(tmem_slot, 512);
+      tmem_relinquish_2sm();
+    } else {
+      tmem_alloc(tmem_slot, 512);
+      tmem_relinquish();
+    }
   }
   const int cta = kPair ? blockIdx.x >> 1 : blockIdx.x;  // or pair of CTAs
   {  // equal ranges of the cost of all items: a thread adds up some sequences, or a share of one's
@@ -452,6 +470,13 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   }
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  // Arrives on a barrier that the issuer waits for, of TMEM (nothing in memory is published).
+  auto tell_issuer = [&](uint64_t* bar) {
+    if constexpr (kPair)
+      mbar_arrive_cluster_relaxed(cluster_map(smem_u32(bar), 0));
+    else
+      mbar_arrive(bar);
+  };
 
   if (warp == 0 || warp >= 10) {
     // ------------------------------------------------------------ TMA producers
@@ -461,18 +486,27 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     uint32_t armed = 0, armed_par = 0;  // stages whose copies were asked for, and their phases
     uint32_t marked = 0, land_par = 0;  // the same of `landed`, the phase after
     bool q_armed = false, bad = false;
-    const int rows = min(1 << a.page_shift, kPfKeys);  // of a box
     auto wait = [&](uint64_t* bar, uint32_t parity, int where) {
       if (!pf_wait(bar, parity, a.err, abort_flag, where)) bad = true;
       return !bad;
     };
-    // One half (kChan channels) of tile kt of K or V into the next ring slot.
-    auto load = [&](const CUtensorMap* tm, const PfItem& it, int kt, int half, uint32_t mark) {
+    // One half (kChan channels) of tile kt of K or V into the next ring slot; of a pair, this CTA's
+    // half of the tile.
+    auto load = [&](bool is_v, const PfItem& it, int kt, int half, uint32_t mark) {
       if (!wait(&empty[stage], phase ^ 1, 610)) return;
+      const int row_bits = kPair && !is_v ? 6 : 7;  // of a chunk
+      const int chunk_bits = S::kStageBits - 7 - row_bits;
+      const int first = kPair && !is_v ? rank << row_bits : 0;
+      const int chan = kPair ? (is_v ? rank * S::kChan : 0) : half * S::kChan;
       // A slot with rows to be zeroed is full when that is done, a moment after its copies.
       const bool any = __any_sync(0xffffffffu, mark != 0);
-      uint64_t* bar = any ? &landed[stage] : &full[stage];
-      if (me == 0 && lane == 0) mbar_arrive_expect_tx(bar, S::kStageBytes);
+      uint64_t* const bar = any ? &landed[stage] : &full[stage];
+      if (me == 0 && lane == 0) {
+        if (!kPair || any || rank == 0)
+          mbar_arrive_expect_tx(bar, (kPair && !any ? 2 : 1) << S::kStageBits);
+        else
+          tell_issuer(bar);
+      }
       if (!any) {
         armed |= 1u << stage;
         armed_par = (armed_par & ~(1u << stage)) | (phase << stage);
@@ -481,23 +515,32 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         land_par ^= 1u << stage;
       }
       __syncwarp();
-      constexpr int kSides = kPair ? 2 : 1;  // a pair's CTAs load half of the boxes each
-      const int boxes = kPfKeys / rows * (S::kChan / 64);
-      for (int i = me + kPfProducers * lane; i < boxes / kSides; i += 32 * kPfProducers) {
-        const int x = kSides * i + rank;
-        const int c = x % (S::kChan / 64), r = x / (S::kChan / 64) * rows;
-        const int j = kt * kPfKeys + r;
+      const int box_bits = min(a.page_shift, row_bits);
+      const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
+      uint8_t* const slot = smem + S::kRing + stage * S::kStageBytes;
+      const int boxes = 1 << (row_bits - box_bits + chunk_bits);
+      for (int x = me + kPfProducers * lane; x < boxes; x += 32 * kPfProducers) {
+        const int c = x & ((1 << chunk_bits) - 1), r = x >> chunk_bits << box_bits;
+        const int j = kt * kPfKeys + first + r;
         // a box outside the pool (past the last page, or of an entry that names none) is zeros
         int pg = j < it.len ? paged_page(a, a.table + (int64_t)it.b * a.s_table, j) : -1;
         if (pg < 0) pg = a.n_pages;
-        (kPair ? tma_load_4d_both : tma_load_4d)(
-            smem + S::kRing + stage * S::kStageBytes + c * S::kChunkBytes + r * 128, tm, bar,
-            half * S::kChan + c * 64, j & ((1 << a.page_shift) - 1), it.h, pg);
+        uint8_t* const dst = slot + ((c << row_bits) + r) * 128;
+        const int in = j & ((1 << a.page_shift) - 1);
+        if (kPair && !any)
+          tma_load_4d_2sm(dst, tm, cluster_map(smem_u32(bar), 0), chan + c * 64, in, it.h, pg);
+        else
+          tma_load_4d(dst, tm, bar, chan + c * 64, in, it.h, pg);
       }
       if (any && me == 0) {
         if (!wait(&landed[stage], ((land_par >> stage) & 1) ^ 1, 614)) return;
-        zero_rows(smem + S::kRing + stage * S::kStageBytes, S::kChan / 64, mark);
-        if (lane == 0) mbar_arrive(&full[stage]);
+        zero_rows(slot, 1 << chunk_bits, 1 << row_bits, first, mark);
+        if (lane == 0) {
+          if constexpr (kPair)
+            mbar_arrive_cluster(cluster_map(smem_u32(&full[stage]), 0));
+          else
+            mbar_arrive(&full[stage]);
+        }
       }
       if (++stage == kStages) {
         stage = 0;
@@ -518,7 +561,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       mark[0] = m;
       // without biases the row limits mask what K holds past the end
 #pragma unroll 1
-      for (int half = 0; half < kHalves && !bad; ++half) load(&tm_k, it, kt, half, kBias ? m : 0u);
+      for (int half = 0; half < kHalves && !bad; ++half) load(false, it, kt, half, kBias ? m : 0u);
     };
     PfWalk walk(a, tokens, start);
     PfItem it;
@@ -553,7 +596,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         if (kt >= it.k0) {
           const uint32_t m = kAhead == 2 && kt + 1 < it.k1 ? mark[1] : mark[0];
 #pragma unroll 1
-          for (int half = 0; half < kHalves && !bad; ++half) load(&tm_v, it, kt, half, m);
+          for (int half = 0; half < kHalves && !bad; ++half) load(true, it, kt, half, m);
         }
         if (kt + kAhead < it.k1 && !bad) load_k(it, kt + kAhead);
       }
@@ -581,6 +624,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         mbar_arrive(&qfull[n_items & 1]);
       }
     }
+    // (The odd CTA's copies count on the even CTA's barriers: its own run out of time here, in
+    // which the copies land, as do the even CTA's where one of the two had asked for no more.)
     if (lane == 0) {
       if (bad || *abort_flag) {
         for (int s = 0; s < kStages; ++s) {
@@ -590,17 +635,17 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         if (q_armed) (void)mbar_wait(&qfull[(n_items - 1) & 1], ((n_items - 1) >> 1) & 1);
       }
     }
-  } else if (warp == 1 && elect_one()) {
+  } else if (warp == 1 && rank == 0 && elect_one()) {
     // ------------------------------------------------------------ MMA issuer
-    constexpr uint32_t idesc_s = idesc_f16(128, kPfKeys, 1);
-    constexpr uint32_t idesc_o = idesc_f16(128, S::kChan, 1) | kIdescBMn;
+    constexpr uint32_t idesc_s = idesc_f16(128 * kSides, kPfKeys, 1);
+    constexpr uint32_t idesc_o = idesc_f16(128 * kSides, S::kChan * kSides, 1) | kIdescBMn;
     int stage = 0;
     uint32_t phase = 0;
     uint32_t n_i = 0, n_odd = 0;  // uses of buffer 0 (two tiles: of both), of buffer 1
     uint32_t n_items = 0;
     bool bad = false, issued = false;
     auto wait = [&](uint64_t* bar, uint32_t parity, int where) {
-      if (mbar_wait(bar, parity)) return true;
+      if (kPair ? mbar_wait_cluster(bar, parity) : mbar_wait(bar, parity)) return true;
       dev_set_error(a.err, DEV_WAIT_TIMEOUT, where);
       *abort_flag = 1;
       bad = true;
@@ -620,21 +665,27 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     const uint64_t k_desc = sdesc_k_sw128(smem_u32(smem + S::kRing));
     const uint64_t v_desc = sdesc_mn_sw128(smem_u32(smem + S::kRing), S::kChunkBytes);
     constexpr uint64_t kChunkStep = S::kChunkBytes >> 4, kStageStep = S::kStageBytes >> 4;
+    constexpr uint64_t kKStep = S::kKRows * 128 >> 4;  // from 64 channels of K to the next
+    constexpr int kSChunks = D / 64 / kHalves;         // of a ring slot of K
+    auto commit = [&](uint64_t* bar) {  // on the barrier of either CTA
+      if constexpr (kPair)
+        tc_commit_2sm_mc(bar, 3);
+      else
+        tc_commit(bar);
+    };
     // S of tile t into buffer buf, over the channels of one ring slot
     auto mma_s = [&](int buf, int t, int half, int s) {
       tc_fence_after();
-      const uint64_t q = q_desc + (t * (D / 64) + half * (S::kChan / 64)) * kChunkStep;
+      const uint64_t q = q_desc + (t * (D / 64) + half * kSChunks) * kChunkStep;
       const uint64_t k = k_desc + s * kStageStep;
 #pragma unroll
-      for (int c = 0; c < S::kChan / 64; ++c)
+      for (int c = 0; c < kSChunks; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          tc_mma_f16(tmem_base + buf * kSCols, q + c * kChunkStep + 2 * e,
-                     k + c * kChunkStep + 2 * e, idesc_s, half + c + e > 0);
+          (kPair ? tc_mma_f16_2sm : tc_mma_f16)(tmem_base + buf * kSCols, q + c * kChunkStep + 2 * e,
+                                                k + c * kKStep + 2 * e, idesc_s, half + c + e > 0);
       issued = true;
     };
-    // Slot s is free when all products so far are done; a pair's when both CTAs' are.
-    auto give = [&](int s) { (kPair ? tc_commit_both : tc_commit)(&empty[s]); };
     // O of tile t, the channels of one ring slot, += P in buffer buf times V
     // (slots [16 e0, 16 e1) of the tile)
     auto mma_o = [&](int buf, int t, int half, int s, bool first, int e0 = 0,
@@ -643,22 +694,24 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       const uint64_t v = v_desc + s * kStageStep;
 #pragma unroll
       for (int e = e0; e < e1; ++e)
-        mma_ts(tmem_base + kOAt + t * D + half * S::kChan, tmem_base + buf * kSCols + kPAt + 8 * e,
-               v + e * (2048 >> 4), idesc_o, !first || e > e0);
+        (kPair ? mma_ts_2sm : mma_ts)(tmem_base + kOAt + t * D + half * S::kChan,
+                                      tmem_base + buf * kSCols + kPAt + 8 * e,
+                                      v + e * (2048 >> 4), idesc_o, !first || e > e0);
     };
     while (!bad && !*abort_flag) {
       if (!wait(&qfull[n_items & 1], (n_items >> 1) & 1, 621)) break;
       const int n_k = shown[n_items & 1].k1 - shown[n_items & 1].k0;
       if (n_k < 1) break;
+      if (kPair && !wait(qpeer, n_items & 1, 636)) break;
       if constexpr (kTiles == 2) {
         int ks = take();
         if (ks < 0) break;
         mma_s(0, 0, 0, ks);
-        tc_commit(&sfull[0]);
+        commit(&sfull[0]);
         mma_s(1, 1, 0, ks);
-        tc_commit(&sfull[1]);
-        give(ks);
-        if (n_k == 1) tc_commit(qfree);
+        commit(&sfull[1]);
+        commit(&empty[ks]);
+        if (n_k == 1) commit(qfree);
 #pragma unroll 1
         for (int j = 0; j < n_k; ++j, ++n_i) {
           const bool more = j + 1 < n_k;
@@ -668,23 +721,23 @@ __global__ void __launch_bounds__(kPfThreads, 1)
           mma_o(0, 0, 0, vs, j == 0, 4, 8);
           if (!wait(&pfull[0], n_i & 1, 627)) break;
           mma_o(0, 0, 0, vs, false, 0, 4);
-          tc_commit(&pvdone[0]);
+          commit(&pvdone[0]);
           if (more) {
             if ((ks = take()) < 0) break;
             mma_s(0, 0, 0, ks);
-            tc_commit(&sfull[0]);
+            commit(&sfull[0]);
           }
           if (!wait(&phalf[1], n_i & 1, 624)) break;
           mma_o(1, 1, 0, vs, j == 0, 4, 8);
           if (!wait(&pfull[1], n_i & 1, 628)) break;
           mma_o(1, 1, 0, vs, false, 0, 4);
-          tc_commit(&pvdone[1]);
-          give(vs);
+          commit(&pvdone[1]);
+          commit(&empty[vs]);
           if (more) {
             mma_s(1, 1, 0, ks);
-            tc_commit(&sfull[1]);
-            give(ks);
-            if (j + 2 == n_k) tc_commit(qfree);
+            commit(&sfull[1]);
+            commit(&empty[ks]);
+            if (j + 2 == n_k) commit(qfree);
           }
         }
       } else {
@@ -696,10 +749,10 @@ __global__ void __launch_bounds__(kPfThreads, 1)
             const int s = take();
             if (s < 0) return;
             mma_s(buf, 0, half, s);
-            give(s);
+            commit(&empty[s]);
           }
-          tc_commit(&sfull[buf]);
-          if (i + 1 == n_k) tc_commit(qfree);
+          commit(&sfull[buf]);
+          if (i + 1 == n_k) commit(qfree);
         };
         auto add_pv = [&](auto buf, uint32_t& uses, int i) {
           if (!wait(&phalf[buf], uses & 1, 625)) return;
@@ -714,9 +767,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 #pragma unroll
           for (int half = 0; half < kHalves; ++half) {
             mma_o(buf, 0, half, vs[half], false, 0, 4);
-            give(vs[half]);
+            commit(&empty[vs[half]]);
           }
-          tc_commit(&pvdone[buf]);
+          commit(&pvdone[buf]);
           ++uses;
         };
         constexpr std::integral_constant<int, 0> b0;
@@ -735,8 +788,19 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       ++n_items;
     }
     if ((bad || *abort_flag) && issued) {
-      tc_commit(drain);
+      commit(drain);
       (void)mbar_wait(drain, 0);
+    }
+  } else if (kPair && warp == 1 && rank == 1 && elect_one()) {
+    // ------------------------------------------------------------ q of the odd CTA
+    for (uint32_t n = 0; !*abort_flag; ++n) {
+      if (!mbar_wait(&qfull[n & 1], (n >> 1) & 1)) {
+        dev_set_error(a.err, DEV_WAIT_TIMEOUT, 637);
+        *abort_flag = 1;
+        break;
+      }
+      if (shown[n & 1].k1 <= shown[n & 1].k0) break;
+      mbar_arrive_cluster(cluster_map(smem_u32(qpeer), 0));
     }
   } else if (warp >= 2) {
     // ------------------------------------------------------------ softmax and output
@@ -896,7 +960,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&phalf[wg]);
+            if (lane == 0) tell_issuer(&phalf[wg]);
           }
         }
         float l0, l1;
@@ -905,7 +969,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();  // and kw is written again
-        if (lane == 0) mbar_arrive(&pfull[wg]);
+        if (lane == 0) tell_issuer(&pfull[wg]);
       }
       if (bad) break;
       // ---- the item's rows
@@ -987,7 +1051,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(ofree);
+      if (lane == 0) tell_issuer(ofree);
     }
   }
   tc_fence_before();
@@ -998,7 +1062,10 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   }
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem_base, 512);
+    if constexpr (kPair)
+      tmem_dealloc_2sm(tmem_base, 512);
+    else
+      tmem_dealloc(tmem_base, 512);
   }
 }
 
@@ -1051,15 +1118,16 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-// dims {channels, slots, KV-heads, pages}; boxes of 64 channels of the slots of a page
-bool pool_tmap(CUtensorMap* m, const PagedArgs& a, const void* ptr) {
+// dims {channels, slots, KV-heads, pages}; boxes of 64 channels of the slots of a page, at most
+// `rows` of them
+bool pool_tmap(CUtensorMap* m, const PagedArgs& a, const void* ptr, int rows) {
   auto enc = tensor_map_encoder();
   if (enc == nullptr) return false;
   const cuuint64_t page = (cuuint64_t)1 << a.page_shift;
   cuuint64_t dims[4] = {(cuuint64_t)a.d, page, (cuuint64_t)a.H, (cuuint64_t)a.n_pages};
   cuuint64_t strides[3] = {(cuuint64_t)a.s_slot * 2, (cuuint64_t)a.s_head * 2,
                            (cuuint64_t)a.s_page * 2};
-  cuuint32_t box[4] = {64, (cuuint32_t)std::min<cuuint64_t>(page, kPfKeys), 1, 1};
+  cuuint32_t box[4] = {64, (cuuint32_t)std::min<cuuint64_t>(page, rows), 1, 1};
   cuuint32_t estr[4] = {1, 1, 1, 1};
   return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box,
              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
@@ -1083,7 +1151,7 @@ bool query_tmap(CUtensorMap* m, const PagedArgs& a, const PagedQuery& q, int tok
 template <int D, bool kBias, bool kPair>
 cudaError_t launch_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
                            const KernelTable& dev, cudaStream_t s) {
-  using S = PfShape<D, kBias>;
+  using S = PfShape<D, kBias, kPair>;
   constexpr int kCluster = kPair ? 2 : 1;
   using Id = KernelId<paged_prefill_kernel<D, kBias, kPair>, kPfThreads, S::kBytes, kCluster>;
   if (dev.of<Id>().status != cudaSuccess) return dev.of<Id>().status;
@@ -1097,7 +1165,8 @@ cudaError_t launch_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
   f.part_ml = reinterpret_cast<float2*>(f.part_o + (int64_t)2 * ranges * rows * (D / 4));
   f.split = reinterpret_cast<PfSplit*>(f.part_ml + (int64_t)2 * ranges * rows);
   CUtensorMap tq, tk, tv;
-  if (!query_tmap(&tq, a, q, f.tile_tokens) || !pool_tmap(&tk, a, a.K) || !pool_tmap(&tv, a, a.V))
+  if (!query_tmap(&tq, a, q, f.tile_tokens) || !pool_tmap(&tk, a, a.K, S::kKRows) ||
+      !pool_tmap(&tv, a, a.V, kPfKeys))
     return cudaErrorInvalidValue;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
@@ -1135,10 +1204,9 @@ size_t paged_prefill_workspace(const PagedArgs& a, int num_sms) {
 cudaError_t launch_paged_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
                                  const KernelTable& dev, cudaStream_t s) {
   // 256 channels in pairs of CTAs where sequences have rows for two tiles. Three prompts of 900 to
-  // 2,300 tokens, 8 KV-heads with 2 query heads each, pages of 16: 216 us against 243; 8,192
-  // tokens: 504 against 577 in pages of 16, 439 against 444 in pages of 128. Where the second tile
-  // has two rows (65 tokens of 2 heads over 2,000 slots, 4 KV-heads): 57 us against 62 for 16
-  // sequences; for 4 sequences of 100 tokens 35 against 33.
+  // 2,300 tokens, 8 KV-heads with 2 query heads each, pages of 16: 178 us against 243. Where the
+  // second tile is almost empty (65 tokens of 2 heads over 2,000 slots, 4 KV-heads, 16 sequences):
+  // 51 us against 62; 4 sequences of 100 tokens 31 against 33, of 150 without a past 21 and 21.
   const bool bias = a.beta != nullptr, pair = paged_mean_rows(a, q.Hq) > 128;
   switch (a.d) {
     case 64:
