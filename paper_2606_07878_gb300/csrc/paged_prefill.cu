@@ -39,9 +39,9 @@
 // that take turns, with S read from TMEM twice. (Held in registers in between: 375 us at a stage of
 // this kernel that took 352 otherwise, for the spills.) Biases cost a read of shared memory and two
 // packed operations per two logits: 1.2 PFLOP/s. 8,192 tokens of 8 KV- and 16 query heads of 256
-// channels (half the softmax for the same products): 350 us, 1.57 PFLOP/s; 412 in pages of 16, for
-// the copies. There each CTA with a tile and all of K and V: 444 and 577; the pair with copies of
-// all of K and V in both, loaded once by multicast: 432 and 490.
+// channels (half the softmax for the same products): 331 us, 1.66 PFLOP/s; 381 in pages of 16, for
+// the copies; 350 and 412 with pages looked up behind the wait for a ring slot. With a tile and all
+// of K and V on each SM: 444 and 577; loaded once for a pair by multicast: 432 and 490.
 #include <algorithm>
 #include <type_traits>
 
@@ -493,11 +493,21 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     // One half (kChan channels) of tile kt of K or V into the next ring slot; of a pair, this CTA's
     // half of the tile.
     auto load = [&](bool is_v, const PfItem& it, int kt, int half, uint32_t mark) {
-      if (!wait(&empty[stage], phase ^ 1, 610)) return;
       const int row_bits = kPair && !is_v ? 6 : 7;  // of a chunk
       const int chunk_bits = S::kStageBits - 7 - row_bits;
       const int first = kPair && !is_v ? rank << row_bits : 0;
       const int chan = kPair ? (is_v ? rank * S::kChan : 0) : half * S::kChan;
+      // this lane's box, if any (16 at most, of 16 slots); its page is looked up ahead of the wait
+      const int box_bits = min(a.page_shift, row_bits);
+      const int x = me + kPfProducers * lane;
+      const bool copies = x < 1 << (row_bits - box_bits + chunk_bits);
+      static_assert(S::kStageBytes / (16 * 128) <= 32, "a box a lane");
+      const int c = x & ((1 << chunk_bits) - 1), r = x >> chunk_bits << box_bits;
+      const int j = kt * kPfKeys + first + r;
+      // a box outside the pool (past the last page, or of an entry that names none) is zeros
+      int pg = copies && j < it.len ? paged_page(a, a.table + (int64_t)it.b * a.s_table, j) : -1;
+      if (pg < 0) pg = a.n_pages;
+      if (!wait(&empty[stage], phase ^ 1, 610)) return;
       // A slot with rows to be zeroed is full when that is done, a moment after its copies.
       const bool any = __any_sync(0xffffffffu, mark != 0);
       uint64_t* const bar = any ? &landed[stage] : &full[stage];
@@ -515,16 +525,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         land_par ^= 1u << stage;
       }
       __syncwarp();
-      const int box_bits = min(a.page_shift, row_bits);
-      const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
       uint8_t* const slot = smem + S::kRing + stage * S::kStageBytes;
-      const int boxes = 1 << (row_bits - box_bits + chunk_bits);
-      for (int x = me + kPfProducers * lane; x < boxes; x += 32 * kPfProducers) {
-        const int c = x & ((1 << chunk_bits) - 1), r = x >> chunk_bits << box_bits;
-        const int j = kt * kPfKeys + first + r;
-        // a box outside the pool (past the last page, or of an entry that names none) is zeros
-        int pg = j < it.len ? paged_page(a, a.table + (int64_t)it.b * a.s_table, j) : -1;
-        if (pg < 0) pg = a.n_pages;
+      if (copies) {
+        const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
         uint8_t* const dst = slot + ((c << row_bits) + r) * 128;
         const int in = j & ((1 << a.page_shift) - 1);
         if (kPair && !any)
@@ -682,8 +685,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       for (int c = 0; c < kSChunks; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          (kPair ? tc_mma_f16_2sm : tc_mma_f16)(tmem_base + buf * kSCols, q + c * kChunkStep + 2 * e,
-                                                k + c * kKStep + 2 * e, idesc_s, half + c + e > 0);
+          (kPair ? tc_mma_f16_2sm : tc_mma_f16)(
+              tmem_base + buf * kSCols, q + c * kChunkStep + 2 * e, k + c * kKStep + 2 * e, idesc_s,
+              half + c + e > 0);
       issued = true;
     };
     // O of tile t, the channels of one ring slot, += P in buffer buf times V
@@ -1204,7 +1208,7 @@ size_t paged_prefill_workspace(const PagedArgs& a, int num_sms) {
 cudaError_t launch_paged_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
                                  const KernelTable& dev, cudaStream_t s) {
   // 256 channels in pairs of CTAs where sequences have rows for two tiles. Three prompts of 900 to
-  // 2,300 tokens, 8 KV-heads with 2 query heads each, pages of 16: 178 us against 243. Where the
+  // 2,300 tokens, 8 KV-heads with 2 query heads each, pages of 16: 172 us against 243. Where the
   // second tile is almost empty (65 tokens of 2 heads over 2,000 slots, 4 KV-heads, 16 sequences):
   // 51 us against 62; 4 sequences of 100 tokens 31 against 33, of 150 without a past 21 and 21.
   const bool bias = a.beta != nullptr, pair = paged_mean_rows(a, q.Hq) > 128;
