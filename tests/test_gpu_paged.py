@@ -178,6 +178,11 @@ def test_decode_matches_64_bits(ctx, d, H, Hq, page, lens, beta, heads_first):
     (256, 4, 8, 256, [900, 0, 65], [300, 5, 0], False, False),
     (256, 1, 1, 16, [130, 257, 1], [0, 128, 77], True, False),
     (256, 8, 24, 32, [333, 40, 700, 2], [0, 1500, 77, 0], True, True),
+    # items in more ranges than a block of the join looks through alone
+    (64, 1, 40, 16, [2], [9000], False, True),
+    (128, 1, 24, 64, [1, 30], [20, 11000], True, False),
+    (256, 1, 12, 16, [3], [9000], True, False),
+    (256, 1, 16, 64, [20], [12000], True, False),
     (64, 1, 200, 16, [3, 1], [70, 0], False, False),
     (128, 1, 2, 16, [(7 * i) % 23 for i in range(500)], [(11 * i) % 50 for i in range(500)], True,
      False),
