@@ -131,8 +131,8 @@ __global__ void __launch_bounds__(kAppendThreads)
 // lies in one range is written by its warp; the parts of another meet in the workspace, and a
 // second launch joins them in their order. Ranges of CTAs instead, whose warps join after every
 // set, with the last CTA of a set joining its parts: 36 / 109 / 170 / 193 us where this takes 32 /
-// 90 / 169 / 180 (8 sequences of 1,312 to 5,408 slots; 256 of 165 to 701; 24 of 8,192 to 32,768; one
-// of 131,072 with 256 channels); the last warp joining in this kernel: 40 / 93 / 181 / 186.
+// 90 / 169 / 180 (8 sequences of 1,312 to 5,408 slots; 256 of 165 to 701; 24 of 8,192 to 32,768;
+// one of 131,072 with 256 channels); the last warp joining in this kernel: 40 / 93 / 181 / 186.
 //
 // Memory bounds the large calls: the 24 sequences are 1.0 GB, 5.95 TB/s and 0.88 of a copy, with
 // the mma.sync pipe at 12%, so the tensor cores of tcgen05 would have nothing to gain. Small calls

@@ -33,7 +33,7 @@
 // Work: a CTA an SM, equal ranges of the cost of all items; what several CTAs share of an item goes
 // to the workspace and a second launch joins it.
 //
-// 8,192 tokens over themselves, 28 query and 4 KV-heads of 128 channels (481 GFLOP): 337 us, 1.43
+// 8,192 tokens over themselves, 28 query and 4 KV-heads of 128 channels (481 GFLOP): 339 us, 1.42
 // PFLOP/s, 0.75 of the library's matrix product. The tensor pipe is busy 71% of the kernel, tensor
 // memory 75%, issue slots 48%: what is left is the chain S, maximum, exponentials, P of two tiles
 // that take turns, with S read from TMEM twice. (Held in registers in between: 375 us at a stage of
