@@ -234,7 +234,7 @@ struct PfShape {
   // one tile only: running maxima and sums, [2][128] each
   static constexpr int kXchAt = kBiasAt + (kBias ? 8 * kPfKeys * 4 : 0);
   static constexpr int kBarAt = kXchAt + (kTiles == 1 ? 2048 : 0);
-  static constexpr int kPlanAt = kBarAt + (3 * kStages + 28) * 8;
+  static constexpr int kPlanAt = kBarAt + (3 * kStages + 30) * 8;
   static constexpr int kBytes = kPlanAt + sizeof(PfPlan);
   static_assert(kBytes <= 232448, "shared memory budget");
 };
@@ -337,8 +337,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   int64_t* warp_cost = plan.warp_cost;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kBarAt);  // ring slot loaded
   uint64_t* empty = full + kStages;   // ring slot consumed
-  // [2] q of item n loaded and the item shown, n & 1. (The softmax of an item of one tile of slots
-  // may wait for it only when the next one's q has come as well.)
+  // [2] q of item n loaded and the item shown, n & 1. An item of one tile of slots may pass the
+  // issuer without the other softmax warpgroup of 256 channels, and the next one's S behind it: the
+  // record is written again only when all warps have said (seen) that they read it.
   uint64_t* qfull = empty + kStages;
   uint64_t* qfree = qfull + 2;       // an item's last S complete
   uint64_t* sfull = qfree + 1;       // [2] S_i complete
@@ -353,9 +354,10 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   uint64_t* phalf = landed + kStages;  // [2] the last 64 slots of P_i written
   uint64_t* qpeer = phalf + 2;  // the other CTA's q loaded
   uint64_t* drain = qpeer + 1;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  uint64_t* seen = drain + 1;  // [2] the softmax warps have read shown[n & 1]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(seen + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((3 * kStages + 26) * 8 + 16 == S::kPlanAt - S::kBarAt, "barriers");
+  static_assert((3 * kStages + 28) * 8 + 16 == S::kPlanAt - S::kBarAt, "barriers");
 
   const PagedArgs& a = f.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -391,6 +393,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     for (int i = 0; i < 8; ++i) mbar_init(&mb[i], 1);
     for (int i = 0; i < 4; ++i) mbar_init(&lb[i], 2);
     mbar_init(drain, 1);
+    mbar_init(&seen[0], 8);
+    mbar_init(&seen[1], 8);
     *abort_flag = 0;
     fence_mbar_init();
     tma_prefetch_desc(&tm_q);
@@ -581,6 +585,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         continue;
       }
       if (me == 0 && n_items > 0 && !wait(qfree, (n_items - 1) & 1, 611)) break;
+      if (me == 0 && n_items > 1 && !wait(&seen[n_items & 1], ((n_items >> 1) - 1) & 1, 615)) break;
       if (me == 0 && lane == 0) {
         shown[n_items & 1] = it;
         if (it.part == 2 && rank == 0) {
@@ -628,6 +633,11 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       }
       if (!bad && !*abort_flag && n_items > 0 && !mbar_wait(qfree, (n_items - 1) & 1)) {
         dev_set_error(a.err, DEV_WAIT_TIMEOUT, 613);
+        *abort_flag = 1;
+      }
+      if (!bad && !*abort_flag && n_items > 1 &&
+          !mbar_wait(&seen[n_items & 1], ((n_items >> 1) - 1) & 1)) {
+        dev_set_error(a.err, DEV_WAIT_TIMEOUT, 616);
         *abort_flag = 1;
       }
       if (!*abort_flag) {  // no more items
@@ -849,6 +859,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     for (uint32_t n_items = 0; !bad && !warp_flag(abort_flag); ++n_items) {
       if (!wait_all(&qfull[n_items & 1], (n_items >> 1) & 1, 629)) break;
       const PfItem it = shown[n_items & 1];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&seen[n_items & 1]);
       if (it.k1 <= it.k0) break;
       const bool valid = row < f.tile_tokens * g && token < it.tokens;
       // (rows of no token are not stored: they need no masks)
