@@ -236,8 +236,9 @@ still_status still_compact_layer_beta(still_ctx* ctx, int32_t layer, const void*
  *   scale  logit scale; 0 means 1 / sqrt(d)
  * d in {64, 128, 256}, t + S >= 1, nq * Hq / H <= 64; tensor pointers 16-byte aligned.
  * Keys are processed in slots whose partial results are merged in a fixed order; the
- * context's workspace holds the partials (grown on demand), so calls that share a context (this
- * one and the compaction calls) must be ordered on one stream or otherwise serialised. */
+ * context's workspace holds the partials (grown on demand, which frees the old one: a captured call
+ * stays valid while no later call needs more), so calls that share a context (this one and the
+ * compaction calls) must be ordered on one stream or otherwise serialised. */
 still_status still_attend_biased(still_ctx* ctx, const void* q, int32_t nq, int32_t Hq,
                                  const void* Ck, const void* Cv, const float* beta, int64_t t,
                                  const void* Kfix, const void* Vfix, int64_t S, int32_t H,
@@ -324,9 +325,10 @@ still_status still_paged_append(still_ctx* ctx, const still_paged_cache* cache,
  * expected finite even where earlier tokens of its call do not see it.
  * out must not overlap q or the pools. Device-side argument faults are recorded as by
  * still_paged_append; what rows that would read a page outside the pool come out as is unspecified.
- * Partial results lie in the context's workspace, whose size depends on head_dim alone (at most 41
- * MB). The first call of a kind allocates it, so it belongs before a capture, and calls that share
- * a context must be ordered on one stream or otherwise serialised. */
+ * Partial results lie in a workspace of these two calls alone (41 MB on 152 SMs). The context's
+ * first call of either allocates it for every size, so that call belongs before a capture; it stays
+ * where it is until still_destroy, so that captured calls stay valid whatever else the context is
+ * used for. Calls that share a context must be ordered on one stream or otherwise serialised. */
 still_status still_paged_decode(still_ctx* ctx, const still_paged_cache* cache,
                                 const still_paged_batch* batch, const void* q, int64_t q_stride,
                                 int32_t Hq, float scale, void* out, void* stream);
@@ -483,8 +485,10 @@ still_status still_workspace_size(const still_ctx* ctx, int64_t max_tokens, int3
  * nothing. still_compact_layer and still_compact_stack enqueue work only on their stream and
  * neither allocate nor synchronize when the workspace suffices: such calls can be captured into
  * a CUDA graph and replayed, whatever sizes were called before (still_create sets the kernels'
- * attributes and asks for their residency on its device). Kernel timing (still_profile_*) should cover only the classes needed while
- * capturing: timed launches become event nodes of the graph. */
+ * attributes and asks for their residency on its device). A call that needs more replaces the
+ * workspace and frees the old one, which captured calls still name: reserve for the largest call
+ * before the first capture. Kernel timing (still_profile_*) should cover only the classes needed
+ * while capturing: timed launches become event nodes of the graph. */
 still_status still_reserve_workspace(still_ctx* ctx, int64_t max_tokens, int32_t max_t);
 
 /* Upper bound on the workspace the context may allocate (default 48 GiB). Calls whose

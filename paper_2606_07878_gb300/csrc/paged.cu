@@ -851,8 +851,12 @@ int paged_mean_rows(const PagedArgs& a, int Hq) {
   return (int)(((int64_t)a.n * (Hq / a.H) + a.B - 1) / a.B);
 }
 
-size_t paged_rows_workspace(const PagedArgs& a, int Hq, int num_sms) {
-  return rows_form(a.d, paged_mean_rows(a, Hq), [&](auto form) { return form.bytes(num_sms); });
+size_t paged_rows_workspace(int num_sms) {
+  size_t most = 0;
+  for (int d : {64, 128, 256})
+    for (int rows : {8, 16})
+      most = std::max(most, rows_form(d, rows, [&](auto form) { return form.bytes(num_sms); }));
+  return most;
 }
 
 cudaError_t launch_paged_rows(const PagedArgs& a, const PagedQuery& p, void* ws, int num_sms,

@@ -53,16 +53,17 @@ struct PagedQuery {
   float scale = 0.f;
 };
 // Few rows (paged.cu), and the join of what several warps share: two launches. ws:
-// paged_rows_workspace bytes.
+// paged_rows_workspace bytes, enough for every call.
 int paged_mean_rows(const PagedArgs& a, int Hq);  // of a sequence and KV-head, rounded up
-size_t paged_rows_workspace(const PagedArgs& a, int Hq, int num_sms);
+size_t paged_rows_workspace(int num_sms);
 cudaError_t launch_paged_rows(const PagedArgs& a, const PagedQuery& q, void* ws, int num_sms,
                               cudaStream_t s);
 
 // Many rows, on the tensor cores (paged_prefill.cu), and the join of what several CTAs share: two
-// launches. paged_prefill_serves: whether a call takes this kernel.
+// launches. paged_prefill_serves: whether a call takes this kernel. ws: paged_prefill_workspace
+// bytes, enough for every call.
 bool paged_prefill_serves(const PagedArgs& a, int Hq);
-size_t paged_prefill_workspace(const PagedArgs& a, int num_sms);
+size_t paged_prefill_workspace(int num_sms);
 cudaError_t launch_paged_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
                                  const KernelTable& dev, cudaStream_t s);
 

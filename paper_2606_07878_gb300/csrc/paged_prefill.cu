@@ -1260,9 +1260,13 @@ bool paged_prefill_serves(const PagedArgs& a, int Hq) {
   return Hq / a.H <= 128 && paged_mean_rows(a, Hq) > (a.d == 256 ? 8 : 16);
 }
 
-size_t paged_prefill_workspace(const PagedArgs& a, int num_sms) {
-  const size_t rows = a.d <= 128 ? 256 : 128;
-  return (size_t)num_sms * (2 * rows * (a.d * 4 + 8) + sizeof(PfSplit));
+size_t paged_prefill_workspace(int num_sms) {
+  size_t most = 0;
+  for (size_t d : {64, 128, 256}) {
+    const size_t rows = d <= 128 ? 256 : 128;
+    most = std::max(most, (size_t)num_sms * (2 * rows * (d * 4 + 8) + sizeof(PfSplit)));
+  }
+  return most;
 }
 
 cudaError_t launch_paged_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,

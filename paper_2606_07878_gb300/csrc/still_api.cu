@@ -173,6 +173,9 @@ struct still_ctx {
   std::vector<LayerW> layers;
   void* ws = nullptr;
   size_t ws_bytes = 0;
+  // Of the attention over paged caches: one size for every call, never freed or moved before
+  // still_destroy, so that a captured step stays valid whatever is called after it.
+  void* paged_ws = nullptr;
   size_t ws_limit = size_t(48) << 30;
   size_t qhat_eager_limit = size_t(2) << 30;
   bool key_fold = true;  // fold W_K into the queries where the layer allows it
@@ -517,6 +520,18 @@ still_status ensure_ws(still_ctx* ctx, size_t bytes) {
     return STILL_ERR_OOM;
   }
   ctx->ws_bytes = bytes;
+  return STILL_OK;
+}
+
+still_status ensure_paged_ws(still_ctx* ctx) {
+  if (ctx->paged_ws != nullptr) return STILL_OK;
+  const int nsm = ctx->kernels.num_sms;
+  if (cudaMalloc(&ctx->paged_ws, std::max(paged_rows_workspace(nsm),
+                                          paged_prefill_workspace(nsm))) != cudaSuccess) {
+    cudaGetLastError();
+    ctx->paged_ws = nullptr;
+    return STILL_ERR_OOM;
+  }
   return STILL_OK;
 }
 
@@ -1501,6 +1516,7 @@ still_status still_destroy(still_ctx* ctx) {
   cudaDeviceSynchronize();
   for (auto& L : ctx->layers) free_layer(L);
   if (ctx->ws) cudaFree(ctx->ws);
+  if (ctx->paged_ws) cudaFree(ctx->paged_ws);
   if (ctx->err) cudaFree(ctx->err);
   delete ctx;
   return STILL_OK;
@@ -1792,15 +1808,12 @@ still_status paged_attend(still_ctx* ctx, const still_paged_cache* cache,
   p.scale = scale > 0.f ? scale : 1.f / std::sqrt((float)a.d);
   CK(cudaSetDevice(ctx->device));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const int nsm = ctx->kernels.num_sms;
-  if (paged_prefill_serves(a, Hq)) {
-    TRY(ensure_ws(ctx, paged_prefill_workspace(a, nsm)));
-    KLAUNCH(STILL_K_PAGED_ATTEND, launch_paged_prefill(a, p, ctx->ws, ctx->kernels, s));
-    ctx->prof.launches[STILL_K_PAGED_ATTEND] += 1;  // the join
-    return STILL_OK;
-  }
-  TRY(ensure_ws(ctx, paged_rows_workspace(a, Hq, nsm)));
-  KLAUNCH(STILL_K_PAGED_ATTEND, launch_paged_rows(a, p, ctx->ws, nsm, s));
+  TRY(ensure_paged_ws(ctx));
+  if (paged_prefill_serves(a, Hq))
+    KLAUNCH(STILL_K_PAGED_ATTEND, launch_paged_prefill(a, p, ctx->paged_ws, ctx->kernels, s));
+  else
+    KLAUNCH(STILL_K_PAGED_ATTEND,
+            launch_paged_rows(a, p, ctx->paged_ws, ctx->kernels.num_sms, s));
   ctx->prof.launches[STILL_K_PAGED_ATTEND] += 1;  // the join
   return STILL_OK;
 }
