@@ -66,5 +66,8 @@ bool paged_prefill_serves(const PagedArgs& a, int Hq);
 size_t paged_prefill_workspace(int num_sms);
 cudaError_t launch_paged_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
                                  const KernelTable& dev, cudaStream_t s);
+// What its plan adds up for items [q0, q1), of `tokens` new tokens each, of a sequence with `count`
+// of them and `len` slots: tiles of 128 slots, and an item's beginning and end as two more.
+int64_t paged_prefill_cost(int count, int len, int tokens, int q0, int q1);
 
 }  // namespace still

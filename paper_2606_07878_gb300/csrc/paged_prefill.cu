@@ -241,9 +241,15 @@ struct PfShape {
 
 STILL_DEV int pf_tiles(const Seq& s, int tokens) { return (s.count + tokens - 1) / tokens; }
 // Tiles of slots that item qt of a sequence sees.
-STILL_DEV int pf_slots(const Seq& s, int tokens, int qt) {
-  const int most = s.len - s.count + min(s.count, (qt + 1) * tokens);
+__host__ __device__ __forceinline__ int pf_slots(const Seq& s, int tokens, int qt) {
+  const int upto = (qt + 1) * tokens, most = s.len - s.count + (upto < s.count ? upto : s.count);
   return most > 0 ? (most + kPfKeys - 1) / kPfKeys : 0;
+}
+// Cost of items [q0, q1) of a sequence and KV-head: a million tokens pass 32 bits.
+__host__ __device__ __forceinline__ int64_t pf_cost(const Seq& s, int tokens, int q0, int q1) {
+  int64_t sum = 0;
+  for (int qt = q0; qt < q1; ++qt) sum += pf_slots(s, tokens, qt) + kPfItemCost;
+  return sum;
 }
 
 // The items of a CTA's range, in order: sequences, tokens, KV-heads. An item's cost is its tiles of
@@ -420,10 +426,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     for (int b = sb0; b < sb1; ++b) {
       const Seq s = paged_seq(a, b);
       const int nq = pf_tiles(s, tokens);
-      int sum = 0;
-      for (int qt = first_item(nq, share); qt < first_item(nq, share + 1); ++qt)
-        sum += pf_slots(s, tokens, qt) + kPfItemCost;
-      mine += (int64_t)sum * a.H;
+      mine += pf_cost(s, tokens, first_item(nq, share), first_item(nq, share + 1)) * a.H;
     }
     int64_t before = mine, total = 0;
 #pragma unroll
@@ -1258,6 +1261,10 @@ bool paged_prefill_serves(const PagedArgs& a, int Hq) {
   // 49 / 48, 64 / 49; 32 rows 49 / 39, 80 / 49, 96 / 49. Groups of more than 128 query heads do not
   // fit a tile.
   return Hq / a.H <= 128 && paged_mean_rows(a, Hq) > (a.d == 256 ? 8 : 16);
+}
+
+int64_t paged_prefill_cost(int count, int len, int tokens, int q0, int q1) {
+  return pf_cost(Seq{0, count, len}, tokens, q0, q1);
 }
 
 size_t paged_prefill_workspace(int num_sms) {

@@ -2299,6 +2299,12 @@ size_t still_internal_reserve(const still_layer_config* cfg, int32_t split_tiles
   return plan_reserve(*cfg, split_tiles, lazy_q != 0, Kp, N, t, limit, &bytes) ? bytes : 0;
 }
 
+// The share of a paged prefill's cost that one thread of its plan adds up (paged_prefill_cost).
+int64_t still_internal_paged_cost(int32_t count, int32_t len, int32_t tokens, int32_t q0,
+                                  int32_t q1) {
+  return paged_prefill_cost(count, len, tokens, q0, q1);
+}
+
 // Fills a context's kernel table with the caller's answers in place of the driver's; returns the
 // number of kernels. out: per kernel the status, then the resident clusters of 1 .. 8 CTAs.
 int still_internal_kernel_table(int32_t sms, int (*set_smem)(const void* fn, int bytes),
