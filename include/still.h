@@ -306,8 +306,9 @@ typedef struct {
  *   rope_theta  0: nothing is rotated and q must be NULL (the slots of a compact cache are at
  *           their positions already: Ck, Cv and beta of the compaction calls go in as they are)
  * Pointers 16-byte aligned, pitches multiples of 8. No two tokens of a call may share a slot.
- * A table entry outside the pool, a length beyond the table or offsets outside 0 .. n are
- * recorded (still_get_device_status: STILL_ERR_CUDA, detail code 2); such a token is skipped. */
+ * A table entry outside the pool, a length beyond the table, offsets outside 0 .. n, and tokens
+ * that no sequence owns (cu_new[0] above 0, cu_new[B] below n) are recorded
+ * (still_get_device_status: STILL_ERR_CUDA, detail code 2); such a token is skipped. */
 still_status still_paged_append(still_ctx* ctx, const still_paged_cache* cache,
                                 const still_paged_batch* batch, int32_t n, const void* k,
                                 int64_t k_stride, const void* v, int64_t v_stride,
@@ -324,7 +325,8 @@ still_status still_paged_append(still_ctx* ctx, const still_paged_cache* cache,
  * still_paged_prefill: any number of tokens per sequence, causal among them. A token's V is
  * expected finite even where earlier tokens of its call do not see it.
  * out must not overlap q or the pools. Device-side argument faults are recorded as by
- * still_paged_append; what rows that would read a page outside the pool come out as is unspecified.
+ * still_paged_append; rows that would read a page outside the pool come out as anything, those of
+ * tokens that no sequence owns stay as they were.
  * Partial results lie in a workspace of these two calls alone (41 MB on 152 SMs). The context's
  * first call of either allocates it for every size, so that call belongs before a capture; it stays
  * where it is until still_destroy, so that captured calls stay valid whatever else the context is

@@ -10,7 +10,8 @@ constexpr float kLog2e = 1.44269504f;
 STILL_DEV uint32_t bf16x2_bits(__nv_bfloat162 x) { return *reinterpret_cast<uint32_t*>(&x); }
 
 // First new token, number of them and slots of sequence b, whatever the arrays hold: an offset
-// outside [0, n] or a length beyond the table is cut, and recorded (by one of those who look).
+// outside [0, n] or a length beyond the table is cut, and recorded (by one of those who look), as
+// are tokens before the first sequence's and behind the last one's, which belong to none.
 struct Seq {
   int first, count, len;
 };
@@ -24,7 +25,8 @@ STILL_DEV Seq paged_seq(const PagedArgs& a, int b) {
   }
   const int cap = (int)min((int64_t)a.table_pages << a.page_shift, (int64_t)0x7fffff00);
   s.len = a.len[b];
-  if (c0 < 0 || c1 < c0 || c1 > a.n || s.len < 0 || s.len > cap) {
+  const bool owned = (b > 0 || c0 == 0) && (b + 1 < a.B || c1 == a.n);
+  if (!owned || c0 < 0 || c1 < c0 || c1 > a.n || s.len < 0 || s.len > cap) {
     if (kRecord) dev_set_error(a.err, DEV_BAD_ARG, 600);
     c0 = min(max(c0, 0), a.n);
     c1 = min(max(c1, c0), a.n);

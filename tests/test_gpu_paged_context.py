@@ -99,3 +99,40 @@ def test_workspace_is_allocated_once(ctx):
         still.still_paged_prefill(ctx, *call)
         torch.cuda.synchronize()
         assert torch.cuda.mem_get_info()[0] == free
+
+
+@pytest.mark.parametrize("new,n", [([7, 3], 11), ([30, 10], 90), ([0, 0], 3)])
+@pytest.mark.parametrize("first", [0, 1])
+def test_tokens_of_no_sequence_are_recorded(new, n, first):
+    """Rows before the first offset or behind the last one: the record says so, their own outputs
+    stay, and everybody else's are right. One call of each kind, and both kernels of prefill."""
+    c = still.still_create(0)
+    try:
+        p = Pages(60, [x + 70 for x in new], 1, 64, 16)
+        cu = torch.tensor([0, new[0], sum(new)], dtype=torch.int32, device=DEV) + first
+        lens = torch.tensor(p.lens, dtype=torch.int32, device=DEV)
+        mine = slice(first, first + sum(new))
+        for Hq in (1, 8):  # the seven and three tokens: few rows, then many
+            q, k, v = fused_rows(61, n + first, [Hq, 1, 1], 64)
+            out = torch.full((n + first, Hq, 64), 7.0, device=DEV, dtype=torch.bfloat16)
+            batch = still.PagedBatch(p.table, lens, cu)
+            K0 = p.K.clone()
+            still.still_paged_prefill(c, p.cache(), batch, q, out)
+            code, det = still.still_get_device_status(c)
+            assert still.STATUS[code] == "STILL_ERR_CUDA" and det[0] == 2
+            assert_rows(out[mine], *attention64(p, q[mine], new), WEIGHTS)
+            assert (out[:first] == 7).all() and (out[first + sum(new):] == 7).all()
+            still.still_paged_append(c, p.cache(), batch, k, v)
+            code, det = still.still_get_device_status(c)
+            assert still.STATUS[code] == "STILL_ERR_CUDA" and det[0] == 2
+            rest = torch.ones(p.K.shape[:2], dtype=torch.bool, device=DEV)
+            at = first
+            for b, m in enumerate(new):
+                slots = torch.arange(p.lens[b] - m, p.lens[b], device=DEV)
+                pages = p.table[b].long()[slots // 16]
+                assert torch.equal(p.K[pages, slots % 16], k[at:at + m])
+                rest[pages, slots % 16] = False
+                at += m
+            assert torch.equal(p.K[rest].view(torch.int16), K0[rest].view(torch.int16))
+    finally:
+        still.still_destroy(c)
