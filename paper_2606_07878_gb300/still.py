@@ -416,15 +416,18 @@ class PagedCache:
     def __init__(self, K, V, beta=None):
         import torch
         assert K.dtype == V.dtype == torch.bfloat16 and K.dim() == 4 and K.shape == V.shape
-        assert K.stride() == V.stride() and K.stride(3) == 1, "K and V must share strides"
         n, page, H, d = K.shape
+        # the stride of an axis of one entry means nothing
+        strides = [[s if size > 1 else d for s, size in zip(x.stride(), x.shape)] for x in (K, V)]
+        assert strides[0] == strides[1] and K.stride(3) == V.stride(3) == 1, \
+            "K and V must share strides"
         if beta is not None:
             assert beta.dtype == torch.float32 and tuple(beta.shape) == (n, H, page)
             assert beta.is_contiguous()
         self.tensors = (K, V, beta)
         self.struct = _PagedCache(K.data_ptr(), V.data_ptr(),
-                                  None if beta is None else beta.data_ptr(), K.stride(0),
-                                  K.stride(1), K.stride(2), n, page, H, d)
+                                  None if beta is None else beta.data_ptr(), *strides[0][:3],
+                                  n, page, H, d)
         self.ref = ctypes.byref(self.struct)
 
 

@@ -31,3 +31,23 @@ def test_pitch_of_a_table(table, pitch):
 def test_tables_that_would_be_read_beyond_their_end(table):
     with pytest.raises(AssertionError):
         batch(table)
+
+
+def strided(shape, strides):
+    x = torch.zeros(sum((n - 1) * s for n, s in zip(shape, strides)) + 1, dtype=torch.bfloat16)
+    return torch.as_strided(x, shape, strides)
+
+
+def test_strides_of_one_page_or_one_head_do_not_count():
+    """A pool of one KV-head in two orders, or of one page cut out of larger pools, is one layout."""
+    for shape, of_k, of_v, want in [
+            ((4, 16, 1, 64), (1024, 64, 64, 1), (1024, 64, 1024, 1), (1024, 64, 64)),
+            ((4, 16, 1, 64), (1024, 64, 3, 1), (1024, 64, 64, 1), (1024, 64, 64)),
+            ((1, 16, 2, 64), (2048, 128, 64, 1), (1, 128, 64, 1), (64, 128, 64)),
+            ((1, 16, 1, 64), (0, 64, 0, 1), (5, 64, 7, 1), (64, 64, 64))]:
+        s = still.PagedCache(strided(shape, of_k), strided(shape, of_v)).struct
+        assert (s.s_page, s.s_slot, s.s_head) == want
+    for of_v in [(2048, 128, 128, 1), (2048, 64, 64, 1), (4096, 128, 64, 1), (4096, 256, 128, 2)]:
+        with pytest.raises(AssertionError):
+            still.PagedCache(strided((4, 16, 2, 64), (2048, 128, 64, 1)),
+                             strided((4, 16, 2, 64), of_v))
