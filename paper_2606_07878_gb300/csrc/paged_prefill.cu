@@ -333,6 +333,10 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   // All of it: no byte is left beside five stages of 256 channels, so the base has to be aligned as
   // it is.
   extern __shared__ __align__(1024) uint8_t smem[];
+  const int cta = kPair ? blockIdx.x >> 1 : blockIdx.x;  // or pair of CTAs
+  // No split item so far. The join reads this record whatever becomes of this CTA.
+  if (threadIdx.x == 0 && (!kPair || (blockIdx.x & 1) == 0))
+    f.split[cta].last = f.split[cta].first = cta;
   if ((smem_u32(smem) & 1023) != 0) {
     dev_set_error(f.a.err, DEV_BAD_ARG, 602);
     return;
@@ -416,7 +420,6 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       tmem_relinquish();
     }
   }
-  const int cta = kPair ? blockIdx.x >> 1 : blockIdx.x;  // or pair of CTAs
   {  // equal ranges of the cost of all items: a thread adds up some sequences, or a share of one's
     const int per = (a.B + kPfThreads - 1) / kPfThreads, shares = max(1, kPfThreads / a.B);
     const int share = threadIdx.x % shares;
@@ -436,7 +439,6 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     }
     if (lane == 31) warp_cost[warp] = before;
     if (threadIdx.x == 0) start.left = 0;
-    if (threadIdx.x == 0 && rank == 0) f.split[cta].last = f.split[cta].first = cta;
     __syncthreads();
     for (int w = 0; w < kPfThreads / 32; ++w) {
       if (w < warp) before += warp_cost[w];

@@ -126,6 +126,15 @@ def test_every_warp_reads_the_item_that_it_was_shown(tiles):
     assert _fault(_programs(tiles, _awaits_readers())) is None
 
 
+def test_the_join_finds_a_record_of_every_cta():
+    """A CTA that leaves early has said before that it splits no item: the join reads the workspace,
+    which nobody cleared, by these records."""
+    src = re.sub(r"//[^\n]*", "", open(SOURCE).read())
+    kernel = src[src.index("paged_prefill_kernel("):src.index("paged_join_kernel(")]
+    record = kernel.index("f.split[cta].last = f.split[cta].first = cta;")
+    assert record < kernel.index("return;")
+
+
 def test_the_search_finds_a_record_written_too_early():
     """Without the wait for its readers an item of one tile of slots is overtaken: the search sees
     what it looks for."""
