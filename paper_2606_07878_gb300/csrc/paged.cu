@@ -11,10 +11,11 @@ namespace {
 // ----------------------------------------------------------------- append
 //
 // Row x of token i (slot j, position p = j + offset) goes to its page, keys and queries rotated in
-// pairs (m, m + d/2) by the angle p w_m (the base model's RoPE). Angles are exact in integers:
-// p * turns[m] modulo 2^64 is the fraction of a turn, whatever p, and its upper half loses 2^-32
-// turns. The sines and cosines of a token are formed once, in shared memory, and serve all its
-// heads.
+// pairs (m, m + d/2) by the angle p w_m (the base model's RoPE). Angles are integers: p * turns[m]
+// modulo 2^64 is the fraction of a turn, and whole turns cost nothing. turns[m] has the 53 bits of
+// a double, 2^-22 rad at positions of 2^31 and less in proportion below; the fraction in fp32,
+// 2^-25 turns, adds as much. The sines and cosines of a token are formed once, in shared memory,
+// and serve all its heads.
 //
 // Memory bounds it: rows are read and written once. Two tokens a CTA: 8,192 tokens of 32 + 8 + 8
 // heads of 128 channels in 37 us (201 MB: 5.5 TB/s, 0.81 of a copy), against 39 with four or one
@@ -820,10 +821,10 @@ struct RowsLaunch {
   }
 };
 
-// Calls f with the form that serves d channels and so many rows per sequence and KV-head: a block
-// of 16 that is half empty costs 15% (4 x 60,000 slots of 128 channels: 51 us against 41 to 45),
-// two blocks of 8 read everything twice. 16 rows of 256 channels do not fit a thread's registers
-// beside their K and V.
+// Calls f with the form that serves d channels and so many rows per sequence and KV-head (on
+// average: any form serves any call): a block of 16 that is half empty costs 15% (4 x 60,000 slots
+// of 128 channels: 51 us against 41 to 45), two blocks of 8 read everything twice. 16 rows of 256
+// channels do not fit a thread's registers beside their K and V.
 template <class F>
 auto rows_form(int d, int rows, F f) {
   const bool two = rows > 8;

@@ -19,7 +19,7 @@
 // registers, and their product starts under the others' exponentials. The running maximum moves
 // (and O is rescaled) only when a tile raises it by more than 2^8.
 //
-// P is bf16: its rounding, 2^-9 of a weight at most, averages out over the slots, and outputs lie
+// P is bf16: its rounding, 2^-8 of a weight at most, averages out over the slots, and outputs lie
 // 0.0023 of their root mean square from 64-bit ones where the rounding of the outputs alone leaves
 // 0.0017. A second product for the rest, as few rows have it, would double PV.
 //
@@ -41,7 +41,9 @@
 // packed operations per two logits: 1.2 PFLOP/s. 8,192 tokens of 8 KV- and 16 query heads of 256
 // channels (half the softmax for the same products): 331 us, 1.66 PFLOP/s; 381 in pages of 16, for
 // the copies; 350 and 412 with pages looked up behind the wait for a ring slot. With a tile and all
-// of K and V on each SM: 444 and 577; loaded once for a pair by multicast: 432 and 490.
+// of K and V on each SM: 444 and 577; loaded once for a pair by multicast: 432 and 490. 64 channels
+// have as many exponentials for half the products: 8,192 tokens of 8 KV- and 32 query heads 336 us
+// where 128 channels take 352, 0.82 against 1.56 PFLOP/s (with biases 416 and 465).
 #include <algorithm>
 #include <type_traits>
 
@@ -1262,6 +1264,14 @@ bool paged_prefill_serves(const PagedArgs& a, int Hq) {
   // channels: 2): 8 rows 28 / 39, 39 / 48, 42 / 49 for 64, 128, 256 channels; 16 rows 33 / 39,
   // 49 / 48, 64 / 49; 32 rows 49 / 39, 80 / 49, 96 / 49. Groups of more than 128 query heads do not
   // fit a tile.
+  //
+  // The counts of new tokens are on the device, so the rule has their mean, and a long prompt among
+  // many single tokens or idle places may go to the few rows' kernel, which reads its past once for
+  // every 8 or 16 of its rows. 256 sequences, 8 KV-heads of 128 channels with 4 query heads each:
+  // one of 769 new tokens with 8,192 slots beside 255 single tokens with 400 is at 16 rows on
+  // average and takes 1,385 us, with 770 it is above and takes 197; beside 255 idle places 1,184
+  // us, and 111 for 1,100 new tokens, which are above. A caller who knows the counts does better
+  // with two calls: the prompts in one (86 us alone), the single tokens in the other.
   return Hq / a.H <= 128 && paged_mean_rows(a, Hq) > (a.d == 256 ? 8 : 16);
 }
 

@@ -449,7 +449,8 @@ class PagedBatch:
         pitch = table.stride(0) if table.shape[0] > 1 else table.shape[1]
         assert pitch >= table.shape[1], "rows of the table share memory"
         self.tensors = (table, lens, cu_new, pos_offset)
-        self.struct = _PagedBatch(table.data_ptr(), pitch, table.shape[1], table.shape[0], lens.data_ptr(),
+        self.struct = _PagedBatch(table.data_ptr(), pitch, table.shape[1], table.shape[0],
+                                  lens.data_ptr(),
                                   None if cu_new is None else cu_new.data_ptr(),
                                   None if pos_offset is None else pos_offset.data_ptr())
         self.ref = ctypes.byref(self.struct)
