@@ -258,7 +258,8 @@ def _own(s):
     if "cache" not in s:
         s["batch"] = still.PagedBatch(s["table"], s["lens"], s["cu_new"], s["offset"])
         if op.endswith("8"):
-            s["cache"] = still.PagedCache8(s["K"], s["V"], s["k_scale"], s["v_scale"], s["beta"])
+            s["cache"] = still.PagedCacheQuant(s["K"], s["V"], s["k_scale"], s["v_scale"],
+                                               s["beta"])
         else:
             s["cache"] = still.PagedCache(s["K"], s["V"], s["beta"])
         if "weigh" in op:
@@ -267,12 +268,13 @@ def _own(s):
         if op == "evict":
             s["to"] = still.PagedCache(s["to_K"], s["to_V"], s["to_beta"])
     if op == "append8":
-        still.still_paged8_append(_context, s["cache"], s["batch"], s["k"], s["v"], q=s["q"],
-                                  q_out=s["out"], beta=s["new_beta"], rope_theta=c["theta"])
+        still.still_paged_append_quant(_context, s["cache"], s["batch"], s["k"], s["v"],
+                                       q=s["q"], q_out=s["out"], beta=s["new_beta"],
+                                       rope_theta=c["theta"])
     elif op == "decode8":
-        still.still_paged8_decode(_context, s["cache"], s["batch"], s["q"], s["out"])
+        still.still_paged_decode_quant(_context, s["cache"], s["batch"], s["q"], s["out"])
     elif op == "prefill8":
-        still.still_paged8_prefill(_context, s["cache"], s["batch"], s["q"], s["out"])
+        still.still_paged_prefill_quant(_context, s["cache"], s["batch"], s["q"], s["out"])
     elif op == "decode_weigh":
         still.still_paged_decode_weigh(_context, s["cache"], s["batch"], s["q"], s["out"],
                                        s["weight"], s["scratch"], decay=c["decay"])
