@@ -345,6 +345,107 @@ still_status still_paged_prefill(still_ctx* ctx, const still_paged_cache* cache,
                                  int64_t q_stride, int32_t Hq, float scale, void* out,
                                  void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * The paged cache in 8 bits: half the memory, and half the reads of a decode. The pools hold e4m3
+ * codes, and every block of 16 slots of a page has, for each KV-head, a scale of its keys and one
+ * of its values; a value is code times scale. Everything else is as in still_paged_cache. */
+#define STILL_PAGED_QUANT_BLOCK 16
+typedef struct {
+  void *K, *V;      /* e4m3 pools, strides in elements (bytes): multiples of 16, 16-byte aligned */
+  float *k_scale, *v_scale; /* [n_pages][H][page_size / 16], positive */
+  float* beta;      /* [n_pages][H][page_size] or NULL, as in still_paged_cache */
+  int64_t s_page, s_slot, s_head;
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+} still_paged_cache_quant;
+
+/* still_paged_append into a cache in 8 bits, arguments as there. Keys are rotated and rounded to
+ * bf16, what a 16-bit cache would hold, and quantised with their block: its scale is the smallest
+ * power of two by which the call's new rows of the block stay within 448, the largest code, or the
+ * scale it has already, if that is larger and slots of the sequence lie in the block before the new
+ * ones; their codes are brought to the new scale (exact but where they become subnormal). A value is
+ * off by at most 2^-4 of itself or 2^-18 of its block's largest, whichever is more, once, and older
+ * ones of a block by half a code step more where the scale grew. NaN stays NaN; an infinity becomes
+ * the largest code of the block.
+ * No two sequences of a call may have new tokens in one block. Scales need no initial values. */
+still_status still_paged_append_quant(still_ctx* ctx, const still_paged_cache_quant* cache,
+                                      const still_paged_batch* batch, int32_t n, const void* k,
+                                      int64_t k_stride, const void* v, int64_t v_stride,
+                                      const void* q, int64_t q_stride, int32_t Hq,
+                                      const float* beta, double rope_theta, void* q_out,
+                                      void* stream);
+/* still_paged_decode and still_paged_prefill over a cache in 8 bits, arguments, workspace and device
+ * status as there. Scales of blocks that hold a visible slot are positive and finite; what the
+ * others hold does not matter, and neither do the codes of masked slots. Queries and weights are
+ * not held in 8 bits: logits are sums in fp32 of exact products, and weights enter the product with
+ * V with an error below 2^-21 of the largest of their row times its block's scale. */
+still_status still_paged_decode_quant(still_ctx* ctx, const still_paged_cache_quant* cache,
+                                      const still_paged_batch* batch, const void* q,
+                                      int64_t q_stride, int32_t Hq, float scale, void* out,
+                                      void* stream);
+still_status still_paged_prefill_quant(still_ctx* ctx, const still_paged_cache_quant* cache,
+                                       const still_paged_batch* batch, int32_t n, const void* q,
+                                       int64_t q_stride, int32_t Hq, float scale, void* out,
+                                       void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Eviction by accumulated attention weight: a cache made smaller without a compactor, by dropping
+ * the slots that attention has had least use for (some of the baselines that the paper compares with
+ * keep a cache this way). A weight is a float per slot and KV-head, [n_pages][H][page_size] like
+ * beta.
+ *
+ * still_paged_weigh and still_paged_decode_weigh update the weights of all slots of the batch's
+ * sequences (slots beyond a sequence's len stay as they are):
+ *   weight = decay weight + sum over the call's tokens and the KV-head's query heads of the softmax
+ *            weight that they give to the slot
+ * where slots of the call's own tokens begin at 0, so that weights need no initial values as long as
+ * every token of a sequence has been weighed when it was new. decay in [0, 1]; with 0 nothing of the
+ * old weight remains, whatever it was: the call's tokens alone count (an observation window at the
+ * end of a prompt). A sequence without new tokens in the call, or a token that sees nothing, changes
+ * nothing but by the decay of sequences that have new tokens.
+ * The sums are fp32 of logits that are fp32 sums of exact products; they do not depend on the order
+ * in which blocks run.
+ *   scratch  still_paged_weigh_scratch bytes of device memory (16-byte aligned) for as long as the
+ *            call runs, too few: STILL_ERR_SHAPE. Calls that may run at once need their own.
+ * still_paged_decode_weigh: still_paged_decode, and the weights beside it, at the cost of the
+ * logits' way through memory. still_paged_weigh: the weights alone, any number of tokens, causal
+ * among them. weight must not overlap beta. Everything else is as in still_paged_decode and
+ * still_paged_prefill, the workspace and the device status included. */
+int64_t still_paged_weigh_scratch(const still_paged_cache* cache, int32_t n, int32_t Hq);
+still_status still_paged_decode_weigh(still_ctx* ctx, const still_paged_cache* cache,
+                                      const still_paged_batch* batch, const void* q,
+                                      int64_t q_stride, int32_t Hq, float scale, void* out,
+                                      float* weight, float decay, void* scratch,
+                                      int64_t scratch_bytes, void* stream);
+still_status still_paged_weigh(still_ctx* ctx, const still_paged_cache* cache,
+                               const still_paged_batch* batch, int32_t n, const void* q,
+                               int64_t q_stride, int32_t Hq, float scale, float* weight,
+                               float decay, void* scratch, int64_t scratch_bytes, void* stream);
+/* Of every sequence and KV-head keeps the first `sinks` slots, the last `recent` ones and the
+ * heaviest of the others, `keep` in all (ties: the lowest slots; NaN: lightest of all), and copies
+ * them, in their order, to slots 0, 1, ... of pages of `to` that to_table lists. Heads choose for
+ * themselves. A sequence of at most `keep` slots is copied whole.
+ *   to        a cache of the same H and d, any page size and strides, in the same pools or others;
+ *             the pages that are written must not be read by this call. Its biases are those of the
+ *             slots, 0 where `cache` has none; without biases it is refused
+ *             (STILL_ERR_INVALID_ARG) if `cache` has some.
+ *   to_table  [B][to_s_table], the first to_table_pages of a row; keep <= to_table_pages page_size
+ *             (STILL_ERR_SHAPE)
+ *   to_weight [to->n_pages][H][to->page_size] the slots' weights, or NULL
+ *   kept      [B][H][keep] the slots they were in, ascending, -1 behind the last one
+ *   to_len    [B] slots of the new sequences
+ *   to_offset [B] position less slot of the tokens that follow (pos_offset + len - to_len), or NULL
+ * keep >= 1, sinks, recent >= 0, sinks + recent <= keep. cu_new is not read. Outputs must not overlap
+ * what is read, to_len and to_offset included. Keys stay rotated to their positions. */
+still_status still_paged_evict(still_ctx* ctx, const still_paged_cache* cache,
+                               const still_paged_batch* batch, const float* weight, int32_t keep,
+                               int32_t sinks, int32_t recent, const still_paged_cache* to,
+                               const int32_t* to_table, int64_t to_s_table, int32_t to_table_pages,
+                               float* to_weight, int32_t* kept, int32_t* to_len,
+                               int64_t* to_offset, void* stream);
+
 /* Compacts layers 0..n_layers-1 (all loaded) over the same positions: the per-layer
  * compactors share nothing at forward time (App. M, "No inter-layer compactor channel"), so
  * this is one stream-ordered launch sequence over the layer stack. K[l], V[l], Ck[l], Cv[l] are device
@@ -553,6 +654,8 @@ typedef enum {
   STILL_K_REPAIR,       /* top-k repair of one-pass cross-attention scores  */
   STILL_K_PAGED_APPEND, /* new tokens into a paged cache                    */
   STILL_K_PAGED_ATTEND, /* attention over a paged cache                     */
+  STILL_K_PAGED_WEIGH,  /* attention weights added up over a paged cache    */
+  STILL_K_PAGED_EVICT,  /* a paged cache without its lightest slots         */
   STILL_K_COUNT
 } still_kernel_class;
 

@@ -3,6 +3,8 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <cstdint>
+
 #include "kernel_table.cuh"
 
 namespace still {
@@ -15,6 +17,10 @@ constexpr int kMinPage = 16;  // slots: the keys of one MMA never leave a page
 // bias is beta[(page_index * H + h) * page + j mod page].
 struct PagedArgs {
   __nv_bfloat16 *K = nullptr, *V = nullptr;
+  // a pool in 8 bits instead: e4m3 codes, and the scale of slots [16 i, 16 i + 16) of a page at
+  // scale[(page_index * H + h) * (page / 16) + i]
+  uint8_t *K8 = nullptr, *V8 = nullptr;
+  float *k_scale = nullptr, *v_scale = nullptr;
   float* beta = nullptr;          // or null: no bias
   int64_t s_page = 0, s_slot = 0, s_head = 0;
   int32_t n_pages = 0, page_shift = 0, H = 0, d = 0;
@@ -51,6 +57,10 @@ struct PagedQuery {
   __nv_bfloat16* out = nullptr;      // [n][Hq][d]
   int32_t Hq = 0;
   float scale = 0.f;
+  // of a decode whose weights are added up: logits [n_pages][H][Hq / H][page], -inf where a row does
+  // not see the slot, and (m, 1 / l) of every row (0: it sees nothing), [n][Hq]
+  float* logits = nullptr;
+  float2* ml = nullptr;
 };
 // Few rows (paged.cu), and the join of what several warps share: two launches. ws:
 // paged_rows_workspace bytes, enough for every call.
@@ -69,5 +79,35 @@ cudaError_t launch_paged_prefill(const PagedArgs& a, const PagedQuery& q, void* 
 // What its plan adds up for items [q0, q1), of `tokens` new tokens each, of a sequence with `count`
 // of them and `len` slots: tiles of 128 slots, and an item's beginning and end as two more.
 int64_t paged_prefill_cost(int count, int len, int tokens, int q0, int q1);
+
+// The same over a pool in 8 bits (paged_quant.cu).
+constexpr int kScaleBlock = 16;  // slots that share a scale
+cudaError_t launch_paged_append_quant(const PagedArgs& a, const PagedAppend& p,
+                                      const RopeTurns& turns, cudaStream_t s);
+size_t paged_rows_quant_workspace(int num_sms);
+cudaError_t launch_paged_rows_quant(const PagedArgs& a, const PagedQuery& q, void* ws, int num_sms,
+                                    cudaStream_t s);
+
+// Attention weights added up slot by slot (paged_weigh.cu), weight as PagedArgs::beta: decay times
+// what was there (0 for this call's own slots) plus what this call's rows give. Decode: three
+// launches, with the attention; else two or three, from keys alone.
+size_t paged_rows_weigh_workspace(int num_sms);
+cudaError_t launch_paged_decode_weigh(const PagedArgs& a, const PagedQuery& q, float* weight,
+                                      float decay, void* ws, int num_sms, cudaStream_t s);
+cudaError_t launch_paged_weigh(const PagedArgs& a, const PagedQuery& q, float* weight, float decay,
+                               void* ws, int num_sms, cudaStream_t s);
+
+// Of every sequence and KV-head the `keep` slots that count, into pages of `to` (paged_evict.cu).
+struct PagedEvict {
+  const float* weight = nullptr;
+  int32_t keep = 0, sinks = 0, recent = 0;
+  PagedArgs to;                     // pools, table and error record alone
+  float* to_weight = nullptr;       // or null
+  int32_t* kept = nullptr;          // [B][H][keep]
+  int32_t* to_len = nullptr;        // [B]
+  int64_t* to_offset = nullptr;     // [B] or null
+};
+cudaError_t launch_paged_evict(const PagedArgs& a, const PagedEvict& e, const KernelTable& dev,
+                               cudaStream_t s);
 
 }  // namespace still

@@ -47,4 +47,68 @@ STILL_DEV int paged_page(const PagedArgs& a, const int32_t* table, int j) {
   return -1;
 }
 
+// The sequence that owns token i (the last one that begins at or before it), by a whole warp that
+// looks at 32 of them at a time.
+STILL_DEV int paged_owner(const PagedArgs& a, int i) {
+  if (a.cu_new == nullptr) return i;
+  const int lane = threadIdx.x & 31;
+  int b = 0;
+  for (int n = a.B; n > 1;) {  // among n from b on
+    const int apart = (n + 31) / 32;
+    const bool before = lane * apart < n && a.cu_new[b + lane * apart] <= i;
+    const int k = max(0, 31 - __clz(__ballot_sync(0xffffffffu, before)));
+    b += k * apart;
+    n = min(apart, n - k * apart);
+  }
+  return b;
+}
+
+// Units of work that sequences have, `units(s)` each, one sequence after another: the share of part
+// `part` of `parts`, and where it begins.
+struct UnitRange {
+  int64_t left;  // units of the share
+  int64_t in;    // the first of them, among those of sequence b
+  int b;
+};
+// By all kThreads threads of a block.
+template <int kThreads, class F>
+STILL_DEV UnitRange unit_range(const PagedArgs& a, int part, int parts, F units) {
+  __shared__ int64_t warp_sum[kThreads / 32];
+  __shared__ UnitRange range;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int per = (a.B + kThreads - 1) / kThreads;  // consecutive sequences of a thread
+  const int b0 = min(a.B, (int)threadIdx.x * per), b1 = min(a.B, b0 + per);
+  int64_t mine = 0;
+  for (int b = b0; b < b1; ++b) mine += units(paged_seq(a, b));
+  int64_t before = mine, total = 0;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t x = __shfl_up_sync(0xffffffffu, before, o);
+    if (lane >= o) before += x;
+  }
+  if (lane == 31) warp_sum[warp] = before;
+  if (threadIdx.x == 0) range.left = 0;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) {
+    if (w < warp) before += warp_sum[w];
+    total += warp_sum[w];
+  }
+  before -= mine;
+  const int64_t each = total / parts, wider = total - each * parts;
+  const int64_t u0 = each * part + min((int64_t)part, wider);
+  const int64_t u1 = u0 + each + (part < wider);
+  if (u1 > u0 && u0 >= before && u0 < before + mine) {
+    int b = b0;
+    for (;; ++b) {
+      const int64_t n = units(paged_seq<false>(a, b));
+      if (u0 < before + n) break;
+      before += n;
+    }
+    range = UnitRange{u1 - u0, u0 - before, b};
+  }
+  __syncthreads();
+  return range;
+}
+
 }  // namespace still

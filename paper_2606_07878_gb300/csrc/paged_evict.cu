@@ -1,0 +1,267 @@
+// Eviction from a paged cache: of every sequence and KV-head the first `sinks` slots, the last
+// `recent` and the heaviest of the others, `keep` in all, move to pages of their own, in their order.
+//
+// Two launches. The first one chooses: weights become 32-bit keys in their order (slots that stay in
+// any case above all others, NaN below), and three steps of 11, 11 and 10 bits find the smallest key
+// that is kept and how many of its equals are (those of the lowest slots). A cluster of CTAs takes a
+// sequence's KV-head, each a part of its slots whose keys stay in shared memory where they fit; a
+// step's histograms are added up through distributed shared memory, by every CTA for itself. The
+// second one moves: 16 bytes a thread, rows of K and V.
+//
+// A head may keep other tokens than its neighbour: a slot's rows of two heads are of two tokens then.
+// Attention does not mind, keys are rotated to their positions already.
+#include <algorithm>
+
+#include "launch.cuh"
+#include "paged_dev.cuh"
+
+namespace still {
+
+namespace {
+
+constexpr int kChooseThreads = 1024;
+constexpr int kChooseWarps = kChooseThreads / 32;
+constexpr int kDigits = 2048;
+constexpr int kChooseCluster = 8;
+constexpr int kChooseKeys = 48 * 1024;  // of a CTA in shared memory
+constexpr int kChooseBytes = kChooseKeys * 4;
+
+STILL_DEV uint32_t key_of(float w) {
+  if (w != w) return 0;                                        // NaN
+  const uint32_t x = __float_as_uint(w + 0.f);                 // -0 is 0
+  return x & 0x80000000u ? ~x : x | 0x80000000u;
+}
+
+STILL_DEV uint32_t ld_cluster_u32(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+template <int kCluster>
+__global__ void __launch_bounds__(kChooseThreads, 1)
+    paged_choose_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedEvict f,
+                        int in_smem) {
+  extern __shared__ uint32_t keys[];
+  __shared__ uint32_t hist[2][kDigits];
+  __shared__ uint32_t warp_sum[kChooseWarps], warp_equal[kChooseWarps];
+  __shared__ uint32_t found[2];   // digit, kept among those above it
+  __shared__ uint32_t counts[2];  // of this CTA: above the smallest key, equal to it
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = kCluster > 1 ? cluster_ctarank() : 0;
+  const int set = blockIdx.x / kCluster, b = set / a.H, h = set % a.H;
+  const Seq s = paged_seq(a, b);
+  const int count = min(s.len, f.keep);
+  int32_t* kept = f.kept + ((int64_t)b * a.H + h) * f.keep;
+  for (int r = count + (int)rank * kChooseThreads + threadIdx.x; r < f.keep;
+       r += kCluster * kChooseThreads)
+    kept[r] = -1;
+  if (h == 0 && rank == 0 && threadIdx.x == 0) {
+    f.to_len[b] = count;
+    if (f.to_offset != nullptr)
+      f.to_offset[b] = (a.pos_offset != nullptr ? a.pos_offset[b] : 0) + s.len - count;
+  }
+  if (s.len <= f.keep) {  // (of the whole cluster)
+    for (int r = (int)rank * kChooseThreads + threadIdx.x; r < count;
+         r += kCluster * kChooseThreads)
+      kept[r] = r;
+    return;
+  }
+  const int32_t* table = a.table + (int64_t)b * a.s_table;
+  // slots [j0, j1) of this CTA
+  const int per = ((s.len + kCluster - 1) / kCluster + 31) & ~31;
+  const int j0 = min(s.len, (int)rank * per), j1 = min(s.len, j0 + per);
+  auto read = [&](int j) -> uint32_t {
+    if (j < f.sinks || j >= s.len - f.recent) return 0xffffffffu;
+    const int pg = paged_page(a, table, j);
+    if (pg < 0) return 0;
+    return key_of(f.weight[(((int64_t)pg * a.H + h) << a.page_shift) +
+                           (j & ((1 << a.page_shift) - 1))]);
+  };
+  const bool held = j1 - j0 <= in_smem;
+  auto key = [&](int j) { return held ? keys[j - j0] : read(j); };
+  for (int i = threadIdx.x; i < kDigits; i += kChooseThreads) hist[0][i] = 0;
+  __syncthreads();
+  uint32_t prefix = 0;       // the digits found so far, in place
+  uint32_t need = f.keep;    // to be kept among the keys that have them
+#pragma unroll 1
+  for (int step = 0; step < 3; ++step) {
+    const int shift = step == 0 ? 21 : step == 1 ? 10 : 0;
+    const uint32_t digits = step == 2 ? 1024 : 2048;
+    const uint32_t above = step == 0 ? 0u : ~0u << (step == 1 ? 21 : 10);
+    uint32_t* const mine = hist[step & 1];
+    for (int j = j0 + threadIdx.x; j < j1; j += kChooseThreads) {
+      uint32_t k;
+      if (step == 0) {
+        k = read(j);
+        if (held) keys[j - j0] = k;
+      } else {
+        k = key(j);
+      }
+      if ((k & above) == prefix) atomicAdd(&mine[(k >> shift) & (digits - 1)], 1u);
+    }
+    if constexpr (kCluster > 1)
+      cluster_sync();
+    else
+      __syncthreads();
+    // all CTAs' counts of two digits, this thread's; digits above them come first
+    uint32_t c[2] = {0, 0};
+    const int top = (int)digits - 1 - 2 * (int)threadIdx.x;  // c[0]: top, c[1]: top - 1
+    if (top > 0) {
+#pragma unroll
+      for (int r = 0; r < kCluster; ++r) {
+        const uint32_t at = kCluster > 1 ? cluster_map(smem_u32(mine), r) : 0;
+        c[0] += kCluster > 1 ? ld_cluster_u32(at + 4 * top) : mine[top];
+        c[1] += kCluster > 1 ? ld_cluster_u32(at + 4 * (top - 1)) : mine[top - 1];
+      }
+    }
+    uint32_t upto = c[0] + c[1];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    if (lane == 31) warp_sum[warp] = upto;
+    for (int i = threadIdx.x; i < kDigits; i += kChooseThreads) hist[(step + 1) & 1][i] = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int w = 0; w < warp; ++w) upto += warp_sum[w];
+    const uint32_t before = upto - c[0] - c[1];
+    if (before < need && upto >= need) {
+      const bool first = before + c[0] >= need;
+      found[0] = first ? top : top - 1;
+      found[1] = first ? before : before + c[0];
+    }
+    __syncthreads();
+    prefix |= found[0] << shift;
+    need -= found[1];
+    // (the other histogram is written next; nobody reads this one again before the next sync of all)
+  }
+  // ---- the kept slots, in order: keys above `prefix`, and the first `need` that equal it
+  const int each = ((j1 - j0 + kChooseWarps - 1) / kChooseWarps + 31) & ~31;
+  const int w0 = min(j1, j0 + warp * each), w1 = min(j1, w0 + each);
+  uint32_t more = 0, equal = 0;
+  for (int j = w0 + lane; j - lane < w1; j += 32) {
+    const uint32_t k = j < w1 ? key(j) : 0;
+    more += __popc(__ballot_sync(0xffffffffu, j < w1 && k > prefix));
+    equal += __popc(__ballot_sync(0xffffffffu, j < w1 && k == prefix));
+  }
+  if (lane == 0) {
+    warp_sum[warp] = more;
+    warp_equal[warp] = equal;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    uint32_t x = 0, y = 0;
+    for (int w = 0; w < kChooseWarps; ++w) {
+      x += warp_sum[w];
+      y += warp_equal[w];
+    }
+    counts[0] = x;
+    counts[1] = y;
+  }
+  if constexpr (kCluster > 1)
+    cluster_sync();
+  else
+    __syncthreads();
+  more = equal = 0;  // before this warp's slots
+  if constexpr (kCluster > 1)
+    for (uint32_t r = 0; r < rank; ++r) {
+      const uint32_t at = cluster_map(smem_u32(counts), r);
+      more += ld_cluster_u32(at);
+      equal += ld_cluster_u32(at + 4);
+    }
+  for (int w = 0; w < warp; ++w) {
+    more += warp_sum[w];
+    equal += warp_equal[w];
+  }
+  const uint32_t below = (1u << lane) - 1;
+  for (int j = w0 + lane; j - lane < w1; j += 32) {
+    const uint32_t k = j < w1 ? key(j) : 0;
+    const uint32_t is_more = __ballot_sync(0xffffffffu, j < w1 && k > prefix);
+    const uint32_t is_equal = __ballot_sync(0xffffffffu, j < w1 && k == prefix);
+    const uint32_t e = equal + __popc(is_equal & below);
+    const uint32_t r = more + __popc(is_more & below) + min(e, need);
+    if ((is_more >> lane & 1) || ((is_equal >> lane & 1) && e < need)) kept[r] = j;
+    more += __popc(is_more);
+    equal += __popc(is_equal);
+  }
+  if constexpr (kCluster > 1) cluster_sync();  // others may read this CTA's counts
+}
+
+// ----------------------------------------------------------------- moving
+constexpr int kMoveThreads = 256;
+
+template <int D>
+__global__ void __launch_bounds__(kMoveThreads)
+    paged_move_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedEvict f) {
+  griddep_wait();
+  constexpr int kPieces = D / 8;                       // of 16 bytes
+  constexpr int kRows = kMoveThreads / kPieces;        // of K and V at a time
+  const int c = threadIdx.x % kPieces * 8;
+  const PagedArgs& t = f.to;
+  const int mask = (1 << a.page_shift) - 1, to_mask = (1 << t.page_shift) - 1;
+  const int64_t rows = (int64_t)a.B * f.keep * a.H;
+  for (int64_t x = (int64_t)blockIdx.x * kRows + threadIdx.x / kPieces; x < rows;
+       x += (int64_t)gridDim.x * kRows) {
+    const int r = (int)(x / a.H % f.keep), h = (int)(x % a.H), b = (int)(x / a.H / f.keep);
+    const int j = f.kept[((int64_t)b * a.H + h) * f.keep + r];
+    if (j < 0) continue;
+    const int pg = paged_page(a, a.table + (int64_t)b * a.s_table, j);
+    const int to = paged_page(t, t.table + (int64_t)b * t.s_table, r);
+    if (pg < 0 || to < 0) continue;
+    const int64_t src = (int64_t)pg * a.s_page + (int64_t)(j & mask) * a.s_slot +
+                        (int64_t)h * a.s_head + c;
+    const int64_t dst = (int64_t)to * t.s_page + (int64_t)(r & to_mask) * t.s_slot +
+                        (int64_t)h * t.s_head + c;
+    const uint4 k = __ldcs(reinterpret_cast<const uint4*>(a.K + src));
+    const uint4 v = __ldcs(reinterpret_cast<const uint4*>(a.V + src));
+    *reinterpret_cast<uint4*>(t.K + dst) = k;
+    *reinterpret_cast<uint4*>(t.V + dst) = v;
+    if (c != 0) continue;
+    const int64_t from = (((int64_t)pg * a.H + h) << a.page_shift) + (j & mask);
+    const int64_t at = (((int64_t)to * a.H + h) << t.page_shift) + (r & to_mask);
+    if (f.to_weight != nullptr) f.to_weight[at] = f.weight[from];
+    if (t.beta != nullptr) t.beta[at] = a.beta != nullptr ? a.beta[from] : 0.f;
+  }
+}
+
+template <int kCluster>
+cudaError_t launch_choose(const PagedArgs& a, const PagedEvict& f, const KernelTable& dev,
+                          cudaStream_t s) {
+  using Id = KernelId<paged_choose_kernel<kCluster>, kChooseThreads, kChooseBytes, kCluster>;
+  if (dev.of<Id>().status != cudaSuccess) return dev.of<Id>().status;
+  const int64_t slots = ((int64_t)a.table_pages << a.page_shift) / kCluster + 64;
+  const int keys = (int)std::min<int64_t>(kChooseKeys, slots);
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = kCluster;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(a.B * a.H * kCluster));
+  cfg.blockDim = dim3(kChooseThreads);
+  cfg.dynamicSmemBytes = (size_t)keys * 4;
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = kCluster > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, paged_choose_kernel<kCluster>, a, f, keys);
+}
+
+}  // namespace
+
+cudaError_t launch_paged_evict(const PagedArgs& a, const PagedEvict& f, const KernelTable& dev,
+                               cudaStream_t s) {
+  const int64_t slots = (int64_t)a.table_pages << a.page_shift;
+  const cudaError_t e = slots > 4096 ? launch_choose<kChooseCluster>(a, f, dev, s)
+                                     : launch_choose<1>(a, f, dev, s);
+  if (e != cudaSuccess) return e;
+  auto kernel = a.d == 64    ? paged_move_kernel<64>
+                : a.d == 128 ? paged_move_kernel<128>
+                             : paged_move_kernel<256>;
+  const int64_t rows = (int64_t)a.B * f.keep * a.H;
+  const int64_t blocks = (rows * (a.d / 8) + kMoveThreads - 1) / kMoveThreads;
+  return launch_chained(kernel, dim3((unsigned)std::min<int64_t>(blocks, 8 * dev.num_sms)),
+                        dim3(kMoveThreads), 0, s, 1, a, f);
+}
+
+}  // namespace still

@@ -1,0 +1,232 @@
+// The paged cache in 8 bits: append with quantisation, and attention of few rows.
+//
+// A pool holds e4m3 codes; slots [16 i, 16 i + 16) of a page and KV-head share a scale of K and one
+// of V, and a value is code times scale.
+#include "paged_rows.cuh"
+
+namespace still {
+
+namespace {
+
+// ----------------------------------------------------------------- append
+//
+// Rows are rotated as paged.cu does and keys rounded to bf16, what a 16-bit cache would hold. A
+// block of 16 slots then takes the smallest power of two s with max |x| <= 448 s over its new rows,
+// or the scale that it has already where that is larger and the block is partly filled; its codes
+// are x / s, rounded to nearest even. Powers of two cost no precision (e4m3 has the same 4 bits at
+// any size; the block's largest value is at least 224 s, so only what lies 2^14 below it meets the
+// subnormal codes) and let a block change its scale without rounding its older codes again, but for
+// those that become subnormal.
+//
+// A warp takes the K or the V rows of a block and KV-head, at most 16 of them: it holds them in
+// registers between their maximum and their codes. The first token of a block (or of a sequence's
+// new tokens) leads it; a CTA looks at a window of tokens for leaders, and rotates the window's
+// queries.
+constexpr int kQuantThreads = 256;
+constexpr int kWindow = 16;  // tokens; 1 where sequences have few of them
+
+// The smallest power of two, 2^-126 at least, by which `top` is at most 448.
+STILL_DEV float least_scale(float top) {
+  const uint32_t bits = __float_as_uint(top);  // top = 1.m 2^(e - 127); 448 = 1.75 2^8
+  const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u);
+  return __uint_as_float((uint32_t)(127 + max(e, -126)) << 23);
+}
+
+// Four codes of x / s; by = 1 / s. Values beyond 448 s, infinities too, become +-448, NaN stays NaN.
+STILL_DEV uint32_t codes4(float x0, float x1, float x2, float x3, float by) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n\t"
+      "mov.b32 %0, {l, h};\n}\n"
+      : "=r"(r)
+      : "f"(x0 * by), "f"(x1 * by), "f"(x2 * by), "f"(x3 * by));
+  return r;
+}
+// Codes times `by`, rounded to codes again.
+STILL_DEV uint32_t recoded(uint32_t x, float by) {
+  const uint32_t lo = f16_of_lower(x), hi = f16_of_upper(x);
+  const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo));
+  const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+  return codes4(a.x, a.y, b.x, b.y, by);
+}
+
+struct Lead {
+  int token, slot, count, page, head_room;  // head_room: slots of the block before `slot`
+};
+
+template <int D>
+__global__ void __launch_bounds__(kQuantThreads)
+    paged_append_quant_kernel(const __grid_constant__ PagedArgs a,
+                              const __grid_constant__ PagedAppend p,
+                              const __grid_constant__ RopeTurns w, int window, int table) {
+  extern __shared__ float2 cs[];  // [table][D / 2] (cos, sin) of tokens from the window's first on
+  __shared__ Lead lead[kWindow];
+  __shared__ long long pos[kWindow];
+  constexpr int kHalf = D / 2;
+  const int i0 = blockIdx.x * window, nt = min(window, a.n - i0);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int t = warp; t < nt; t += kQuantThreads / 32) {
+    const int i = i0 + t, b = paged_owner(a, i);
+    if (lane == 0) {
+      const long long offset = a.pos_offset != nullptr ? a.pos_offset[b] : 0;
+      const Seq s = paged_seq(a, b);
+      const int at = i - s.first, j = s.len - s.count + at;
+      Lead x{i, j, 0, -1, j & (kScaleBlock - 1)};
+      if (at >= 0 && at < s.count && j >= 0 &&
+          (x.head_room == 0 || j == max(0, s.len - s.count))) {
+        x.count = min(kScaleBlock - x.head_room, s.len - j);
+        x.page = paged_page(a, a.table + (int64_t)b * a.s_table, j);
+      }
+      lead[t] = x;
+      pos[t] = j + offset;
+    }
+  }
+  __syncthreads();
+  if (p.rotate) {
+    for (int x = threadIdx.x; x < table * kHalf; x += kQuantThreads) {
+      // (tokens behind the window matter where they are of the last one's block)
+      const int t = x / kHalf, known = min(t, nt - 1);
+      const unsigned long long turn =
+          (unsigned long long)(pos[known] + t - known) * w.turns[x % kHalf];
+      float sn, cn;
+      sincospif((float)(int)(turn >> 32) * 0x1p-31f, &sn, &cn);
+      cs[x] = make_float2(cn, sn);
+    }
+    __syncthreads();
+  }
+  constexpr int kLanes = D / 16;  // threads of a row: 8 channels of each half
+  auto rotate = [&](uint4& lo, uint4& hi, const float2* ang) {
+    __nv_bfloat162* l = reinterpret_cast<__nv_bfloat162*>(&lo);
+    __nv_bfloat162* u = reinterpret_cast<__nv_bfloat162*>(&hi);
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const float2 x0 = __bfloat1622float2(l[m]), x1 = __bfloat1622float2(u[m]);
+      const float2 e = ang[2 * m], o = ang[2 * m + 1];
+      l[m] = __floats2bfloat162_rn(x0.x * e.x - x1.x * e.y, x0.y * o.x - x1.y * o.y);
+      u[m] = __floats2bfloat162_rn(x1.x * e.x + x0.x * e.y, x1.y * o.x + x0.y * o.y);
+    }
+  };
+  // ---- queries
+  for (int x = threadIdx.x; x < nt * p.Hq * kLanes; x += kQuantThreads) {
+    const int c = x % kLanes * 8, h = x / kLanes % p.Hq, t = x / kLanes / p.Hq;
+    const int64_t i = i0 + t;
+    const __nv_bfloat16* src = p.q + i * p.s_q + (int64_t)h * D + c;
+    uint4 lo = *reinterpret_cast<const uint4*>(src);
+    uint4 hi = *reinterpret_cast<const uint4*>(src + kHalf);
+    rotate(lo, hi, cs + t * kHalf + c);
+    __nv_bfloat16* dst = p.q_out + (i * p.Hq + h) * D + c;
+    *reinterpret_cast<uint4*>(dst) = lo;
+    *reinterpret_cast<uint4*>(dst + kHalf) = hi;
+  }
+  // ---- blocks of keys and values
+  constexpr int kAtOnce = 32 / kLanes;                 // rows
+  constexpr int kSteps = kScaleBlock / kAtOnce;
+  const int c = lane % kLanes * 8, r0 = lane / kLanes;
+  for (int u = warp; u < nt * 2 * a.H; u += kQuantThreads / 32) {
+    const Lead x = lead[u / (2 * a.H)];
+    if (x.count == 0 || x.page < 0) continue;
+    const int h = u % (2 * a.H) >> 1;
+    const bool key = (u & 1) == 0;
+    const __nv_bfloat16* src =
+        (key ? p.k + x.token * p.s_k : p.v + x.token * p.s_v) + (int64_t)h * D + c;
+    const int64_t pitch = key ? p.s_k : p.s_v;
+    uint4 lo[kSteps], hi[kSteps];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const int r = r0 + i * kAtOnce;
+      lo[i] = hi[i] = make_uint4(0, 0, 0, 0);
+      if (r < x.count) {
+        lo[i] = *reinterpret_cast<const uint4*>(src + r * pitch);
+        hi[i] = *reinterpret_cast<const uint4*>(src + r * pitch + kHalf);
+      }
+    }
+    const int in = x.slot & ((1 << a.page_shift) - 1);  // in its page
+    const int64_t head = (int64_t)x.page * a.H + h;
+    float* const scale =
+        (key ? a.k_scale : a.v_scale) + (head << (a.page_shift - 4)) + (in >> 4);
+    float old = x.head_room > 0 ? *scale : 0.f;
+    if (!(old > 0.f && old <= 3.4e38f)) old = 0.f;
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const int r = r0 + i * kAtOnce;
+      if (key && p.rotate && r < x.count)
+        rotate(lo[i], hi[i], cs + (x.token - i0 + r) * kHalf + c);
+#pragma unroll
+      for (int m = 0; m < 8; ++m) {
+        const uint32_t y = m < 4 ? word(lo[i], m) : word(hi[i], m - 4);
+        const float x0 = fabsf(__uint_as_float(y << 16));
+        const float x1 = fabsf(__uint_as_float(y & 0xffff0000u));
+        top = max3(top, x0 <= 3.4e38f ? x0 : 0.f, x1 <= 3.4e38f ? x1 : 0.f);
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float s = fmaxf(old, least_scale(top)), by = 1.f / s;
+    uint8_t* const dst = (key ? a.K8 : a.V8) + (int64_t)x.page * a.s_page +
+                         (int64_t)(in - x.head_room) * a.s_slot + (int64_t)h * a.s_head + c;
+    if (old > 0.f && s > old) {  // the block's older codes
+#pragma unroll 1
+      for (int r = r0; r < x.head_room; r += kAtOnce) {
+        uint2* l = reinterpret_cast<uint2*>(dst + r * a.s_slot);
+        uint2* u2 = reinterpret_cast<uint2*>(dst + r * a.s_slot + kHalf);
+        const uint2 y = *l, z = *u2;
+        *l = make_uint2(recoded(y.x, old * by), recoded(y.y, old * by));
+        *u2 = make_uint2(recoded(z.x, old * by), recoded(z.y, old * by));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const int r = r0 + i * kAtOnce;
+      if (r >= x.count) continue;
+      uint32_t y[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const uint32_t y0 = m < 2 ? word(lo[i], 2 * m) : word(hi[i], 2 * m - 4);
+        const uint32_t y1 = m < 2 ? word(lo[i], 2 * m + 1) : word(hi[i], 2 * m - 3);
+        y[m] = codes4(__uint_as_float(y0 << 16), __uint_as_float(y0 & 0xffff0000u),
+                      __uint_as_float(y1 << 16), __uint_as_float(y1 & 0xffff0000u), by);
+      }
+      uint8_t* to = dst + (int64_t)(x.head_room + r) * a.s_slot;
+      *reinterpret_cast<uint2*>(to) = make_uint2(y[0], y[1]);
+      *reinterpret_cast<uint2*>(to + kHalf) = make_uint2(y[2], y[3]);
+    }
+    if (lane == 0) *scale = s;
+    if (key && a.beta != nullptr && lane < x.count)
+      a.beta[(head << a.page_shift) + in + lane] =
+          p.beta != nullptr ? p.beta[(int64_t)(x.token + lane) * a.H + h] : 0.f;
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_paged_append_quant(const PagedArgs& a, const PagedAppend& p,
+                                      const RopeTurns& turns, cudaStream_t s) {
+  const int window = a.n / a.B >= kWindow / 2 ? kWindow : 1;
+  // a block reaches 15 tokens behind the window's last
+  const int table = a.cu_new == nullptr ? 1 : window + kScaleBlock - 1;
+  const size_t smem = p.rotate ? (size_t)table * (a.d / 2) * sizeof(float2) : 0;
+  auto kernel = a.d == 64    ? paged_append_quant_kernel<64>
+                : a.d == 128 ? paged_append_quant_kernel<128>
+                             : paged_append_quant_kernel<256>;
+  kernel<<<(a.n + window - 1) / window, kQuantThreads, smem, s>>>(a, p, turns, window, table);
+  return cudaGetLastError();
+}
+
+size_t paged_rows_quant_workspace(int num_sms) {
+  size_t most = 0;
+  for (int d : {64, 128, 256})
+    for (int rows : {8, 16})
+      most = std::max(most, rows_form<kRowsE4m3>(
+                                d, rows, [&](auto form) { return form.bytes(num_sms); }));
+  return most;
+}
+
+cudaError_t launch_paged_rows_quant(const PagedArgs& a, const PagedQuery& p, void* ws, int num_sms,
+                                    cudaStream_t s) {
+  return rows_form<kRowsE4m3>(a.d, paged_mean_rows(a, p.Hq),
+                              [&](auto form) { return form.run(a, p, ws, num_sms, s); });
+}
+
+}  // namespace still

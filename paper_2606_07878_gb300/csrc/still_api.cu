@@ -526,8 +526,10 @@ still_status ensure_ws(still_ctx* ctx, size_t bytes) {
 still_status ensure_paged_ws(still_ctx* ctx) {
   if (ctx->paged_ws != nullptr) return STILL_OK;
   const int nsm = ctx->kernels.num_sms;
-  if (cudaMalloc(&ctx->paged_ws, std::max(paged_rows_workspace(nsm),
-                                          paged_prefill_workspace(nsm))) != cudaSuccess) {
+  if (cudaMalloc(&ctx->paged_ws,
+                 std::max({paged_rows_workspace(nsm), paged_prefill_workspace(nsm),
+                           paged_rows_quant_workspace(nsm), paged_rows_weigh_workspace(nsm)})) !=
+      cudaSuccess) {
     cudaGetLastError();
     ctx->paged_ws = nullptr;
     return STILL_ERR_OOM;
@@ -1788,24 +1790,52 @@ bool bad_rows(const void* p, int64_t pitch) {  // 16-byte aligned rows
   return (reinterpret_cast<uintptr_t>(p) & 15) != 0 || (pitch & 7) != 0;
 }
 
-still_status paged_attend(still_ctx* ctx, const still_paged_cache* cache,
-                          const still_paged_batch* batch, int64_t n, const void* q,
-                          int64_t q_stride, int32_t Hq, float scale, void* out, void* stream) {
-  PagedArgs a;
-  TRY(paged_args(ctx, cache, batch, n, a));
+// The same of a cache in 8 bits.
+still_status paged_args(still_ctx* ctx, const still_paged_cache_quant* c,
+                        const still_paged_batch* b, int64_t n, PagedArgs& a) {
+  if (c == nullptr) return STILL_ERR_INVALID_ARG;
+  const still_paged_cache common = {c->K,        c->V,       c->beta,      c->s_page, c->s_slot,
+                                    c->s_head,   c->n_pages, c->page_size, c->n_kv_heads,
+                                    c->head_dim};
+  TRY(paged_args(ctx, &common, b, n, a));
+  if (c->k_scale == nullptr || c->v_scale == nullptr) return STILL_ERR_INVALID_ARG;
+  if (((c->s_page | c->s_slot | c->s_head) & 15) ||
+      ((reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale)) & 3))
+    return STILL_ERR_ALIGNMENT;
+  a.K = a.V = nullptr;
+  a.K8 = static_cast<uint8_t*>(c->K);
+  a.V8 = static_cast<uint8_t*>(c->V);
+  a.k_scale = c->k_scale;
+  a.v_scale = c->v_scale;
+  return STILL_OK;
+}
+
+// Host checks of the rows that attend; `out` may be null where nothing is attended (weigh).
+still_status paged_query(const PagedArgs& a, int64_t n, const void* q, int64_t q_stride, int32_t Hq,
+                         float scale, void* out, bool has_out, PagedQuery& p) {
   if (Hq < a.H || Hq % a.H != 0 || q_stride < (int64_t)Hq * a.d || !(scale >= 0.f) ||
       !std::isfinite(scale))
     return STILL_ERR_INVALID_ARG;
   if (Hq / a.H > 1024 || n * (Hq / a.H) > INT32_MAX / 2) return STILL_ERR_UNSUPPORTED;
   if (n == 0) return STILL_OK;
-  if (q == nullptr || out == nullptr) return STILL_ERR_INVALID_ARG;
+  if (q == nullptr || (has_out && out == nullptr)) return STILL_ERR_INVALID_ARG;
   if (bad_rows(q, q_stride) || bad_rows(out, 0)) return STILL_ERR_ALIGNMENT;
-  PagedQuery p;
   p.q = static_cast<const bf16*>(q);
   p.s_q = q_stride;
   p.out = static_cast<bf16*>(out);
   p.Hq = Hq;
   p.scale = scale > 0.f ? scale : 1.f / std::sqrt((float)a.d);
+  return STILL_OK;
+}
+
+still_status paged_attend(still_ctx* ctx, const still_paged_cache* cache,
+                          const still_paged_batch* batch, int64_t n, const void* q,
+                          int64_t q_stride, int32_t Hq, float scale, void* out, void* stream) {
+  PagedArgs a;
+  PagedQuery p;
+  TRY(paged_args(ctx, cache, batch, n, a));
+  TRY(paged_query(a, n, q, q_stride, Hq, scale, out, true, p));
+  if (n == 0) return STILL_OK;
   CK(cudaSetDevice(ctx->device));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   TRY(ensure_paged_ws(ctx));
@@ -1818,17 +1848,11 @@ still_status paged_attend(still_ctx* ctx, const still_paged_cache* cache,
   return STILL_OK;
 }
 
-}  // namespace
-
-extern "C" {
-
-still_status still_paged_append(still_ctx* ctx, const still_paged_cache* cache,
-                                const still_paged_batch* batch, int32_t n, const void* k,
-                                int64_t k_stride, const void* v, int64_t v_stride,
-                                const void* q, int64_t q_stride, int32_t Hq, const float* beta,
-                                double rope_theta, void* q_out, void* stream) {
-  PagedArgs a;
-  TRY(paged_args(ctx, cache, batch, n, a));
+// Host checks of an append's rows, and the angles of the context.
+still_status paged_append_args(still_ctx* ctx, const PagedArgs& a, int32_t n, const void* k,
+                               int64_t k_stride, const void* v, int64_t v_stride, const void* q,
+                               int64_t q_stride, int32_t Hq, const float* beta, double rope_theta,
+                               void* q_out, PagedAppend& p) {
   const int64_t row = (int64_t)a.H * a.d;
   if (k_stride < row || v_stride < row || (a.cu_new == nullptr && n != a.B) ||
       (beta != nullptr && a.beta == nullptr) || !std::isfinite(rope_theta) || rope_theta < 0 ||
@@ -1844,7 +1868,6 @@ still_status still_paged_append(still_ctx* ctx, const still_paged_cache* cache,
       (q != nullptr && (bad_rows(q, q_stride) || bad_rows(q_out, 0))) ||
       (reinterpret_cast<uintptr_t>(beta) & 3))
     return STILL_ERR_ALIGNMENT;
-  PagedAppend p;
   p.q = static_cast<const bf16*>(q);
   p.k = static_cast<const bf16*>(k);
   p.v = static_cast<const bf16*>(v);
@@ -1864,6 +1887,67 @@ still_status still_paged_append(still_ctx* ctx, const still_paged_cache* cache,
     ctx->turns_theta = rope_theta;
     ctx->turns_d = a.d;
   }
+  return STILL_OK;
+}
+
+still_status paged_attend_quant(still_ctx* ctx, const still_paged_cache_quant* cache,
+                                const still_paged_batch* batch, int64_t n, const void* q,
+                                int64_t q_stride, int32_t Hq, float scale, void* out,
+                                void* stream) {
+  PagedArgs a;
+  PagedQuery p;
+  TRY(paged_args(ctx, cache, batch, n, a));
+  TRY(paged_query(a, n, q, q_stride, Hq, scale, out, true, p));
+  if (n == 0) return STILL_OK;
+  CK(cudaSetDevice(ctx->device));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  TRY(ensure_paged_ws(ctx));
+  KLAUNCH(STILL_K_PAGED_ATTEND,
+          launch_paged_rows_quant(a, p, ctx->paged_ws, ctx->kernels.num_sms, s));
+  ctx->prof.launches[STILL_K_PAGED_ATTEND] += 1;  // the join
+  return STILL_OK;
+}
+
+// Bytes of the rows' (m, 1 / l) at the head of a weigh call's scratch, and of the logits behind.
+int64_t weigh_rows_bytes(int64_t n, int64_t Hq) { return (n * Hq * 8 + 255) / 256 * 256; }
+int64_t weigh_logits_bytes(const still_paged_cache* c, int64_t Hq) {
+  return (int64_t)c->n_pages * c->page_size * Hq * 4;
+}
+
+still_status paged_weigh_args(still_ctx* ctx, const still_paged_cache* cache,
+                              const still_paged_batch* batch, int64_t n, const void* q,
+                              int64_t q_stride, int32_t Hq, float scale, void* out, bool decode,
+                              const float* weight, float decay, void* scratch, int64_t bytes,
+                              PagedArgs& a, PagedQuery& p) {
+  TRY(paged_args(ctx, cache, batch, n, a));
+  TRY(paged_query(a, n, q, q_stride, Hq, scale, out, decode, p));
+  if (n == 0) return STILL_OK;
+  if (weight == nullptr || scratch == nullptr || !(decay >= 0.f) || !(decay <= 1.f))
+    return STILL_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(weight) & 3) || (reinterpret_cast<uintptr_t>(scratch) & 15))
+    return STILL_ERR_ALIGNMENT;
+  const int64_t rows = weigh_rows_bytes(n, Hq);
+  if (bytes < rows + (decode ? weigh_logits_bytes(cache, Hq) : 0)) return STILL_ERR_SHAPE;
+  p.ml = static_cast<float2*>(scratch);
+  p.logits = reinterpret_cast<float*>(static_cast<char*>(scratch) + rows);
+  return STILL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+still_status still_paged_append(still_ctx* ctx, const still_paged_cache* cache,
+                                const still_paged_batch* batch, int32_t n, const void* k,
+                                int64_t k_stride, const void* v, int64_t v_stride,
+                                const void* q, int64_t q_stride, int32_t Hq, const float* beta,
+                                double rope_theta, void* q_out, void* stream) {
+  PagedArgs a;
+  PagedAppend p;
+  TRY(paged_args(ctx, cache, batch, n, a));
+  TRY(paged_append_args(ctx, a, n, k, k_stride, v, v_stride, q, q_stride, Hq, beta, rope_theta,
+                        q_out, p));
+  if (n == 0) return STILL_OK;
   CK(cudaSetDevice(ctx->device));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   KLAUNCH(STILL_K_PAGED_APPEND, launch_paged_append(a, p, ctx->turns, ctx->kernels.num_sms, s));
@@ -1884,6 +1968,129 @@ still_status still_paged_prefill(still_ctx* ctx, const still_paged_cache* cache,
                                  void* stream) {
   if (batch != nullptr && batch->cu_new == nullptr && n != batch->B) return STILL_ERR_INVALID_ARG;
   return paged_attend(ctx, cache, batch, n, q, q_stride, Hq, scale, out, stream);
+}
+
+still_status still_paged_append_quant(still_ctx* ctx, const still_paged_cache_quant* cache,
+                                      const still_paged_batch* batch, int32_t n, const void* k,
+                                      int64_t k_stride, const void* v, int64_t v_stride,
+                                      const void* q, int64_t q_stride, int32_t Hq,
+                                      const float* beta, double rope_theta, void* q_out,
+                                      void* stream) {
+  PagedArgs a;
+  PagedAppend p;
+  TRY(paged_args(ctx, cache, batch, n, a));
+  TRY(paged_append_args(ctx, a, n, k, k_stride, v, v_stride, q, q_stride, Hq, beta, rope_theta,
+                        q_out, p));
+  if (n == 0) return STILL_OK;
+  CK(cudaSetDevice(ctx->device));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  KLAUNCH(STILL_K_PAGED_APPEND, launch_paged_append_quant(a, p, ctx->turns, s));
+  return STILL_OK;
+}
+
+still_status still_paged_decode_quant(still_ctx* ctx, const still_paged_cache_quant* cache,
+                                      const still_paged_batch* batch, const void* q,
+                                      int64_t q_stride, int32_t Hq, float scale, void* out,
+                                      void* stream) {
+  if (batch != nullptr && batch->cu_new != nullptr) return STILL_ERR_INVALID_ARG;
+  return paged_attend_quant(ctx, cache, batch, batch != nullptr ? batch->B : 0, q, q_stride, Hq,
+                            scale, out, stream);
+}
+
+still_status still_paged_prefill_quant(still_ctx* ctx, const still_paged_cache_quant* cache,
+                                       const still_paged_batch* batch, int32_t n, const void* q,
+                                       int64_t q_stride, int32_t Hq, float scale, void* out,
+                                       void* stream) {
+  if (batch != nullptr && batch->cu_new == nullptr && n != batch->B) return STILL_ERR_INVALID_ARG;
+  return paged_attend_quant(ctx, cache, batch, n, q, q_stride, Hq, scale, out, stream);
+}
+
+int64_t still_paged_weigh_scratch(const still_paged_cache* cache, int32_t n, int32_t Hq) {
+  if (cache == nullptr || n < 0 || Hq < 1 || cache->n_pages < 1 || cache->page_size < 1) return 0;
+  return weigh_rows_bytes(n, Hq) + weigh_logits_bytes(cache, Hq);
+}
+
+still_status still_paged_decode_weigh(still_ctx* ctx, const still_paged_cache* cache,
+                                      const still_paged_batch* batch, const void* q,
+                                      int64_t q_stride, int32_t Hq, float scale, void* out,
+                                      float* weight, float decay, void* scratch,
+                                      int64_t scratch_bytes, void* stream) {
+  if (batch != nullptr && batch->cu_new != nullptr) return STILL_ERR_INVALID_ARG;
+  PagedArgs a;
+  PagedQuery p;
+  const int64_t n = batch != nullptr ? batch->B : 0;
+  TRY(paged_weigh_args(ctx, cache, batch, n, q, q_stride, Hq, scale, out, true, weight, decay,
+                       scratch, scratch_bytes, a, p));
+  if (n == 0) return STILL_OK;
+  CK(cudaSetDevice(ctx->device));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  TRY(ensure_paged_ws(ctx));
+  KLAUNCH(STILL_K_PAGED_ATTEND, launch_paged_decode_weigh(a, p, weight, decay, ctx->paged_ws,
+                                                          ctx->kernels.num_sms, s));
+  ctx->prof.launches[STILL_K_PAGED_ATTEND] += 2;  // the join, the weights
+  return STILL_OK;
+}
+
+still_status still_paged_weigh(still_ctx* ctx, const still_paged_cache* cache,
+                               const still_paged_batch* batch, int32_t n, const void* q,
+                               int64_t q_stride, int32_t Hq, float scale, float* weight,
+                               float decay, void* scratch, int64_t scratch_bytes, void* stream) {
+  if (batch != nullptr && batch->cu_new == nullptr && n != batch->B) return STILL_ERR_INVALID_ARG;
+  PagedArgs a;
+  PagedQuery p;
+  TRY(paged_weigh_args(ctx, cache, batch, n, q, q_stride, Hq, scale, nullptr, false, weight, decay,
+                       scratch, scratch_bytes, a, p));
+  if (n == 0) return STILL_OK;
+  CK(cudaSetDevice(ctx->device));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  TRY(ensure_paged_ws(ctx));
+  KLAUNCH(STILL_K_PAGED_WEIGH, launch_paged_weigh(a, p, weight, decay, ctx->paged_ws,
+                                                  ctx->kernels.num_sms, s));
+  ctx->prof.launches[STILL_K_PAGED_WEIGH] += 2;
+  return STILL_OK;
+}
+
+still_status still_paged_evict(still_ctx* ctx, const still_paged_cache* cache,
+                               const still_paged_batch* batch, const float* weight, int32_t keep,
+                               int32_t sinks, int32_t recent, const still_paged_cache* to,
+                               const int32_t* to_table, int64_t to_s_table, int32_t to_table_pages,
+                               float* to_weight, int32_t* kept, int32_t* to_len,
+                               int64_t* to_offset, void* stream) {
+  if (batch == nullptr) return STILL_ERR_INVALID_ARG;
+  still_paged_batch from = *batch, into = *batch;
+  from.cu_new = nullptr;  // who owns new tokens does not matter here
+  into.cu_new = nullptr;
+  into.pos_offset = nullptr;
+  into.table = to_table;
+  into.s_table = to_s_table;
+  into.table_pages = to_table_pages;
+  PagedArgs a;
+  PagedEvict f;
+  TRY(paged_args(ctx, cache, &from, batch->B, a));
+  TRY(paged_args(ctx, to, &into, batch->B, f.to));
+  if (weight == nullptr || kept == nullptr || to_len == nullptr || keep < 1 || sinks < 0 ||
+      recent < 0 || (int64_t)sinks + recent > keep || (a.beta != nullptr && f.to.beta == nullptr))
+    return STILL_ERR_INVALID_ARG;
+  if (f.to.H != a.H || f.to.d != a.d || keep > (int64_t)f.to.table_pages << f.to.page_shift)
+    return STILL_ERR_SHAPE;
+  if ((int64_t)a.B * a.H > INT32_MAX / 16) return STILL_ERR_UNSUPPORTED;
+  if (((reinterpret_cast<uintptr_t>(weight) | reinterpret_cast<uintptr_t>(to_weight) |
+        reinterpret_cast<uintptr_t>(kept) | reinterpret_cast<uintptr_t>(to_len)) & 3) ||
+      (reinterpret_cast<uintptr_t>(to_offset) & 7))
+    return STILL_ERR_ALIGNMENT;
+  f.weight = weight;
+  f.keep = keep;
+  f.sinks = sinks;
+  f.recent = recent;
+  f.to_weight = to_weight;
+  f.kept = kept;
+  f.to_len = to_len;
+  f.to_offset = to_offset;
+  CK(cudaSetDevice(ctx->device));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  KLAUNCH(STILL_K_PAGED_EVICT, launch_paged_evict(a, f, ctx->kernels, s));
+  ctx->prof.launches[STILL_K_PAGED_EVICT] += 1;  // choosing and moving
+  return STILL_OK;
 }
 
 still_status still_compact_layer_noalloc(still_ctx* ctx, int32_t layer, const void* K,
@@ -2244,7 +2451,7 @@ const char* still_kernel_class_name(int32_t cls) {
       "strip", "rope_tables", "keyproj", "q_rope", "scores", "softmax", "px", "px_split",
       "vo", "rmsnorm", "sa_proj", "sa_v", "sa_scores", "sa_softmax", "sa_pv", "sa_out",
       "ffn1", "ffn2", "heads", "norms", "load", "ca_fused", "beta", "decode", "repair",
-      "paged_append", "paged_attend"};
+      "paged_append", "paged_attend", "paged_weigh", "paged_evict"};
   return cls >= 0 && cls < STILL_K_COUNT ? names[cls] : "unknown";
 }
 

@@ -32,7 +32,9 @@ EXPORTS = [
     "still_lookahead_totals", "still_lookahead_compact_layer", "still_lookahead_compact_stack",
     "still_set_beta_head", "still_compact_layer_beta", "still_attend_biased", "still_set_key_fold",
     "still_attend_biased_stack", "still_paged_append", "still_paged_decode",
-    "still_paged_prefill",
+    "still_paged_prefill", "still_paged_append_quant", "still_paged_decode_quant",
+    "still_paged_prefill_quant", "still_paged_weigh_scratch", "still_paged_decode_weigh",
+    "still_paged_weigh", "still_paged_evict",
 ]
 
 NOALLOC_SCRATCH_MIB = 64  # STILL_NOALLOC_SCRATCH_MIB in include/still.h
@@ -40,7 +42,8 @@ NOALLOC_SCRATCH_MIB = 64  # STILL_NOALLOC_SCRATCH_MIB in include/still.h
 KERNEL_CLASSES = ["strip", "rope_tables", "keyproj", "q_rope", "scores", "softmax", "px",
                   "px_split", "vo", "rmsnorm", "sa_proj", "sa_v", "sa_scores", "sa_softmax",
                   "sa_pv", "sa_out", "ffn1", "ffn2", "heads", "norms", "load", "ca_fused",
-                  "beta", "decode", "repair", "paged_append", "paged_attend"]
+                  "beta", "decode", "repair", "paged_append", "paged_attend", "paged_weigh",
+                  "paged_evict"]
 
 
 class StillError(RuntimeError):
@@ -96,6 +99,15 @@ class PosSegment(ctypes.Structure):
 
 class _PagedCache(ctypes.Structure):
     _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("beta", ctypes.c_void_p),
+                ("s_page", ctypes.c_int64), ("s_slot", ctypes.c_int64),
+                ("s_head", ctypes.c_int64), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
+class _PagedCacheQuant(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("beta", ctypes.c_void_p),
                 ("s_page", ctypes.c_int64), ("s_slot", ctypes.c_int64),
                 ("s_head", ctypes.c_int64), ("n_pages", ctypes.c_int32),
                 ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
@@ -182,6 +194,19 @@ def lib():
             "still_paged_decode": ([P, P, P, P, I64, I32, ctypes.c_float, P, P], ctypes.c_int),
             "still_paged_prefill": ([P, P, P, I32, P, I64, I32, ctypes.c_float, P, P],
                                     ctypes.c_int),
+            "still_paged_append_quant": ([P, P, P, I32, P, I64, P, I64, P, I64, I32, P, D, P, P],
+                                         ctypes.c_int),
+            "still_paged_decode_quant": ([P, P, P, P, I64, I32, ctypes.c_float, P, P],
+                                         ctypes.c_int),
+            "still_paged_prefill_quant": ([P, P, P, I32, P, I64, I32, ctypes.c_float, P, P],
+                                          ctypes.c_int),
+            "still_paged_weigh_scratch": ([P, I32, I32], I64),
+            "still_paged_decode_weigh": ([P, P, P, P, I64, I32, ctypes.c_float, P, P,
+                                          ctypes.c_float, P, I64, P], ctypes.c_int),
+            "still_paged_weigh": ([P, P, P, I32, P, I64, I32, ctypes.c_float, P, ctypes.c_float,
+                                   P, I64, P], ctypes.c_int),
+            "still_paged_evict": ([P, P, P, P, I32, I32, I32, P, P, I64, I32, P, P, P, P, P],
+                                  ctypes.c_int),
             "still_lookahead_pass_info": ([I64, I64, I32, ctypes.POINTER(LookaheadPass)],
                                           ctypes.c_int),
             "still_lookahead_totals": ([I64, I64, I32, PI64, PI64], ctypes.c_int),
@@ -407,6 +432,27 @@ def still_attend_biased_stack(ctx, q, Ck, Cv, beta, Kfix, Vfix, out, scale=0.0, 
                                            _stream(stream)), "still_attend_biased_stack")
 
 
+def _pool_strides(K, V):
+    """Strides of pools [n_pages, page_size, H, d]; that of an axis of one entry means nothing."""
+    assert K.dim() == 4 and K.shape == V.shape and K.dtype == V.dtype
+    d = K.shape[3]
+    strides = [[s if size > 1 else d for s, size in zip(x.stride(), x.shape)] for x in (K, V)]
+    assert strides[0] == strides[1] and K.stride(3) == V.stride(3) == 1, \
+        "K and V must share strides"
+    return strides[0][:3]
+
+
+def _per_slot(x, cache_shape, what, slots=1):
+    """Pointer of [n_pages, H, page_size / slots] fp32 (None: NULL)."""
+    import torch
+    if x is None:
+        return None
+    n, page, H, _ = cache_shape
+    assert x.dtype == torch.float32 and tuple(x.shape) == (n, H, page // slots), what
+    assert x.is_contiguous(), what
+    return x.data_ptr()
+
+
 class PagedCache:
     """A layer's pages (still_paged_cache): K, V [n_pages, page_size, H, d] bf16 CUDA tensors of
     equal strides with contiguous channels (any order in memory, such as a transposed
@@ -415,19 +461,30 @@ class PagedCache:
 
     def __init__(self, K, V, beta=None):
         import torch
-        assert K.dtype == V.dtype == torch.bfloat16 and K.dim() == 4 and K.shape == V.shape
+        assert K.dtype == V.dtype == torch.bfloat16
         n, page, H, d = K.shape
-        # the stride of an axis of one entry means nothing
-        strides = [[s if size > 1 else d for s, size in zip(x.stride(), x.shape)] for x in (K, V)]
-        assert strides[0] == strides[1] and K.stride(3) == V.stride(3) == 1, \
-            "K and V must share strides"
-        if beta is not None:
-            assert beta.dtype == torch.float32 and tuple(beta.shape) == (n, H, page)
-            assert beta.is_contiguous()
+        strides = _pool_strides(K, V)
         self.tensors = (K, V, beta)
-        self.struct = _PagedCache(K.data_ptr(), V.data_ptr(),
-                                  None if beta is None else beta.data_ptr(), *strides[0][:3],
-                                  n, page, H, d)
+        self.struct = _PagedCache(K.data_ptr(), V.data_ptr(), _per_slot(beta, K.shape, "beta"),
+                                  *strides, n, page, H, d)
+        self.ref = ctypes.byref(self.struct)
+
+
+class PagedCacheQuant:
+    """A layer's pages in 8 bits (still_paged_cache_quant): K, V as PagedCache's in
+    torch.float8_e4m3fn, k_scale, v_scale [n_pages, H, page_size / 16] fp32 contiguous."""
+
+    def __init__(self, K, V, k_scale, v_scale, beta=None):
+        import torch
+        assert K.dtype == V.dtype == torch.float8_e4m3fn
+        n, page, H, d = K.shape
+        strides = _pool_strides(K, V)
+        assert k_scale is not None and v_scale is not None
+        self.tensors = (K, V, k_scale, v_scale, beta)
+        self.struct = _PagedCacheQuant(K.data_ptr(), V.data_ptr(),
+                                       _per_slot(k_scale, K.shape, "k_scale", 16),
+                                       _per_slot(v_scale, K.shape, "v_scale", 16),
+                                       _per_slot(beta, K.shape, "beta"), *strides, n, page, H, d)
         self.ref = ctypes.byref(self.struct)
 
 
@@ -465,10 +522,7 @@ def _rows(x, H, d):
     return x.data_ptr(), sn if n > 1 else H * d
 
 
-def still_paged_append(ctx, cache, batch, k, v, q=None, q_out=None, beta=None, rope_theta=0.0,
-                       stream=None):
-    """k, v [n, H, d] and q [n, Hq, d] bf16 (heads contiguous, any token pitch: slices of a fused
-    projection), q_out [n, Hq, d] contiguous; beta [n, H] fp32 or None."""
+def _paged_append(name, ctx, cache, batch, k, v, q, q_out, beta, rope_theta, stream):
     H, d = cache.struct.n_kv_heads, cache.struct.head_dim
     kp, ks = _rows(k, H, d)
     vp, vs = _rows(v, H, d)
@@ -485,9 +539,23 @@ def still_paged_append(ctx, cache, batch, k, v, q=None, q_out=None, beta=None, r
         qo = q_out.data_ptr()
         assert q_out.shape == q.shape and q.shape[0] == n and q_out.is_contiguous()
         assert q_out.dtype == q.dtype
-    _check(lib().still_paged_append(ctx, cache.ref, batch.ref, n, kp, ks, vp, vs, qp, qs, Hq,
-                                    None if beta is None else beta.data_ptr(), rope_theta, qo,
-                                    _stream(stream)), "still_paged_append")
+    _check(getattr(lib(), name)(ctx, cache.ref, batch.ref, n, kp, ks, vp, vs, qp, qs, Hq,
+                                None if beta is None else beta.data_ptr(), rope_theta, qo,
+                                _stream(stream)), name)
+
+
+def still_paged_append(ctx, cache, batch, k, v, q=None, q_out=None, beta=None, rope_theta=0.0,
+                       stream=None):
+    """k, v [n, H, d] and q [n, Hq, d] bf16 (heads contiguous, any token pitch: slices of a fused
+    projection), q_out [n, Hq, d] contiguous; beta [n, H] fp32 or None."""
+    _paged_append("still_paged_append", ctx, cache, batch, k, v, q, q_out, beta, rope_theta, stream)
+
+
+def still_paged_append_quant(ctx, cache, batch, k, v, q=None, q_out=None, beta=None,
+                             rope_theta=0.0, stream=None):
+    """still_paged_append into a PagedCacheQuant."""
+    _paged_append("still_paged_append_quant", ctx, cache, batch, k, v, q, q_out, beta, rope_theta,
+                  stream)
 
 
 def still_paged_decode(ctx, cache, batch, q, out, scale=0.0, stream=None):
@@ -508,6 +576,83 @@ def still_paged_prefill(ctx, cache, batch, q, out, scale=0.0, stream=None):
     assert out.shape == q.shape and out.is_contiguous() and out.dtype == q.dtype
     _check(lib().still_paged_prefill(ctx, cache.ref, batch.ref, n, qp, qs, Hq, scale,
                                      out.data_ptr(), _stream(stream)), "still_paged_prefill")
+
+
+def still_paged_decode_quant(ctx, cache, batch, q, out, scale=0.0, stream=None):
+    """still_paged_decode over a PagedCacheQuant."""
+    n, Hq, d = q.shape
+    qp, qs = _rows(q, Hq, cache.struct.head_dim)
+    assert out.shape == q.shape and out.is_contiguous() and out.dtype == q.dtype
+    assert n == batch.struct.B
+    _check(lib().still_paged_decode_quant(ctx, cache.ref, batch.ref, qp, qs, Hq, scale,
+                                          out.data_ptr(), _stream(stream)),
+           "still_paged_decode_quant")
+
+
+def still_paged_prefill_quant(ctx, cache, batch, q, out, scale=0.0, stream=None):
+    """still_paged_prefill over a PagedCacheQuant."""
+    n, Hq, d = q.shape
+    qp, qs = _rows(q, Hq, cache.struct.head_dim)
+    assert out.shape == q.shape and out.is_contiguous() and out.dtype == q.dtype
+    _check(lib().still_paged_prefill_quant(ctx, cache.ref, batch.ref, n, qp, qs, Hq, scale,
+                                           out.data_ptr(), _stream(stream)),
+           "still_paged_prefill_quant")
+
+
+def still_paged_weigh_scratch(cache, n, Hq):
+    """Bytes of scratch for still_paged_decode_weigh and still_paged_weigh with n new tokens."""
+    return lib().still_paged_weigh_scratch(cache.ref, n, Hq)
+
+
+def _scratch(x):
+    assert x.is_contiguous()
+    return x.data_ptr(), x.numel() * x.element_size()
+
+
+def still_paged_decode_weigh(ctx, cache, batch, q, out, weight, scratch, decay=1.0, scale=0.0,
+                             stream=None):
+    """still_paged_decode that also adds up weights: weight [n_pages, H, page_size] fp32
+    contiguous, scratch any contiguous CUDA tensor of still_paged_weigh_scratch bytes."""
+    n, Hq, d = q.shape
+    qp, qs = _rows(q, Hq, cache.struct.head_dim)
+    assert out.shape == q.shape and out.is_contiguous() and out.dtype == q.dtype
+    assert n == batch.struct.B and weight is not None
+    _check(lib().still_paged_decode_weigh(ctx, cache.ref, batch.ref, qp, qs, Hq, scale,
+                                          out.data_ptr(),
+                                          _per_slot(weight, cache.tensors[0].shape, "weight"),
+                                          decay, *_scratch(scratch), _stream(stream)),
+           "still_paged_decode_weigh")
+
+
+def still_paged_weigh(ctx, cache, batch, q, weight, scratch, decay=1.0, scale=0.0, stream=None):
+    """Weights of the packed new tokens q [n, Hq, d] (heads contiguous, any token pitch); weight
+    and scratch as still_paged_decode_weigh's."""
+    n, Hq, d = q.shape
+    qp, qs = _rows(q, Hq, cache.struct.head_dim)
+    assert weight is not None
+    _check(lib().still_paged_weigh(ctx, cache.ref, batch.ref, n, qp, qs, Hq, scale,
+                                   _per_slot(weight, cache.tensors[0].shape, "weight"), decay,
+                                   *_scratch(scratch), _stream(stream)), "still_paged_weigh")
+
+
+def still_paged_evict(ctx, cache, batch, weight, keep, sinks, recent, to, to_table, kept, to_lens,
+                      to_weight=None, to_offset=None, stream=None):
+    """weight [n_pages, H, page_size] fp32; `to` a PagedCache, to_table [B, pages] int32; written:
+    kept [B, H, keep] int32, to_lens [B] int32, to_weight (like weight, of `to`) and to_offset [B]
+    int64 or None."""
+    import torch
+    into = PagedBatch(to_table, to_lens, None, to_offset)
+    B, H = batch.struct.B, cache.struct.n_kv_heads
+    assert weight is not None and into.struct.B == B
+    assert kept.dtype == torch.int32 and tuple(kept.shape) == (B, H, keep)
+    assert kept.is_contiguous()
+    _check(lib().still_paged_evict(ctx, cache.ref, batch.ref,
+                                   _per_slot(weight, cache.tensors[0].shape, "weight"), keep,
+                                   sinks, recent, to.ref, to_table.data_ptr(),
+                                   into.struct.s_table, into.struct.table_pages,
+                                   _per_slot(to_weight, to.tensors[0].shape, "to_weight"),
+                                   kept.data_ptr(), to_lens.data_ptr(), into.struct.pos_offset,
+                                   _stream(stream)), "still_paged_evict")
 
 
 def still_lookahead_pass_info(k: int, c: int, t: int) -> dict:
