@@ -379,8 +379,11 @@ still_status still_paged_append_quant(still_ctx* ctx, const still_paged_cache_qu
 /* still_paged_decode and still_paged_prefill over a cache in 8 bits, arguments, workspace and device
  * status as there. Scales of blocks that hold a visible slot are positive and finite; what the
  * others hold does not matter, and neither do the codes of masked slots. Queries and weights are
- * not held in 8 bits: logits are sums in fp32 of exact products, and weights enter the product with
- * V with an error below 2^-21 of the largest of their row times its block's scale. */
+ * not held in 8 bits. Where a call has few rows (still_paged_decode; without cu_new up to twice as
+ * many) logits are sums in fp32 of exact products, and weights enter the product with V with an error
+ * below 2^-21 of the largest of their row times its block's scale. In every other call with at most
+ * 128 query heads to a KV-head weights enter it as bf16 (2^-8), and so do values, exact where scales
+ * are powers of two and rounded otherwise. */
 still_status still_paged_decode_quant(still_ctx* ctx, const still_paged_cache_quant* cache,
                                       const still_paged_batch* batch, const void* q,
                                       int64_t q_stride, int32_t Hq, float scale, void* out,

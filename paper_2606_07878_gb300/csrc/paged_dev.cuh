@@ -8,6 +8,19 @@ namespace still {
 constexpr float kLog2e = 1.44269504f;
 
 STILL_DEV uint32_t bf16x2_bits(__nv_bfloat162 x) { return *reinterpret_cast<uint32_t*>(&x); }
+// The lower and the upper two e4m3 codes of a word as fp16 pairs (exact).
+STILL_DEV uint32_t f16_of_lower(uint32_t x) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n}\n"
+      : "=r"(r) : "r"(x));
+  return r;
+}
+STILL_DEV uint32_t f16_of_upper(uint32_t x) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n}\n"
+      : "=r"(r) : "r"(x));
+  return r;
+}
 
 // First new token, number of them and slots of sequence b, whatever the arrays hold: an offset
 // outside [0, n] or a length beyond the table is cut, and recorded (by one of those who look), as

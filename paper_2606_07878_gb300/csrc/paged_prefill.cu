@@ -44,51 +44,18 @@
 // of K and V on each SM: 444 and 577; loaded once for a pair by multicast: 432 and 490. 64 channels
 // have as many exponentials for half the products: 8,192 tokens of 8 KV- and 32 query heads 336 us
 // where 128 channels take 352, 0.82 against 1.56 PFLOP/s (with biases 416 and 465).
-#include <algorithm>
 #include <type_traits>
 
-#include "gemm_host.cuh"
-#include "paged_dev.cuh"
+#include "paged_tc.cuh"
 
 namespace still {
 
 namespace {
 
-constexpr int kPfThreads = 384;
 constexpr int kPfProducers = 3;     // warps
-constexpr int kPfKeys = 128;        // slots of a tile
+constexpr int kPfConverters = 4;    // warps, of a pool in 8 bits
 constexpr float kPfMoveLog2 = 8.f;  // P <= 2^8 needs no more of bf16's range
-// of an item's beginning and end, in tiles of slots (1: 379 and 249 us for 8,192 tokens and for
-// three short prompts of 256 channels; 2: 345 and 240; 4: 350 and 247)
-constexpr int kPfItemCost = 2;
 
-struct PrefillParams {
-  PagedArgs a;
-  PagedQuery q;
-  int32_t tile_tokens = 0;  // floor(128 / g)
-  // parts of items that lie in several CTAs' ranges: what CTA c continues (2 c), begins (2 c + 1)
-  float4* part_o = nullptr;   // [2 x CTAs][d / 4][rows of an item]
-  float2* part_ml = nullptr;  // [2 x CTAs][rows of an item] (m, l), m in the kernel's units
-  struct PfSplit* split = nullptr;  // [CTAs]
-};
-
-// The item that CTA c begins and does not end, and the one in which its range begins.
-struct PfSplit {
-  int32_t last;    // the CTA that ends it; c: there is none
-  int32_t token0, tokens, h;
-  int32_t first;   // the CTA that begins that one
-};
-
-// D[tmem] (+)= A[tmem, 128 lanes x 16] * B[smem, MN-major], kind::f16.
-STILL_DEV void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
-                      uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
 // The same on a CTA pair, issued by the even CTA: A's rows [0, 128) from its TMEM, [128, 256) from
 // the odd CTA's, and half of B's columns from each one's shared memory.
 STILL_DEV void mma_ts_2sm(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
@@ -100,45 +67,6 @@ STILL_DEV void mma_ts_2sm(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint
       "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// One lane of a converged warp, as the compiler knows: behind it operands stay uniform.
-STILL_DEV bool elect_one() {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred q;\n\t"
-      "elect.sync _|q, 0xffffffff;\n\t"
-      "selp.b32 %0, 1, 0, q;\n}\n"
-      : "=r"(r));
-  return r != 0;
-}
-// Shared-memory descriptor of an MN-major operand, 128-byte swizzle: rows (k) of 64 contiguous
-// elements, 8 rows an atom of 1024 bytes, atoms along k 1024 bytes apart, the next 64 elements
-// `chunk` bytes further.
-STILL_DEV uint64_t sdesc_mn_sw128(uint32_t saddr, int chunk) {
-  uint64_t d = 0;
-  d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
-  d |= (uint64_t)(chunk >> 4) << 16;
-  d |= (uint64_t)(1024 >> 4) << 32;
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)2 << 61;
-  return d;
-}
-constexpr uint32_t kIdescBMn = 1u << 16;  // B is MN-major
-
-STILL_DEV void tma_load_3d(void* dst, const CUtensorMap* m, uint64_t* bar, int x, int y, int z) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes "
-      "[%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
-      : "memory");
-}
-STILL_DEV void tma_load_4d(void* dst, const CUtensorMap* m, uint64_t* bar, int x, int y, int z,
-                           int w) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes "
-      "[%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
-      : "memory");
-}
 // The same, its completion on an mbarrier of either CTA of the pair (a shared::cluster address).
 STILL_DEV void tma_load_4d_2sm(void* dst, const CUtensorMap* m, uint32_t bar_cluster, int x, int y,
                                int z, int w) {
@@ -148,22 +76,6 @@ STILL_DEV void tma_load_4d_2sm(void* dst, const CUtensorMap* m, uint32_t bar_clu
       "l"(reinterpret_cast<uint64_t>(m)), "r"(bar_cluster), "r"(x), "r"(y), "r"(z), "r"(w)
       : "memory");
 }
-// 32 lanes x 32 columns of 32 bits from registers; complete after tmem_wait_st.
-STILL_DEV void tmem_st32_issue(uint32_t taddr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(
-          taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
-      "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
-      "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
-      "r"(r[29]), "r"(r[30]), "r"(r[31])
-      : "memory");
-}
-STILL_DEV void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
 // Zeroes rows of a ring slot whose chunks have `rows` rows, slots [first, first + rows) of a tile:
 // those that lane i marks in its bits for slots [4 i, 4 i + 4).
 STILL_DEV void zero_rows(uint8_t* slot, int chunks, int rows, int first, uint32_t marks) {
@@ -181,39 +93,20 @@ STILL_DEV void zero_rows(uint8_t* slot, int chunks, int rows, int first, uint32_
   __syncwarp();
 }
 
-// What a CTA does of an item.
-struct PfItem {
-  int b, h, len;
-  int token0, tokens;  // its tokens, packed rows
-  int see;             // slots that the first of them sees (below 1: none)
-  int k0, k1;          // tiles of slots [k0, k1)
-  int part;            // 0: all of the item, else where the part goes: 1 + (it is the first)
-  int last;            // the CTA that ends an item which this one begins
-};
-
-// Where a CTA's range begins, in shared memory.
-struct PfStart {
-  int64_t base;  // cost of all items before this one
-  int64_t total, left;  // of all items, of this CTA's range
-  int b, qt, h, off;    // off: cost of this item that lies before the range
-  int nct;              // CTAs that have a range
-};
-
-// A whole warp waits for a phase; false (and a record, and the flag for the others) at the limit.
-STILL_DEV bool pf_wait(uint64_t* bar, uint32_t parity, int* err, volatile int* abort_flag,
-                       int where) {
-  const bool ok = __all_sync(0xffffffffu, mbar_wait(bar, parity));
-  if (!ok && (threadIdx.x & 31) == 0) {
-    dev_set_error(err, DEV_WAIT_TIMEOUT, where);
-    *abort_flag = 1;
-  }
-  return ok;
-}
-
 struct PfPlan {  // in shared memory
   PfStart start;
   PfItem shown[2];  // items n & 1 as the producer shows them to the others
-  int64_t warp_cost[kPfThreads / 32];
+  int64_t warp_cost[16];
+};
+
+// The warps of a CTA. Of a pool in 8 bits a warpgroup converts codes, and the softmax warps begin at
+// a warpgroup of their own, so that registers can be dealt out: 4 x 128 threads of 128 each become
+// 96 (loads, products), 160, 160 (softmax) and 96 (codes), or 112, 144, 144 and 112 without biases.
+template <bool kQuant>
+struct PfRoles {
+  static constexpr int kThreads = kQuant ? 512 : 384;
+  static constexpr int kSoftmax = kQuant ? 4 : 2;       // the first of eight
+  static constexpr int kFirst = kSoftmax + 8;           // producer or converter behind them
 };
 
 template <int D, bool kBias, bool kPair>
@@ -238,99 +131,206 @@ struct PfShape {
   static constexpr int kBarAt = kXchAt + (kTiles == 1 ? 2048 : 0);
   static constexpr int kPlanAt = kBarAt + (3 * kStages + 30) * 8;
   static constexpr int kBytes = kPlanAt + sizeof(PfPlan);
+  static constexpr int kConvertRegs = kBias ? 96 : 112;  // of a pool in 8 bits (PfRoles)
   static_assert(kBytes <= 232448, "shared memory budget");
 };
 
-STILL_DEV int pf_tiles(const Seq& s, int tokens) { return (s.count + tokens - 1) / tokens; }
-// Tiles of slots that item qt of a sequence sees.
-__host__ __device__ __forceinline__ int pf_slots(const Seq& s, int tokens, int qt) {
-  const int upto = (qt + 1) * tokens, most = s.len - s.count + (upto < s.count ? upto : s.count);
-  return most > 0 ? (most + kPfKeys - 1) / kPfKeys : 0;
-}
-// Cost of items [q0, q1) of a sequence and KV-head: a million tokens pass 32 bits.
-__host__ __device__ __forceinline__ int64_t pf_cost(const Seq& s, int tokens, int q0, int q1) {
-  int64_t sum = 0;
-  for (int qt = q0; qt < q1; ++qt) sum += pf_slots(s, tokens, qt) + kPfItemCost;
-  return sum;
-}
-
-// The items of a CTA's range, in order: sequences, tokens, KV-heads. An item's cost is its tiles of
-// slots, then kPfItemCost for its beginning and end.
-struct PfWalk {
-  const PagedArgs& a;
-  int tokens;  // of an item
-  int64_t base, left, total;
-  int b, qt, h, off, nq, nct;
-  Seq s;
-  STILL_DEV PfWalk(const PagedArgs& args, int item_tokens, const PfStart& p)
-      : a(args), tokens(item_tokens), base(p.base), left(p.left), total(p.total), b(p.b), qt(p.qt),
-        h(p.h), off(p.off), nct(p.nct) {
-    if (left > 0) {
-      s = paged_seq<false>(a, b);
-      nq = pf_tiles(s, tokens);
-    }
-  }
-  STILL_DEV bool next(PfItem& it) {
-    while (left > 0) {
-      const int kt = pf_slots(s, tokens, qt), cost = kt + kPfItemCost;
-      const int end = (int)min((int64_t)cost, off + left);
-      const bool begins = off == 0;
-      it.b = b;
-      it.h = h;
-      it.len = s.len;
-      it.token0 = s.first + qt * tokens;
-      it.tokens = min(tokens, s.count - qt * tokens);
-      it.see = s.len - s.count + qt * tokens + 1;
-      it.k0 = min(off, kt);
-      it.k1 = min(end, kt);
-      it.part = begins && end >= kt ? 0 : begins ? 2 : 1;
-      if (it.part == 2) it.last = (int)(((base + kt) * nct - 1) / total);
-      left -= end - off;
-      off = 0;
-      if (end == cost) {
-        base += cost;
-        if (++h == a.H) {
-          h = 0;
-          if (++qt == nq) {
-            qt = nq = 0;
-            while (left > 0 && nq == 0) {
-              s = paged_seq<false>(a, ++b);
-              nq = pf_tiles(s, tokens);
-            }
-          }
+// A pool in 8 bits: a warpgroup loads codes into registers, one ring slot ahead of the one that it
+// converts, multiplies them by their block's scale and stores bf16 as TMA would have (rows of 128
+// bytes, 128-byte swizzle). Everything behind works as for a pool in bf16. With scales that are powers
+// of two nothing is rounded.
+template <int D, bool kBias, bool kPair, class Zero>
+STILL_DEV void pf_convert(const PrefillParams& f, int tokens, const PfStart& start, uint8_t* smem,
+                          uint64_t* full, uint64_t* empty, volatile int* abort_flag, int rank,
+                          Zero zero_item) {
+  using S = PfShape<D, kBias, kPair>;
+  constexpr int kStages = S::kStages, kHalves = S::kHalves, kAhead = S::kTiles == 2 ? 1 : 2;
+  constexpr int kPieces = S::kStageBytes / 32 / (32 * kPfConverters);  // of 16 codes, of a thread
+  const PagedArgs& a = f.a;
+  const int lane = threadIdx.x & 31;
+  const int me = threadIdx.x & (32 * kPfConverters - 1);
+  const int mask = (1 << a.page_shift) - 1;
+  // Half a tile of K or V, a ring slot: rows of kKRows or 128 slots, pieces of 16 channels.
+  struct Unit {
+    int b, h, len, kt;
+    int half;
+    bool v;
+  };
+  PfWalk walk(a, tokens, start);
+  PfItem it;
+  bool have = false;
+  int kt = 0, sub = 0;
+  // The ring slots in the order in which the issuer takes them.
+  auto next = [&](Unit& u) -> bool {
+    for (;;) {
+      if (!have) {
+        if (warp_flag(abort_flag) || !walk.next(it)) return false;
+        if (it.k0 == it.k1) {
+          if (me < 32 && rank == 0) zero_item(it);
+          continue;
+        }
+        have = true;
+        kt = it.k0 - kAhead;
+        sub = 0;
+      }
+      while (kt < it.k1) {
+        const bool v = sub < kHalves;
+        const int t = v ? kt : kt + kAhead;
+        if (sub < 2 * kHalves && t >= it.k0 && t < it.k1) {
+          u = Unit{it.b, it.h, it.len, t, v ? sub : sub - kHalves, v};
+          ++sub;
+          return true;
+        }
+        if (v) {
+          sub = kHalves;
+        } else {
+          sub = 0;
+          ++kt;
         }
       }
-      if (it.k0 < it.k1 || (begins && kt == 0)) return true;
+      have = false;
     }
-    return false;
-  }
-};
-
-// Biases of a tile of slots, loaded ahead by a warp: lane i holds those of slots [4 i, 4 i + 4).
-struct PfBias {
-  static constexpr int kPer = kPfKeys / 32;
-  float v[kPer];
-  STILL_DEV void load(const PagedArgs& a, const PfItem& it, int slot0, int lane) {
-    const int j = slot0 + kPer * lane;
+  };
+  auto first_of = [&](const Unit& u) {  // slot of its first row
+    return u.kt * kPfKeys + (kPair && !u.v ? rank * S::kKRows : 0);
+  };
+  // Lane i: the page of its i-th 16 slots (-1: none), the scale there, biases of four slots.
+  auto look_up = [&](const Unit& u) {
+    const int j = first_of(u) + kScaleBlock * lane;
+    const int rows = kPair && !u.v ? S::kKRows : kPfKeys;
+    if (kScaleBlock * lane >= rows || j >= u.len) return -1;
+    return paged_page(a, a.table + (int64_t)u.b * a.s_table, j);
+  };
+  auto scale_of = [&](const Unit& u, int pg) {
+    if (pg < 0) return 0.f;
+    const int in = (first_of(u) + kScaleBlock * lane) & mask;
+    return (u.v ? a.v_scale : a.k_scale)[((((int64_t)pg * a.H + u.h) << a.page_shift) + in) >> 4];
+  };
+  // Bits of slots 4 lane + e of the unit that count.
+  auto counts_of = [&](const Unit& u, int pg) {
+    uint32_t m = 0;
+    const int j = first_of(u) + 4 * lane;
+    const int at = __shfl_sync(0xffffffffu, pg, lane >> 2);
+    const float* beta = a.beta + ((((int64_t)max(at, 0) * a.H + u.h) << a.page_shift) + (j & mask));
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) v[e] = 0.f;
-    if (j >= it.len) return;
-    const int pg = paged_page<false>(a, a.table + (int64_t)it.b * a.s_table, j);
-    const int in = j & ((1 << a.page_shift) - 1);
-    const float* at = a.beta + ((((int64_t)max(pg, 0) * a.H + it.h) << a.page_shift) + in);
+    for (int e = 0; e < 4; ++e)
+      if (at >= 0 && j + e < u.len && (!kBias || beta[e] != -INFINITY)) m |= 1u << e;
+    return m;
+  };
+  // A thread's piece i: row and 16 channels of a unit (a row has 2^bits pieces).
+  auto bits_of = [&](const Unit& u) { return kPair && !u.v ? 4 : S::kChan == 64 ? 2 : 3; };
+  auto load = [&](const Unit& u, int pg, int i) {
+    const int bits = bits_of(u);
+    const int row = (me >> bits) + i * (32 * kPfConverters >> bits), j = first_of(u) + row;
+    const int at = __shfl_sync(0xffffffffu, pg, row >> 4);
+    const int chan = 16 * (me & ((1 << bits) - 1)) +
+                     (kPair ? (u.v ? rank * S::kChan : 0) : u.half * S::kChan);
+    if (at < 0 || j >= u.len) return make_uint4(0, 0, 0, 0);
+    return __ldg(reinterpret_cast<const uint4*>((u.v ? a.V8 : a.K8) + (int64_t)at * a.s_page +
+                                                (int64_t)(j & mask) * a.s_slot +
+                                                (int64_t)u.h * a.s_head + chan));
+  };
+  int stage = 0;
+  uint32_t phase = 0;
+  uint4 x[kPieces];
+  Unit u{}, then{};
+  int pg = -1, then_pg = -1;
+  bool ok = next(u), more = false, bad = false;
+  float scale = 0.f;
+  uint32_t counts = 0;
+  if (ok) {
+    pg = look_up(u);
+    scale = scale_of(u, pg);
+    counts = counts_of(u, pg);
 #pragma unroll
-    for (int e = 0; e < kPer; ++e)
-      v[e] = pg < 0 ? -INFINITY : j + e < it.len ? at[e] : 0.f;
+    for (int i = 0; i < kPieces; ++i) x[i] = load(u, pg, i);
+    more = next(then);
+    if (more) then_pg = look_up(then);
   }
-};
+#pragma unroll 1
+  while (ok) {
+    // the unit after the next: its pages; the next one's codes are asked for below
+    Unit third{};
+    const bool third_ok = more && next(third);
+    const int third_pg = third_ok ? look_up(third) : -1;
+    const float then_scale = more ? scale_of(then, then_pg) : 0.f;
+    const uint32_t then_counts = more ? counts_of(then, then_pg) : 0;
+    if (!pf_wait(&empty[stage], phase ^ 1, a.err, abort_flag, 610)) {
+      bad = true;
+      break;
+    }
+    uint8_t* const slot = smem + S::kRing + stage * S::kStageBytes;
+    const int bits = bits_of(u), row_bits = kPair && !u.v ? 6 : 7;
+    const int piece = me & ((1 << bits) - 1);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int row = (me >> bits) + i * (32 * kPfConverters >> bits);
+      float s = __shfl_sync(0xffffffffu, scale, row >> 4);
+      if (!((__shfl_sync(0xffffffffu, counts, row >> 2) >> (row & 3)) & 1)) {
+        s = 0.f;  // (a block that is masked whole may have any scale)
+        x[i] = make_uint4(0, 0, 0, 0);
+      }
+      const uint64_t s2 = pack2(s, s);
+      uint32_t w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t c = e < 2 ? x[i].x : e < 4 ? x[i].y : e < 6 ? x[i].z : x[i].w;
+        const uint32_t y = e & 1 ? f16_of_upper(c) : f16_of_lower(c);
+        const float2 z = __half22float2(*reinterpret_cast<const __half2*>(&y));
+        float z0, z1;
+        unpack2(mul2(pack2(z.x, z.y), s2), z0, z1);
+        w[e] = bf16x2_bits(__floats2bfloat162_rn(z0, z1));
+      }
+      if (more) x[i] = load(then, then_pg, i);
+      // (the second four of eight lanes begin with their second half: no bank twice)
+      uint8_t* const at = slot + (((piece >> 2) << row_bits) + row) * 128;
+      const int unit = 2 * (piece & 3), flip = (piece >> 2) & 1;
+      const uint4 lo = make_uint4(w[0], w[1], w[2], w[3]), hi = make_uint4(w[4], w[5], w[6], w[7]);
+      *reinterpret_cast<uint4*>(at + (((unit + flip) ^ (row & 7)) << 4)) = flip ? hi : lo;
+      *reinterpret_cast<uint4*>(at + (((unit + 1 - flip) ^ (row & 7)) << 4)) = flip ? lo : hi;
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      if constexpr (kPair)
+        mbar_arrive_cluster(cluster_map(smem_u32(&full[stage]), 0));
+      else
+        mbar_arrive(&full[stage]);
+    }
+    if (++stage == kStages) {
+      stage = 0;
+      phase ^= 1;
+    }
+    u = then;
+    then = third;
+    pg = then_pg;
+    then_pg = third_pg;
+    scale = then_scale;
+    counts = then_counts;
+    ok = more;
+    more = third_ok;
+  }
+  // The last arrivals of the issuer's commits, before the CTA leaves.
+  for (int i = 0; me == 0 && !bad && i < kStages && !*abort_flag; ++i) {
+    if (!mbar_wait(&empty[stage], phase ^ 1)) {
+      dev_set_error(a.err, DEV_WAIT_TIMEOUT, 612);
+      *abort_flag = 1;
+    }
+    if (++stage == kStages) {
+      stage = 0;
+      phase ^= 1;
+    }
+  }
+}
 
-template <int D, bool kBias, bool kPair>
-__global__ void __launch_bounds__(kPfThreads, 1)
+template <int D, bool kBias, bool kPair, bool kQuant>
+__global__ void __launch_bounds__(PfRoles<kQuant>::kThreads, 1)
     paged_prefill_kernel(const __grid_constant__ CUtensorMap tm_q,
                          const __grid_constant__ CUtensorMap tm_k,
                          const __grid_constant__ CUtensorMap tm_v,
                          const __grid_constant__ PrefillParams f) {
   using S = PfShape<D, kBias, kPair>;
+  using R = PfRoles<kQuant>;
   constexpr int kTiles = S::kTiles, kStages = S::kStages, kHalves = S::kHalves;
   // All of it: no byte is left beside five stages of 256 channels, so the base has to be aligned as
   // it is.
@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(&full[s], kSides);
+      mbar_init(&full[s], kQuant ? kPfConverters * kSides : kSides);
       mbar_init(&empty[s], 1);
       mbar_init(&landed[s], 1);
     }
@@ -410,8 +410,10 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     *abort_flag = 0;
     fence_mbar_init();
     tma_prefetch_desc(&tm_q);
-    tma_prefetch_desc(&tm_k);
-    tma_prefetch_desc(&tm_v);
+    if constexpr (!kQuant) {
+      tma_prefetch_desc(&tm_k);
+      tma_prefetch_desc(&tm_v);
+    }
   }
   if (warp == 1) {
     if constexpr (kPair) {
@@ -422,59 +424,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       tmem_relinquish();
     }
   }
-  {  // equal ranges of the cost of all items: a thread adds up some sequences, or a share of one's
-    const int per = (a.B + kPfThreads - 1) / kPfThreads, shares = max(1, kPfThreads / a.B);
-    const int share = threadIdx.x % shares;
-    const int sb0 = min(a.B, (int)threadIdx.x / shares * per), sb1 = min(a.B, sb0 + per);
-    auto first_item = [&](int nq, int x) { return (int)((int64_t)nq * x / shares); };
-    int64_t mine = 0;
-    for (int b = sb0; b < sb1; ++b) {
-      const Seq s = paged_seq(a, b);
-      const int nq = pf_tiles(s, tokens);
-      mine += pf_cost(s, tokens, first_item(nq, share), first_item(nq, share + 1)) * a.H;
-    }
-    int64_t before = mine, total = 0;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t x = __shfl_up_sync(0xffffffffu, before, o);
-      if (lane >= o) before += x;
-    }
-    if (lane == 31) warp_cost[warp] = before;
-    if (threadIdx.x == 0) start.left = 0;
-    __syncthreads();
-    for (int w = 0; w < kPfThreads / 32; ++w) {
-      if (w < warp) before += warp_cost[w];
-      total += warp_cost[w];
-    }
-    before -= mine;
-    // no range is shorter than an item's beginning and a tile
-    const int64_t most = kPair ? gridDim.x / 2 : gridDim.x;
-    const int nct = (int)max((int64_t)1, min(most, total / (kPfItemCost + 1)));
-    const int64_t u0 = cta < nct ? total * cta / nct : total;
-    if (u0 >= before && u0 < before + mine) {
-      PfStart p;
-      p.total = total;
-      p.left = total * (cta + 1) / nct - u0;
-      p.nct = nct;
-      for (p.b = sb0;; ++p.b) {
-        const Seq s = paged_seq(a, p.b);
-        const int nq = first_item(pf_tiles(s, tokens), share + 1);
-        for (p.qt = first_item(pf_tiles(s, tokens), share); p.qt < nq; ++p.qt) {
-          const int cost = pf_slots(s, tokens, p.qt) + kPfItemCost;
-          if (u0 < before + (int64_t)cost * a.H) {
-            p.h = (int)((u0 - before) / cost);
-            p.base = before + (int64_t)cost * p.h;
-            p.off = (int)(u0 - p.base);
-            break;
-          }
-          before += (int64_t)cost * a.H;
-        }
-        if (p.qt < nq) break;
-      }
-      start = p;
-      if (p.off > 0 && rank == 0) f.split[cta].first = (int)(((p.base + 1) * nct - 1) / total);
-    }
-  }
+  // no range is shorter than an item's beginning and a tile
+  pf_plan<R::kThreads>(a, tokens, cta, kPair ? gridDim.x / 2 : gridDim.x, start, warp_cost,
+                      rank == 0 ? &f.split[cta] : nullptr);
   tc_fence_before();
   __syncthreads();
   if constexpr (kPair) {  // the other's barriers
@@ -491,9 +443,92 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       mbar_arrive(bar);
   };
 
-  if (warp == 0 || warp >= 10) {
+  // Item n_items as the others read it, and its q, when the one of that record has been read (by a
+  // whole warp; false at a time-out).
+  auto show = [&](int n_items, const PfItem& it) {
+    if (n_items > 0 && !pf_wait(qfree, (n_items - 1) & 1, a.err, abort_flag, 611)) return false;
+    if (n_items > 1 &&
+        !pf_wait(&seen[n_items & 1], ((n_items >> 1) - 1) & 1, a.err, abort_flag, 615))
+      return false;
+    if (lane == 0) {
+      shown[n_items & 1] = it;
+      if (it.part == 2 && rank == 0) {
+        PfSplit& sp = f.split[cta];
+        sp.last = it.last;
+        sp.token0 = it.token0;
+        sp.tokens = it.tokens;
+        sp.h = it.h;
+      }
+      const uint32_t box = (uint32_t)f.tile_tokens * g * 128;
+      mbar_arrive_expect_tx(&qfull[n_items & 1], box * kTiles * (D / 64));
+      for (int t = 0; t < kTiles; ++t)
+        for (int c = 0; c < D / 64; ++c)
+          tma_load_3d(smem + (t * (D / 64) + c) * S::kChunkBytes, &tm_q, &qfull[n_items & 1],
+                      c * 64, it.h * g, it.token0 + (t + rank) * f.tile_tokens);
+    }
+    return true;
+  };
+  // No more items behind n_items of them: when the last one's q and records have been read.
+  auto end_items = [&](int n_items) {
+    if (n_items > 0 && !*abort_flag && !mbar_wait(qfree, (n_items - 1) & 1)) {
+      dev_set_error(a.err, DEV_WAIT_TIMEOUT, 613);
+      *abort_flag = 1;
+    }
+    if (n_items > 1 && !*abort_flag &&
+        !mbar_wait(&seen[n_items & 1], ((n_items >> 1) - 1) & 1)) {
+      dev_set_error(a.err, DEV_WAIT_TIMEOUT, 616);
+      *abort_flag = 1;
+    }
+    if (!*abort_flag) {
+      shown[n_items & 1].k0 = shown[n_items & 1].k1 = 0;
+      mbar_arrive(&qfull[n_items & 1]);
+    }
+  };
+  // Rows that see nothing, by a warp.
+  auto zero_item = [&](const PfItem& it) {
+    for (int x = lane; x < it.tokens * g * (D / 8); x += 32) {
+      const int t = x / (g * (D / 8));
+      reinterpret_cast<uint4*>(f.q.out + ((int64_t)(it.token0 + t) * f.q.Hq + it.h * g) *
+                                             D)[x % (g * (D / 8))] = make_uint4(0, 0, 0, 0);
+    }
+  };
+  // K tiles that are loaded before the first one of V, in the order in which the issuer takes them
+  constexpr int kAhead = kTiles == 2 ? 1 : 2;
+  if constexpr (kQuant) {
+    if (warp >= R::kSoftmax && warp < R::kFirst)
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(256 - S::kConvertRegs));
+    else
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kConvertRegs));
+  }
+
+  if (kQuant && warp == 0) {
+    // ------------------------------------------------------------ items and their q
+    int n_items = 0;
+    bool bad = false, q_armed = false;
+    PfWalk walk(a, tokens, start);
+    PfItem it;
+    while (!bad && !warp_flag(abort_flag) && walk.next(it)) {
+      if (it.k0 == it.k1) continue;
+      if (!show(n_items, it)) {
+        bad = true;
+        break;
+      }
+      q_armed = true;
+      ++n_items;
+    }
+    if (lane == 0) {
+      if (!bad) end_items(n_items);
+      if ((bad || *abort_flag) && q_armed)
+        (void)mbar_wait(&qfull[(n_items - 1) & 1], ((n_items - 1) >> 1) & 1);
+    }
+  } else if (kQuant && warp >= R::kFirst) {
+    // ------------------------------------------------------------ codes to bf16
+    if constexpr (kQuant)
+      pf_convert<D, kBias, kPair>(f, tokens, start, smem, full, empty, abort_flag, rank,
+                                  zero_item);
+  } else if (!kQuant && (warp == 0 || warp >= R::kFirst)) {
     // ------------------------------------------------------------ TMA producers
-    const int me = warp == 0 ? 0 : warp - 9;  // 0 also loads q, arms the barriers and zeroes rows
+    const int me = warp == 0 ? 0 : warp - R::kFirst + 1;  // 0 also loads q, arms the barriers and zeroes rows
     int stage = 0, n_items = 0;
     uint32_t phase = 0;
     uint32_t armed = 0, armed_par = 0;  // stages whose copies were asked for, and their phases
@@ -583,36 +618,15 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     PfItem it;
     while (!bad && !warp_flag(abort_flag) && walk.next(it)) {
       if (it.k0 == it.k1) {  // its rows see nothing
-        if (me == 1 && rank == 0)
-          for (int x = lane; x < it.tokens * g * (D / 8); x += 32) {
-            const int t = x / (g * (D / 8));
-            reinterpret_cast<uint4*>(f.q.out + ((int64_t)(it.token0 + t) * f.q.Hq + it.h * g) *
-                                                   D)[x % (g * (D / 8))] = make_uint4(0, 0, 0, 0);
-          }
+        if (me == 1 && rank == 0) zero_item(it);
         continue;
       }
-      if (me == 0 && n_items > 0 && !wait(qfree, (n_items - 1) & 1, 611)) break;
-      if (me == 0 && n_items > 1 && !wait(&seen[n_items & 1], ((n_items >> 1) - 1) & 1, 615)) break;
-      if (me == 0 && lane == 0) {
-        shown[n_items & 1] = it;
-        if (it.part == 2 && rank == 0) {
-          PfSplit& sp = f.split[cta];
-          sp.last = it.last;
-          sp.token0 = it.token0;
-          sp.tokens = it.tokens;
-          sp.h = it.h;
-        }
-        const uint32_t box = (uint32_t)f.tile_tokens * g * 128;
-        mbar_arrive_expect_tx(&qfull[n_items & 1], box * kTiles * (D / 64));
-        for (int t = 0; t < kTiles; ++t)
-          for (int c = 0; c < D / 64; ++c)
-            tma_load_3d(smem + (t * (D / 64) + c) * S::kChunkBytes, &tm_q, &qfull[n_items & 1],
-                        c * 64, it.h * g, it.token0 + (t + rank) * f.tile_tokens);
+      if (me == 0 && !show(n_items, it)) {
+        bad = true;
+        break;
       }
       q_armed = true;
       ++n_items;
-      // in the order in which the issuer takes them: K up to kAhead tiles before V
-      constexpr int kAhead = kTiles == 2 ? 1 : 2;
       if constexpr (kBias) beta.load(a, it, it.k0 * kPfKeys, lane);
 #pragma unroll 1
       for (int kt = it.k0 - kAhead; kt < it.k1 && !bad; ++kt) {
@@ -638,19 +652,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
           phase ^= 1;
         }
       }
-      if (!bad && !*abort_flag && n_items > 0 && !mbar_wait(qfree, (n_items - 1) & 1)) {
-        dev_set_error(a.err, DEV_WAIT_TIMEOUT, 613);
-        *abort_flag = 1;
-      }
-      if (!bad && !*abort_flag && n_items > 1 &&
-          !mbar_wait(&seen[n_items & 1], ((n_items >> 1) - 1) & 1)) {
-        dev_set_error(a.err, DEV_WAIT_TIMEOUT, 616);
-        *abort_flag = 1;
-      }
-      if (!*abort_flag) {  // no more items
-        shown[n_items & 1].k0 = shown[n_items & 1].k1 = 0;
-        mbar_arrive(&qfull[n_items & 1]);
-      }
+      end_items(n_items);
     }
     // (The odd CTA's copies count on the even CTA's barriers: its own run out of time here, in
     // which the copies land, as do the even CTA's where one of the two had asked for no more.)
@@ -831,10 +833,10 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       if (shown[n & 1].k1 <= shown[n & 1].k0) break;
       mbar_arrive_cluster(cluster_map(smem_u32(qpeer), 0));
     }
-  } else if (warp >= 2) {
+  } else if (warp >= R::kSoftmax) {
     // ------------------------------------------------------------ softmax and output
     constexpr int kOCols = S::kOCols;
-    const int sw = warp - 2;
+    const int sw = warp - R::kSoftmax;
     const int quarter = warp & 3;  // TMEM lanes [32 quarter, + 32)
     const int wg = sw >> 2;        // its buffer of S: its tile, or every other tile of slots
     const int row = quarter * 32 + lane;
@@ -1189,42 +1191,14 @@ __global__ void __launch_bounds__(256)
   }
 }
 
-// dims {channels, slots, KV-heads, pages}; boxes of 64 channels of the slots of a page, at most
-// `rows` of them
-bool pool_tmap(CUtensorMap* m, const PagedArgs& a, const void* ptr, int rows) {
-  auto enc = tensor_map_encoder();
-  if (enc == nullptr) return false;
-  const cuuint64_t page = (cuuint64_t)1 << a.page_shift;
-  cuuint64_t dims[4] = {(cuuint64_t)a.d, page, (cuuint64_t)a.H, (cuuint64_t)a.n_pages};
-  cuuint64_t strides[3] = {(cuuint64_t)a.s_slot * 2, (cuuint64_t)a.s_head * 2,
-                           (cuuint64_t)a.s_page * 2};
-  cuuint32_t box[4] = {64, (cuuint32_t)std::min<cuuint64_t>(page, rows), 1, 1};
-  cuuint32_t estr[4] = {1, 1, 1, 1};
-  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box,
-             estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-             CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-bool query_tmap(CUtensorMap* m, const PagedArgs& a, const PagedQuery& q, int tokens) {
-  auto enc = tensor_map_encoder();
-  if (enc == nullptr) return false;
-  cuuint64_t dims[3] = {(cuuint64_t)a.d, (cuuint64_t)q.Hq, (cuuint64_t)a.n};
-  cuuint64_t strides[2] = {(cuuint64_t)a.d * 2, (cuuint64_t)q.s_q * 2};
-  cuuint32_t box[3] = {64, (cuuint32_t)(q.Hq / a.H), (cuuint32_t)tokens};
-  cuuint32_t estr[3] = {1, 1, 1};
-  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16*>(q.q), dims,
-             strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-             CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-template <int D, bool kBias, bool kPair>
+template <int D, bool kBias, bool kPair, bool kQuant>
 cudaError_t launch_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
                            const KernelTable& dev, cudaStream_t s) {
   using S = PfShape<D, kBias, kPair>;
   constexpr int kCluster = kPair ? 2 : 1;
-  using Id = KernelId<paged_prefill_kernel<D, kBias, kPair>, kPfThreads, S::kBytes, kCluster>;
+  constexpr int threads = PfRoles<kQuant>::kThreads;
+  constexpr auto kernel = paged_prefill_kernel<D, kBias, kPair, kQuant>;
+  using Id = KernelId<kernel, threads, S::kBytes, kCluster>;
   if (dev.of<Id>().status != cudaSuccess) return dev.of<Id>().status;
   constexpr int rows = 128 * S::kTiles * kCluster;
   const int ranges = kPair ? dev.persistent_clusters<Id>(2) : dev.num_sms;
@@ -1236,8 +1210,9 @@ cudaError_t launch_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
   f.part_ml = reinterpret_cast<float2*>(f.part_o + (int64_t)2 * ranges * rows * (D / 4));
   f.split = reinterpret_cast<PfSplit*>(f.part_ml + (int64_t)2 * ranges * rows);
   CUtensorMap tq, tk, tv;
-  if (!query_tmap(&tq, a, q, f.tile_tokens) || !pool_tmap(&tk, a, a.K, S::kKRows) ||
-      !pool_tmap(&tv, a, a.V, kPfKeys))
+  if (!query_tmap(&tq, a, q, f.tile_tokens)) return cudaErrorInvalidValue;
+  tk = tv = tq;  // (not read)
+  if (!kQuant && (!pool_tmap(&tk, a, a.K, S::kKRows) || !pool_tmap(&tv, a, a.V, kPfKeys)))
     return cudaErrorInvalidValue;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
@@ -1245,13 +1220,12 @@ cudaError_t launch_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(kCluster * ranges);
-  cfg.blockDim = dim3(kPfThreads);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = S::kBytes;
   cfg.stream = s;
   cfg.attrs = &attr;
   cfg.numAttrs = kPair ? 1 : 0;
-  const cudaError_t e =
-      cudaLaunchKernelEx(&cfg, paged_prefill_kernel<D, kBias, kPair>, tq, tk, tv, f);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, tq, tk, tv, f);
   if (e != cudaSuccess) return e;
   return launch_chained(paged_join_kernel<D>, dim3(ranges, rows / 32), dim3(256), 0, s, 1, f, rows,
                         (kBias ? 1.f : q.scale) * kLog2e);
@@ -1272,7 +1246,11 @@ bool paged_prefill_serves(const PagedArgs& a, int Hq) {
   // average and takes 1,385 us, with 770 it is above and takes 197; beside 255 idle places 1,184
   // us, and 111 for 1,100 new tokens, which are above. A caller who knows the counts does better
   // with two calls: the prompts in one (86 us alone), the single tokens in the other.
-  return Hq / a.H <= 128 && paged_mean_rows(a, Hq) > (a.d == 256 ? 8 : 16);
+  const int few = a.d == 256 ? 8 : 16;
+  // Single tokens over a pool in 8 bits stay with the few rows' kernel, whose weights are exact to
+  // 2^-21, while it reads the pool no more than twice.
+  if (a.K8 != nullptr && a.cu_new == nullptr && Hq / a.H <= 2 * few) return false;
+  return Hq / a.H <= 128 && paged_mean_rows(a, Hq) > few;
 }
 
 int64_t paged_prefill_cost(int count, int len, int tokens, int q0, int q1) {
@@ -1294,22 +1272,18 @@ cudaError_t launch_paged_prefill(const PagedArgs& a, const PagedQuery& q, void* 
   // 2,300 tokens, 8 KV-heads with 2 query heads each, pages of 16: 172 us against 243. Where the
   // second tile is almost empty (65 tokens of 2 heads over 2,000 slots, 4 KV-heads, 16 sequences):
   // 51 us against 62; 4 sequences of 100 tokens 31 against 33, of 150 without a past 21 and 21.
-  const bool bias = a.beta != nullptr, pair = paged_mean_rows(a, q.Hq) > 128;
-  switch (a.d) {
-    case 64:
-      return bias ? launch_prefill<64, true, false>(a, q, ws, dev, s)
-                  : launch_prefill<64, false, false>(a, q, ws, dev, s);
-    case 128:
-      return bias ? launch_prefill<128, true, false>(a, q, ws, dev, s)
-                  : launch_prefill<128, false, false>(a, q, ws, dev, s);
-    case 256:
-      if (pair)
-        return bias ? launch_prefill<256, true, true>(a, q, ws, dev, s)
-                    : launch_prefill<256, false, true>(a, q, ws, dev, s);
-      return bias ? launch_prefill<256, true, false>(a, q, ws, dev, s)
-                  : launch_prefill<256, false, false>(a, q, ws, dev, s);
-  }
-  return cudaErrorInvalidValue;
+  const bool pair = paged_mean_rows(a, q.Hq) > 128;
+  auto run = [&](auto bias, auto quant) {
+    constexpr bool kBias = decltype(bias)::value, kQuant = decltype(quant)::value;
+    return a.d == 64    ? launch_prefill<64, kBias, false, kQuant>(a, q, ws, dev, s)
+           : a.d == 128 ? launch_prefill<128, kBias, false, kQuant>(a, q, ws, dev, s)
+           : pair       ? launch_prefill<256, kBias, true, kQuant>(a, q, ws, dev, s)
+                        : launch_prefill<256, kBias, false, kQuant>(a, q, ws, dev, s);
+  };
+  const std::true_type yes;
+  const std::false_type no;
+  if (a.K8 != nullptr) return a.beta != nullptr ? run(yes, yes) : run(no, yes);
+  return a.beta != nullptr ? run(yes, no) : run(no, no);
 }
 
 }  // namespace still

@@ -86,19 +86,6 @@ STILL_DEV void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uin
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// The lower and the upper two e4m3 codes of a word as fp16 pairs (exact).
-STILL_DEV uint32_t f16_of_lower(uint32_t x) {
-  uint32_t r;
-  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n}\n"
-      : "=r"(r) : "r"(x));
-  return r;
-}
-STILL_DEV uint32_t f16_of_upper(uint32_t x) {
-  uint32_t r;
-  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n}\n"
-      : "=r"(r) : "r"(x));
-  return r;
-}
 STILL_DEV uint32_t f16x2_bits(__half2 x) { return *reinterpret_cast<uint32_t*>(&x); }
 
 // NB: blocks of 8 rows of a set.

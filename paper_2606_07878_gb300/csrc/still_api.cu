@@ -1902,8 +1902,11 @@ still_status paged_attend_quant(still_ctx* ctx, const still_paged_cache_quant* c
   CK(cudaSetDevice(ctx->device));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   TRY(ensure_paged_ws(ctx));
-  KLAUNCH(STILL_K_PAGED_ATTEND,
-          launch_paged_rows_quant(a, p, ctx->paged_ws, ctx->kernels.num_sms, s));
+  if (paged_prefill_serves(a, Hq))
+    KLAUNCH(STILL_K_PAGED_ATTEND, launch_paged_prefill(a, p, ctx->paged_ws, ctx->kernels, s));
+  else
+    KLAUNCH(STILL_K_PAGED_ATTEND,
+            launch_paged_rows_quant(a, p, ctx->paged_ws, ctx->kernels.num_sms, s));
   ctx->prof.launches[STILL_K_PAGED_ATTEND] += 1;  // the join
   return STILL_OK;
 }
