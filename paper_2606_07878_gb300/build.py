@@ -15,7 +15,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libstill.so")
 SOURCES = ["still_api.cu", "kernels.cu", "ca_pair.cu", "paged.cu", "paged_prefill.cu",
-           "paged_quant.cu", "paged_weigh.cu", "paged_evict.cu"]
+           "paged_quant.cu", "paged_weigh.cu", "paged_weigh_tc.cu",
+           "paged_evict.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
          "-I" + os.path.join(os.path.dirname(HERE), "include")]

@@ -89,13 +89,18 @@ cudaError_t launch_paged_rows_quant(const PagedArgs& a, const PagedQuery& q, voi
                                     cudaStream_t s);
 
 // Attention weights added up slot by slot (paged_weigh.cu), weight as PagedArgs::beta: decay times
-// what was there (0 for this call's own slots) plus what this call's rows give. Decode: three
-// launches, with the attention; else two or three, from keys alone.
+// what was there (0 for this call's own slots) plus what this call's rows give. Three launches, with
+// the attention (decode) or from keys alone.
 size_t paged_rows_weigh_workspace(int num_sms);
 cudaError_t launch_paged_decode_weigh(const PagedArgs& a, const PagedQuery& q, float* weight,
                                       float decay, void* ws, int num_sms, cudaStream_t s);
 cudaError_t launch_paged_weigh(const PagedArgs& a, const PagedQuery& q, float* weight, float decay,
                                void* ws, int num_sms, cudaStream_t s);
+// The same of many rows, on the tensor cores (paged_weigh_tc.cu): four launches.
+bool paged_weigh_tc_serves(const PagedArgs& a, int Hq);
+size_t paged_weigh_tc_workspace(int num_sms);
+cudaError_t launch_paged_weigh_tc(const PagedArgs& a, const PagedQuery& q, float* weight,
+                                  float decay, void* ws, const KernelTable& dev, cudaStream_t s);
 
 // Of every sequence and KV-head the `keep` slots that count, into pages of `to` (paged_evict.cu).
 struct PagedEvict {

@@ -156,7 +156,7 @@ STILL_DEV void pf_convert(const PrefillParams& f, int tokens, const PfStart& sta
     int half;
     bool v;
   };
-  PfWalk walk(a, tokens, start);
+  PfWalk walk(a, PfRowItems{tokens}, start);
   PfItem it;
   bool have = false;
   int kt = 0, sub = 0;
@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(PfRoles<kQuant>::kThreads, 1)
     }
   }
   // no range is shorter than an item's beginning and a tile
-  pf_plan<R::kThreads>(a, tokens, cta, kPair ? gridDim.x / 2 : gridDim.x, start, warp_cost,
+  pf_plan<R::kThreads>(a, PfRowItems{tokens}, cta, kPair ? gridDim.x / 2 : gridDim.x, start, warp_cost,
                       rank == 0 ? &f.split[cta] : nullptr);
   tc_fence_before();
   __syncthreads();
@@ -505,7 +505,7 @@ __global__ void __launch_bounds__(PfRoles<kQuant>::kThreads, 1)
     // ------------------------------------------------------------ items and their q
     int n_items = 0;
     bool bad = false, q_armed = false;
-    PfWalk walk(a, tokens, start);
+    PfWalk walk(a, PfRowItems{tokens}, start);
     PfItem it;
     while (!bad && !warp_flag(abort_flag) && walk.next(it)) {
       if (it.k0 == it.k1) continue;
@@ -614,7 +614,7 @@ __global__ void __launch_bounds__(PfRoles<kQuant>::kThreads, 1)
 #pragma unroll 1
       for (int half = 0; half < kHalves && !bad; ++half) load(false, it, kt, half, kBias ? m : 0u);
     };
-    PfWalk walk(a, tokens, start);
+    PfWalk walk(a, PfRowItems{tokens}, start);
     PfItem it;
     while (!bad && !warp_flag(abort_flag) && walk.next(it)) {
       if (it.k0 == it.k1) {  // its rows see nothing
@@ -1254,7 +1254,7 @@ bool paged_prefill_serves(const PagedArgs& a, int Hq) {
 }
 
 int64_t paged_prefill_cost(int count, int len, int tokens, int q0, int q1) {
-  return pf_cost(Seq{0, count, len}, tokens, q0, q1);
+  return pf_cost(PfRowItems{tokens}, Seq{0, count, len}, q0, q1);
 }
 
 size_t paged_prefill_workspace(int num_sms) {

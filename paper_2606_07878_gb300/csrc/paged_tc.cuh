@@ -126,46 +126,62 @@ STILL_DEV bool pf_wait(uint64_t* bar, uint32_t parity, int* err, volatile int* a
   return ok;
 }
 
-STILL_DEV int pf_tiles(const Seq& s, int tokens) { return (s.count + tokens - 1) / tokens; }
+__host__ __device__ __forceinline__ int pf_tiles(const Seq& s, int tokens) {
+  return (s.count + tokens - 1) / tokens;
+}
 // Tiles of slots that item qt of a sequence sees.
 __host__ __device__ __forceinline__ int pf_slots(const Seq& s, int tokens, int qt) {
   const int upto = (qt + 1) * tokens, most = s.len - s.count + (upto < s.count ? upto : s.count);
   return most > 0 ? (most + kPfKeys - 1) / kPfKeys : 0;
 }
-// Cost of items [q0, q1) of a sequence and KV-head: a million tokens pass 32 bits.
-__host__ __device__ __forceinline__ int64_t pf_cost(const Seq& s, int tokens, int q0, int q1) {
+// Items of `tokens` tokens each and the tiles of slots that they see: how many of a sequence, the
+// tiles of one, what is shown of it.
+struct PfRowItems {
+  using Item = PfItem;
+  int tokens;
+  __host__ __device__ int items(const Seq& s) const { return pf_tiles(s, tokens); }
+  __host__ __device__ int tiles(const Seq& s, int x) const { return pf_slots(s, tokens, x); }
+  STILL_DEV void fill(PfItem& it, const Seq& s, int x) const {
+    it.len = s.len;
+    it.token0 = s.first + x * tokens;
+    it.tokens = min(tokens, s.count - x * tokens);
+    it.see = s.len - s.count + x * tokens + 1;
+  }
+};
+
+// Cost of items [x0, x1) of a sequence and KV-head: a million tokens pass 32 bits.
+template <class G>
+__host__ __device__ __forceinline__ int64_t pf_cost(const G& items, const Seq& s, int x0, int x1) {
   int64_t sum = 0;
-  for (int qt = q0; qt < q1; ++qt) sum += pf_slots(s, tokens, qt) + kPfItemCost;
+  for (int x = x0; x < x1; ++x) sum += items.tiles(s, x) + kPfItemCost;
   return sum;
 }
 
-// The items of a CTA's range, in order: sequences, tokens, KV-heads. An item's cost is its tiles of
-// slots, then kPfItemCost for its beginning and end.
+// The items of a CTA's range, in order: sequences, their items, KV-heads. An item's cost is its
+// tiles, then kPfItemCost for its beginning and end.
+template <class G>
 struct PfWalk {
   const PagedArgs& a;
-  int tokens;  // of an item
+  G items;
   int64_t base, left, total;
   int b, qt, h, off, nq, nct;
   Seq s;
-  STILL_DEV PfWalk(const PagedArgs& args, int item_tokens, const PfStart& p)
-      : a(args), tokens(item_tokens), base(p.base), left(p.left), total(p.total), b(p.b), qt(p.qt),
+  STILL_DEV PfWalk(const PagedArgs& args, const G& g, const PfStart& p)
+      : a(args), items(g), base(p.base), left(p.left), total(p.total), b(p.b), qt(p.qt),
         h(p.h), off(p.off), nct(p.nct) {
     if (left > 0) {
       s = paged_seq<false>(a, b);
-      nq = pf_tiles(s, tokens);
+      nq = items.items(s);
     }
   }
-  STILL_DEV bool next(PfItem& it) {
+  STILL_DEV bool next(typename G::Item& it) {
     while (left > 0) {
-      const int kt = pf_slots(s, tokens, qt), cost = kt + kPfItemCost;
+      const int kt = items.tiles(s, qt), cost = kt + kPfItemCost;
       const int end = (int)min((int64_t)cost, off + left);
       const bool begins = off == 0;
       it.b = b;
       it.h = h;
-      it.len = s.len;
-      it.token0 = s.first + qt * tokens;
-      it.tokens = min(tokens, s.count - qt * tokens);
-      it.see = s.len - s.count + qt * tokens + 1;
+      items.fill(it, s, qt);
       it.k0 = min(off, kt);
       it.k1 = min(end, kt);
       it.part = begins && end >= kt ? 0 : begins ? 2 : 1;
@@ -180,7 +196,7 @@ struct PfWalk {
             qt = nq = 0;
             while (left > 0 && nq == 0) {
               s = paged_seq<false>(a, ++b);
-              nq = pf_tiles(s, tokens);
+              nq = items.items(s);
             }
           }
         }
@@ -194,8 +210,8 @@ struct PfWalk {
 // Equal ranges of the cost of all items for `most` CTAs (or pairs) at most, by all threads of a block:
 // where the range of CTA `cta` begins, and in split (if any) the CTA that begins its first item. No
 // range is shorter than an item's beginning and a tile.
-template <int kThreads>
-STILL_DEV void pf_plan(const PagedArgs& a, int tokens, int cta, int64_t most, PfStart& start,
+template <int kThreads, class G>
+STILL_DEV void pf_plan(const PagedArgs& a, const G& items, int cta, int64_t most, PfStart& start,
                        int64_t* warp_cost, PfSplit* split) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // a thread adds up some sequences, or a share of one's
@@ -206,8 +222,8 @@ STILL_DEV void pf_plan(const PagedArgs& a, int tokens, int cta, int64_t most, Pf
   int64_t mine = 0;
   for (int b = sb0; b < sb1; ++b) {
     const Seq s = paged_seq(a, b);
-    const int nq = pf_tiles(s, tokens);
-    mine += pf_cost(s, tokens, first_item(nq, share), first_item(nq, share + 1)) * a.H;
+    const int nq = items.items(s);
+    mine += pf_cost(items, s, first_item(nq, share), first_item(nq, share + 1)) * a.H;
   }
   int64_t before = mine, total = 0;
 #pragma unroll
@@ -232,9 +248,9 @@ STILL_DEV void pf_plan(const PagedArgs& a, int tokens, int cta, int64_t most, Pf
     p.nct = nct;
     for (p.b = sb0;; ++p.b) {
       const Seq s = paged_seq(a, p.b);
-      const int nq = first_item(pf_tiles(s, tokens), share + 1);
-      for (p.qt = first_item(pf_tiles(s, tokens), share); p.qt < nq; ++p.qt) {
-        const int cost = pf_slots(s, tokens, p.qt) + kPfItemCost;
+      const int nq = first_item(items.items(s), share + 1);
+      for (p.qt = first_item(items.items(s), share); p.qt < nq; ++p.qt) {
+        const int cost = items.tiles(s, p.qt) + kPfItemCost;
         if (u0 < before + (int64_t)cost * a.H) {
           p.h = (int)((u0 - before) / cost);
           p.base = before + (int64_t)cost * p.h;

@@ -528,7 +528,8 @@ still_status ensure_paged_ws(still_ctx* ctx) {
   const int nsm = ctx->kernels.num_sms;
   if (cudaMalloc(&ctx->paged_ws,
                  std::max({paged_rows_workspace(nsm), paged_prefill_workspace(nsm),
-                           paged_rows_quant_workspace(nsm), paged_rows_weigh_workspace(nsm)})) !=
+                           paged_rows_quant_workspace(nsm), paged_rows_weigh_workspace(nsm),
+                           paged_weigh_tc_workspace(nsm)})) !=
       cudaSuccess) {
     cudaGetLastError();
     ctx->paged_ws = nullptr;
@@ -2047,8 +2048,14 @@ still_status still_paged_weigh(still_ctx* ctx, const still_paged_cache* cache,
   CK(cudaSetDevice(ctx->device));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   TRY(ensure_paged_ws(ctx));
-  KLAUNCH(STILL_K_PAGED_WEIGH, launch_paged_weigh(a, p, weight, decay, ctx->paged_ws,
-                                                  ctx->kernels.num_sms, s));
+  if (paged_weigh_tc_serves(a, Hq)) {
+    KLAUNCH(STILL_K_PAGED_WEIGH,
+            launch_paged_weigh_tc(a, p, weight, decay, ctx->paged_ws, ctx->kernels, s));
+    ctx->prof.launches[STILL_K_PAGED_WEIGH] += 1;
+  } else {
+    KLAUNCH(STILL_K_PAGED_WEIGH, launch_paged_weigh(a, p, weight, decay, ctx->paged_ws,
+                                                    ctx->kernels.num_sms, s));
+  }
   ctx->prof.launches[STILL_K_PAGED_WEIGH] += 2;
   return STILL_OK;
 }
