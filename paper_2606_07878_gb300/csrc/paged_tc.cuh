@@ -81,6 +81,16 @@ STILL_DEV void tma_load_4d(void* dst, const CUtensorMap* m, uint64_t* bar, int x
       "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
       : "memory");
 }
+// 32 lanes x 16 columns of 32 bits into registers; complete after tmem_wait_ld.
+STILL_DEV void tmem_ld16_issue(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
 // 32 lanes x 32 columns of 32 bits from registers; complete after tmem_wait_st.
 STILL_DEV void tmem_st32_issue(uint32_t taddr, const uint32_t* r) {
   asm volatile(

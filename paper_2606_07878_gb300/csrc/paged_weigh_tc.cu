@@ -19,9 +19,15 @@
 // logits are natural up to the subtraction, as a bias of the lowest float would be -inf in units of
 // log 2.
 //
+// A thread of the sums has a lane of both held tiles and half of the columns: what belongs to a column
+// (biases; m and l) is read from shared memory once for two values. A broadcast of 16 bytes takes
+// the load unit as long as 32 different ones, four cycles: with a thread to a lane of one held tile
+// and m and 1 / l apart these reads were the bound, 212 us of the second pass over 6,001 tokens of 28
+// heads against 117 of the first. So m and log l are one number there, where it is small enough
+// that its rounding stays below 2^-20 of a weight.
+//
 // Roles: warp 0 TMA (a box per page and 64 channels), 1 MMA issuer and TMEM, 2 what belongs to the
-// streamed tile's columns (biases; m and 1 / l), 4 .. 11 sums, four warps per held tile. Ranges of
-// equal cost as in the prefill (paged_tc.cuh); what several CTAs share of an item goes to the
+// streamed tile's columns and to held slots, 4 .. 11 sums. Ranges of equal cost as in the prefill (paged_tc.cuh); what several CTAs share of an item goes to the
 // workspace and a second launch joins it. Every wait is bounded.
 #include <type_traits>
 
@@ -35,7 +41,12 @@ namespace {
 constexpr int kWtThreads = 384;
 constexpr int kWtHeld = 256;        // rows or slots of an item
 constexpr int kWtMost = 1024;       // a tile's sum in units of e^m that moves m
-constexpr int kWtCols = 4;          // streamed tiles whose column values are held
+// Streamed tiles whose column values are held, [kWtCols][kWtColFloats]: three of every column, a flag,
+// and of the tile that is an item's first the held slots' biases and pages.
+constexpr int kWtCols = 4;
+constexpr int kWtFlagAt = 384, kWtBiasAt = 388, kWtPageAt = kWtBiasAt + kWtHeld;
+constexpr int kWtColFloats = kWtPageAt + kWtHeld;
+constexpr float kWtFold = 32.f;     // |m + log2 l| below which they are one number
 
 // An item of either pass: `x` counts blocks of 2 tile_tokens tokens or of 256 slots.
 struct WtItem {
@@ -98,9 +109,10 @@ struct WtShape {
   static constexpr int kHeldBytes = 2 * kChunks * kChunkBytes;
   static constexpr int kStages = D == 64 ? 8 : 5;      // a chunk of a streamed tile each
   static constexpr int kRing = kHeldBufs * kHeldBytes;
-  static constexpr int kColAt = kRing + kStages * kChunkBytes;  // [kWtCols][2][128] floats
-  static constexpr int kBarAt = kColAt + kWtCols * 1024;
-  static constexpr int kPlanAt = kBarAt + (2 * kStages + 2 * kWtCols + 15) * 8 + 16;
+  static constexpr int kColAt = kRing + kStages * kChunkBytes;
+  static constexpr int kXchAt = kColAt + kWtCols * kWtColFloats * 4;  // [256] float2
+  static constexpr int kBarAt = kXchAt + kWtHeld * 8;
+  static constexpr int kPlanAt = kBarAt + (2 * kStages + 2 * kWtCols + 13) * 8 + 16;
   static constexpr int kBytes = kPlanAt + sizeof(WtPlan);
   static_assert(kBytes <= 232448, "shared memory budget");
 };
@@ -142,12 +154,14 @@ __global__ void __launch_bounds__(kWtThreads, 1)
   uint64_t* qfull = colfree + kWtCols;   // [2] item n & 1 shown and its held tiles loaded
   uint64_t* qfree = qfull + 2;           // [2] its last product complete
   uint64_t* seen = qfree + 2;            // [2] its record read by all
-  uint64_t* sfull = seen + 2;            // [2][2] S of held tile t, buffer i, complete
-  uint64_t* sfree = sfull + 4;           // [2][2] and read
-  uint64_t* drain = sfree + 4;
+  uint64_t* sfull = seen + 2;            // [2] S of both held tiles, buffer i, complete
+  uint64_t* sfree = sfull + 2;           // [2] and read
+  uint64_t* xfull = sfree + 2;           // the second half's sums of an item
+  uint64_t* xfree = xfull + 1;           // and read
+  uint64_t* drain = xfree + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((2 * kStages + 2 * kWtCols + 15) * 8 + 16 == S::kPlanAt - S::kBarAt, "barriers");
+  static_assert((2 * kStages + 2 * kWtCols + 13) * 8 + 16 == S::kPlanAt - S::kBarAt, "barriers");
 
   const PagedArgs& a = f.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -169,11 +183,11 @@ __global__ void __launch_bounds__(kWtThreads, 1)
       mbar_init(&qfull[i], 1);
       mbar_init(&qfree[i], 1);
       mbar_init(&seen[i], 10);
-    }
-    for (int i = 0; i < 4; ++i) {
       mbar_init(&sfull[i], 1);
-      mbar_init(&sfree[i], 4);
+      mbar_init(&sfree[i], 8);
     }
+    mbar_init(xfull, 4);
+    mbar_init(xfree, 4);
     mbar_init(drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
@@ -341,7 +355,7 @@ __global__ void __launch_bounds__(kWtThreads, 1)
     constexpr uint32_t idesc = idesc_f16(128, 128, 1);
     int stage = 0;
     uint32_t phase = 0;
-    uint32_t uses[2] = {0, 0};  // of the held tiles
+    uint32_t uses = 0;  // of the buffers of S
     bool bad = false, issued = false;
     auto wait = [&](uint64_t* bar, uint32_t parity, int where) {
       if (mbar_wait(bar, parity)) return true;
@@ -364,8 +378,7 @@ __global__ void __launch_bounds__(kWtThreads, 1)
           held_desc + (S::kHeldBufs == 2 ? n & 1 : 0) * (uint64_t)(S::kHeldBytes >> 4);
 #pragma unroll 1
       for (int k = 0; k < n_k && !bad; ++k) {
-        if (!wait(&sfree[uses[0] & 1], ((uses[0] >> 1) & 1) ^ 1, 652)) break;
-        if (two && !wait(&sfree[2 + (uses[1] & 1)], ((uses[1] >> 1) & 1) ^ 1, 653)) break;
+        if (!wait(&sfree[uses & 1], ((uses >> 1) & 1) ^ 1, 652)) break;
 #pragma unroll 1
         for (int c = 0; c < kChunks; ++c) {
           if (!wait(&full[stage], phase, 654)) break;
@@ -377,7 +390,7 @@ __global__ void __launch_bounds__(kWtThreads, 1)
             const uint64_t x = held + (t * kChunks + c) * kStep;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              tc_mma_f16(tmem_base + (2 * t + (uses[t] & 1)) * 128, x + 2 * e, b + 2 * e, idesc,
+              tc_mma_f16(tmem_base + (2 * t + (uses & 1)) * 128, x + 2 * e, b + 2 * e, idesc,
                          c + e > 0);
           }
           issued = true;
@@ -388,12 +401,8 @@ __global__ void __launch_bounds__(kWtThreads, 1)
           }
         }
         if (bad) break;
-        tc_commit(&sfull[uses[0] & 1]);
-        ++uses[0];
-        if (two) {
-          tc_commit(&sfull[2 + (uses[1] & 1)]);
-          ++uses[1];
-        }
+        tc_commit(&sfull[uses & 1]);
+        ++uses;
       }
       if (!bad) tc_commit(&qfree[n & 1]);
     }
@@ -413,6 +422,17 @@ __global__ void __launch_bounds__(kWtThreads, 1)
       if (lane == 0) mbar_arrive(&seen[n & 1]);
       if (it.k1 <= it.k0) break;
       if constexpr (kCols) {
+        // held slots, of which lane i has those from 8 i on: one page
+        int page = -1;
+        float beta[8];
+        if constexpr (kSecond) {
+          const int j = it.x * kWtHeld + 8 * lane;
+          if (j < it.len) page = paged_page(a, a.table + (int64_t)it.b * a.s_table, j);
+          const float* at =
+              a.beta + ((((int64_t)max(page, 0) * a.H + it.h) << a.page_shift) + (j & mask));
+#pragma unroll
+          for (int e = 0; e < 8; ++e) beta[e] = kBias && page >= 0 && j + e < it.len ? at[e] : 0.f;
+        }
         float v[4], w[4];
         auto load = [&](int k) {
           const int tile = tile_of(it, k);
@@ -423,8 +443,7 @@ __global__ void __launch_bounds__(kWtThreads, 1)
               float2 x = make_float2(0.f, 0.f);
               if (c < tile_rows && token < it.count && token >= it.count - it.len)
                 x = f.q.ml[(int64_t)(it.first + token) * f.q.Hq + it.h * g + c % g];
-              // a row that sees nothing, or none at all: e^-inf
-              v[e] = x.y == 0.f ? -INFINITY : -x.x;
+              v[e] = x.x;
               w[e] = x.y;
             }
           } else {
@@ -433,10 +452,7 @@ __global__ void __launch_bounds__(kWtThreads, 1)
             const float* at =
                 a.beta + ((((int64_t)max(pg, 0) * a.H + it.h) << a.page_shift) + (j & mask));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              v[e] = pg >= 0 && j + e < it.len ? at[e] : -INFINITY;
-              w[e] = 0.f;
-            }
+            for (int e = 0; e < 4; ++e) v[e] = pg >= 0 && j + e < it.len ? at[e] : -INFINITY;
           }
         };
         load(it.k0);
@@ -447,10 +463,37 @@ __global__ void __launch_bounds__(kWtThreads, 1)
             bad = true;
             break;
           }
-          float* const at = reinterpret_cast<float*>(smem + S::kColAt) + 256 * i;
-          *reinterpret_cast<float4*>(at + 4 * lane) = make_float4(v[0], v[1], v[2], v[3]);
-          if constexpr (kSecond)
-            *reinterpret_cast<float4*>(at + 128 + 4 * lane) = make_float4(w[0], w[1], w[2], w[3]);
+          float* const at = reinterpret_cast<float*>(smem + S::kColAt) + kWtColFloats * i;
+          float4* const at4 = reinterpret_cast<float4*>(at) + lane;
+          bool odd = false;  // the tile's general form is needed
+          if constexpr (kSecond) {
+            float by[4], sum[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              // a row that sees nothing, or none at all: e^-inf
+              const bool none = w[e] == 0.f;
+              const float log_l = kBias ? -logf(w[e]) : -log2f(w[e]);
+              by[e] = none ? -INFINITY : -v[e];
+              sum[e] = none ? -INFINITY : -(v[e] + log_l);
+              odd |= !none && !(fabsf(sum[e]) < (kBias ? kWtFold / kLog2e : kWtFold));
+            }
+            at4[0] = make_float4(by[0], by[1], by[2], by[3]);
+            at4[32] = make_float4(w[0], w[1], w[2], w[3]);
+            at4[64] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+            if (k == it.k0) {
+              float4* const b4 = reinterpret_cast<float4*>(at + kWtBiasAt + 8 * lane);
+              int4* const p4 = reinterpret_cast<int4*>(at + kWtPageAt + 8 * lane);
+              b4[0] = make_float4(beta[0], beta[1], beta[2], beta[3]);
+              b4[1] = make_float4(beta[4], beta[5], beta[6], beta[7]);
+              p4[0] = p4[1] = make_int4(page, page, page, page);
+            }
+          } else {
+            at4[0] = make_float4(v[0], v[1], v[2], v[3]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) odd |= v[e] == -INFINITY;
+          }
+          odd = __any_sync(0xffffffffu, odd);
+          if (lane == 0) at[kWtFlagAt] = odd ? 1.f : 0.f;
           if (k + 1 < it.k1) load(k + 1);
           __syncwarp();
           if (lane == 0) mbar_arrive(&colfull[i]);
@@ -459,12 +502,15 @@ __global__ void __launch_bounds__(kWtThreads, 1)
     }
   } else if (warp >= 4) {
     // ------------------------------------------------------------ sums
-    const int t = (warp - 4) >> 2, quarter = warp & 3;
-    const int row = quarter * 32 + lane;  // of the held tile
-    const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16) + 256 * t;
+    const int half = (warp - 4) >> 2, quarter = warp & 3;  // columns [64 half, + 64)
+    const int row = quarter * 32 + lane;                   // of both held tiles
+    const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16) + 64 * half;
+    float2* const xch = reinterpret_cast<float2*>(smem + S::kXchAt) + row;  // [2][128]
     const float k_log2 = f.q.scale * kLog2e;
     const float unit = kBias ? kLog2e : 1.f;  // of m, in log 2
-    uint32_t uses = 0, col_uses = 0;
+    const uint64_t sc = pack2(f.q.scale, f.q.scale);
+    const uint64_t k2 = kBias ? pack2(kLog2e, kLog2e) : pack2(k_log2, k_log2);
+    uint32_t uses = 0;  // of S, and of the columns' values
     bool bad = false;
     auto wait_all = [&](uint64_t* bar, uint32_t parity, int where) -> bool {
       if (!pf_wait(bar, parity, a.err, abort_flag, where)) bad = true;
@@ -476,190 +522,260 @@ __global__ void __launch_bounds__(kWtThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&seen[n & 1]);
       if (it.k1 <= it.k0) break;
-      const bool works = t == 0 || is_two(it);
-      // pass 1: this row's token among the sequence's; pass 2: this slot
-      const int token = (2 * it.x + t) * f.tile_tokens + row / g;
-      const int slot = it.x * kWtHeld + 128 * t + row;
       const int past = it.len - it.count;
-      const bool valid = kSecond ? slot < it.len : row < tile_rows && token < it.count;
-      const int see = valid ? max(0, past + token + 1) : INT32_MAX;         // pass 1: slots
-      const int least = kSecond ? 0 : __reduce_min_sync(0xffffffffu, see);  // that every row sees
-      float beta = 0.f;
-      int page = -1;
-      if constexpr (kSecond) {
-        if (works && valid) page = paged_page(a, a.table + (int64_t)it.b * a.s_table, slot);
-        if constexpr (kBias)
-          if (page >= 0)
-            beta = a.beta[(((int64_t)page * a.H + it.h) << a.page_shift) + (slot & mask)];
+      // pass 1: rows, the slots that they see; pass 2: slots
+      bool valid[2];
+      int see[2], page[2] = {-1, -1};
+      float beta[2] = {0.f, 0.f}, before[2] = {0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int token = (2 * it.x + t) * f.tile_tokens + row / g;
+        valid[t] = !kSecond && row < tile_rows && token < it.count;
+        see[t] = valid[t] ? max(0, past + token + 1) : INT32_MAX;
       }
-      Sum2 sum;
-      float m = -INFINITY;
+      const int least = kSecond ? 0 : __reduce_min_sync(0xffffffffu, min(see[0], see[1]));
+      const int slot0 = it.x * kWtHeld + row;  // the other one 128 behind
+      Sum2 sum[2];
+      float m[2] = {-INFINITY, -INFINITY};
 #pragma unroll 1
-      for (int k = it.k0; k < it.k1; ++k) {
+      for (int k = it.k0; k < it.k1; ++k, ++uses) {
         const int tile = tile_of(it, k);
-        const int i = col_uses % kWtCols;
-        const float* const cols = reinterpret_cast<const float*>(smem + S::kColAt) + 256 * i;
-        if constexpr (kCols)
-          if (!wait_all(&colfull[i], (col_uses / kWtCols) & 1, 672)) break;
-        if (works) {
-          if (!wait_all(&sfull[2 * t + (uses & 1)], (uses >> 1) & 1, 673)) break;
-          tc_fence_after();
-          const uint32_t s_at = lanes + (uses & 1) * 128;
-          uint32_t v[64];
-          // Columns [c, c + 64): S, with biases logits; -inf where a row does not see the slot.
-          auto read = [&](int c) {
-            tmem_ld32_issue(s_at + c, v);
-            tmem_ld32_issue(s_at + c + 32, v + 32);
-            tmem_wait_ld();
-            tmem_landed(v);
-            tmem_landed(v + 32);
-            if constexpr (kBias) {
-              const uint64_t sc = pack2(f.q.scale, f.q.scale);
-#pragma unroll
-              for (int e = 0; e < 64; e += 4) {
-                float4 b4 = make_float4(beta, beta, beta, beta);
-                if constexpr (!kSecond) b4 = *reinterpret_cast<const float4*>(cols + c + e);
-                float u[4];
-                unpack2(fma2(pack2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), sc,
-                             pack2(b4.x, b4.y)), u[0], u[1]);
-                unpack2(fma2(pack2(__uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])), sc,
-                             pack2(b4.z, b4.w)), u[2], u[3]);
-                if constexpr (!kSecond) {  // whatever a masked slot's K holds
-                  u[0] = b4.x == -INFINITY ? -INFINITY : u[0];
-                  u[1] = b4.y == -INFINITY ? -INFINITY : u[1];
-                  u[2] = b4.z == -INFINITY ? -INFINITY : u[2];
-                  u[3] = b4.w == -INFINITY ? -INFINITY : u[3];
-                }
-#pragma unroll
-                for (int x = 0; x < 4; ++x) v[e + x] = __float_as_uint(u[x]);
-              }
-            }
-            if (!kSecond && least < tile * 128 + c + 64) {
-              const int upto = see - tile * 128 - c;  // columns that this row sees
-#pragma unroll
-              for (int e = 0; e < 64; ++e) v[e] = e < upto ? v[e] : 0xff800000u;
-            }
-          };
-          // e^(s - by) of the 64 columns that v holds, two at a time
-          auto weights = [&](int e, uint64_t by2, uint64_t k2) {
-            const uint64_t x = pack2(__uint_as_float(v[e]), __uint_as_float(v[e + 1]));
-            float u0, u1;
-            unpack2(kBias ? mul2(add2(x, by2), k2) : fma2(x, k2, by2), u0, u1);
-            return pack2(ex2_ftz(u0), ex2_ftz(u1));
-          };
-          const float to_log2 = kBias ? kLog2e : k_log2;
-          const uint64_t k2 = pack2(to_log2, to_log2);
-          if constexpr (!kSecond) {
-            auto top = [&]() {  // of the tile, in units of m
-              float m0 = -INFINITY, m1 = -INFINITY;
-#pragma unroll 1
-              for (int c = 0; c < 128; c += 64) {
-                read(c);
-#pragma unroll
-                for (int e = 0; e < 64; e += 4) {
-                  m0 = max3(m0, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
-                  m1 = max3(m1, __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
-                }
-              }
-              const float x = fmaxf(m0, m1);
-              return kBias || x == -INFINITY ? x : x * k_log2;
-            };
-            auto add_up = [&]() {
-              const float by = m == -INFINITY ? 0.f : m;  // nothing seen yet: 2^-inf
-              const uint64_t by2 = pack2(-by, -by);
-              uint64_t s0 = 0ull, s1 = 0ull;
-#pragma unroll 1
-              for (int c = 0; c < 128; c += 64) {
-                read(c);
-#pragma unroll
-                for (int e = 0; e < 64; e += 4) {
-                  s0 = add2(s0, weights(e, by2, k2));
-                  s1 = add2(s1, weights(e + 2, by2, k2));
-                }
-              }
-              float x0, x1;
-              unpack2(add2(s0, s1), x0, x1);
-              return x0 + x1;
-            };
-            if (__any_sync(0xffffffffu, valid && m == -INFINITY)) {
-              const float x = top();
-              if (m == -INFINITY) m = x;
-            }
-            float x = add_up();
-            if (__any_sync(0xffffffffu, valid && !(x <= (float)kWtMost))) {
-              const float higher = fmaxf(m, top());
-              if (higher > m) {
-                const float down = ex2_ftz((m - higher) * unit);
-                sum.s *= down;
-                sum.c *= down;
-                m = higher;
-              }
-              x = add_up();
-            }
-            sum.add(x);
-          } else {
-            // columns [lo, hi) are rows that see this slot
-            const int token0 = tile * f.tile_tokens;
-            const int lo = (slot - past - token0) * g;
-            const int hi = min(f.tile_tokens, it.count - token0) * g;
-            const bool all = !__any_sync(0xffffffffu, lo > 0) && hi == tile_rows;
-            uint64_t s0 = 0ull, s1 = 0ull;
-#pragma unroll 1
-            for (int c = 0; c < 128; c += 64) {
-              read(c);
-#pragma unroll
-              for (int e = 0; e < 64; e += 4) {
-                const float4 b4 = *reinterpret_cast<const float4*>(cols + c + e);
-                const float4 w4 = *reinterpret_cast<const float4*>(cols + 128 + c + e);
-                const uint64_t p0 = weights(e, pack2(b4.x, b4.y), k2);
-                const uint64_t p1 = weights(e + 2, pack2(b4.z, b4.w), k2);
-                if (all) {
-                  s0 = fma2(p0, pack2(w4.x, w4.y), s0);
-                  s1 = fma2(p1, pack2(w4.z, w4.w), s1);
-                } else {  // (a row of NaN counts where it is seen alone)
-                  float u[4];
-                  unpack2(mul2(p0, pack2(w4.x, w4.y)), u[0], u[1]);
-                  unpack2(mul2(p1, pack2(w4.z, w4.w)), u[2], u[3]);
-#pragma unroll
-                  for (int x = 0; x < 4; ++x)
-                    u[x] = c + e + x >= lo && c + e + x < hi ? u[x] : 0.f;
-                  s0 = add2(s0, pack2(u[0], u[1]));
-                  s1 = add2(s1, pack2(u[2], u[3]));
-                }
-              }
-            }
-            float x0, x1;
-            unpack2(add2(s0, s1), x0, x1);
-            sum.add(x0 + x1);
-          }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sfree[2 * t + (uses & 1)]);
-          ++uses;
-        }
+        const int i = uses % kWtCols;
+        const float* const cols =
+            reinterpret_cast<const float*>(smem + S::kColAt) + kWtColFloats * i + 64 * half;
+        bool odd = false;
         if constexpr (kCols) {
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&colfree[i]);
-          ++col_uses;
+          if (!wait_all(&colfull[i], (uses / kWtCols) & 1, 672)) break;
+          odd = cols[kWtFlagAt - 64 * half] != 0.f;
+          if (kSecond && k == it.k0) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              beta[t] = cols[kWtBiasAt - 64 * half + 128 * t + row];
+              page[t] = __float_as_int(cols[kWtPageAt - 64 * half + 128 * t + row]);
+              const int slot = slot0 + 128 * t;
+              if (slot >= it.len) page[t] = -1;
+              if (half == 0 && it.part == 0 && f.decay != 0.f && page[t] >= 0 && slot < past)
+                before[t] = f.weight[(((int64_t)page[t] * a.H + it.h) << a.page_shift) +
+                                     (slot & mask)];
+            }
+          }
         }
+        if (!wait_all(&sfull[uses & 1], (uses >> 1) & 1, 673)) break;
+        tc_fence_after();
+        const uint32_t s_at = lanes + (uses & 1) * 128;
+        // 16 columns of both tiles
+        auto issue = [&](int c, uint32_t* v) {
+          tmem_ld16_issue(s_at + c, v);
+          tmem_ld16_issue(s_at + 256 + c, v + 16);
+        };
+        // Four columns of tile t: S, with biases logits; -inf where a row does not see the slot.
+        auto logits = [&](auto masked, const uint32_t* v, int t, int c, const float4& b4,
+                          uint64_t (&x)[2]) {
+          x[0] = pack2(__uint_as_float(v[0]), __uint_as_float(v[1]));
+          x[1] = pack2(__uint_as_float(v[2]), __uint_as_float(v[3]));
+          if constexpr (kBias) {
+            x[0] = fma2(x[0], sc, kSecond ? pack2(beta[t], beta[t]) : pack2(b4.x, b4.y));
+            x[1] = fma2(x[1], sc, kSecond ? pack2(beta[t], beta[t]) : pack2(b4.z, b4.w));
+          }
+          if constexpr (!kSecond && decltype(masked)::value) {
+            float u[4];
+            unpack2(x[0], u[0], u[1]);
+            unpack2(x[1], u[2], u[3]);
+            const int upto = see[t] - tile * 128 - 64 * half - c;
+            const float b[4] = {b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              u[e] = e < upto && !(kBias && b[e] == -INFINITY) ? u[e] : -INFINITY;
+            x[0] = pack2(u[0], u[1]);
+            x[1] = pack2(u[2], u[3]);
+          }
+        };
+        // e^(s + by), two at a time
+        auto weights = [&](uint64_t x, uint64_t by2) {
+          float u0, u1;
+          unpack2(kBias ? mul2(add2(x, by2), k2) : fma2(x, k2, by2), u0, u1);
+          return pack2(ex2_ftz(u0), ex2_ftz(u1));
+        };
+        // All 64 columns, the next 16 on their way meanwhile.
+        auto pass = [&](auto f4) {
+          uint32_t va[32], vb[32];
+          issue(0, va);
+          tmem_wait_ld();
+          tmem_landed(va);
+#pragma unroll
+          for (int c = 0; c < 64; c += 32) {
+            issue(c + 16, vb);
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) f4(c + e, va + e);
+            tmem_wait_ld();
+            tmem_landed(vb);
+            if (c == 0) issue(32, va);
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) f4(c + 16 + e, vb + e);
+            if (c == 0) {
+              tmem_wait_ld();
+              tmem_landed(va);
+            }
+          }
+        };
+        auto column4 = [&](int at) { return *reinterpret_cast<const float4*>(cols + at); };
+        float x[2];
+        if constexpr (!kSecond) {
+          auto top = [&]() {  // of both rows, in units of m
+            x[0] = x[1] = -INFINITY;
+            pass([&](int c, const uint32_t* v) {
+              const float4 b4 = kBias ? column4(c) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+              for (int t = 0; t < 2; ++t) {
+                uint64_t y[2];
+                float u[4];
+                logits(std::true_type(), v + 16 * t, t, c, b4, y);
+                unpack2(y[0], u[0], u[1]);
+                unpack2(y[1], u[2], u[3]);
+                x[t] = max3(max3(x[t], u[0], u[1]), u[2], u[3]);
+              }
+            });
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+              if (!kBias && x[t] != -INFINITY) x[t] *= k_log2;
+          };
+          auto add_up = [&](auto masked) {
+            uint64_t by2[2], s0[2] = {0ull, 0ull}, s1[2] = {0ull, 0ull};
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              const float by = m[t] == -INFINITY ? 0.f : -m[t];  // nothing seen yet: 2^-inf
+              by2[t] = pack2(by, by);
+            }
+            pass([&](int c, const uint32_t* v) {
+              const float4 b4 = kBias ? column4(c) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+              for (int t = 0; t < 2; ++t) {
+                uint64_t y[2];
+                logits(masked, v + 16 * t, t, c, b4, y);
+                s0[t] = add2(s0[t], weights(y[0], by2[t]));
+                s1[t] = add2(s1[t], weights(y[1], by2[t]));
+              }
+            });
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              float x0, x1;
+              unpack2(add2(s0[t], s1[t]), x0, x1);
+              x[t] = x0 + x1;
+            }
+          };
+          const bool masked = odd || least < tile * 128 + 64 * half + 64;
+          bool moves = (valid[0] && m[0] == -INFINITY) || (valid[1] && m[1] == -INFINITY);
+#pragma unroll 1
+          for (int i = 0; i < 2; ++i) {
+            if (__any_sync(0xffffffffu, moves)) {
+              top();
+#pragma unroll
+              for (int t = 0; t < 2; ++t)
+                if (x[t] > m[t]) {
+                  const float down = ex2_ftz((m[t] - x[t]) * unit);
+                  sum[t].s *= down;
+                  sum[t].c *= down;
+                  m[t] = x[t];
+                }
+            }
+            if (masked)
+              add_up(std::true_type());
+            else
+              add_up(std::false_type());
+            moves = (valid[0] && !(x[0] <= kWtMost)) || (valid[1] && !(x[1] <= kWtMost));
+            if (!__any_sync(0xffffffffu, moves)) break;
+          }
+        } else {
+          // columns [lo, hi) are rows that see the first slot
+          const int token0 = tile * f.tile_tokens;
+          const int lo = (slot0 - past - token0) * g - 64 * half;
+          const int hi = min(f.tile_tokens, it.count - token0) * g - 64 * half;
+          uint64_t s0[2] = {0ull, 0ull}, s1[2] = {0ull, 0ull};
+          if (!odd && hi + 64 * half == tile_rows &&
+              !__any_sync(0xffffffffu, lo + 128 * g > 0)) {
+            pass([&](int c, const uint32_t* v) {
+              const float4 b4 = column4(256 + c);
+#pragma unroll
+              for (int t = 0; t < 2; ++t) {
+                uint64_t y[2];
+                logits(std::false_type(), v + 16 * t, t, c, b4, y);
+                s0[t] = add2(s0[t], weights(y[0], pack2(b4.x, b4.y)));
+                s1[t] = add2(s1[t], weights(y[1], pack2(b4.z, b4.w)));
+              }
+            });
+          } else {
+            pass([&](int c, const uint32_t* v) {
+              const float4 b4 = column4(c), w4 = column4(128 + c);
+#pragma unroll
+              for (int t = 0; t < 2; ++t) {
+                uint64_t y[2];
+                float u[4];
+                logits(std::false_type(), v + 16 * t, t, c, b4, y);
+                // (a row of NaN counts where it is seen alone)
+                unpack2(mul2(weights(y[0], pack2(b4.x, b4.y)), pack2(w4.x, w4.y)), u[0], u[1]);
+                unpack2(mul2(weights(y[1], pack2(b4.z, b4.w)), pack2(w4.z, w4.w)), u[2], u[3]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  u[e] = c + e >= lo + 128 * t * g && c + e < hi ? u[e] : 0.f;
+                s0[t] = add2(s0[t], pack2(u[0], u[1]));
+                s1[t] = add2(s1[t], pack2(u[2], u[3]));
+              }
+            });
+          }
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            float x0, x1;
+            unpack2(add2(s0[t], s1[t]), x0, x1);
+            x[t] = x0 + x1;
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&sfree[uses & 1]);
+          if (kCols) mbar_arrive(&colfree[i]);
+        }
+        sum[0].add(x[0]);
+        sum[1].add(x[1]);
       }
       if (bad) break;
-      if (!works) continue;
-      const int64_t part = (int64_t)(2 * cta + it.part - 1) * kWtHeld + 128 * t + row;
-      if constexpr (kSecond) {
-        if (beta == -INFINITY) sum.s = 0.f;  // masked
-        if (it.part != 0) {
-          f.part[part] = make_float2(sum.s, 0.f);
-        } else if (page >= 0) {
-          float* const w = f.weight + (((int64_t)page * a.H + it.h) << a.page_shift) + (slot & mask);
-          *w = (slot < past && f.decay != 0.f ? f.decay * *w : 0.f) + sum.s;
+      // ---- the halves together, in their order
+      if (half == 1) {
+        if (n > 0 && !wait_all(xfree, (n - 1) & 1, 674)) break;
+        xch[0] = make_float2(m[0], sum[0].s);
+        xch[128] = make_float2(m[1], sum[1].s);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(xfull);
+        continue;
+      }
+      if (!wait_all(xfull, n & 1, 675)) break;
+      const float2 other[2] = {xch[0], xch[128]};
+      __syncwarp();
+      if (lane == 0) mbar_arrive(xfree);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int64_t part = (int64_t)(2 * cta + it.part - 1) * kWtHeld + 128 * t + row;
+        if constexpr (kSecond) {
+          const int slot = slot0 + 128 * t;
+          const float all = beta[t] == -INFINITY ? 0.f : sum[t].s + other[t].y;  // -inf: masked
+          if (it.part != 0)
+            f.part[part] = make_float2(all, 0.f);
+          else if (page[t] >= 0)
+            f.weight[(((int64_t)page[t] * a.H + it.h) << a.page_shift) + (slot & mask)] =
+                f.decay * before[t] + all;
+        } else {
+          const float top = fmaxf(m[t], other[t].x);
+          const float l0 = m[t] == top ? sum[t].s : sum[t].s * exp2f((m[t] - top) * unit);
+          const float l1 =
+              other[t].x == top ? other[t].y : other[t].y * exp2f((other[t].x - top) * unit);
+          const float l = l0 + l1;
+          const int token = (2 * it.x + t) * f.tile_tokens + row / g;
+          if (it.part != 0)
+            f.part[part] = make_float2(top, l);
+          else if (valid[t])
+            f.q.ml[(int64_t)(it.first + token) * f.q.Hq + it.h * g + row % g] =
+                make_float2(top, l == 0.f ? 0.f : 1.f / l);
         }
-      } else {
-        if (it.part != 0)
-          f.part[part] = make_float2(m, sum.s);
-        else if (valid)
-          f.q.ml[(int64_t)(it.first + token) * f.q.Hq + it.h * g + row % g] =
-              make_float2(m, sum.s == 0.f ? 0.f : 1.f / sum.s);
       }
     }
   }
