@@ -19,7 +19,7 @@
 // logits are natural up to the subtraction, as a bias of the lowest float would be -inf in units of
 // log 2.
 //
-// A thread of the sums has a lane of both held tiles and half of the columns: what belongs to a column
+// A thread of the sums has a lane of both held tiles and a quarter of the columns: what belongs to a column
 // (biases; m and l) is read from shared memory once for two values. A broadcast of 16 bytes takes
 // the load unit as long as 32 different ones, four cycles: with a thread to a lane of one held tile
 // and m and 1 / l apart these reads were the bound, 212 us of the second pass over 6,001 tokens of 28
@@ -27,7 +27,7 @@
 // that its rounding stays below 2^-20 of a weight.
 //
 // Roles: warp 0 TMA (a box per page and 64 channels), 1 MMA issuer and TMEM, 2 what belongs to the
-// streamed tile's columns and to held slots, 4 .. 11 sums. Ranges of equal cost as in the prefill (paged_tc.cuh); what several CTAs share of an item goes to the
+// streamed tile's columns and to held slots, 4 .. 19 sums. Ranges of equal cost as in the prefill (paged_tc.cuh); what several CTAs share of an item goes to the
 // workspace and a second launch joins it. Every wait is bounded.
 #include <type_traits>
 
@@ -38,14 +38,15 @@ namespace still {
 
 namespace {
 
-constexpr int kWtThreads = 384;
+constexpr int kWtThreads = 640;
+constexpr int kWtSums = 16;          // warps that add up: four to a quarter of the columns
 constexpr int kWtHeld = 256;        // rows or slots of an item
 constexpr int kWtMost = 1024;       // a tile's sum in units of e^m that moves m
 // Streamed tiles whose column values are held, [kWtCols][kWtColFloats]: three of every column, a flag,
 // and of the tile that is an item's first the held slots' biases and pages.
 constexpr int kWtCols = 4;
 constexpr int kWtFlagAt = 384, kWtBiasAt = 388, kWtPageAt = kWtBiasAt + kWtHeld;
-constexpr int kWtColFloats = kWtPageAt + kWtHeld;
+constexpr int kWtColFloats = kWtPageAt + kWtHeld / 8;  // (8 slots lie in one page)
 constexpr float kWtFold = 32.f;     // |m + log2 l| below which they are one number
 
 // An item of either pass: `x` counts blocks of 2 tile_tokens tokens or of 256 slots.
@@ -110,8 +111,8 @@ struct WtShape {
   static constexpr int kStages = D == 64 ? 8 : 5;      // a chunk of a streamed tile each
   static constexpr int kRing = kHeldBufs * kHeldBytes;
   static constexpr int kColAt = kRing + kStages * kChunkBytes;
-  static constexpr int kXchAt = kColAt + kWtCols * kWtColFloats * 4;  // [256] float2
-  static constexpr int kBarAt = kXchAt + kWtHeld * 8;
+  static constexpr int kXchAt = kColAt + kWtCols * kWtColFloats * 4;  // [3][256] float2
+  static constexpr int kBarAt = kXchAt + 3 * kWtHeld * 8;
   static constexpr int kPlanAt = kBarAt + (2 * kStages + 2 * kWtCols + 13) * 8 + 16;
   static constexpr int kBytes = kPlanAt + sizeof(WtPlan);
   static_assert(kBytes <= 232448, "shared memory budget");
@@ -156,7 +157,7 @@ __global__ void __launch_bounds__(kWtThreads, 1)
   uint64_t* seen = qfree + 2;            // [2] its record read by all
   uint64_t* sfull = seen + 2;            // [2] S of both held tiles, buffer i, complete
   uint64_t* sfree = sfull + 2;           // [2] and read
-  uint64_t* xfull = sfree + 2;           // the second half's sums of an item
+  uint64_t* xfull = sfree + 2;           // the other quarters' sums of an item
   uint64_t* xfree = xfull + 1;           // and read
   uint64_t* drain = xfree + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
@@ -177,16 +178,16 @@ __global__ void __launch_bounds__(kWtThreads, 1)
     }
     for (int i = 0; i < kWtCols; ++i) {
       mbar_init(&colfull[i], 1);
-      mbar_init(&colfree[i], 8);
+      mbar_init(&colfree[i], kWtSums);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&qfull[i], 1);
       mbar_init(&qfree[i], 1);
-      mbar_init(&seen[i], 10);
+      mbar_init(&seen[i], kWtSums + 2);
       mbar_init(&sfull[i], 1);
-      mbar_init(&sfree[i], 8);
+      mbar_init(&sfree[i], kWtSums);
     }
-    mbar_init(xfull, 4);
+    mbar_init(xfull, kWtSums - 4);
     mbar_init(xfree, 4);
     mbar_init(drain, 1);
     *abort_flag = 0;
@@ -482,10 +483,9 @@ __global__ void __launch_bounds__(kWtThreads, 1)
             at4[64] = make_float4(sum[0], sum[1], sum[2], sum[3]);
             if (k == it.k0) {
               float4* const b4 = reinterpret_cast<float4*>(at + kWtBiasAt + 8 * lane);
-              int4* const p4 = reinterpret_cast<int4*>(at + kWtPageAt + 8 * lane);
               b4[0] = make_float4(beta[0], beta[1], beta[2], beta[3]);
               b4[1] = make_float4(beta[4], beta[5], beta[6], beta[7]);
-              p4[0] = p4[1] = make_int4(page, page, page, page);
+              at[kWtPageAt + lane] = __int_as_float(page);
             }
           } else {
             at4[0] = make_float4(v[0], v[1], v[2], v[3]);
@@ -502,10 +502,10 @@ __global__ void __launch_bounds__(kWtThreads, 1)
     }
   } else if (warp >= 4) {
     // ------------------------------------------------------------ sums
-    const int half = (warp - 4) >> 2, quarter = warp & 3;  // columns [64 half, + 64)
-    const int row = quarter * 32 + lane;                   // of both held tiles
-    const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16) + 64 * half;
-    float2* const xch = reinterpret_cast<float2*>(smem + S::kXchAt) + row;  // [2][128]
+    const int c0 = 32 * ((warp - 4) >> 2);     // columns [c0, c0 + 32)
+    const int row = (warp & 3) * 32 + lane;    // of both held tiles
+    const uint32_t lanes = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + c0;
+    float2* const xch = reinterpret_cast<float2*>(smem + S::kXchAt) + row;  // [3][2][128]
     const float k_log2 = f.q.scale * kLog2e;
     const float unit = kBias ? kLog2e : 1.f;  // of m, in log 2
     const uint64_t sc = pack2(f.q.scale, f.q.scale);
@@ -542,19 +542,19 @@ __global__ void __launch_bounds__(kWtThreads, 1)
         const int tile = tile_of(it, k);
         const int i = uses % kWtCols;
         const float* const cols =
-            reinterpret_cast<const float*>(smem + S::kColAt) + kWtColFloats * i + 64 * half;
+            reinterpret_cast<const float*>(smem + S::kColAt) + kWtColFloats * i + c0;
         bool odd = false;
         if constexpr (kCols) {
           if (!wait_all(&colfull[i], (uses / kWtCols) & 1, 672)) break;
-          odd = cols[kWtFlagAt - 64 * half] != 0.f;
+          odd = cols[kWtFlagAt - c0] != 0.f;
           if (kSecond && k == it.k0) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-              beta[t] = cols[kWtBiasAt - 64 * half + 128 * t + row];
-              page[t] = __float_as_int(cols[kWtPageAt - 64 * half + 128 * t + row]);
+              beta[t] = cols[kWtBiasAt - c0 + 128 * t + row];
+              page[t] = __float_as_int(cols[kWtPageAt - c0 + 16 * t + row / 8]);
               const int slot = slot0 + 128 * t;
               if (slot >= it.len) page[t] = -1;
-              if (half == 0 && it.part == 0 && f.decay != 0.f && page[t] >= 0 && slot < past)
+              if (c0 == 0 && it.part == 0 && f.decay != 0.f && page[t] >= 0 && slot < past)
                 before[t] = f.weight[(((int64_t)page[t] * a.H + it.h) << a.page_shift) +
                                      (slot & mask)];
             }
@@ -581,7 +581,7 @@ __global__ void __launch_bounds__(kWtThreads, 1)
             float u[4];
             unpack2(x[0], u[0], u[1]);
             unpack2(x[1], u[2], u[3]);
-            const int upto = see[t] - tile * 128 - 64 * half - c;
+            const int upto = see[t] - tile * 128 - c0 - c;
             const float b[4] = {b4.x, b4.y, b4.z, b4.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -596,26 +596,15 @@ __global__ void __launch_bounds__(kWtThreads, 1)
           unpack2(kBias ? mul2(add2(x, by2), k2) : fma2(x, k2, by2), u0, u1);
           return pack2(ex2_ftz(u0), ex2_ftz(u1));
         };
-        // All 64 columns, the next 16 on their way meanwhile.
-        auto pass = [&](auto f4) {
-          uint32_t va[32], vb[32];
-          issue(0, va);
-          tmem_wait_ld();
-          tmem_landed(va);
+        auto pass = [&](auto f4) {  // all 32 columns
 #pragma unroll
-          for (int c = 0; c < 64; c += 32) {
-            issue(c + 16, vb);
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) f4(c + e, va + e);
+          for (int c = 0; c < 32; c += 16) {
+            uint32_t v[32];
+            issue(c, v);
             tmem_wait_ld();
-            tmem_landed(vb);
-            if (c == 0) issue(32, va);
+            tmem_landed(v);
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) f4(c + 16 + e, vb + e);
-            if (c == 0) {
-              tmem_wait_ld();
-              tmem_landed(va);
-            }
+            for (int e = 0; e < 16; e += 4) f4(c + e, v + e);
           }
         };
         auto column4 = [&](int at) { return *reinterpret_cast<const float4*>(cols + at); };
@@ -663,7 +652,7 @@ __global__ void __launch_bounds__(kWtThreads, 1)
               x[t] = x0 + x1;
             }
           };
-          const bool masked = odd || least < tile * 128 + 64 * half + 64;
+          const bool masked = odd || least < tile * 128 + c0 + 32;
           bool moves = (valid[0] && m[0] == -INFINITY) || (valid[1] && m[1] == -INFINITY);
 #pragma unroll 1
           for (int i = 0; i < 2; ++i) {
@@ -688,10 +677,10 @@ __global__ void __launch_bounds__(kWtThreads, 1)
         } else {
           // columns [lo, hi) are rows that see the first slot
           const int token0 = tile * f.tile_tokens;
-          const int lo = (slot0 - past - token0) * g - 64 * half;
-          const int hi = min(f.tile_tokens, it.count - token0) * g - 64 * half;
+          const int lo = (slot0 - past - token0) * g - c0;
+          const int hi = min(f.tile_tokens, it.count - token0) * g - c0;
           uint64_t s0[2] = {0ull, 0ull}, s1[2] = {0ull, 0ull};
-          if (!odd && hi + 64 * half == tile_rows &&
+          if (!odd && hi + c0 == tile_rows &&
               !__any_sync(0xffffffffu, lo + 128 * g > 0)) {
             pass([&](int c, const uint32_t* v) {
               const float4 b4 = column4(256 + c);
@@ -739,17 +728,21 @@ __global__ void __launch_bounds__(kWtThreads, 1)
         sum[1].add(x[1]);
       }
       if (bad) break;
-      // ---- the halves together, in their order
-      if (half == 1) {
+      // ---- the quarters together, in their order
+      if (c0 > 0) {
         if (n > 0 && !wait_all(xfree, (n - 1) & 1, 674)) break;
-        xch[0] = make_float2(m[0], sum[0].s);
-        xch[128] = make_float2(m[1], sum[1].s);
+        xch[8 * c0 - 256] = make_float2(m[0], sum[0].s);
+        xch[8 * c0 - 128] = make_float2(m[1], sum[1].s);
         __syncwarp();
         if (lane == 0) mbar_arrive(xfull);
         continue;
       }
       if (!wait_all(xfull, n & 1, 675)) break;
-      const float2 other[2] = {xch[0], xch[128]};
+      float2 other[3][2];
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) other[i][t] = xch[256 * i + 128 * t];
       __syncwarp();
       if (lane == 0) mbar_arrive(xfree);
 #pragma unroll
@@ -757,18 +750,22 @@ __global__ void __launch_bounds__(kWtThreads, 1)
         const int64_t part = (int64_t)(2 * cta + it.part - 1) * kWtHeld + 128 * t + row;
         if constexpr (kSecond) {
           const int slot = slot0 + 128 * t;
-          const float all = beta[t] == -INFINITY ? 0.f : sum[t].s + other[t].y;  // -inf: masked
+          const float sums = (sum[t].s + other[0][t].y) + (other[1][t].y + other[2][t].y);
+          const float all = beta[t] == -INFINITY ? 0.f : sums;  // masked
           if (it.part != 0)
             f.part[part] = make_float2(all, 0.f);
           else if (page[t] >= 0)
             f.weight[(((int64_t)page[t] * a.H + it.h) << a.page_shift) + (slot & mask)] =
                 f.decay * before[t] + all;
         } else {
-          const float top = fmaxf(m[t], other[t].x);
-          const float l0 = m[t] == top ? sum[t].s : sum[t].s * exp2f((m[t] - top) * unit);
-          const float l1 =
-              other[t].x == top ? other[t].y : other[t].y * exp2f((other[t].x - top) * unit);
-          const float l = l0 + l1;
+          const float top =
+              max3(fmaxf(m[t], other[0][t].x), other[1][t].x, other[2][t].x);
+          auto brought = [&](float from, float x) {
+            return from == top ? x : x * exp2f((from - top) * unit);
+          };
+          const float l = (brought(m[t], sum[t].s) + brought(other[0][t].x, other[0][t].y)) +
+                          (brought(other[1][t].x, other[1][t].y) +
+                           brought(other[2][t].x, other[2][t].y));
           const int token = (2 * it.x + t) * f.tile_tokens + row / g;
           if (it.part != 0)
             f.part[part] = make_float2(top, l);
