@@ -53,7 +53,7 @@ namespace still {
 namespace {
 
 constexpr int kPfProducers = 3;     // warps
-constexpr int kPfConverters = 4;    // warps, of a pool in 8 bits
+constexpr int kPfConverters = 8;    // warps, of a pool in 8 bits
 constexpr float kPfMoveLog2 = 8.f;  // P <= 2^8 needs no more of bf16's range
 
 // The same on a CTA pair, issued by the even CTA: A's rows [0, 128) from its TMEM, [128, 256) from
@@ -96,20 +96,27 @@ STILL_DEV void zero_rows(uint8_t* slot, int chunks, int rows, int first, uint32_
 struct PfPlan {  // in shared memory
   PfStart start;
   PfItem shown[2];  // items n & 1 as the producer shows them to the others
-  int64_t warp_cost[16];
+  int64_t warp_cost[20];
 };
 
-// The warps of a CTA. Of a pool in 8 bits a warpgroup converts codes, and the softmax warps begin at
-// a warpgroup of their own, so that registers can be dealt out: 4 x 128 threads of 128 each become
-// 96 (loads, products), 160, 160 (softmax) and 96 (codes), or 112, 144, 144 and 112 without biases.
-template <bool kQuant>
+// The warps of a CTA. Of a pool in 8 bits two warpgroups convert codes, and the softmax warps begin
+// at a warpgroup of their own, so that registers can be dealt out: 5 x 128 threads of 96 each become
+// 144 for the softmax and 64 for all others, 152 and 56 with biases.
+template <bool kBias, bool kQuant>
 struct PfRoles {
-  static constexpr int kThreads = kQuant ? 512 : 384;
+  static constexpr int kThreads = kQuant ? 640 : 384;
   static constexpr int kSoftmax = kQuant ? 4 : 2;       // the first of eight
   static constexpr int kFirst = kSoftmax + 8;           // producer or converter behind them
+  static constexpr int kSoftmaxRegs = kBias ? 152 : 144, kOtherRegs = kBias ? 56 : 64;
+  static_assert(256 * kSoftmaxRegs + 384 * kOtherRegs <= 640 * 96, "registers of a CTA");
+};
+// A ring slot of codes, and what the converters have to know of it.
+struct PfRaw {
+  float scale[kPfKeys / kScaleBlock];  // of its 16 slots each
+  uint32_t counts[4];                  // bit i of word e: slot 4 i + e counts
 };
 
-template <int D, bool kBias, bool kPair>
+template <int D, bool kBias, bool kPair, bool kQuant>
 struct PfShape {
   static constexpr int kTiles = D <= 128 ? 2 : 1;  // of an item on an SM
   // A ring slot holds 128 slots of kChan channels; a pair's CTA has one with its half of a tile: of
@@ -122,51 +129,45 @@ struct PfShape {
   static_assert(kStageBytes == kPfKeys * kChan * 2, "a ring slot");
   static constexpr int kChunkBytes = kPfKeys * 128;  // 64 channels of 128 rows
   static constexpr int kQBytes = kTiles * (D / 64) * kChunkBytes;
-  static constexpr int kStages = D == 64 ? 8 : kBias ? 4 : 5;
+  static constexpr int kStages = kQuant ? (D == 64 ? 5 : 3) : D == 64 ? 8 : kBias ? 4 : 5;
+  // ring slots of codes, of 8 bits where those above have 16
+  static constexpr int kRaws = kQuant ? (D == 64 ? 4 : 3) : 0, kRawBytes = kStageBytes / 2;
   static constexpr int kOCols = kTiles == 2 ? D : D / 2;  // O columns per softmax thread
   static constexpr int kRing = kQBytes;
-  static constexpr int kBiasAt = kRing + kStages * kStageBytes;  // [8 warps][128]
+  static constexpr int kRawAt = kRing + kStages * kStageBytes;
+  static constexpr int kBiasAt = kRawAt + kRaws * kRawBytes;  // [8 warps][128]
   // one tile only: running maxima and sums, [2][128] each
   static constexpr int kXchAt = kBiasAt + (kBias ? 8 * kPfKeys * 4 : 0);
   static constexpr int kBarAt = kXchAt + (kTiles == 1 ? 2048 : 0);
   static constexpr int kPlanAt = kBarAt + (3 * kStages + 30) * 8;
-  static constexpr int kBytes = kPlanAt + sizeof(PfPlan);
-  static constexpr int kConvertRegs = kBias ? 96 : 112;  // of a pool in 8 bits (PfRoles)
+  static constexpr int kRawBarAt = (kPlanAt + sizeof(PfPlan) + 15) / 16 * 16;
+  static constexpr int kRawInfoAt = kRawBarAt + 2 * 4 * 8;
+  static constexpr int kBytes =
+      kQuant ? kRawInfoAt + kRaws * (int)sizeof(PfRaw) : kPlanAt + (int)sizeof(PfPlan);
   static_assert(kBytes <= 232448, "shared memory budget");
 };
 
-// A pool in 8 bits: a warpgroup loads codes into registers, one ring slot ahead of the one that it
-// converts, multiplies them by their block's scale and stores bf16 as TMA would have (rows of 128
-// bytes, 128-byte swizzle). Everything behind works as for a pool in bf16. With scales that are powers
-// of two nothing is rounded.
-template <int D, bool kBias, bool kPair, class Zero>
-STILL_DEV void pf_convert(const PrefillParams& f, int tokens, const PfStart& start, uint8_t* smem,
-                          uint64_t* full, uint64_t* empty, volatile int* abort_flag, int rank,
-                          Zero zero_item) {
-  using S = PfShape<D, kBias, kPair>;
-  constexpr int kStages = S::kStages, kHalves = S::kHalves, kAhead = S::kTiles == 2 ? 1 : 2;
-  constexpr int kPieces = S::kStageBytes / 32 / (32 * kPfConverters);  // of 16 codes, of a thread
-  const PagedArgs& a = f.a;
-  const int lane = threadIdx.x & 31;
-  const int me = threadIdx.x & (32 * kPfConverters - 1);
-  const int mask = (1 << a.page_shift) - 1;
-  // Half a tile of K or V, a ring slot: rows of kKRows or 128 slots, pieces of 16 channels.
-  struct Unit {
-    int b, h, len, kt;
-    int half;
-    bool v;
-  };
-  PfWalk walk(a, PfRowItems{tokens}, start);
+// A ring slot of codes: half a tile of K or V, all of its channels or of its slots in a pair.
+struct PfUnit {
+  int b, h, len, kt;
+  int half;
+  bool v;
+};
+// The ring slots of a CTA's items in the order in which the issuer takes them.
+template <int kHalves, int kAhead>
+struct PfUnits {
+  PfWalk<PfRowItems> walk;
   PfItem it;
   bool have = false;
   int kt = 0, sub = 0;
-  // The ring slots in the order in which the issuer takes them.
-  auto next = [&](Unit& u) -> bool {
+  // false at the end; `nothing` gets the items whose rows see nothing
+  template <class Zero>
+  STILL_DEV bool next(PfUnit& u, volatile int* abort_flag, Zero nothing) {
     for (;;) {
       if (!have) {
         if (warp_flag(abort_flag) || !walk.next(it)) return false;
         if (it.k0 == it.k1) {
-          if (me < 32 && rank == 0) zero_item(it);
+          nothing(it);
           continue;
         }
         have = true;
@@ -177,7 +178,7 @@ STILL_DEV void pf_convert(const PrefillParams& f, int tokens, const PfStart& sta
         const bool v = sub < kHalves;
         const int t = v ? kt : kt + kAhead;
         if (sub < 2 * kHalves && t >= it.k0 && t < it.k1) {
-          u = Unit{it.b, it.h, it.len, t, v ? sub : sub - kHalves, v};
+          u = PfUnit{it.b, it.h, it.len, t, v ? sub : sub - kHalves, v};
           ++sub;
           return true;
         }
@@ -190,24 +191,41 @@ STILL_DEV void pf_convert(const PrefillParams& f, int tokens, const PfStart& sta
       }
       have = false;
     }
-  };
-  auto first_of = [&](const Unit& u) {  // slot of its first row
+  }
+};
+
+// A pool in 8 bits: a warp fetches codes into a ring of their own (TMA, a box per page), with their
+// scales and which slots count, one slot ahead of the copies; two warpgroups multiply codes by their
+// block's scale and store bf16 as TMA would have (rows of 128 bytes, 128-byte swizzle). Everything
+// behind works as for a pool in bf16. With scales that are powers of two nothing is rounded.
+template <int D, bool kBias, bool kPair, class Zero>
+STILL_DEV void pf_fetch(const PrefillParams& f, int tokens, const PfStart& start, uint8_t* smem,
+                        const CUtensorMap& tm_k, const CUtensorMap& tm_v, volatile int* abort_flag,
+                        int rank, Zero zero_item) {
+  using S = PfShape<D, kBias, kPair, true>;
+  const PagedArgs& a = f.a;
+  const int lane = threadIdx.x & 31;
+  const int mask = (1 << a.page_shift) - 1;
+  uint64_t* const raw_full = reinterpret_cast<uint64_t*>(smem + S::kRawBarAt);
+  uint64_t* const raw_empty = raw_full + S::kRaws;
+  PfRaw* const info = reinterpret_cast<PfRaw*>(smem + S::kRawInfoAt);
+  PfUnits<S::kHalves, S::kTiles == 2 ? 1 : 2> units{PfWalk(a, PfRowItems{tokens}, start)};
+  auto rows_of = [&](const PfUnit& u) { return kPair && !u.v ? S::kKRows : kPfKeys; };
+  auto first_of = [&](const PfUnit& u) {  // slot of its first row
     return u.kt * kPfKeys + (kPair && !u.v ? rank * S::kKRows : 0);
   };
-  // Lane i: the page of its i-th 16 slots (-1: none), the scale there, biases of four slots.
-  auto look_up = [&](const Unit& u) {
+  // Lane i: the page of its i-th 16 slots (-1: none), the scale there; which of slots 4 i + e count.
+  auto page_of = [&](const PfUnit& u) {
     const int j = first_of(u) + kScaleBlock * lane;
-    const int rows = kPair && !u.v ? S::kKRows : kPfKeys;
-    if (kScaleBlock * lane >= rows || j >= u.len) return -1;
+    if (kScaleBlock * lane >= rows_of(u) || j >= u.len) return -1;
     return paged_page(a, a.table + (int64_t)u.b * a.s_table, j);
   };
-  auto scale_of = [&](const Unit& u, int pg) {
+  auto scale_of = [&](const PfUnit& u, int pg) {
     if (pg < 0) return 0.f;
     const int in = (first_of(u) + kScaleBlock * lane) & mask;
     return (u.v ? a.v_scale : a.k_scale)[((((int64_t)pg * a.H + u.h) << a.page_shift) + in) >> 4];
   };
-  // Bits of slots 4 lane + e of the unit that count.
-  auto counts_of = [&](const Unit& u, int pg) {
+  auto counts_of = [&](const PfUnit& u, int pg) {
     uint32_t m = 0;
     const int j = first_of(u) + 4 * lane;
     const int at = __shfl_sync(0xffffffffu, pg, lane >> 2);
@@ -217,56 +235,106 @@ STILL_DEV void pf_convert(const PrefillParams& f, int tokens, const PfStart& sta
       if (at >= 0 && j + e < u.len && (!kBias || beta[e] != -INFINITY)) m |= 1u << e;
     return m;
   };
-  // A thread's piece i: row and 16 channels of a unit (a row has 2^bits pieces).
-  auto bits_of = [&](const Unit& u) { return kPair && !u.v ? 4 : S::kChan == 64 ? 2 : 3; };
-  auto load = [&](const Unit& u, int pg, int i) {
-    const int bits = bits_of(u);
-    const int row = (me >> bits) + i * (32 * kPfConverters >> bits), j = first_of(u) + row;
-    const int at = __shfl_sync(0xffffffffu, pg, row >> 4);
-    const int chan = 16 * (me & ((1 << bits) - 1)) +
-                     (kPair ? (u.v ? rank * S::kChan : 0) : u.half * S::kChan);
-    if (at < 0 || j >= u.len) return make_uint4(0, 0, 0, 0);
-    return __ldg(reinterpret_cast<const uint4*>((u.v ? a.V8 : a.K8) + (int64_t)at * a.s_page +
-                                                (int64_t)(j & mask) * a.s_slot +
-                                                (int64_t)u.h * a.s_head + chan));
-  };
-  int stage = 0;
-  uint32_t phase = 0;
-  uint4 x[kPieces];
-  Unit u{}, then{};
-  int pg = -1, then_pg = -1;
-  bool ok = next(u), more = false, bad = false;
-  float scale = 0.f;
-  uint32_t counts = 0;
-  if (ok) {
-    pg = look_up(u);
-    scale = scale_of(u, pg);
-    counts = counts_of(u, pg);
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) x[i] = load(u, pg, i);
-    more = next(then);
-    if (more) then_pg = look_up(then);
-  }
+  int raw = 0;
+  uint32_t phase = 0, armed = 0, armed_par = 0;
+  bool bad = false;
+  PfUnit u{}, then{};
+  bool ok = units.next(u, abort_flag, zero_item);
+  int pg = ok ? page_of(u) : -1;
 #pragma unroll 1
   while (ok) {
-    // the unit after the next: its pages; the next one's codes are asked for below
-    Unit third{};
-    const bool third_ok = more && next(third);
-    const int third_pg = third_ok ? look_up(third) : -1;
-    const float then_scale = more ? scale_of(then, then_pg) : 0.f;
-    const uint32_t then_counts = more ? counts_of(then, then_pg) : 0;
-    if (!pf_wait(&empty[stage], phase ^ 1, a.err, abort_flag, 610)) {
+    const float scale = scale_of(u, pg);
+    const uint32_t counts = counts_of(u, pg);
+    const bool more = units.next(then, abort_flag, zero_item);
+    const int then_pg = more ? page_of(then) : -1;
+    if (!pf_wait(&raw_empty[raw], phase ^ 1, a.err, abort_flag, 617)) {
+      bad = true;
+      break;
+    }
+    if (lane < kPfKeys / kScaleBlock) info[raw].scale[lane] = scale;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t w = __ballot_sync(0xffffffffu, (counts >> e) & 1);
+      if (lane == e) info[raw].counts[e] = w;
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive_expect_tx(&raw_full[raw], S::kRawBytes);
+    armed |= 1u << raw;
+    armed_par = (armed_par & ~(1u << raw)) | (phase << raw);
+    __syncwarp();
+    const int box_bits = min(a.page_shift, kPair && !u.v ? 6 : 7);
+    const int r = lane << box_bits, at = __shfl_sync(0xffffffffu, pg, (r >> 4) & 31);
+    if (r < rows_of(u)) {
+      const int chan = kPair ? (u.v ? rank * S::kChan : 0) : u.half * S::kChan;
+      const int pitch = kPair && !u.v ? D : S::kChan;
+      tma_load_4d(smem + S::kRawAt + raw * S::kRawBytes + r * pitch, u.v ? &tm_v : &tm_k,
+                  &raw_full[raw], chan, (first_of(u) + r) & mask, u.h, at < 0 ? a.n_pages : at);
+    }
+    if (++raw == S::kRaws) {
+      raw = 0;
+      phase ^= 1;
+    }
+    u = then;
+    pg = then_pg;
+    ok = more;
+  }
+  // Nobody leaves before the copies have landed: the converters have read them all, or waits here.
+  if (lane == 0) {
+    for (int i = 0; i < S::kRaws && !bad && !*abort_flag; ++i) {
+      if (!mbar_wait(&raw_empty[raw], phase ^ 1)) {
+        dev_set_error(a.err, DEV_WAIT_TIMEOUT, 618);
+        *abort_flag = 1;
+      }
+      if (++raw == S::kRaws) {
+        raw = 0;
+        phase ^= 1;
+      }
+    }
+    if (bad || *abort_flag)
+      for (int i = 0; i < S::kRaws; ++i)
+        if (armed & (1u << i)) (void)mbar_wait(&raw_full[i], (armed_par >> i) & 1);
+  }
+}
+
+template <int D, bool kBias, bool kPair>
+STILL_DEV void pf_convert(const PrefillParams& f, int tokens, const PfStart& start, uint8_t* smem,
+                          uint64_t* full, uint64_t* empty, volatile int* abort_flag) {
+  using S = PfShape<D, kBias, kPair, true>;
+  constexpr int kStages = S::kStages;
+  constexpr int kPieces = S::kRawBytes / 16 / (32 * kPfConverters);  // of 16 codes, of a thread
+  const PagedArgs& a = f.a;
+  const int lane = threadIdx.x & 31;
+  const int me = threadIdx.x - 32 * PfRoles<kBias, true>::kFirst;
+  uint64_t* const raw_full = reinterpret_cast<uint64_t*>(smem + S::kRawBarAt);
+  uint64_t* const raw_empty = raw_full + S::kRaws;
+  const PfRaw* const info = reinterpret_cast<const PfRaw*>(smem + S::kRawInfoAt);
+  PfUnits<S::kHalves, S::kTiles == 2 ? 1 : 2> units{PfWalk(a, PfRowItems{tokens}, start)};
+  int stage = 0, raw = 0;
+  uint32_t phase = 0, raw_phase = 0;
+  bool bad = false;
+  PfUnit u{};
+#pragma unroll 1
+  while (units.next(u, abort_flag, [](const PfItem&) {})) {
+    const bool k_half = kPair && !u.v;  // 64 rows of 256 channels
+    const int bits = k_half ? 4 : S::kChan == 64 ? 2 : 3, row_bits = k_half ? 6 : 7;
+    if (!pf_wait(&raw_full[raw], raw_phase, a.err, abort_flag, 619)) bad = true;
+    const uint8_t* const from = smem + S::kRawAt + raw * S::kRawBytes;
+    uint4 x[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+      x[i] = *reinterpret_cast<const uint4*>(from + 16 * (me + i * 32 * kPfConverters));
+    if (bad || !pf_wait(&empty[stage], phase ^ 1, a.err, abort_flag, 610)) {
       bad = true;
       break;
     }
     uint8_t* const slot = smem + S::kRing + stage * S::kStageBytes;
-    const int bits = bits_of(u), row_bits = kPair && !u.v ? 6 : 7;
     const int piece = me & ((1 << bits) - 1);
+    const int unit = 2 * (piece & 3), flip = (piece >> 2) & 1;
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int row = (me >> bits) + i * (32 * kPfConverters >> bits);
-      float s = __shfl_sync(0xffffffffu, scale, row >> 4);
-      if (!((__shfl_sync(0xffffffffu, counts, row >> 2) >> (row & 3)) & 1)) {
+      float s = info[raw].scale[row >> 4];
+      if (!((info[raw].counts[row & 3] >> (row >> 2)) & 1)) {
         s = 0.f;  // (a block that is masked whole may have any scale)
         x[i] = make_uint4(0, 0, 0, 0);
       }
@@ -281,10 +349,8 @@ STILL_DEV void pf_convert(const PrefillParams& f, int tokens, const PfStart& sta
         unpack2(mul2(pack2(z.x, z.y), s2), z0, z1);
         w[e] = bf16x2_bits(__floats2bfloat162_rn(z0, z1));
       }
-      if (more) x[i] = load(then, then_pg, i);
       // (the second four of eight lanes begin with their second half: no bank twice)
       uint8_t* const at = slot + (((piece >> 2) << row_bits) + row) * 128;
-      const int unit = 2 * (piece & 3), flip = (piece >> 2) & 1;
       const uint4 lo = make_uint4(w[0], w[1], w[2], w[3]), hi = make_uint4(w[4], w[5], w[6], w[7]);
       *reinterpret_cast<uint4*>(at + (((unit + flip) ^ (row & 7)) << 4)) = flip ? hi : lo;
       *reinterpret_cast<uint4*>(at + (((unit + 1 - flip) ^ (row & 7)) << 4)) = flip ? lo : hi;
@@ -292,6 +358,7 @@ STILL_DEV void pf_convert(const PrefillParams& f, int tokens, const PfStart& sta
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) {
+      mbar_arrive(&raw_empty[raw]);
       if constexpr (kPair)
         mbar_arrive_cluster(cluster_map(smem_u32(&full[stage]), 0));
       else
@@ -301,14 +368,10 @@ STILL_DEV void pf_convert(const PrefillParams& f, int tokens, const PfStart& sta
       stage = 0;
       phase ^= 1;
     }
-    u = then;
-    then = third;
-    pg = then_pg;
-    then_pg = third_pg;
-    scale = then_scale;
-    counts = then_counts;
-    ok = more;
-    more = third_ok;
+    if (++raw == S::kRaws) {
+      raw = 0;
+      raw_phase ^= 1;
+    }
   }
   // The last arrivals of the issuer's commits, before the CTA leaves.
   for (int i = 0; me == 0 && !bad && i < kStages && !*abort_flag; ++i) {
@@ -324,13 +387,13 @@ STILL_DEV void pf_convert(const PrefillParams& f, int tokens, const PfStart& sta
 }
 
 template <int D, bool kBias, bool kPair, bool kQuant>
-__global__ void __launch_bounds__(PfRoles<kQuant>::kThreads, 1)
+__global__ void __launch_bounds__(PfRoles<kBias, kQuant>::kThreads, 1)
     paged_prefill_kernel(const __grid_constant__ CUtensorMap tm_q,
                          const __grid_constant__ CUtensorMap tm_k,
                          const __grid_constant__ CUtensorMap tm_v,
                          const __grid_constant__ PrefillParams f) {
-  using S = PfShape<D, kBias, kPair>;
-  using R = PfRoles<kQuant>;
+  using S = PfShape<D, kBias, kPair, kQuant>;
+  using R = PfRoles<kBias, kQuant>;
   constexpr int kTiles = S::kTiles, kStages = S::kStages, kHalves = S::kHalves;
   // All of it: no byte is left beside five stages of 256 channels, so the base has to be aligned as
   // it is.
@@ -405,15 +468,20 @@ __global__ void __launch_bounds__(PfRoles<kQuant>::kThreads, 1)
     for (int i = 0; i < 8; ++i) mbar_init(&mb[i], 1);
     for (int i = 0; i < 4; ++i) mbar_init(&lb[i], 2);
     mbar_init(drain, 1);
+    if constexpr (kQuant) {
+      uint64_t* const raw_full = reinterpret_cast<uint64_t*>(smem + S::kRawBarAt);
+      for (int i = 0; i < S::kRaws; ++i) {
+        mbar_init(&raw_full[i], 1);
+        mbar_init(&raw_full[S::kRaws + i], kPfConverters);
+      }
+    }
     mbar_init(&seen[0], 8);
     mbar_init(&seen[1], 8);
     *abort_flag = 0;
     fence_mbar_init();
     tma_prefetch_desc(&tm_q);
-    if constexpr (!kQuant) {
-      tma_prefetch_desc(&tm_k);
-      tma_prefetch_desc(&tm_v);
-    }
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
   }
   if (warp == 1) {
     if constexpr (kPair) {
@@ -494,346 +562,351 @@ __global__ void __launch_bounds__(PfRoles<kQuant>::kThreads, 1)
   };
   // K tiles that are loaded before the first one of V, in the order in which the issuer takes them
   constexpr int kAhead = kTiles == 2 ? 1 : 2;
-  if constexpr (kQuant) {
-    if (warp >= R::kSoftmax && warp < R::kFirst)
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(256 - S::kConvertRegs));
-    else
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kConvertRegs));
-  }
-
-  if (kQuant && warp == 0) {
-    // ------------------------------------------------------------ items and their q
-    int n_items = 0;
-    bool bad = false, q_armed = false;
-    PfWalk walk(a, PfRowItems{tokens}, start);
-    PfItem it;
-    while (!bad && !warp_flag(abort_flag) && walk.next(it)) {
-      if (it.k0 == it.k1) continue;
-      if (!show(n_items, it)) {
-        bad = true;
-        break;
-      }
-      q_armed = true;
-      ++n_items;
-    }
-    if (lane == 0) {
-      if (!bad) end_items(n_items);
-      if ((bad || *abort_flag) && q_armed)
-        (void)mbar_wait(&qfull[(n_items - 1) & 1], ((n_items - 1) >> 1) & 1);
-    }
-  } else if (kQuant && warp >= R::kFirst) {
-    // ------------------------------------------------------------ codes to bf16
+  if (warp < R::kSoftmax || warp >= R::kFirst) {
     if constexpr (kQuant)
-      pf_convert<D, kBias, kPair>(f, tokens, start, smem, full, empty, abort_flag, rank,
-                                  zero_item);
-  } else if (!kQuant && (warp == 0 || warp >= R::kFirst)) {
-    // ------------------------------------------------------------ TMA producers
-    const int me = warp == 0 ? 0 : warp - R::kFirst + 1;  // 0 also loads q, arms the barriers and zeroes rows
-    int stage = 0, n_items = 0;
-    uint32_t phase = 0;
-    uint32_t armed = 0, armed_par = 0;  // stages whose copies were asked for, and their phases
-    uint32_t marked = 0, land_par = 0;  // the same of `landed`, the phase after
-    bool q_armed = false, bad = false;
-    auto wait = [&](uint64_t* bar, uint32_t parity, int where) {
-      if (!pf_wait(bar, parity, a.err, abort_flag, where)) bad = true;
-      return !bad;
-    };
-    // One half (kChan channels) of tile kt of K or V into the next ring slot; of a pair, this CTA's
-    // half of the tile.
-    auto load = [&](bool is_v, const PfItem& it, int kt, int half, uint32_t mark) {
-      const int row_bits = kPair && !is_v ? 6 : 7;  // of a chunk
-      const int chunk_bits = S::kStageBits - 7 - row_bits;
-      const int first = kPair && !is_v ? rank << row_bits : 0;
-      const int chan = kPair ? (is_v ? rank * S::kChan : 0) : half * S::kChan;
-      // this lane's box, if any (16 at most, of 16 slots); its page is looked up ahead of the wait
-      const int box_bits = min(a.page_shift, row_bits);
-      const int x = me + kPfProducers * lane;
-      const bool copies = x < 1 << (row_bits - box_bits + chunk_bits);
-      static_assert(S::kStageBytes / (16 * 128) <= 32, "a box a lane");
-      const int c = x & ((1 << chunk_bits) - 1), r = x >> chunk_bits << box_bits;
-      const int j = kt * kPfKeys + first + r;
-      // a box outside the pool (past the last page, or of an entry that names none) is zeros
-      int pg = copies && j < it.len ? paged_page(a, a.table + (int64_t)it.b * a.s_table, j) : -1;
-      if (pg < 0) pg = a.n_pages;
-      if (!wait(&empty[stage], phase ^ 1, 610)) return;
-      // A slot with rows to be zeroed is full when that is done, a moment after its copies.
-      const bool any = __any_sync(0xffffffffu, mark != 0);
-      uint64_t* const bar = any ? &landed[stage] : &full[stage];
-      if (me == 0 && lane == 0) {
-        if (!kPair || any || rank == 0)
-          mbar_arrive_expect_tx(bar, (kPair && !any ? 2 : 1) << S::kStageBits);
-        else
-          tell_issuer(bar);
-      }
-      if (!any) {
-        armed |= 1u << stage;
-        armed_par = (armed_par & ~(1u << stage)) | (phase << stage);
-      } else {
-        marked |= 1u << stage;
-        land_par ^= 1u << stage;
-      }
-      __syncwarp();
-      uint8_t* const slot = smem + S::kRing + stage * S::kStageBytes;
-      if (copies) {
-        const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
-        uint8_t* const dst = slot + ((c << row_bits) + r) * 128;
-        const int in = j & ((1 << a.page_shift) - 1);
-        if (kPair && !any)
-          tma_load_4d_2sm(dst, tm, cluster_map(smem_u32(bar), 0), chan + c * 64, in, it.h, pg);
-        else
-          tma_load_4d(dst, tm, bar, chan + c * 64, in, it.h, pg);
-      }
-      if (any && me == 0) {
-        if (!wait(&landed[stage], ((land_par >> stage) & 1) ^ 1, 614)) return;
-        zero_rows(slot, 1 << chunk_bits, 1 << row_bits, first, mark);
-        if (lane == 0) {
-          if constexpr (kPair)
-            mbar_arrive_cluster(cluster_map(smem_u32(&full[stage]), 0));
-          else
-            mbar_arrive(&full[stage]);
-        }
-      }
-      if (++stage == kStages) {
-        stage = 0;
-        phase ^= 1;
-      }
-    };
-    PfBias beta;  // of the next tile of K
-    uint32_t mark[2] = {0, 0};  // of the tile of K loaded last and of the one before
-    // K of tile kt, tiles in order: which of its slots count is found out here
-    auto load_k = [&](const PfItem& it, int kt) {
-      uint32_t m = 0;
-      const int j = kt * kPfKeys + 4 * lane;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (j + e >= it.len || (kBias && beta.v[e] == -INFINITY)) m |= 1u << e;
-      if (kBias && kt + 1 < it.k1) beta.load(a, it, (kt + 1) * kPfKeys, lane);
-      mark[1] = mark[0];
-      mark[0] = m;
-      // without biases the row limits mask what K holds past the end
-#pragma unroll 1
-      for (int half = 0; half < kHalves && !bad; ++half) load(false, it, kt, half, kBias ? m : 0u);
-    };
-    PfWalk walk(a, PfRowItems{tokens}, start);
-    PfItem it;
-    while (!bad && !warp_flag(abort_flag) && walk.next(it)) {
-      if (it.k0 == it.k1) {  // its rows see nothing
-        if (me == 1 && rank == 0) zero_item(it);
-        continue;
-      }
-      if (me == 0 && !show(n_items, it)) {
-        bad = true;
-        break;
-      }
-      q_armed = true;
-      ++n_items;
-      if constexpr (kBias) beta.load(a, it, it.k0 * kPfKeys, lane);
-#pragma unroll 1
-      for (int kt = it.k0 - kAhead; kt < it.k1 && !bad; ++kt) {
-        if (kt >= it.k0) {
-          const uint32_t m = kAhead == 2 && kt + 1 < it.k1 ? mark[1] : mark[0];
-#pragma unroll 1
-          for (int half = 0; half < kHalves && !bad; ++half) load(true, it, kt, half, m);
-        }
-        if (kt + kAhead < it.k1 && !bad) load_k(it, kt + kAhead);
-      }
-    }
-    // The CTA may leave only when nothing is on its way into its shared memory: the last arrivals
-    // of the issuer's commits, or copies that nobody waited for.
-    if (me == 0 && lane == 0 && !bad) {
-      for (int i = 0; i < kStages && !bad && !*abort_flag; ++i) {
-        if (!mbar_wait(&empty[stage], phase ^ 1)) {
-          dev_set_error(a.err, DEV_WAIT_TIMEOUT, 612);
-          *abort_flag = 1;
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R::kOtherRegs));
+    if (kQuant && warp == 0) {
+      // ------------------------------------------------------------ items and their q
+      int n_items = 0;
+      bool bad = false, q_armed = false;
+      PfWalk walk(a, PfRowItems{tokens}, start);
+      PfItem it;
+      while (!bad && !warp_flag(abort_flag) && walk.next(it)) {
+        if (it.k0 == it.k1) continue;
+        if (!show(n_items, it)) {
           bad = true;
+          break;
+        }
+        q_armed = true;
+        ++n_items;
+      }
+      if (lane == 0) {
+        if (!bad) end_items(n_items);
+        if ((bad || *abort_flag) && q_armed)
+          (void)mbar_wait(&qfull[(n_items - 1) & 1], ((n_items - 1) >> 1) & 1);
+      }
+    } else if (kQuant && (warp == 2 || warp >= R::kFirst)) {
+      // ------------------------------------------------------------ codes, and codes to bf16
+      if constexpr (kQuant) {
+        if (warp == 2)
+          pf_fetch<D, kBias, kPair>(f, tokens, start, smem, tm_k, tm_v, abort_flag, rank,
+                                    [&](const PfItem& it) {
+                                      if (rank == 0) zero_item(it);
+                                    });
+        else
+          pf_convert<D, kBias, kPair>(f, tokens, start, smem, full, empty, abort_flag);
+      }
+    } else if (!kQuant && (warp == 0 || warp >= R::kFirst)) {
+      // ------------------------------------------------------------ TMA producers
+      const int me = warp == 0 ? 0 : warp - R::kFirst + 1;  // 0 also loads q, arms the barriers and zeroes rows
+      int stage = 0, n_items = 0;
+      uint32_t phase = 0;
+      uint32_t armed = 0, armed_par = 0;  // stages whose copies were asked for, and their phases
+      uint32_t marked = 0, land_par = 0;  // the same of `landed`, the phase after
+      bool q_armed = false, bad = false;
+      auto wait = [&](uint64_t* bar, uint32_t parity, int where) {
+        if (!pf_wait(bar, parity, a.err, abort_flag, where)) bad = true;
+        return !bad;
+      };
+      // One half (kChan channels) of tile kt of K or V into the next ring slot; of a pair, this CTA's
+      // half of the tile.
+      auto load = [&](bool is_v, const PfItem& it, int kt, int half, uint32_t mark) {
+        const int row_bits = kPair && !is_v ? 6 : 7;  // of a chunk
+        const int chunk_bits = S::kStageBits - 7 - row_bits;
+        const int first = kPair && !is_v ? rank << row_bits : 0;
+        const int chan = kPair ? (is_v ? rank * S::kChan : 0) : half * S::kChan;
+        // this lane's box, if any (16 at most, of 16 slots); its page is looked up ahead of the wait
+        const int box_bits = min(a.page_shift, row_bits);
+        const int x = me + kPfProducers * lane;
+        const bool copies = x < 1 << (row_bits - box_bits + chunk_bits);
+        static_assert(S::kStageBytes / (16 * 128) <= 32, "a box a lane");
+        const int c = x & ((1 << chunk_bits) - 1), r = x >> chunk_bits << box_bits;
+        const int j = kt * kPfKeys + first + r;
+        // a box outside the pool (past the last page, or of an entry that names none) is zeros
+        int pg = copies && j < it.len ? paged_page(a, a.table + (int64_t)it.b * a.s_table, j) : -1;
+        if (pg < 0) pg = a.n_pages;
+        if (!wait(&empty[stage], phase ^ 1, 610)) return;
+        // A slot with rows to be zeroed is full when that is done, a moment after its copies.
+        const bool any = __any_sync(0xffffffffu, mark != 0);
+        uint64_t* const bar = any ? &landed[stage] : &full[stage];
+        if (me == 0 && lane == 0) {
+          if (!kPair || any || rank == 0)
+            mbar_arrive_expect_tx(bar, (kPair && !any ? 2 : 1) << S::kStageBits);
+          else
+            tell_issuer(bar);
+        }
+        if (!any) {
+          armed |= 1u << stage;
+          armed_par = (armed_par & ~(1u << stage)) | (phase << stage);
+        } else {
+          marked |= 1u << stage;
+          land_par ^= 1u << stage;
+        }
+        __syncwarp();
+        uint8_t* const slot = smem + S::kRing + stage * S::kStageBytes;
+        if (copies) {
+          const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
+          uint8_t* const dst = slot + ((c << row_bits) + r) * 128;
+          const int in = j & ((1 << a.page_shift) - 1);
+          if (kPair && !any)
+            tma_load_4d_2sm(dst, tm, cluster_map(smem_u32(bar), 0), chan + c * 64, in, it.h, pg);
+          else
+            tma_load_4d(dst, tm, bar, chan + c * 64, in, it.h, pg);
+        }
+        if (any && me == 0) {
+          if (!wait(&landed[stage], ((land_par >> stage) & 1) ^ 1, 614)) return;
+          zero_rows(slot, 1 << chunk_bits, 1 << row_bits, first, mark);
+          if (lane == 0) {
+            if constexpr (kPair)
+              mbar_arrive_cluster(cluster_map(smem_u32(&full[stage]), 0));
+            else
+              mbar_arrive(&full[stage]);
+          }
         }
         if (++stage == kStages) {
           stage = 0;
           phase ^= 1;
         }
-      }
-      end_items(n_items);
-    }
-    // (The odd CTA's copies count on the even CTA's barriers: its own run out of time here, in
-    // which the copies land, as do the even CTA's where one of the two had asked for no more.)
-    if (lane == 0) {
-      if (bad || *abort_flag) {
-        for (int s = 0; s < kStages; ++s) {
-          if (armed & (1u << s)) (void)mbar_wait(&full[s], (armed_par >> s) & 1);
-          if (marked & (1u << s)) (void)mbar_wait(&landed[s], ((land_par >> s) & 1) ^ 1);
-        }
-        if (q_armed) (void)mbar_wait(&qfull[(n_items - 1) & 1], ((n_items - 1) >> 1) & 1);
-      }
-    }
-  } else if (warp == 1 && rank == 0 && elect_one()) {
-    // ------------------------------------------------------------ MMA issuer
-    constexpr uint32_t idesc_s = idesc_f16(128 * kSides, kPfKeys, 1);
-    constexpr uint32_t idesc_o = idesc_f16(128 * kSides, S::kChan * kSides, 1) | kIdescBMn;
-    int stage = 0;
-    uint32_t phase = 0;
-    uint32_t n_i = 0, n_odd = 0;  // uses of buffer 0 (two tiles: of both), of buffer 1
-    uint32_t n_items = 0;
-    bool bad = false, issued = false;
-    auto wait = [&](uint64_t* bar, uint32_t parity, int where) {
-      if (kPair ? mbar_wait_cluster(bar, parity) : mbar_wait(bar, parity)) return true;
-      dev_set_error(a.err, DEV_WAIT_TIMEOUT, where);
-      *abort_flag = 1;
-      bad = true;
-      return false;
-    };
-    // The next ring slot, loaded; -1 at a time-out.
-    auto take = [&]() -> int {
-      if (!wait(&full[stage], phase, 620)) return -1;
-      const int s = stage;
-      if (++stage == kStages) {
-        stage = 0;
-        phase ^= 1;
-      }
-      return s;
-    };
-    const uint64_t q_desc = sdesc_k_sw128(smem_u32(smem));
-    const uint64_t k_desc = sdesc_k_sw128(smem_u32(smem + S::kRing));
-    const uint64_t v_desc = sdesc_mn_sw128(smem_u32(smem + S::kRing), S::kChunkBytes);
-    constexpr uint64_t kChunkStep = S::kChunkBytes >> 4, kStageStep = S::kStageBytes >> 4;
-    constexpr uint64_t kKStep = S::kKRows * 128 >> 4;  // from 64 channels of K to the next
-    constexpr int kSChunks = D / 64 / kHalves;         // of a ring slot of K
-    auto commit = [&](uint64_t* bar) {  // on the barrier of either CTA
-      if constexpr (kPair)
-        tc_commit_2sm_mc(bar, 3);
-      else
-        tc_commit(bar);
-    };
-    // S of tile t into buffer buf, over the channels of one ring slot
-    auto mma_s = [&](int buf, int t, int half, int s) {
-      tc_fence_after();
-      const uint64_t q = q_desc + (t * (D / 64) + half * kSChunks) * kChunkStep;
-      const uint64_t k = k_desc + s * kStageStep;
-#pragma unroll
-      for (int c = 0; c < kSChunks; ++c)
+      };
+      PfBias beta;  // of the next tile of K
+      uint32_t mark[2] = {0, 0};  // of the tile of K loaded last and of the one before
+      // K of tile kt, tiles in order: which of its slots count is found out here
+      auto load_k = [&](const PfItem& it, int kt) {
+        uint32_t m = 0;
+        const int j = kt * kPfKeys + 4 * lane;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          (kPair ? tc_mma_f16_2sm : tc_mma_f16)(
-              tmem_base + buf * kSCols, q + c * kChunkStep + 2 * e, k + c * kKStep + 2 * e, idesc_s,
-              half + c + e > 0);
-      issued = true;
-    };
-    // O of tile t, the channels of one ring slot, += P in buffer buf times V
-    // (slots [16 e0, 16 e1) of the tile)
-    auto mma_o = [&](int buf, int t, int half, int s, bool first, int e0 = 0,
-                     int e1 = kPfKeys / 16) {
-      tc_fence_after();
-      const uint64_t v = v_desc + s * kStageStep;
-#pragma unroll
-      for (int e = e0; e < e1; ++e)
-        (kPair ? mma_ts_2sm : mma_ts)(tmem_base + kOAt + t * D + half * S::kChan,
-                                      tmem_base + buf * kSCols + kPAt + 8 * e,
-                                      v + e * (2048 >> 4), idesc_o, !first || e > e0);
-    };
-    while (!bad && !*abort_flag) {
-      if (!wait(&qfull[n_items & 1], (n_items >> 1) & 1, 621)) break;
-      const int n_k = shown[n_items & 1].k1 - shown[n_items & 1].k0;
-      if (n_k < 1) break;
-      if (kPair && !wait(qpeer, n_items & 1, 636)) break;
-      if constexpr (kTiles == 2) {
-        int ks = take();
-        if (ks < 0) break;
-        mma_s(0, 0, 0, ks);
-        commit(&sfull[0]);
-        mma_s(1, 1, 0, ks);
-        commit(&sfull[1]);
-        commit(&empty[ks]);
-        if (n_k == 1) commit(qfree);
+          if (j + e >= it.len || (kBias && beta.v[e] == -INFINITY)) m |= 1u << e;
+        if (kBias && kt + 1 < it.k1) beta.load(a, it, (kt + 1) * kPfKeys, lane);
+        mark[1] = mark[0];
+        mark[0] = m;
+        // without biases the row limits mask what K holds past the end
 #pragma unroll 1
-        for (int j = 0; j < n_k; ++j, ++n_i) {
-          const bool more = j + 1 < n_k;
-          const int vs = take();
-          if (vs < 0 || !wait(&phalf[0], n_i & 1, 622)) break;
-          if (j == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 623)) break;
-          mma_o(0, 0, 0, vs, j == 0, 4, 8);
-          if (!wait(&pfull[0], n_i & 1, 627)) break;
-          mma_o(0, 0, 0, vs, false, 0, 4);
-          commit(&pvdone[0]);
-          if (more) {
-            if ((ks = take()) < 0) break;
-            mma_s(0, 0, 0, ks);
-            commit(&sfull[0]);
-          }
-          if (!wait(&phalf[1], n_i & 1, 624)) break;
-          mma_o(1, 1, 0, vs, j == 0, 4, 8);
-          if (!wait(&pfull[1], n_i & 1, 628)) break;
-          mma_o(1, 1, 0, vs, false, 0, 4);
-          commit(&pvdone[1]);
-          commit(&empty[vs]);
-          if (more) {
-            mma_s(1, 1, 0, ks);
-            commit(&sfull[1]);
-            commit(&empty[ks]);
-            if (j + 2 == n_k) commit(qfree);
-          }
+        for (int half = 0; half < kHalves && !bad; ++half) load(false, it, kt, half, kBias ? m : 0u);
+      };
+      PfWalk walk(a, PfRowItems{tokens}, start);
+      PfItem it;
+      while (!bad && !warp_flag(abort_flag) && walk.next(it)) {
+        if (it.k0 == it.k1) {  // its rows see nothing
+          if (me == 1 && rank == 0) zero_item(it);
+          continue;
         }
-      } else {
-        // S and P take buffers 0 and 1 in turn, from 0 on in every item (constants: with a buffer
-        // and a half that the loop counts, issuing takes longer than the products)
-        auto make_s = [&](auto buf, int i) {
-#pragma unroll
-          for (int half = 0; half < kHalves; ++half) {
-            const int s = take();
-            if (s < 0) return;
-            mma_s(buf, 0, half, s);
-            commit(&empty[s]);
-          }
-          commit(&sfull[buf]);
-          if (i + 1 == n_k) commit(qfree);
-        };
-        auto add_pv = [&](auto buf, uint32_t& uses, int i) {
-          if (!wait(&phalf[buf], uses & 1, 625)) return;
-          if (i == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 626)) return;
-          int vs[kHalves];
-#pragma unroll
-          for (int half = 0; half < kHalves; ++half) {
-            if ((vs[half] = take()) < 0) return;
-            mma_o(buf, 0, half, vs[half], i == 0, 4, 8);
-          }
-          if (!wait(&pfull[buf], uses & 1, 635)) return;
-#pragma unroll
-          for (int half = 0; half < kHalves; ++half) {
-            mma_o(buf, 0, half, vs[half], false, 0, 4);
-            commit(&empty[vs[half]]);
-          }
-          commit(&pvdone[buf]);
-          ++uses;
-        };
-        constexpr std::integral_constant<int, 0> b0;
-        constexpr std::integral_constant<int, 1> b1;
-        make_s(b0, 0);
-        if (n_k > 1 && !bad) make_s(b1, 1);
+        if (me == 0 && !show(n_items, it)) {
+          bad = true;
+          break;
+        }
+        q_armed = true;
+        ++n_items;
+        if constexpr (kBias) beta.load(a, it, it.k0 * kPfKeys, lane);
 #pragma unroll 1
-        for (int i = 0; i < n_k && !bad; i += 2) {
-          add_pv(b0, n_i, i);
-          if (i + 2 < n_k && !bad) make_s(b0, i + 2);
-          if (i + 1 == n_k || bad) break;
-          add_pv(b1, n_odd, i + 1);
-          if (i + 3 < n_k && !bad) make_s(b1, i + 3);
+        for (int kt = it.k0 - kAhead; kt < it.k1 && !bad; ++kt) {
+          if (kt >= it.k0) {
+            const uint32_t m = kAhead == 2 && kt + 1 < it.k1 ? mark[1] : mark[0];
+#pragma unroll 1
+            for (int half = 0; half < kHalves && !bad; ++half) load(true, it, kt, half, m);
+          }
+          if (kt + kAhead < it.k1 && !bad) load_k(it, kt + kAhead);
         }
       }
-      ++n_items;
-    }
-    if ((bad || *abort_flag) && issued) {
-      commit(drain);
-      (void)mbar_wait(drain, 0);
-    }
-  } else if (kPair && warp == 1 && rank == 1 && elect_one()) {
-    // ------------------------------------------------------------ q of the odd CTA
-    for (uint32_t n = 0; !*abort_flag; ++n) {
-      if (!mbar_wait(&qfull[n & 1], (n >> 1) & 1)) {
-        dev_set_error(a.err, DEV_WAIT_TIMEOUT, 637);
+      // The CTA may leave only when nothing is on its way into its shared memory: the last arrivals
+      // of the issuer's commits, or copies that nobody waited for.
+      if (me == 0 && lane == 0 && !bad) {
+        for (int i = 0; i < kStages && !bad && !*abort_flag; ++i) {
+          if (!mbar_wait(&empty[stage], phase ^ 1)) {
+            dev_set_error(a.err, DEV_WAIT_TIMEOUT, 612);
+            *abort_flag = 1;
+            bad = true;
+          }
+          if (++stage == kStages) {
+            stage = 0;
+            phase ^= 1;
+          }
+        }
+        end_items(n_items);
+      }
+      // (The odd CTA's copies count on the even CTA's barriers: its own run out of time here, in
+      // which the copies land, as do the even CTA's where one of the two had asked for no more.)
+      if (lane == 0) {
+        if (bad || *abort_flag) {
+          for (int s = 0; s < kStages; ++s) {
+            if (armed & (1u << s)) (void)mbar_wait(&full[s], (armed_par >> s) & 1);
+            if (marked & (1u << s)) (void)mbar_wait(&landed[s], ((land_par >> s) & 1) ^ 1);
+          }
+          if (q_armed) (void)mbar_wait(&qfull[(n_items - 1) & 1], ((n_items - 1) >> 1) & 1);
+        }
+      }
+    } else if (warp == 1 && rank == 0 && elect_one()) {
+      // ------------------------------------------------------------ MMA issuer
+      constexpr uint32_t idesc_s = idesc_f16(128 * kSides, kPfKeys, 1);
+      constexpr uint32_t idesc_o = idesc_f16(128 * kSides, S::kChan * kSides, 1) | kIdescBMn;
+      int stage = 0;
+      uint32_t phase = 0;
+      uint32_t n_i = 0, n_odd = 0;  // uses of buffer 0 (two tiles: of both), of buffer 1
+      uint32_t n_items = 0;
+      bool bad = false, issued = false;
+      auto wait = [&](uint64_t* bar, uint32_t parity, int where) {
+        if (kPair ? mbar_wait_cluster(bar, parity) : mbar_wait(bar, parity)) return true;
+        dev_set_error(a.err, DEV_WAIT_TIMEOUT, where);
         *abort_flag = 1;
-        break;
+        bad = true;
+        return false;
+      };
+      // The next ring slot, loaded; -1 at a time-out.
+      auto take = [&]() -> int {
+        if (!wait(&full[stage], phase, 620)) return -1;
+        const int s = stage;
+        if (++stage == kStages) {
+          stage = 0;
+          phase ^= 1;
+        }
+        return s;
+      };
+      const uint64_t q_desc = sdesc_k_sw128(smem_u32(smem));
+      const uint64_t k_desc = sdesc_k_sw128(smem_u32(smem + S::kRing));
+      const uint64_t v_desc = sdesc_mn_sw128(smem_u32(smem + S::kRing), S::kChunkBytes);
+      constexpr uint64_t kChunkStep = S::kChunkBytes >> 4, kStageStep = S::kStageBytes >> 4;
+      constexpr uint64_t kKStep = S::kKRows * 128 >> 4;  // from 64 channels of K to the next
+      constexpr int kSChunks = D / 64 / kHalves;         // of a ring slot of K
+      auto commit = [&](uint64_t* bar) {  // on the barrier of either CTA
+        if constexpr (kPair)
+          tc_commit_2sm_mc(bar, 3);
+        else
+          tc_commit(bar);
+      };
+      // S of tile t into buffer buf, over the channels of one ring slot
+      auto mma_s = [&](int buf, int t, int half, int s) {
+        tc_fence_after();
+        const uint64_t q = q_desc + (t * (D / 64) + half * kSChunks) * kChunkStep;
+        const uint64_t k = k_desc + s * kStageStep;
+#pragma unroll
+        for (int c = 0; c < kSChunks; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            (kPair ? tc_mma_f16_2sm : tc_mma_f16)(
+                tmem_base + buf * kSCols, q + c * kChunkStep + 2 * e, k + c * kKStep + 2 * e, idesc_s,
+                half + c + e > 0);
+        issued = true;
+      };
+      // O of tile t, the channels of one ring slot, += P in buffer buf times V
+      // (slots [16 e0, 16 e1) of the tile)
+      auto mma_o = [&](int buf, int t, int half, int s, bool first, int e0 = 0,
+                       int e1 = kPfKeys / 16) {
+        tc_fence_after();
+        const uint64_t v = v_desc + s * kStageStep;
+#pragma unroll
+        for (int e = e0; e < e1; ++e)
+          (kPair ? mma_ts_2sm : mma_ts)(tmem_base + kOAt + t * D + half * S::kChan,
+                                        tmem_base + buf * kSCols + kPAt + 8 * e,
+                                        v + e * (2048 >> 4), idesc_o, !first || e > e0);
+      };
+      while (!bad && !*abort_flag) {
+        if (!wait(&qfull[n_items & 1], (n_items >> 1) & 1, 621)) break;
+        const int n_k = shown[n_items & 1].k1 - shown[n_items & 1].k0;
+        if (n_k < 1) break;
+        if (kPair && !wait(qpeer, n_items & 1, 636)) break;
+        if constexpr (kTiles == 2) {
+          int ks = take();
+          if (ks < 0) break;
+          mma_s(0, 0, 0, ks);
+          commit(&sfull[0]);
+          mma_s(1, 1, 0, ks);
+          commit(&sfull[1]);
+          commit(&empty[ks]);
+          if (n_k == 1) commit(qfree);
+#pragma unroll 1
+          for (int j = 0; j < n_k; ++j, ++n_i) {
+            const bool more = j + 1 < n_k;
+            const int vs = take();
+            if (vs < 0 || !wait(&phalf[0], n_i & 1, 622)) break;
+            if (j == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 623)) break;
+            mma_o(0, 0, 0, vs, j == 0, 4, 8);
+            if (!wait(&pfull[0], n_i & 1, 627)) break;
+            mma_o(0, 0, 0, vs, false, 0, 4);
+            commit(&pvdone[0]);
+            if (more) {
+              if ((ks = take()) < 0) break;
+              mma_s(0, 0, 0, ks);
+              commit(&sfull[0]);
+            }
+            if (!wait(&phalf[1], n_i & 1, 624)) break;
+            mma_o(1, 1, 0, vs, j == 0, 4, 8);
+            if (!wait(&pfull[1], n_i & 1, 628)) break;
+            mma_o(1, 1, 0, vs, false, 0, 4);
+            commit(&pvdone[1]);
+            commit(&empty[vs]);
+            if (more) {
+              mma_s(1, 1, 0, ks);
+              commit(&sfull[1]);
+              commit(&empty[ks]);
+              if (j + 2 == n_k) commit(qfree);
+            }
+          }
+        } else {
+          // S and P take buffers 0 and 1 in turn, from 0 on in every item (constants: with a buffer
+          // and a half that the loop counts, issuing takes longer than the products)
+          auto make_s = [&](auto buf, int i) {
+#pragma unroll
+            for (int half = 0; half < kHalves; ++half) {
+              const int s = take();
+              if (s < 0) return;
+              mma_s(buf, 0, half, s);
+              commit(&empty[s]);
+            }
+            commit(&sfull[buf]);
+            if (i + 1 == n_k) commit(qfree);
+          };
+          auto add_pv = [&](auto buf, uint32_t& uses, int i) {
+            if (!wait(&phalf[buf], uses & 1, 625)) return;
+            if (i == 0 && n_items > 0 && !wait(ofree, (n_items - 1) & 1, 626)) return;
+            int vs[kHalves];
+#pragma unroll
+            for (int half = 0; half < kHalves; ++half) {
+              if ((vs[half] = take()) < 0) return;
+              mma_o(buf, 0, half, vs[half], i == 0, 4, 8);
+            }
+            if (!wait(&pfull[buf], uses & 1, 635)) return;
+#pragma unroll
+            for (int half = 0; half < kHalves; ++half) {
+              mma_o(buf, 0, half, vs[half], false, 0, 4);
+              commit(&empty[vs[half]]);
+            }
+            commit(&pvdone[buf]);
+            ++uses;
+          };
+          constexpr std::integral_constant<int, 0> b0;
+          constexpr std::integral_constant<int, 1> b1;
+          make_s(b0, 0);
+          if (n_k > 1 && !bad) make_s(b1, 1);
+#pragma unroll 1
+          for (int i = 0; i < n_k && !bad; i += 2) {
+            add_pv(b0, n_i, i);
+            if (i + 2 < n_k && !bad) make_s(b0, i + 2);
+            if (i + 1 == n_k || bad) break;
+            add_pv(b1, n_odd, i + 1);
+            if (i + 3 < n_k && !bad) make_s(b1, i + 3);
+          }
+        }
+        ++n_items;
       }
-      if (shown[n & 1].k1 <= shown[n & 1].k0) break;
-      mbar_arrive_cluster(cluster_map(smem_u32(qpeer), 0));
+      if ((bad || *abort_flag) && issued) {
+        commit(drain);
+        (void)mbar_wait(drain, 0);
+      }
+    } else if (kPair && warp == 1 && rank == 1 && elect_one()) {
+      // ------------------------------------------------------------ q of the odd CTA
+      for (uint32_t n = 0; !*abort_flag; ++n) {
+        if (!mbar_wait(&qfull[n & 1], (n >> 1) & 1)) {
+          dev_set_error(a.err, DEV_WAIT_TIMEOUT, 637);
+          *abort_flag = 1;
+          break;
+        }
+        if (shown[n & 1].k1 <= shown[n & 1].k0) break;
+        mbar_arrive_cluster(cluster_map(smem_u32(qpeer), 0));
+      }
     }
-  } else if (warp >= R::kSoftmax) {
+  } else {
+    if constexpr (kQuant)
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R::kSoftmaxRegs));
     // ------------------------------------------------------------ softmax and output
     constexpr int kOCols = S::kOCols;
     const int sw = warp - R::kSoftmax;
@@ -1194,9 +1267,9 @@ __global__ void __launch_bounds__(256)
 template <int D, bool kBias, bool kPair, bool kQuant>
 cudaError_t launch_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
                            const KernelTable& dev, cudaStream_t s) {
-  using S = PfShape<D, kBias, kPair>;
+  using S = PfShape<D, kBias, kPair, kQuant>;
   constexpr int kCluster = kPair ? 2 : 1;
-  constexpr int threads = PfRoles<kQuant>::kThreads;
+  constexpr int threads = PfRoles<kBias, kQuant>::kThreads;
   constexpr auto kernel = paged_prefill_kernel<D, kBias, kPair, kQuant>;
   using Id = KernelId<kernel, threads, S::kBytes, kCluster>;
   if (dev.of<Id>().status != cudaSuccess) return dev.of<Id>().status;
@@ -1211,8 +1284,9 @@ cudaError_t launch_prefill(const PagedArgs& a, const PagedQuery& q, void* ws,
   f.split = reinterpret_cast<PfSplit*>(f.part_ml + (int64_t)2 * ranges * rows);
   CUtensorMap tq, tk, tv;
   if (!query_tmap(&tq, a, q, f.tile_tokens)) return cudaErrorInvalidValue;
-  tk = tv = tq;  // (not read)
-  if (!kQuant && (!pool_tmap(&tk, a, a.K, S::kKRows) || !pool_tmap(&tv, a, a.V, kPfKeys)))
+  if (kQuant ? !codes_tmap(&tk, a, a.K8, kPair ? D : S::kChan, S::kKRows) ||
+                   !codes_tmap(&tv, a, a.V8, S::kChan, kPfKeys)
+             : !pool_tmap(&tk, a, a.K, S::kKRows) || !pool_tmap(&tv, a, a.V, kPfKeys))
     return cudaErrorInvalidValue;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;

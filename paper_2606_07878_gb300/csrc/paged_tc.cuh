@@ -311,6 +311,21 @@ bool pool_tmap(CUtensorMap* m, const PagedArgs& a, const void* ptr, int rows) {
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same of a pool in 8 bits: boxes of `chan` channels, rows of `chan` bytes.
+bool codes_tmap(CUtensorMap* m, const PagedArgs& a, const void* ptr, int chan, int rows) {
+  auto enc = tensor_map_encoder();
+  if (enc == nullptr) return false;
+  const cuuint64_t page = (cuuint64_t)1 << a.page_shift;
+  cuuint64_t dims[4] = {(cuuint64_t)a.d, page, (cuuint64_t)a.H, (cuuint64_t)a.n_pages};
+  cuuint64_t strides[3] = {(cuuint64_t)a.s_slot, (cuuint64_t)a.s_head, (cuuint64_t)a.s_page};
+  cuuint32_t box[4] = {(cuuint32_t)chan, (cuuint32_t)std::min<cuuint64_t>(page, rows), 1, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(ptr), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool query_tmap(CUtensorMap* m, const PagedArgs& a, const PagedQuery& q, int tokens) {
   auto enc = tensor_map_encoder();
   if (enc == nullptr) return false;
