@@ -100,8 +100,8 @@ struct PfPlan {  // in shared memory
 };
 
 // The warps of a CTA. Of a pool in 8 bits two warpgroups convert codes, and the softmax warps begin
-// at a warpgroup of their own, so that registers can be dealt out: 5 x 128 threads of 96 each become
-// 144 for the softmax and 64 for all others, 152 and 56 with biases.
+// at a warpgroup of their own, so that registers can be dealt out: 5 x 128 threads of 96 each
+// become 144 for the softmax and 64 for all others, 152 and 56 with biases.
 template <bool kBias, bool kQuant>
 struct PfRoles {
   static constexpr int kThreads = kQuant ? 640 : 384;
@@ -114,6 +114,7 @@ struct PfRoles {
 struct PfRaw {
   float scale[kPfKeys / kScaleBlock];  // of its 16 slots each
   uint32_t counts[4];                  // bit i of word e: slot 4 i + e counts
+  int32_t kind[4];                     // [0]: of keys (0), of values (1), none any more (2)
 };
 
 template <int D, bool kBias, bool kPair, bool kQuant>
@@ -195,9 +196,10 @@ struct PfUnits {
 };
 
 // A pool in 8 bits: a warp fetches codes into a ring of their own (TMA, a box per page), with their
-// scales and which slots count, one slot ahead of the copies; two warpgroups multiply codes by their
-// block's scale and store bf16 as TMA would have (rows of 128 bytes, 128-byte swizzle). Everything
-// behind works as for a pool in bf16. With scales that are powers of two nothing is rounded.
+// scales and which slots count, one slot ahead of the copies; two warpgroups multiply codes by
+// their block's scale and store bf16 as TMA would have (rows of 128 bytes, 128-byte swizzle).
+// Everything behind works as for a pool in bf16. With scales that are powers of two nothing is
+// rounded.
 template <int D, bool kBias, bool kPair, class Zero>
 STILL_DEV void pf_fetch(const PrefillParams& f, int tokens, const PfStart& start, uint8_t* smem,
                         const CUtensorMap& tm_k, const CUtensorMap& tm_v, volatile int* abort_flag,
@@ -214,7 +216,8 @@ STILL_DEV void pf_fetch(const PrefillParams& f, int tokens, const PfStart& start
   auto first_of = [&](const PfUnit& u) {  // slot of its first row
     return u.kt * kPfKeys + (kPair && !u.v ? rank * S::kKRows : 0);
   };
-  // Lane i: the page of its i-th 16 slots (-1: none), the scale there; which of slots 4 i + e count.
+  // Lane i: the page of its i-th 16 slots (-1: none), the scale there; which of slots 4 i + e
+  // count.
   auto page_of = [&](const PfUnit& u) {
     const int j = first_of(u) + kScaleBlock * lane;
     if (kScaleBlock * lane >= rows_of(u) || j >= u.len) return -1;
@@ -252,6 +255,7 @@ STILL_DEV void pf_fetch(const PrefillParams& f, int tokens, const PfStart& start
       break;
     }
     if (lane < kPfKeys / kScaleBlock) info[raw].scale[lane] = scale;
+    if (lane == 0) info[raw].kind[0] = u.v;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const uint32_t w = __ballot_sync(0xffffffffu, (counts >> e) & 1);
@@ -278,17 +282,12 @@ STILL_DEV void pf_fetch(const PrefillParams& f, int tokens, const PfStart& start
     pg = then_pg;
     ok = more;
   }
-  // Nobody leaves before the copies have landed: the converters have read them all, or waits here.
+  // The end; copies have landed when the converters have come so far, or by the waits below.
+  if (!bad && !pf_wait(&raw_empty[raw], phase ^ 1, a.err, abort_flag, 618)) bad = true;
   if (lane == 0) {
-    for (int i = 0; i < S::kRaws && !bad && !*abort_flag; ++i) {
-      if (!mbar_wait(&raw_empty[raw], phase ^ 1)) {
-        dev_set_error(a.err, DEV_WAIT_TIMEOUT, 618);
-        *abort_flag = 1;
-      }
-      if (++raw == S::kRaws) {
-        raw = 0;
-        phase ^= 1;
-      }
+    if (!bad) {
+      info[raw].kind[0] = 2;
+      mbar_arrive(&raw_full[raw]);
     }
     if (bad || *abort_flag)
       for (int i = 0; i < S::kRaws; ++i)
@@ -297,33 +296,35 @@ STILL_DEV void pf_fetch(const PrefillParams& f, int tokens, const PfStart& start
 }
 
 template <int D, bool kBias, bool kPair>
-STILL_DEV void pf_convert(const PrefillParams& f, int tokens, const PfStart& start, uint8_t* smem,
-                          uint64_t* full, uint64_t* empty, volatile int* abort_flag) {
+STILL_DEV void pf_convert(const PagedArgs& a, uint8_t* smem, uint64_t* full, uint64_t* empty,
+                          volatile int* abort_flag) {
   using S = PfShape<D, kBias, kPair, true>;
   constexpr int kStages = S::kStages;
   constexpr int kPieces = S::kRawBytes / 16 / (32 * kPfConverters);  // of 16 codes, of a thread
-  const PagedArgs& a = f.a;
   const int lane = threadIdx.x & 31;
   const int me = threadIdx.x - 32 * PfRoles<kBias, true>::kFirst;
   uint64_t* const raw_full = reinterpret_cast<uint64_t*>(smem + S::kRawBarAt);
   uint64_t* const raw_empty = raw_full + S::kRaws;
   const PfRaw* const info = reinterpret_cast<const PfRaw*>(smem + S::kRawInfoAt);
-  PfUnits<S::kHalves, S::kTiles == 2 ? 1 : 2> units{PfWalk(a, PfRowItems{tokens}, start)};
   int stage = 0, raw = 0;
   uint32_t phase = 0, raw_phase = 0;
   bool bad = false;
-  PfUnit u{};
 #pragma unroll 1
-  while (units.next(u, abort_flag, [](const PfItem&) {})) {
-    const bool k_half = kPair && !u.v;  // 64 rows of 256 channels
+  while (!warp_flag(abort_flag)) {
+    if (!pf_wait(&raw_full[raw], raw_phase, a.err, abort_flag, 619)) {
+      bad = true;
+      break;
+    }
+    const int kind = info[raw].kind[0];
+    if (kind == 2) break;
+    const bool k_half = kPair && kind == 0;  // 64 rows of 256 channels
     const int bits = k_half ? 4 : S::kChan == 64 ? 2 : 3, row_bits = k_half ? 6 : 7;
-    if (!pf_wait(&raw_full[raw], raw_phase, a.err, abort_flag, 619)) bad = true;
     const uint8_t* const from = smem + S::kRawAt + raw * S::kRawBytes;
     uint4 x[kPieces];
 #pragma unroll
     for (int i = 0; i < kPieces; ++i)
       x[i] = *reinterpret_cast<const uint4*>(from + 16 * (me + i * 32 * kPfConverters));
-    if (bad || !pf_wait(&empty[stage], phase ^ 1, a.err, abort_flag, 610)) {
+    if (!pf_wait(&empty[stage], phase ^ 1, a.err, abort_flag, 610)) {
       bad = true;
       break;
     }
@@ -493,8 +494,8 @@ __global__ void __launch_bounds__(PfRoles<kBias, kQuant>::kThreads, 1)
     }
   }
   // no range is shorter than an item's beginning and a tile
-  pf_plan<R::kThreads>(a, PfRowItems{tokens}, cta, kPair ? gridDim.x / 2 : gridDim.x, start, warp_cost,
-                      rank == 0 ? &f.split[cta] : nullptr);
+  pf_plan<R::kThreads>(a, PfRowItems{tokens}, cta, kPair ? gridDim.x / 2 : gridDim.x, start,
+                       warp_cost, rank == 0 ? &f.split[cta] : nullptr);
   tc_fence_before();
   __syncthreads();
   if constexpr (kPair) {  // the other's barriers
@@ -594,11 +595,12 @@ __global__ void __launch_bounds__(PfRoles<kBias, kQuant>::kThreads, 1)
                                       if (rank == 0) zero_item(it);
                                     });
         else
-          pf_convert<D, kBias, kPair>(f, tokens, start, smem, full, empty, abort_flag);
+          pf_convert<D, kBias, kPair>(a, smem, full, empty, abort_flag);
       }
     } else if (!kQuant && (warp == 0 || warp >= R::kFirst)) {
       // ------------------------------------------------------------ TMA producers
-      const int me = warp == 0 ? 0 : warp - R::kFirst + 1;  // 0 also loads q, arms the barriers and zeroes rows
+      // 0 also loads q, arms the barriers and zeroes rows
+      const int me = warp == 0 ? 0 : warp - R::kFirst + 1;
       int stage = 0, n_items = 0;
       uint32_t phase = 0;
       uint32_t armed = 0, armed_par = 0;  // stages whose copies were asked for, and their phases
@@ -608,14 +610,15 @@ __global__ void __launch_bounds__(PfRoles<kBias, kQuant>::kThreads, 1)
         if (!pf_wait(bar, parity, a.err, abort_flag, where)) bad = true;
         return !bad;
       };
-      // One half (kChan channels) of tile kt of K or V into the next ring slot; of a pair, this CTA's
-      // half of the tile.
+      // One half (kChan channels) of tile kt of K or V into the next ring slot; of a pair, this
+      // CTA's half of the tile.
       auto load = [&](bool is_v, const PfItem& it, int kt, int half, uint32_t mark) {
         const int row_bits = kPair && !is_v ? 6 : 7;  // of a chunk
         const int chunk_bits = S::kStageBits - 7 - row_bits;
         const int first = kPair && !is_v ? rank << row_bits : 0;
         const int chan = kPair ? (is_v ? rank * S::kChan : 0) : half * S::kChan;
-        // this lane's box, if any (16 at most, of 16 slots); its page is looked up ahead of the wait
+        // this lane's box, if any (16 at most, of 16 slots); its page is looked up ahead of the
+        // wait
         const int box_bits = min(a.page_shift, row_bits);
         const int x = me + kPfProducers * lane;
         const bool copies = x < 1 << (row_bits - box_bits + chunk_bits);
@@ -682,7 +685,8 @@ __global__ void __launch_bounds__(PfRoles<kBias, kQuant>::kThreads, 1)
         mark[0] = m;
         // without biases the row limits mask what K holds past the end
 #pragma unroll 1
-        for (int half = 0; half < kHalves && !bad; ++half) load(false, it, kt, half, kBias ? m : 0u);
+        for (int half = 0; half < kHalves && !bad; ++half)
+          load(false, it, kt, half, kBias ? m : 0u);
       };
       PfWalk walk(a, PfRowItems{tokens}, start);
       PfItem it;
@@ -783,8 +787,8 @@ __global__ void __launch_bounds__(PfRoles<kBias, kQuant>::kThreads, 1)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             (kPair ? tc_mma_f16_2sm : tc_mma_f16)(
-                tmem_base + buf * kSCols, q + c * kChunkStep + 2 * e, k + c * kKStep + 2 * e, idesc_s,
-                half + c + e > 0);
+                tmem_base + buf * kSCols, q + c * kChunkStep + 2 * e, k + c * kKStep + 2 * e,
+                idesc_s, half + c + e > 0);
         issued = true;
       };
       // O of tile t, the channels of one ring slot, += P in buffer buf times V
