@@ -263,17 +263,25 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
     const int in = e0 & mask, most = end - e0 - 1;
     const int64_t page = max(pg, 0);
     const __nv_bfloat16* base = a.K + page * a.s_page + (int64_t)h * a.s_head + 8 * lj;
-    const uint8_t* codes = a.K8 + page * a.s_page + (int64_t)h * a.s_head + 16 * lj;
-    if constexpr (kE4m3) ks = a.k_scale[scale_at(page, h, in)];
+    if constexpr (kE4m3) {
+      const int64_t at = scale_at(page, h, in);
+      ks = a.k_scale[at];
+      vs = a.v_scale[at];
+      // (a batch that is whole takes two additions where `min` takes two products)
+      const uint8_t* codes =
+          a.K8 + page * a.s_page + in * a.s_slot + (int64_t)h * a.s_head + 16 * lj;
+      const uint8_t* row = codes + min(lg, most) * a.s_slot;
+#pragma unroll
+      for (int c = 0; c < kKx; ++c) kx[0][c] = ld_once(row + 64 * c);
+      row = most >= 15 ? row + 8 * a.s_slot : codes + min(lg + 8, most) * a.s_slot;
+#pragma unroll
+      for (int c = 0; c < kKx; ++c) kx[1][c] = ld_once(row + 64 * c);
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int r = in + min(lg + 8 * i, most);
 #pragma unroll
-      for (int c = 0; c < kKx; ++c)
-        if constexpr (kE4m3)
-          kx[i][c] = ld_once(codes + r * a.s_slot + 64 * c);
-        else
-          kx[i][c] = ld_once(base + r * a.s_slot + 32 * c);
+      for (int c = 0; !kE4m3 && c < kKx; ++c) kx[i][c] = ld_once(base + r * a.s_slot + 32 * c);
       bias[i] = pg < 0               ? -INFINITY
                 : a.beta != nullptr ? a.beta[page * beta_page + ((int64_t)h << a.page_shift) + r]
                                     : 0.f;
@@ -284,19 +292,22 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
     if constexpr (kE4m3) {
       const int64_t page = max(pg, 0);
       constexpr int kLane = D < 256 ? D / 8 : 16;  // contiguous channels of a lane
-      const uint8_t* codes = a.V8 + page * a.s_page + (int64_t)h * a.s_head + kLane * lg;
-      vs = a.v_scale[scale_at(page, h, in)];
+      const uint8_t* codes =
+          a.V8 + page * a.s_page + in * a.s_slot + (int64_t)h * a.s_head + kLane * lg;
+      const uint8_t* first = codes + 2 * lj * a.s_slot;
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        const int r = in + min(2 * lj + (v & 1) + 8 * (v >> 1), most);
+        const uint8_t* row = most >= 15 ? first + ((v & 1) + 8 * (v >> 1)) * a.s_slot
+                                        : codes + min(2 * lj + (v & 1) + 8 * (v >> 1), most) *
+                                                      a.s_slot;
         if constexpr (D == 64) {
-          const uint2 x = __ldcs(reinterpret_cast<const uint2*>(codes + r * a.s_slot));
+          const uint2 x = __ldcs(reinterpret_cast<const uint2*>(row));
           vq[v][0] = x.x;
           vq[v][1] = x.y;
         } else {
 #pragma unroll
           for (int x = 0; x < D / 128; ++x) {
-            const uint4 y = ld_once(codes + r * a.s_slot + 128 * x);
+            const uint4 y = ld_once(row + 128 * x);
 #pragma unroll
             for (int w = 0; w < 4; ++w) vq[v][4 * x + w] = word(y, w);
           }
@@ -318,7 +329,8 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
   float m[NB][2], l[NB][2];   // rows 2 lj, 2 lj + 1 of a block; l: this lane's share
   // O^T: rows 2 lj (+1); channels 64 x + 8 lg + 2 w (+1), of e4m3 those of four_at
   float o[NB][kStats ? 1 : D / 64][4][4];
-  float rho[NB][2], fq[NB][2];  // e4m3: what O and the products with q are multiples of
+  // e4m3: what O and the products with q are multiples of, the first one's inverse
+  float rho[NB][2], by_rho[NB][2], fq[NB][2];
   // the first of the four channels that groups 2 t and 2 t + 1 (group 4 x + w) hold
   auto four_at = [&](int t) {
     if constexpr (kE4m3 && D == 256) return 128 * (t >> 2) + 16 * lg + 4 * (t & 3);
@@ -389,7 +401,7 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
     for (int k = 0; k < NB; ++k) {
       m[k][0] = m[k][1] = -INFINITY;
       l[k][0] = l[k][1] = 0.f;
-      rho[k][0] = rho[k][1] = 0.f;
+      rho[k][0] = rho[k][1] = by_rho[k][0] = by_rho[k][1] = 0.f;
 #pragma unroll
       for (int x = 0; x < (kStats ? 1 : D / 64); ++x)
 #pragma unroll
@@ -406,6 +418,7 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
     float c[NB][4];
     const float b0 = bias[0], b1 = bias[1];
     [[maybe_unused]] const float kscale = ks;
+    [[maybe_unused]] float vscale = vs;
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
       float c2[4] = {0.f, 0.f, 0.f, 0.f};
@@ -445,6 +458,7 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
               vq[v][x] = 0;
             else
               vx[v][x] = make_uint4(0, 0, 0, 0);
+      if ((dead0 & dead1) == 0xffffffffu) vscale = 0.f;  // (it may be anything)
     }
     [[maybe_unused]] uint32_t hi[NB][2], lo[NB][2];
 #pragma unroll
@@ -475,11 +489,14 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
           const float f = n == m[k][e] ? 1.f : exp2f((m[k][e] - n) * kLog2e);
           m[k][e] = n;
           l[k][e] *= f;
-          if constexpr (kE4m3) {
+          const bool in_rho = kE4m3 && rho[k][e] * f >= 0x1p-126f;  // O is brought along by it
+          if (in_rho) {
             rho[k][e] *= f;
-          } else if constexpr (!kStats) {
+            by_rho[k][e] = 1.f / rho[k][e];
+          }
+          if (!kStats && !in_rho) {
 #pragma unroll
-            for (int x = 0; x < D / 64; ++x)
+            for (int x = 0; x < (kStats ? 0 : D / 64); ++x)
 #pragma unroll
               for (int w = 0; w < 4; ++w) {
                 o[k][x][w][e] *= f;
@@ -488,23 +505,21 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
           }
         }
       }
-      // e4m3: O is a multiple of rho, and a weight times the batch's scale of V enters as a multiple
-      // of it too. rho is raised when one of them would pass 2^8.
+      // e4m3: O is a multiple of rho, and a weight times the batch's scale of V enters
+      // as a multiple of it too. rho is raised when one of them would pass 2^8 (and how large they
+      // are is looked at where the scale alone does).
       [[maybe_unused]] float by_v[2] = {1.f, 1.f};
       if constexpr (kE4m3) {
-        float up[2];
-        bool raise = false;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          up[e] = top[e] == -INFINITY ? 0.f : vs * exp2f((top[e] - m[k][e]) * kLog2e);
-          raise |= up[e] > 256.f * rho[k][e];
-        }
-        if (__any_sync(0xffffffffu, raise)) {
+        if (__any_sync(0xffffffffu, vscale > 256.f * rho[k][0] || vscale > 256.f * rho[k][1])) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            if (!(up[e] > 256.f * rho[k][e])) continue;
-            const float f = rho[k][e] / up[e];
-            rho[k][e] = up[e];
+            const float up =
+                top[e] == -INFINITY ? 0.f : vscale * ex2_ftz((top[e] - m[k][e]) * kLog2e);
+            if (!(up > 256.f * rho[k][e])) continue;
+            const float next = fmaxf(up, 0x1p-126f);  // it has an inverse
+            const float f = rho[k][e] / next;
+            rho[k][e] = next;
+            by_rho[k][e] = 1.f / next;
 #pragma unroll
             for (int x = 0; x < D / 64; ++x)
 #pragma unroll
@@ -515,7 +530,7 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
           }
         }
 #pragma unroll
-        for (int e = 0; e < 2; ++e) by_v[e] = up[e] > 0.f ? vs / rho[k][e] : 0.f;
+        for (int e = 0; e < 2; ++e) by_v[e] = vscale * by_rho[k][e];
       }
       if constexpr (kKind == kRowsWeigh) {  // (a batch lies in one page)
         const int64_t row = (page_now * a.H + head_now) * g + row_now + 8 * k + 2 * lj;
@@ -530,8 +545,8 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
       const float by1 = m[k][1] == -INFINITY ? 0.f : m[k][1];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float w0 = exp2f((c[k][2 * i] - by0) * kLog2e);
-        const float w1 = exp2f((c[k][2 * i + 1] - by1) * kLog2e);
+        const float x0 = (c[k][2 * i] - by0) * kLog2e, x1 = (c[k][2 * i + 1] - by1) * kLog2e;
+        const float w0 = kE4m3 ? ex2_ftz(x0) : exp2f(x0), w1 = kE4m3 ? ex2_ftz(x1) : exp2f(x1);
         l[k][0] += w0;
         l[k][1] += w1;
         if constexpr (kE4m3) {
