@@ -42,7 +42,7 @@ template <int kCluster>
 __global__ void __launch_bounds__(kChooseThreads, 1)
     paged_choose_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedEvict f,
                         int in_smem) {
-  extern __shared__ uint32_t keys[];
+  extern __shared__ __align__(16) uint32_t keys[];
   __shared__ uint32_t hist[2][kDigits];
   __shared__ uint32_t warp_sum[kChooseWarps], warp_equal[kChooseWarps];
   __shared__ uint32_t found[2];   // digit, kept among those above it
@@ -71,15 +71,23 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
   // slots [j0, j1) of this CTA
   const int per = ((s.len + kCluster - 1) / kCluster + 31) & ~31;
   const int j0 = min(s.len, (int)rank * per), j1 = min(s.len, j0 + per);
-  auto read = [&](int j) -> uint32_t {
-    if (j < f.sinks || j >= s.len - f.recent) return 0xffffffffu;
+  // Keys of four slots from j (a multiple of 4) on: they lie in one page.
+  auto read = [&](int j) {
+    uint32_t k[4] = {0, 0, 0, 0};
     const int pg = paged_page(a, table, j);
-    if (pg < 0) return 0;
-    return key_of(f.weight[(((int64_t)pg * a.H + h) << a.page_shift) +
-                           (j & ((1 << a.page_shift) - 1))]);
+    const float* at = f.weight + ((((int64_t)max(pg, 0) * a.H + h) << a.page_shift) +
+                                  (j & ((1 << a.page_shift) - 1)));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (j + e >= j1) continue;
+      const bool stays = j + e < f.sinks || j + e >= s.len - f.recent;
+      k[e] = stays ? 0xffffffffu : pg < 0 ? 0 : key_of(at[e]);
+    }
+    return make_uint4(k[0], k[1], k[2], k[3]);
   };
   const bool held = j1 - j0 <= in_smem;
-  auto key = [&](int j) { return held ? keys[j - j0] : read(j); };
+  uint4* const keys4 = reinterpret_cast<uint4*>(keys);
+  auto four = [&](int j) { return held ? keys4[(j - j0) / 4] : read(j); };
   for (int i = threadIdx.x; i < kDigits; i += kChooseThreads) hist[0][i] = 0;
   __syncthreads();
   uint32_t prefix = 0;       // the digits found so far, in place
@@ -90,15 +98,32 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
     const uint32_t digits = step == 2 ? 1024 : 2048;
     const uint32_t above = step == 0 ? 0u : ~0u << (step == 1 ? 21 : 10);
     uint32_t* const mine = hist[step & 1];
-    for (int j = j0 + threadIdx.x; j < j1; j += kChooseThreads) {
-      uint32_t k;
-      if (step == 0) {
-        k = read(j);
-        if (held) keys[j - j0] = k;
-      } else {
-        k = key(j);
+    auto count = [&](int j, const uint4& k) {
+      const uint32_t x[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (j + e < j1 && (x[e] & above) == prefix)
+          atomicAdd(&mine[(x[e] >> shift) & (digits - 1)], 1u);
+    };
+    if (step == 0) {  // several reads on their way at a time: page, weight
+      constexpr int kAtOnce = 4;
+      for (int j = j0 + 4 * threadIdx.x; j < j1; j += 4 * kAtOnce * kChooseThreads) {
+        uint4 k[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          const int x = j + 4 * i * kChooseThreads;
+          if (x < j1) k[i] = read(x);
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          const int x = j + 4 * i * kChooseThreads;
+          if (x >= j1) break;
+          if (held) keys4[(x - j0) / 4] = k[i];
+          count(x, k[i]);
+        }
       }
-      if ((k & above) == prefix) atomicAdd(&mine[(k >> shift) & (digits - 1)], 1u);
+    } else {
+      for (int j = j0 + 4 * threadIdx.x; j < j1; j += 4 * kChooseThreads) count(j, four(j));
     }
     if constexpr (kCluster > 1)
       cluster_sync();
@@ -138,14 +163,25 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
     // (the other histogram is written next; nobody reads this one again before the next sync of all)
   }
   // ---- the kept slots, in order: keys above `prefix`, and the first `need` that equal it
-  const int each = ((j1 - j0 + kChooseWarps - 1) / kChooseWarps + 31) & ~31;
+  // (counts of both in one word, 16 bits each: a warp has 128 slots at a time)
+  const int each = ((j1 - j0 + kChooseWarps - 1) / kChooseWarps + 127) & ~127;
   const int w0 = min(j1, j0 + warp * each), w1 = min(j1, w0 + each);
+  auto tally = [&](int j, const uint4& k) {
+    uint32_t n = 0;
+    const uint32_t x[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (j + e < w1) n += x[e] > prefix ? 1u : x[e] == prefix ? 0x10000u : 0u;
+    return n;
+  };
   uint32_t more = 0, equal = 0;
-  for (int j = w0 + lane; j - lane < w1; j += 32) {
-    const uint32_t k = j < w1 ? key(j) : 0;
-    more += __popc(__ballot_sync(0xffffffffu, j < w1 && k > prefix));
-    equal += __popc(__ballot_sync(0xffffffffu, j < w1 && k == prefix));
+  for (int j = w0 + 4 * lane; j < w1; j += 128) {
+    const uint32_t n = tally(j, four(j));
+    more += n & 0xffffu;
+    equal += n >> 16;
   }
+  more = __reduce_add_sync(0xffffffffu, more);
+  equal = __reduce_add_sync(0xffffffffu, equal);
   if (lane == 0) {
     warp_sum[warp] = more;
     warp_equal[warp] = equal;
@@ -175,16 +211,29 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
     more += warp_sum[w];
     equal += warp_equal[w];
   }
-  const uint32_t below = (1u << lane) - 1;
-  for (int j = w0 + lane; j - lane < w1; j += 32) {
-    const uint32_t k = j < w1 ? key(j) : 0;
-    const uint32_t is_more = __ballot_sync(0xffffffffu, j < w1 && k > prefix);
-    const uint32_t is_equal = __ballot_sync(0xffffffffu, j < w1 && k == prefix);
-    const uint32_t e = equal + __popc(is_equal & below);
-    const uint32_t r = more + __popc(is_more & below) + min(e, need);
-    if ((is_more >> lane & 1) || ((is_equal >> lane & 1) && e < need)) kept[r] = j;
-    more += __popc(is_more);
-    equal += __popc(is_equal);
+  for (int j0w = w0; j0w < w1; j0w += 128) {
+    const int j = j0w + 4 * lane;
+    const uint4 k = j < w1 ? four(j) : make_uint4(0, 0, 0, 0);
+    const uint32_t n = tally(j, k);
+    uint32_t upto = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    const uint32_t all = __shfl_sync(0xffffffffu, upto, 31);
+    uint32_t m = more + ((upto - n) & 0xffffu), q = equal + ((upto - n) >> 16);
+    const uint32_t x[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (j + e >= w1) break;
+      if (x[e] > prefix)
+        kept[m++ + min(q, need)] = j + e;
+      else if (x[e] == prefix && q++ < need)
+        kept[m + q - 1] = j + e;
+    }
+    more += all & 0xffffu;
+    equal += all >> 16;
   }
   if constexpr (kCluster > 1) cluster_sync();  // others may read this CTA's counts
 }
