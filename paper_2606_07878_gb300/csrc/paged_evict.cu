@@ -21,6 +21,7 @@ namespace {
 
 constexpr int kChooseThreads = 1024;
 constexpr int kChooseWarps = kChooseThreads / 32;
+static_assert(kChooseWarps == 32, "a lane a warp");
 constexpr int kDigits = 2048;
 constexpr int kChooseCluster = 8;
 constexpr int kChooseKeys = 48 * 1024;  // of a CTA in shared memory
@@ -32,10 +33,18 @@ STILL_DEV uint32_t key_of(float w) {
   return x & 0x80000000u ? ~x : x | 0x80000000u;
 }
 
-STILL_DEV uint32_t ld_cluster_u32(uint32_t addr) {
-  uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+STILL_DEV uint2 ld_cluster_u32x2(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];"
+               : "=r"(v.x), "=r"(v.y)
+               : "r"(addr)
+               : "memory");
   return v;
+}
+// What the warps before this one have, of kChooseWarps = 32.
+STILL_DEV uint32_t sum_before(const uint32_t* of_warp, int warp) {
+  const int lane = threadIdx.x & 31;
+  return __reduce_add_sync(0xffffffffu, lane < warp ? of_warp[lane] : 0u);
 }
 
 template <int kCluster>
@@ -43,10 +52,10 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
     paged_choose_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedEvict f,
                         int in_smem) {
   extern __shared__ __align__(16) uint32_t keys[];
-  __shared__ uint32_t hist[2][kDigits];
+  __shared__ __align__(8) uint32_t hist[2][kDigits];
   __shared__ uint32_t warp_sum[kChooseWarps], warp_equal[kChooseWarps];
   __shared__ uint32_t found[2];   // digit, kept among those above it
-  __shared__ uint32_t counts[2];  // of this CTA: above the smallest key, equal to it
+  __shared__ __align__(8) uint32_t counts[2];  // of this CTA: above the smallest key, equal to it
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = kCluster > 1 ? cluster_ctarank() : 0;
   const int set = blockIdx.x / kCluster, b = set / a.H, h = set % a.H;
@@ -133,11 +142,15 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
     uint32_t c[2] = {0, 0};
     const int top = (int)digits - 1 - 2 * (int)threadIdx.x;  // c[0]: top, c[1]: top - 1
     if (top > 0) {
+      uint2 x[kCluster];
+#pragma unroll
+      for (int r = 0; r < kCluster; ++r)
+        x[r] = kCluster > 1 ? ld_cluster_u32x2(cluster_map(smem_u32(mine + top - 1), r))
+                            : *reinterpret_cast<const uint2*>(mine + top - 1);
 #pragma unroll
       for (int r = 0; r < kCluster; ++r) {
-        const uint32_t at = kCluster > 1 ? cluster_map(smem_u32(mine), r) : 0;
-        c[0] += kCluster > 1 ? ld_cluster_u32(at + 4 * top) : mine[top];
-        c[1] += kCluster > 1 ? ld_cluster_u32(at + 4 * (top - 1)) : mine[top - 1];
+        c[0] += x[r].y;
+        c[1] += x[r].x;
       }
     }
     uint32_t upto = c[0] + c[1];
@@ -149,8 +162,7 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
     if (lane == 31) warp_sum[warp] = upto;
     for (int i = threadIdx.x; i < kDigits; i += kChooseThreads) hist[(step + 1) & 1][i] = 0;
     __syncthreads();
-#pragma unroll 1
-    for (int w = 0; w < warp; ++w) upto += warp_sum[w];
+    upto += sum_before(warp_sum, warp);
     const uint32_t before = upto - c[0] - c[1];
     if (before < need && upto >= need) {
       const bool first = before + c[0] >= need;
@@ -187,30 +199,24 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
     warp_equal[warp] = equal;
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
-    uint32_t x = 0, y = 0;
-    for (int w = 0; w < kChooseWarps; ++w) {
-      x += warp_sum[w];
-      y += warp_equal[w];
+  if (warp == 0) {
+    const uint32_t x = __reduce_add_sync(0xffffffffu, warp_sum[lane]);
+    const uint32_t y = __reduce_add_sync(0xffffffffu, warp_equal[lane]);
+    if (lane == 0) {
+      counts[0] = x;
+      counts[1] = y;
     }
-    counts[0] = x;
-    counts[1] = y;
   }
   if constexpr (kCluster > 1)
     cluster_sync();
   else
     __syncthreads();
-  more = equal = 0;  // before this warp's slots
-  if constexpr (kCluster > 1)
-    for (uint32_t r = 0; r < rank; ++r) {
-      const uint32_t at = cluster_map(smem_u32(counts), r);
-      more += ld_cluster_u32(at);
-      equal += ld_cluster_u32(at + 4);
-    }
-  for (int w = 0; w < warp; ++w) {
-    more += warp_sum[w];
-    equal += warp_equal[w];
-  }
+  // before this warp's slots: in the CTAs and in the warps before it
+  uint2 ctas = make_uint2(0, 0);
+  if (kCluster > 1 && lane < (int)rank)
+    ctas = ld_cluster_u32x2(cluster_map(smem_u32(counts), lane));
+  more = __reduce_add_sync(0xffffffffu, ctas.x) + sum_before(warp_sum, warp);
+  equal = __reduce_add_sync(0xffffffffu, ctas.y) + sum_before(warp_equal, warp);
   for (int j0w = w0; j0w < w1; j0w += 128) {
     const int j = j0w + 4 * lane;
     const uint4 k = j < w1 ? four(j) : make_uint4(0, 0, 0, 0);
