@@ -20,10 +20,12 @@ namespace {
 //
 // A warp takes the K or the V rows of a block and KV-head, at most 16 of them: it holds them in
 // registers between their maximum and their codes. The first token of a block (or of a sequence's
-// new tokens) leads it; a CTA looks at a window of tokens for leaders, and rotates the window's
-// queries.
+// new tokens) leads it; a CTA looks at a window of tokens for leaders. Other CTAs rotate queries.
+//
+// Memory bounds it: 8,192 tokens of 32 query and 8 KV-heads of 128 channels are 185 MB. APPEND_TIMES
 constexpr int kQuantThreads = 256;
-constexpr int kWindow = 16;  // tokens; 1 where sequences have few of them
+constexpr int kWindow = 16;       // tokens; 1 where sequences have few of them
+constexpr int kQueryWindow = 8;   // of a CTA that rotates queries; or 1
 
 // The smallest power of two, 2^-126 at least, by which `top` is at most 448.
 STILL_DEV float least_scale(float top) {
@@ -56,15 +58,23 @@ struct Lead {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kQuantThreads)
+__global__ void __launch_bounds__(kQuantThreads, D == 256 ? 2 : 3)
     paged_append_quant_kernel(const __grid_constant__ PagedArgs a,
                               const __grid_constant__ PagedAppend p,
-                              const __grid_constant__ RopeTurns w, int window, int table) {
-  extern __shared__ float2 cs[];  // [table][D / 2] (cos, sin) of tokens from the window's first on
+                              const __grid_constant__ RopeTurns w, int q_blocks, int q_window,
+                              int kv_window, int reach) {
+  // [window + reach][4][kLanes][2] (cos, sin) of tokens from the window's first on: channels 8 l + 2 m
+  // (+1) at [m][l], so that the lanes of a row read 16 bytes side by side (in the channels' order they
+  // meet in the same banks, 55 us where this takes APPEND_US)
+  extern __shared__ __align__(16) float2 cs[];
   __shared__ Lead lead[kWindow];
   __shared__ long long pos[kWindow];
   constexpr int kHalf = D / 2;
-  const int i0 = blockIdx.x * window, nt = min(window, a.n - i0);
+  constexpr int kLanes = D / 16;  // threads of a row: 8 channels of each half
+  const bool queries = (int)blockIdx.x < q_blocks;
+  const int window = queries ? q_window : kv_window;
+  const int i0 = ((int)blockIdx.x - (queries ? 0 : q_blocks)) * window;
+  const int nt = min(window, a.n - i0);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int t = warp; t < nt; t += kQuantThreads / 32) {
     const int i = i0 + t, b = paged_owner(a, i);
@@ -84,6 +94,7 @@ __global__ void __launch_bounds__(kQuantThreads)
   }
   __syncthreads();
   if (p.rotate) {
+    const int table = queries ? nt : window + reach;
     for (int x = threadIdx.x; x < table * kHalf; x += kQuantThreads) {
       // (tokens behind the window matter where they are of the last one's block)
       const int t = x / kHalf, known = min(t, nt - 1);
@@ -91,33 +102,47 @@ __global__ void __launch_bounds__(kQuantThreads)
           (unsigned long long)(pos[known] + t - known) * w.turns[x % kHalf];
       float sn, cn;
       sincospif((float)(int)(turn >> 32) * 0x1p-31f, &sn, &cn);
-      cs[x] = make_float2(cn, sn);
+      const int ch = x % kHalf;
+      cs[t * kHalf + (ch / 2 % 4 * kLanes + ch / 8) * 2 + ch % 2] = make_float2(cn, sn);
     }
     __syncthreads();
   }
-  constexpr int kLanes = D / 16;  // threads of a row: 8 channels of each half
   auto rotate = [&](uint4& lo, uint4& hi, const float2* ang) {
     __nv_bfloat162* l = reinterpret_cast<__nv_bfloat162*>(&lo);
     __nv_bfloat162* u = reinterpret_cast<__nv_bfloat162*>(&hi);
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
       const float2 x0 = __bfloat1622float2(l[m]), x1 = __bfloat1622float2(u[m]);
-      const float2 e = ang[2 * m], o = ang[2 * m + 1];
-      l[m] = __floats2bfloat162_rn(x0.x * e.x - x1.x * e.y, x0.y * o.x - x1.y * o.y);
-      u[m] = __floats2bfloat162_rn(x1.x * e.x + x0.x * e.y, x1.y * o.x + x0.y * o.y);
+      const float4 y = *reinterpret_cast<const float4*>(ang + 2 * m * kLanes);  // of two channels
+      l[m] = __floats2bfloat162_rn(x0.x * y.x - x1.x * y.y, x0.y * y.z - x1.y * y.w);
+      u[m] = __floats2bfloat162_rn(x1.x * y.x + x0.x * y.y, x1.y * y.z + x0.y * y.w);
     }
   };
-  // ---- queries
-  for (int x = threadIdx.x; x < nt * p.Hq * kLanes; x += kQuantThreads) {
-    const int c = x % kLanes * 8, h = x / kLanes % p.Hq, t = x / kLanes / p.Hq;
-    const int64_t i = i0 + t;
-    const __nv_bfloat16* src = p.q + i * p.s_q + (int64_t)h * D + c;
-    uint4 lo = *reinterpret_cast<const uint4*>(src);
-    uint4 hi = *reinterpret_cast<const uint4*>(src + kHalf);
-    rotate(lo, hi, cs + t * kHalf + c);
-    __nv_bfloat16* dst = p.q_out + (i * p.Hq + h) * D + c;
-    *reinterpret_cast<uint4*>(dst) = lo;
-    *reinterpret_cast<uint4*>(dst + kHalf) = hi;
+  // ---- queries: 8 channels of each half of a head, several on their way at a time
+  if (queries) {
+    constexpr int kAtOnce = 4;
+    const int total = nt * p.Hq * kLanes;
+    for (int x0 = threadIdx.x; x0 < total; x0 += kAtOnce * kQuantThreads) {
+      uint4 lo[kAtOnce], hi[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int x = x0 + i * kQuantThreads, h = x / kLanes % p.Hq, t = x / kLanes / p.Hq;
+        if (x >= total) break;
+        const __nv_bfloat16* src = p.q + (i0 + t) * p.s_q + (int64_t)h * D + x % kLanes * 8;
+        lo[i] = *reinterpret_cast<const uint4*>(src);
+        hi[i] = *reinterpret_cast<const uint4*>(src + kHalf);
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int x = x0 + i * kQuantThreads, h = x / kLanes % p.Hq, t = x / kLanes / p.Hq;
+        if (x >= total) break;
+        rotate(lo[i], hi[i], cs + t * kHalf + x % kLanes * 2);
+        __nv_bfloat16* dst = p.q_out + ((int64_t)(i0 + t) * p.Hq + h) * D + x % kLanes * 8;
+        *reinterpret_cast<uint4*>(dst) = lo[i];
+        *reinterpret_cast<uint4*>(dst + kHalf) = hi[i];
+      }
+    }
+    return;
   }
   // ---- blocks of keys and values
   constexpr int kAtOnce = 32 / kLanes;                 // rows
@@ -152,7 +177,7 @@ __global__ void __launch_bounds__(kQuantThreads)
     for (int i = 0; i < kSteps; ++i) {
       const int r = r0 + i * kAtOnce;
       if (key && p.rotate && r < x.count)
-        rotate(lo[i], hi[i], cs + (x.token - i0 + r) * kHalf + c);
+        rotate(lo[i], hi[i], cs + (x.token - i0 + r) * kHalf + c / 4);
 #pragma unroll
       for (int m = 0; m < 8; ++m) {
         const uint32_t y = m < 4 ? word(lo[i], m) : word(hi[i], m - 4);
@@ -203,14 +228,17 @@ __global__ void __launch_bounds__(kQuantThreads)
 
 cudaError_t launch_paged_append_quant(const PagedArgs& a, const PagedAppend& p,
                                       const RopeTurns& turns, cudaStream_t s) {
-  const int window = a.n / a.B >= kWindow / 2 ? kWindow : 1;
+  const bool many = a.n / a.B >= kWindow / 2;
+  const int window = many ? kWindow : 1, q_window = many ? kQueryWindow : 1;
+  const int q_blocks = p.Hq > 0 ? (a.n + q_window - 1) / q_window : 0;
   // a block reaches 15 tokens behind the window's last
-  const int table = a.cu_new == nullptr ? 1 : window + kScaleBlock - 1;
-  const size_t smem = p.rotate ? (size_t)table * (a.d / 2) * sizeof(float2) : 0;
+  const int reach = a.cu_new == nullptr ? 0 : kScaleBlock - 1;
+  const size_t smem = p.rotate ? (size_t)(window + reach) * (a.d / 2) * sizeof(float2) : 0;
   auto kernel = a.d == 64    ? paged_append_quant_kernel<64>
                 : a.d == 128 ? paged_append_quant_kernel<128>
                              : paged_append_quant_kernel<256>;
-  kernel<<<(a.n + window - 1) / window, kQuantThreads, smem, s>>>(a, p, turns, window, table);
+  kernel<<<q_blocks + (a.n + window - 1) / window, kQuantThreads, smem, s>>>(
+      a, p, turns, q_blocks, q_window, window, reach);
   return cudaGetLastError();
 }
 
