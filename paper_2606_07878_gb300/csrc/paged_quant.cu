@@ -61,19 +61,19 @@ template <int D>
 __global__ void __launch_bounds__(kQuantThreads, D == 256 ? 2 : 3)
     paged_append_quant_kernel(const __grid_constant__ PagedArgs a,
                               const __grid_constant__ PagedAppend p,
-                              const __grid_constant__ RopeTurns w, int q_blocks, int q_window,
-                              int kv_window, int reach) {
-  // [window + reach][4][kLanes][2] (cos, sin) of tokens from the window's first on: channels 8 l + 2 m
-  // (+1) at [m][l], so that the lanes of a row read 16 bytes side by side (in the channels' order they
+                              const __grid_constant__ RopeTurns w, int kv_blocks, int kv_window,
+                              int q_window, int reach) {
+  // [window + reach][4][kLanes] two cosines and two sines of tokens from the window's first on: of
+  // channels 8 l + 2 m (+1) at [m][l], so that the lanes of a row read 16 bytes side by side (in the channels' order they
   // meet in the same banks, 55 us where this takes APPEND_US)
   extern __shared__ __align__(16) float2 cs[];
   __shared__ Lead lead[kWindow];
   __shared__ long long pos[kWindow];
   constexpr int kHalf = D / 2;
   constexpr int kLanes = D / 16;  // threads of a row: 8 channels of each half
-  const bool queries = (int)blockIdx.x < q_blocks;
+  const bool queries = (int)blockIdx.x >= kv_blocks;  // (the longer ones first)
   const int window = queries ? q_window : kv_window;
-  const int i0 = ((int)blockIdx.x - (queries ? 0 : q_blocks)) * window;
+  const int i0 = ((int)blockIdx.x - (queries ? kv_blocks : 0)) * window;
   const int nt = min(window, a.n - i0);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int t = warp; t < nt; t += kQuantThreads / 32) {
@@ -103,44 +103,62 @@ __global__ void __launch_bounds__(kQuantThreads, D == 256 ? 2 : 3)
       float sn, cn;
       sincospif((float)(int)(turn >> 32) * 0x1p-31f, &sn, &cn);
       const int ch = x % kHalf;
-      cs[t * kHalf + (ch / 2 % 4 * kLanes + ch / 8) * 2 + ch % 2] = make_float2(cn, sn);
+      float* at = reinterpret_cast<float*>(cs + t * kHalf + (ch / 2 % 4 * kLanes + ch / 8) * 2);
+      at[ch % 2] = cn;
+      at[2 + ch % 2] = sn;
     }
     __syncthreads();
   }
   auto rotate = [&](uint4& lo, uint4& hi, const float2* ang) {
-    __nv_bfloat162* l = reinterpret_cast<__nv_bfloat162*>(&lo);
-    __nv_bfloat162* u = reinterpret_cast<__nv_bfloat162*>(&hi);
+    uint32_t* l = reinterpret_cast<uint32_t*>(&lo);
+    uint32_t* u = reinterpret_cast<uint32_t*>(&hi);
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
-      const float2 x0 = __bfloat1622float2(l[m]), x1 = __bfloat1622float2(u[m]);
+      const uint64_t x0 = bf16_pair(l[m]), x1 = bf16_pair(u[m]);
       const float4 y = *reinterpret_cast<const float4*>(ang + 2 * m * kLanes);  // of two channels
-      l[m] = __floats2bfloat162_rn(x0.x * y.x - x1.x * y.y, x0.y * y.z - x1.y * y.w);
-      u[m] = __floats2bfloat162_rn(x1.x * y.x + x0.x * y.y, x1.y * y.z + x0.y * y.w);
+      const uint64_t c = pack2(y.x, y.y), s = pack2(y.z, y.w);
+      float z0, z1;
+      unpack2(fma2(x0, c, neg2(mul2(x1, s))), z0, z1);
+      l[m] = bf16x2_bits(__floats2bfloat162_rn(z0, z1));
+      unpack2(fma2(x0, s, mul2(x1, c)), z0, z1);
+      u[m] = bf16x2_bits(__floats2bfloat162_rn(z0, z1));
     }
   };
   // ---- queries: 8 channels of each half of a head, several on their way at a time
   if (queries) {
-    constexpr int kAtOnce = 4;
-    const int total = nt * p.Hq * kLanes;
-    for (int x0 = threadIdx.x; x0 < total; x0 += kAtOnce * kQuantThreads) {
+    constexpr int kAtOnce = 4, kStep = kQuantThreads / kLanes;  // rows
+    const int rows = nt * p.Hq, l = threadIdx.x % kLanes;
+    const int dt = kStep / p.Hq, dh = kStep % p.Hq;
+    const __nv_bfloat16* const from = p.q + i0 * p.s_q + l * 8;
+    __nv_bfloat16* const to = p.q_out + (int64_t)i0 * p.Hq * D + l * 8;
+    int r = threadIdx.x / kLanes, t = r / p.Hq, h = r % p.Hq;
+    while (r < rows) {
       uint4 lo[kAtOnce], hi[kAtOnce];
+      int at[kAtOnce];  // the rows' tokens
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) {
-        const int x = x0 + i * kQuantThreads, h = x / kLanes % p.Hq, t = x / kLanes / p.Hq;
-        if (x >= total) break;
-        const __nv_bfloat16* src = p.q + (i0 + t) * p.s_q + (int64_t)h * D + x % kLanes * 8;
-        lo[i] = *reinterpret_cast<const uint4*>(src);
-        hi[i] = *reinterpret_cast<const uint4*>(src + kHalf);
+        at[i] = t;
+        if (r + i * kStep < rows) {
+          const __nv_bfloat16* src = from + t * p.s_q + h * D;
+          lo[i] = __ldcs(reinterpret_cast<const uint4*>(src));
+          hi[i] = __ldcs(reinterpret_cast<const uint4*>(src + kHalf));
+        }
+        t += dt;
+        h += dh;
+        if (h >= p.Hq) {
+          h -= p.Hq;
+          ++t;
+        }
       }
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) {
-        const int x = x0 + i * kQuantThreads, h = x / kLanes % p.Hq, t = x / kLanes / p.Hq;
-        if (x >= total) break;
-        rotate(lo[i], hi[i], cs + t * kHalf + x % kLanes * 2);
-        __nv_bfloat16* dst = p.q_out + ((int64_t)(i0 + t) * p.Hq + h) * D + x % kLanes * 8;
+        if (r + i * kStep >= rows) break;
+        rotate(lo[i], hi[i], cs + at[i] * kHalf + l * 2);
+        __nv_bfloat16* dst = to + (int64_t)(r + i * kStep) * D;
         *reinterpret_cast<uint4*>(dst) = lo[i];
         *reinterpret_cast<uint4*>(dst + kHalf) = hi[i];
       }
+      r += kAtOnce * kStep;
     }
     return;
   }
@@ -237,8 +255,9 @@ cudaError_t launch_paged_append_quant(const PagedArgs& a, const PagedAppend& p,
   auto kernel = a.d == 64    ? paged_append_quant_kernel<64>
                 : a.d == 128 ? paged_append_quant_kernel<128>
                              : paged_append_quant_kernel<256>;
-  kernel<<<q_blocks + (a.n + window - 1) / window, kQuantThreads, smem, s>>>(
-      a, p, turns, q_blocks, q_window, window, reach);
+  const int kv_blocks = (a.n + window - 1) / window;
+  kernel<<<kv_blocks + q_blocks, kQuantThreads, smem, s>>>(a, p, turns, kv_blocks, window, q_window,
+                                                           reach);
   return cudaGetLastError();
 }
 
