@@ -22,7 +22,10 @@ namespace {
 // registers between their maximum and their codes. The first token of a block (or of a sequence's
 // new tokens) leads it; a CTA looks at a window of tokens for leaders. Other CTAs rotate queries.
 //
-// Memory bounds it: 8,192 tokens of 32 query and 8 KV-heads of 128 channels are 185 MB. APPEND_TIMES
+// Memory and the latency of its reads bound it: 8,192 tokens of 32 query and 8 KV-heads of 128
+// channels are 185 MB, 43 us (4.3 TB/s). One grid for both, a window's queries before its keys and
+// values, took 57; keys and values behind the queries 49 (a CTA of theirs takes longer: the grid's
+// end waits for it).
 constexpr int kQuantThreads = 256;
 constexpr int kWindow = 16;       // tokens; 1 where sequences have few of them
 constexpr int kQueryWindow = 8;   // of a CTA that rotates queries; or 1
@@ -64,8 +67,8 @@ __global__ void __launch_bounds__(kQuantThreads, D == 256 ? 2 : 3)
                               const __grid_constant__ RopeTurns w, int kv_blocks, int kv_window,
                               int q_window, int reach) {
   // [window + reach][4][kLanes] two cosines and two sines of tokens from the window's first on: of
-  // channels 8 l + 2 m (+1) at [m][l], so that the lanes of a row read 16 bytes side by side (in the channels' order they
-  // meet in the same banks, 55 us where this takes APPEND_US)
+  // channels 8 l + 2 m (+1) at [m][l], so that the lanes of a row read 16 bytes side by side (in the
+  // channels' order they meet in the same banks: 55 us where this took 50)
   extern __shared__ __align__(16) float2 cs[];
   __shared__ Lead lead[kWindow];
   __shared__ long long pos[kWindow];

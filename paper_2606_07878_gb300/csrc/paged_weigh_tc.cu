@@ -11,23 +11,32 @@
 //
 // so that sums stay in a thread's registers in either, in a fixed order, and S (fp32, in TMEM) is
 // read once. In pass 1 m is the row's maximum over its first tile, and moves only when a tile's sum
-// passes 2^10: any m near the maximum serves, since the second pass divides by the same. Both passes
-// compute e^(s - m) by the same instructions from the same S. Sums of a tile are added to the total
-// with their rounding carried along (two floats).
+// passes 2^10: any m near the maximum serves, since the second pass divides by the same. Both
+// passes compute e^(s - m) by the same instructions from the same S. Sums of a tile are added to
+// the total with their rounding carried along (two floats).
 //
-// Without biases S itself is kept: e^(scale s - m) = 2^(fma(s, scale log2 e, -m log2 e)). With biases
-// logits are natural up to the subtraction, as a bias of the lowest float would be -inf in units of
-// log 2.
+// Without biases S itself is kept: e^(scale s - m) = 2^(fma(s, scale log2 e, -m log2 e)). With
+// biases logits are natural up to the subtraction, as a bias of the lowest float would be -inf in
+// units of log 2.
 //
-// A thread of the sums has a lane of both held tiles and a quarter of the columns: what belongs to a column
-// (biases; m and l) is read from shared memory once for two values. A broadcast of 16 bytes takes
-// the load unit as long as 32 different ones, four cycles: with a thread to a lane of one held tile
-// and m and 1 / l apart these reads were the bound, 212 us of the second pass over 6,001 tokens of 28
-// heads against 117 of the first. So m and log l are one number there, where it is small enough
-// that its rounding stays below 2^-20 of a weight.
+// A thread of the sums has a lane of both held tiles and a quarter of the columns: what belongs to
+// a column (biases; m and l) is read from shared memory once for two values. With a thread to a
+// lane of one held tile and m and 1 / l apart the second pass over 6,001 tokens of 28 heads took
+// 212 us. So m and log l are one number there, where it is small enough that its rounding stays
+// below 2^-20 of a weight: 149.
+//
+// Measured: 6,001 tokens of 28 query and 4 KV-heads of 128 channels, 117 us the first pass, 149 the
+// second (129 GFLOP each: 1.1 and 0.87 PFLOP/s, the tensor pipe busy 51% and 44%); 64 tokens behind
+// each of four sequences of 9,000 to 32,700 slots with biases, 55 and 76 (170 MB of keys, twice).
+// What bounds both is the warps that add up: 0.9 us a streamed tile against 0.53 of products, 4.4
+// instructions an exponential where the formula has 2, half the rest what a warp does once a tile
+// (waits, masks, sums of two floats), and in short items 1 to 2 us from one item to the next.
+// Tried without gain: four S tiles apart (a held tile each), a warp of its own for the held tiles'
+// copies or for the items' ends, two warps for the columns, a deeper ring with one held item.
 //
 // Roles: warp 0 TMA (a box per page and 64 channels), 1 MMA issuer and TMEM, 2 what belongs to the
-// streamed tile's columns and to held slots, 4 .. 19 sums. Ranges of equal cost as in the prefill (paged_tc.cuh); what several CTAs share of an item goes to the
+// streamed tile's columns and to held slots, 4 .. 19 sums. Ranges of equal cost as in the prefill
+// (paged_tc.cuh); what several CTAs share of an item goes to the
 // workspace and a second launch joins it. Every wait is bounded.
 #include <type_traits>
 
@@ -42,8 +51,8 @@ constexpr int kWtThreads = 640;
 constexpr int kWtSums = 16;          // warps that add up: four to a quarter of the columns
 constexpr int kWtHeld = 256;        // rows or slots of an item
 constexpr int kWtMost = 1024;       // a tile's sum in units of e^m that moves m
-// Streamed tiles whose column values are held, [kWtCols][kWtColFloats]: three of every column, a flag,
-// and of the tile that is an item's first the held slots' biases and pages.
+// Streamed tiles whose column values are held, [kWtCols][kWtColFloats]: three of every column, a
+// flag, and of the tile that is an item's first the held slots' biases and pages.
 constexpr int kWtCols = 4;
 constexpr int kWtFlagAt = 384, kWtBiasAt = 388, kWtPageAt = kWtBiasAt + kWtHeld;
 constexpr int kWtColFloats = kWtPageAt + kWtHeld / 8;  // (8 slots lie in one page)
