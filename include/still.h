@@ -412,6 +412,7 @@ still_status still_paged_prefill_quant(still_ctx* ctx, const still_paged_cache_q
  * in which blocks run.
  *   scratch  still_paged_weigh_scratch bytes of device memory (16-byte aligned) for as long as the
  *            call runs, too few: STILL_ERR_SHAPE. Calls that may run at once need their own.
+ * No two sequences of a call may share a page: their weights would be written at once.
  * still_paged_decode_weigh: still_paged_decode, and the weights beside it, at the cost of the
  * logits' way through memory. still_paged_weigh: the weights alone, any number of tokens, causal
  * among them. weight must not overlap beta. Everything else is as in still_paged_decode and
@@ -431,9 +432,9 @@ still_status still_paged_weigh(still_ctx* ctx, const still_paged_cache* cache,
  * them, in their order, to slots 0, 1, ... of pages of `to` that to_table lists. Heads choose for
  * themselves. A sequence of at most `keep` slots is copied whole.
  *   to        a cache of the same H and d, any page size and strides, in the same pools or others;
- *             the pages that are written must not be read by this call. Its biases are those of the
- *             slots, 0 where `cache` has none; without biases it is refused
- *             (STILL_ERR_INVALID_ARG) if `cache` has some.
+ *             the pages that are written are each one sequence's and must not be read by this
+ *             call. Its biases are those of the slots, 0 where `cache` has none; without biases it
+ *             is refused (STILL_ERR_INVALID_ARG) if `cache` has some.
  *   to_table  [B][to_s_table], the first to_table_pages of a row; keep <= to_table_pages page_size
  *             (STILL_ERR_SHAPE)
  *   to_weight [to->n_pages][H][to->page_size] the slots' weights, or NULL

@@ -1,15 +1,23 @@
 // Eviction from a paged cache: of every sequence and KV-head the first `sinks` slots, the last
-// `recent` and the heaviest of the others, `keep` in all, move to pages of their own, in their order.
+// `recent` and the heaviest of the others, `keep` in all, move to pages of their own, in their
+// order.
 //
-// Two launches. The first one chooses: weights become 32-bit keys in their order (slots that stay in
-// any case above all others, NaN below), and three steps of 11, 11 and 10 bits find the smallest key
-// that is kept and how many of its equals are (those of the lowest slots). A cluster of CTAs takes a
-// sequence's KV-head, each a part of its slots whose keys stay in shared memory where they fit; a
-// step's histograms are added up through distributed shared memory, by every CTA for itself. The
-// second one moves: 16 bytes a thread, rows of K and V.
+// Two launches. The first one chooses: weights become 32-bit keys in their order (slots that stay
+// in any case above all others, NaN below), and three steps of 11, 11 and 10 bits find the smallest
+// key that is kept and how many of its equals are (those of the lowest slots). A cluster of CTAs
+// takes a sequence's KV-head, each a part of its slots whose keys stay in shared memory where they
+// fit; a step's histograms are added up through distributed shared memory, by every CTA for itself.
+// The second one moves: 16 bytes a thread, rows of K and V.
 //
-// A head may keep other tokens than its neighbour: a slot's rows of two heads are of two tokens then.
-// Attention does not mind, keys are rotated to their positions already.
+// 131,072 slots of 8 KV-heads of 128 channels to 16,384 take 49 us, 24 to choose and 22 to move
+// (134 MB, 6.2 TB/s); 32 sequences of 700 to 1,500 slots of 2 heads to 164 take 14. What is left of
+// the choice is latency: the reads of pages and weights (4.8 us; 16 slots a thread, four reads on
+// their way; one slot at a time took 40 us for the choice) and three rounds of histograms (count,
+// wait for the cluster, read eight histograms, 3 to 4 us each). Sums over warps and CTAs by a lane
+// each instead of one after another: 33 -> 24 us.
+//
+// A head may keep other tokens than its neighbour: a slot's rows of two heads are of two tokens
+// then. Attention does not mind, keys are rotated to their positions already.
 #include <algorithm>
 
 #include "launch.cuh"
@@ -172,7 +180,8 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
     __syncthreads();
     prefix |= found[0] << shift;
     need -= found[1];
-    // (the other histogram is written next; nobody reads this one again before the next sync of all)
+    // (the other histogram is written next; nobody reads this one again before the next sync of
+    // all)
   }
   // ---- the kept slots, in order: keys above `prefix`, and the first `need` that equal it
   // (counts of both in one word, 16 bits each: a warp has 128 slots at a time)
@@ -306,6 +315,7 @@ cudaError_t launch_choose(const PagedArgs& a, const PagedEvict& f, const KernelT
 
 cudaError_t launch_paged_evict(const PagedArgs& a, const PagedEvict& f, const KernelTable& dev,
                                cudaStream_t s) {
+  // A cluster where the table has room for more slots than four a thread of one CTA.
   const int64_t slots = (int64_t)a.table_pages << a.page_shift;
   const cudaError_t e = slots > 4096 ? launch_choose<kChooseCluster>(a, f, dev, s)
                                      : launch_choose<1>(a, f, dev, s);

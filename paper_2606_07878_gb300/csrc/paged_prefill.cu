@@ -26,6 +26,17 @@
 // Slots that do not count are zeroed in shared memory before their products (a weight of 0 times
 // a stale NaN would be NaN): those past the sequence's end, and those with a bias of -inf.
 //
+// A pool in 8 bits (pf_fetch, pf_convert) goes through a ring of codes first; two warpgroups turn
+// them into bf16 in the ring that the products read. Codes in the products themselves
+// (kind::f8f6f4) would want q and P in 8 bits, twice for their rests. The prompt below takes 447 us
+// from codes, 1.08 PFLOP/s, where bf16 takes 339 (the tensor pipe busy 48%): 409 with a quarter of
+// the conversion, so most of the difference is the codes' second way through shared memory (16 KB
+// read and 32 written for a tile's 32 of operands), which the products share. With codes loaded by
+// the converters themselves, one ring slot ahead in registers: 843 us with four warps (a warp
+// issues an instruction every 4 to 5 clocks, and a tile took 3,600); by TMA with eight 491, and 449
+// since they are told what a slot holds instead of walking the items. Four ring slots of bf16 and
+// two of codes: 467; three and four: 445, within what two runs differ by.
+//
 // CTA = 12 warps: 0, 10 and 11 TMA producers (a copy takes about 40 clocks to issue, and pages of
 // 16 slots are 64 copies for K and V of 128 slots and 256 channels: 352 us with one producer, 235
 // with three), 1 MMA issuer and TMEM allocation, 2..9 softmax and output. Every wait is bounded.
@@ -1325,8 +1336,10 @@ bool paged_prefill_serves(const PagedArgs& a, int Hq) {
   // us, and 111 for 1,100 new tokens, which are above. A caller who knows the counts does better
   // with two calls: the prompts in one (86 us alone), the single tokens in the other.
   const int few = a.d == 256 ? 8 : 16;
-  // Single tokens over a pool in 8 bits stay with the few rows' kernel, whose weights are exact to
-  // 2^-21, while it reads the pool no more than twice.
+  // Over a pool in 8 bits, in the same order: 8 rows 36 / 54, 40 / 63, 41 / 58; 16 rows 45 / 54,
+  // 56 / 63, 57 / 57; 32 rows 64 / 54, 86 / 62, 85 / 58; two sequences of 60,000 slots (128 channels)
+  // 16 rows 75 / 74, 32 rows 117 / 74. Single tokens over it stay with the few rows' kernel, whose
+  // weights are exact to 2^-21, while it reads the pool no more than twice.
   if (a.K8 != nullptr && a.cu_new == nullptr && Hq / a.H <= 2 * few) return false;
   return Hq / a.H <= 128 && paged_mean_rows(a, Hq) > few;
 }

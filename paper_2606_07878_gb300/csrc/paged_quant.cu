@@ -37,7 +37,8 @@ STILL_DEV float least_scale(float top) {
   return __uint_as_float((uint32_t)(127 + max(e, -126)) << 23);
 }
 
-// Four codes of x / s; by = 1 / s. Values beyond 448 s, infinities too, become +-448, NaN stays NaN.
+// Four codes of x / s; by = 1 / s. Values beyond 448 s, infinities too, become +-448, NaN stays
+// NaN.
 STILL_DEV uint32_t codes4(float x0, float x1, float x2, float x3, float by) {
   uint32_t r;
   asm("{\n\t.reg .b16 l, h;\n\t"
@@ -67,8 +68,8 @@ __global__ void __launch_bounds__(kQuantThreads, D == 256 ? 2 : 3)
                               const __grid_constant__ RopeTurns w, int kv_blocks, int kv_window,
                               int q_window, int reach) {
   // [window + reach][4][kLanes] two cosines and two sines of tokens from the window's first on: of
-  // channels 8 l + 2 m (+1) at [m][l], so that the lanes of a row read 16 bytes side by side (in the
-  // channels' order they meet in the same banks: 55 us where this took 50)
+  // channels 8 l + 2 m (+1) at [m][l], so that the lanes of a row read 16 bytes side by side (in
+  // the channels' order they meet in the same banks: 55 us where this took 50)
   extern __shared__ __align__(16) float2 cs[];
   __shared__ Lead lead[kWindow];
   __shared__ long long pos[kWindow];

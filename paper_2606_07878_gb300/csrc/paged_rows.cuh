@@ -1,6 +1,6 @@
 // Attention of few rows over a paged cache, and the join of what several warps share: for pools in
-// bf16 (paged.cu), in e4m3 with scales of blocks (paged_quant.cu), and with the logits and the rows'
-// maxima and sums kept for a second pass (paged_weigh.cu).
+// bf16 (paged.cu), in e4m3 with scales of blocks (paged_quant.cu), and with the logits and the
+// rows' maxima and sums kept for a second pass (paged_weigh.cu).
 #pragma once
 #include <algorithm>
 #include <cuda_fp16.h>
@@ -37,6 +37,13 @@ namespace {
 // set, with the last CTA of a set joining its parts: 36 / 109 / 170 / 193 us where this takes 32 /
 // 90 / 169 / 180 (8 sequences of 1,312 to 5,408 slots; 256 of 165 to 701; 24 of 8,192 to 32,768;
 // one of 131,072 with 256 channels); the last warp joining in this kernel: 40 / 93 / 181 / 186.
+//
+// In 8 bits 16 slots are half the bytes for the same instructions and more: codes become fp16 (two
+// an instruction), weights fp16 hi + lo of weight x scale / rho, a number that follows the row's
+// largest. The 24 sequences take 129 us (0.5 GB, 4.1 TB/s). They took 145 where a warp issued 545
+// instructions a batch, 250 of them in the integer and conversion pipe, with an address product for
+// every row, a division and two exponentials more; 153 with two batches on their way at a time, 132
+// with a fourth CTA on an SM (both spill).
 //
 // Memory bounds the large calls: the 24 sequences are 1.0 GB, 5.95 TB/s and 0.88 of a copy, with
 // the mma.sync pipe at 12%, so the tensor cores of tcgen05 would have nothing to gain. Small calls
@@ -510,11 +517,13 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
       // are is looked at where the scale alone does).
       [[maybe_unused]] float by_v[2] = {1.f, 1.f};
       if constexpr (kE4m3) {
+        bool none[2] = {false, false};
         if (__any_sync(0xffffffffu, vscale > 256.f * rho[k][0] || vscale > 256.f * rho[k][1])) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const float up =
                 top[e] == -INFINITY ? 0.f : vscale * ex2_ftz((top[e] - m[k][e]) * kLog2e);
+            none[e] = up == 0.f;  // (the scale over rho may be infinite)
             if (!(up > 256.f * rho[k][e])) continue;
             const float next = fmaxf(up, 0x1p-126f);  // it has an inverse
             const float f = rho[k][e] / next;
@@ -530,7 +539,7 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
           }
         }
 #pragma unroll
-        for (int e = 0; e < 2; ++e) by_v[e] = vscale * by_rho[k][e];
+        for (int e = 0; e < 2; ++e) by_v[e] = none[e] ? 0.f : vscale * by_rho[k][e];
       }
       if constexpr (kKind == kRowsWeigh) {  // (a batch lies in one page)
         const int64_t row = (page_now * a.H + head_now) * g + row_now + 8 * k + 2 * lj;

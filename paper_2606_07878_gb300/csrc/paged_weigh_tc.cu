@@ -871,7 +871,11 @@ cudaError_t launch_passes(const PagedArgs& a, const PagedQuery& q, float* weight
 }  // namespace
 
 bool paged_weigh_tc_serves(const PagedArgs& a, int Hq) {
-  return Hq / a.H <= 128 && paged_mean_rows(a, Hq) > 16;
+  // Measured, us, few rows' kernels / this one, 16 sequences of 5,000 slots and 4 KV-heads (256
+  // channels: 2): 8 rows 55 / 65, 66 / 73, 59 / 67 for 64, 128, 256 channels; 16 rows 67 / 65,
+  // 82 / 73, 82 / 67; 64 rows 169 / 65, 209 / 73, 207 / 67. Two of 60,000 slots (128 channels): 8 rows
+  // 86 / 91, 16 rows 107 / 91. The mean is all the host has, as in paged_prefill_serves.
+  return Hq / a.H <= 128 && paged_mean_rows(a, Hq) > 8;
 }
 
 size_t paged_weigh_tc_workspace(int num_sms) {

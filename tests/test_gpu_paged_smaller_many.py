@@ -189,3 +189,21 @@ def test_large_groups_of_single_tokens(ctx):  # noqa: F811
         still.still_paged_decode_quant(ctx, p.cache(), batch_of(p), q, out)
         few = g <= (16 if d == 256 else 32)
         assert_rows(out, *attention64(p, q, [1] * 3), 2.0 ** -11 + 2.0 ** -20 if few else MANY)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_scales_beyond_an_exponent_apart(ctx, d):  # noqa: F811
+    """A block whose scale is 2^160 of the others' and whose weights are below the smallest float."""
+    p = QuantPages(53, [64], 1, d, 16)
+    q, = fused_rows(54, 1, [4], d)
+    q = q.abs().contiguous()
+    far = int(p.table[0, 2])
+    p.codes[0].view(torch.uint8)[far] = 0xf8  # keys of -256 each
+    for page in p.table[0, :4].tolist():
+        p.scales[0][page] = 2.0 ** -8
+        p.scales[1][page] = 2.0 ** 100 if page == far else 2.0 ** -60
+    p.scales[0][far] = 2.0 ** 8
+    p.read()
+    out = torch.empty_like(q)
+    still.still_paged_decode_quant(ctx, p.cache(), batch_of(p), q, out)
+    assert_rows(out, *attention64(p, q, [1]), 2.0 ** -11 + 2.0 ** -20)
