@@ -315,10 +315,14 @@ cudaError_t launch_choose(const PagedArgs& a, const PagedEvict& f, const KernelT
 
 cudaError_t launch_paged_evict(const PagedArgs& a, const PagedEvict& f, const KernelTable& dev,
                                cudaStream_t s) {
-  // A cluster where the table has room for more slots than four a thread of one CTA.
+  // A CTA or a cluster for a sequence's KV-head, by the slots that the table has room for. Measured,
+  // us for the call (64 slots kept, 8 KV-heads): one CTA 15 up to 4,000 slots, 19 at 8,000 and 23 at
+  // 16,000, about 0.55 for 1,000 more; a cluster 21 at any of them, but a CTA fills an SM: 72 for 8
+  // sequences (four waves of clusters, one CTA each 15 to 24) and 440 for 64 (38 to 52).
   const int64_t slots = (int64_t)a.table_pages << a.page_shift;
-  const cudaError_t e = slots > 4096 ? launch_choose<kChooseCluster>(a, f, dev, s)
-                                     : launch_choose<1>(a, f, dev, s);
+  const int64_t waves = ((int64_t)a.B * a.H * kChooseCluster + dev.num_sms - 1) / dev.num_sms;
+  const cudaError_t e = slots > 38000 * waves - 25000 ? launch_choose<kChooseCluster>(a, f, dev, s)
+                                                      : launch_choose<1>(a, f, dev, s);
   if (e != cudaSuccess) return e;
   auto kernel = a.d == 64    ? paged_move_kernel<64>
                 : a.d == 128 ? paged_move_kernel<128>

@@ -207,3 +207,46 @@ def test_scales_beyond_an_exponent_apart(ctx, d):  # noqa: F811
     out = torch.empty_like(q)
     still.still_paged_decode_quant(ctx, p.cache(), batch_of(p), q, out)
     assert_rows(out, *attention64(p, q, [1]), 2.0 ** -11 + 2.0 ** -20)
+
+
+@pytest.mark.parametrize("B,H,n,keep", [
+    (1, 2, 14000, 700),     # a cluster each, keys in its shared memory
+    (2, 1, 60001, 30000),
+    (8, 8, 60001, 333),     # one CTA each, more keys than it holds
+    (20, 8, 9000, 8999),    # one CTA each, and held
+])
+def test_choices_of_clusters_and_of_single_ctas(ctx, B, H, n, keep):  # noqa: F811
+    """Weights of few different sizes, so that the border falls among equals: the lowest slots stay."""
+    d, page, sinks, recent = 64, 64, 5, 40
+    lens = [n - 37 * b for b in range(B)]
+    g = torch.Generator(device=DEV).manual_seed(55)
+    need = -(-n // page)
+    pools = [torch.randint(-9, 9, (B * need, page, H, d), generator=g, device=DEV).bfloat16()
+             for _ in "KV"]
+    table = torch.randperm(B * need, generator=g, device=DEV).to(torch.int32).view(B, need)
+    w = torch.randint(-3, 50, (B * need, H, page), generator=g, device=DEV).float()
+    w = torch.where(w < 0, torch.where(w < -2, NAN, -math.inf), (w - 7) / 8)
+    to_need = -(-keep // page)
+    to = [torch.zeros(B * to_need, page, H, d, device=DEV, dtype=torch.bfloat16) for _ in "KV"]
+    to_table = torch.arange(B * to_need, dtype=torch.int32, device=DEV).view(B, to_need)
+    kept = torch.full((B, H, keep), -9, dtype=torch.int32, device=DEV)
+    to_lens = torch.full((B,), -9, dtype=torch.int32, device=DEV)
+    still.still_paged_evict(ctx, still.PagedCache(*pools), still.PagedBatch(table, i32(lens)), w, keep,
+                            sinks, recent, still.PagedCache(*to), to_table, kept, to_lens)
+    assert to_lens.tolist() == [min(keep, m) for m in lens]
+    j = torch.arange(n, device=DEV)
+    for b, m in enumerate(lens):
+        x = w[table[b].long()[j // page], :, j % page].T.double()  # [H, n]
+        x = torch.where(torch.isnan(x), -1e30, x.clamp_min(-1e20))
+        x[:, :sinks] = math.inf
+        x[:, m - recent:] = math.inf
+        x[:, m:] = -math.inf
+        count = min(keep, m)
+        idx = x.sort(dim=1, descending=True, stable=True).indices[:, :count].sort(1).values
+        assert torch.equal(kept[b, :, :count].long(), idx)
+        assert (kept[b, :, count:] == -1).all()
+        r = torch.arange(count, device=DEV)
+        for h in range(H):
+            src, dst = table[b].long()[idx[h] // page], to_table[b].long()[r // page]
+            for old, new in zip(pools, to):
+                assert torch.equal(new[dst, r % page, h], old[src, idx[h] % page, h])
