@@ -496,9 +496,15 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
           const float f = n == m[k][e] ? 1.f : exp2f((m[k][e] - n) * kLog2e);
           m[k][e] = n;
           l[k][e] *= f;
-          const bool in_rho = kE4m3 && rho[k][e] * f >= 0x1p-126f;  // O is brought along by it
-          if (in_rho) {
-            rho[k][e] *= f;
+          // e4m3: rho brings O along, down to the smallest normal float, and O takes the rest. (A rho
+          // that stayed above it would be the unit of the weights that follow.)
+          bool in_rho = kE4m3;
+          float rest = f;
+          if (kE4m3 && rho[k][e] > 0.f) {
+            const float next = rho[k][e] * f;
+            in_rho = next >= 0x1p-126f;
+            rest = f * 0x1p126f * rho[k][e];
+            rho[k][e] = in_rho ? next : 0x1p-126f;
             by_rho[k][e] = 1.f / rho[k][e];
           }
           if (!kStats && !in_rho) {
@@ -506,15 +512,15 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
             for (int x = 0; x < (kStats ? 0 : D / 64); ++x)
 #pragma unroll
               for (int w = 0; w < 4; ++w) {
-                o[k][x][w][e] *= f;
-                o[k][x][w][e + 2] *= f;
+                o[k][x][w][e] *= rest;
+                o[k][x][w][e + 2] *= rest;
               }
           }
         }
       }
-      // e4m3: O is a multiple of rho, and a weight times the batch's scale of V enters
-      // as a multiple of it too. rho is raised when one of them would pass 2^8 (and how large they
-      // are is looked at where the scale alone does).
+      // e4m3: O is a multiple of rho (at least 2^-126, 0 before anything is seen), and a weight times
+      // the batch's scale of V enters as a multiple of it too. rho is raised when one of them would
+      // pass 2^8 (and how large they are is looked at where the scale alone does).
       [[maybe_unused]] float by_v[2] = {1.f, 1.f};
       if constexpr (kE4m3) {
         bool none[2] = {false, false};

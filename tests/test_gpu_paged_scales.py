@@ -1,0 +1,63 @@
+"""The paged cache in 8 bits where its scales are far apart: values before and behind a maximum that
+jumps, blocks of zeros."""
+import math
+
+import pytest
+import torch
+
+from paper_2606_07878_gb300 import still
+from test_gpu_paged import DEV, NAN, assert_rows, attention64, batch_of, ctx, fused_rows  # noqa: F401
+from test_gpu_paged_quant import FEW, QuantPages
+
+pytestmark = pytest.mark.gpu
+
+LOWEST = torch.finfo(torch.float32).min
+
+
+def blocks(p, b):
+    """Pages of sequence b, of 16 slots: a block each."""
+    assert p.page == 16
+    return p.table[b, :-(-p.lens[b] // 16)].tolist()
+
+
+def decode(ctx, p, q):  # noqa: F811
+    out = torch.full_like(q, NAN)
+    still.still_paged_decode_quant(ctx, p.cache(), batch_of(p), q, out)
+    return out
+
+
+def assert_small_rows(out, ref, size, weights):
+    """assert_rows where outputs may be subnormal: their rounding is 2^-134 at most there."""
+    assert torch.isfinite(out).all()
+    assert ((out.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + weights * size + 2.0 ** -134).all()
+
+
+@pytest.mark.parametrize("d,Hq", [(64, 4), (128, 4), (128, 16), (256, 5)])
+@pytest.mark.parametrize("apart", [8, 16, 24, 40, 90])
+def test_values_behind_a_maximum_that_jumps(ctx, d, Hq, apart):  # noqa: F811
+    """Every other block has biases of the lowest float and values 2^apart times the others': they
+    weigh nothing, and what they were multiples of must not stay the unit of those that do."""
+    p = QuantPages(61, [240, 3000], 1, d, 16, beta=True)
+    for b in range(2):
+        for page in blocks(p, b)[::2]:
+            p.beta[page] = LOWEST
+            p.scales[1][page] *= 2.0 ** apart
+    p.read()
+    q, = fused_rows(62, 2, [Hq], d)
+    assert_rows(decode(ctx, p, q), *attention64(p, q, [1, 1]), FEW)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("old,new", [(-12, -120), (-20, -124), (40, -60), (100, -14)])
+def test_both_sides_of_a_jump_count(ctx, d, old, new):  # noqa: F811
+    """Weights of e^-80 = 2^-115.4 on values of 448 2^old beside weights of 1 on values of 2^new: sums
+    of either side are of the same size, though 2^old 2^-115.4 may lie below the normal floats."""
+    p = QuantPages(63, [240], 1, d, 16, beta=True)
+    for i, page in enumerate(blocks(p, 0)):
+        p.beta[page] = 0.0 if i % 2 else -80.0
+        p.scales[1][page] = 2.0 ** (new if i % 2 else old)
+        p.codes[1].view(torch.uint8)[page] = 0x38 if i % 2 else 0x7e  # 1, 448
+    p.read()
+    q, = fused_rows(64, 1, [4], d)
+    q = (q.float() / 16).bfloat16()  # logits within 1 of their bias
+    assert_small_rows(decode(ctx, p, q), *attention64(p, q, [1]), FEW)
