@@ -520,7 +520,9 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
       }
       // e4m3: O is a multiple of rho (at least 2^-126, 0 before anything is seen), and a weight times
       // the batch's scale of V enters as a multiple of it too. rho is raised when one of them would
-      // pass 2^8 (and how large they are is looked at where the scale alone does).
+      // pass 2^8 (and how large they are is looked at where the scale alone does), or when the scale
+      // over rho would pass the largest float (no weight but 0 is below 2^-126, so the largest of the
+      // row times the scale is 4 rho at least then).
       [[maybe_unused]] float by_v[2] = {1.f, 1.f};
       if constexpr (kE4m3) {
         bool none[2] = {false, false};
@@ -530,7 +532,8 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
             const float up =
                 top[e] == -INFINITY ? 0.f : vscale * ex2_ftz((top[e] - m[k][e]) * kLog2e);
             none[e] = up == 0.f;  // (the scale over rho may be infinite)
-            if (!(up > 256.f * rho[k][e])) continue;
+            const bool wide = up > 0.f && vscale * by_rho[k][e] > 3.4e38f;  // for small weights
+            if (!(up > 256.f * rho[k][e]) && !wide) continue;
             const float next = fmaxf(up, 0x1p-126f);  // it has an inverse
             const float f = rho[k][e] / next;
             rho[k][e] = next;

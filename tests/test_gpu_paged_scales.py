@@ -61,3 +61,21 @@ def test_both_sides_of_a_jump_count(ctx, d, old, new):  # noqa: F811
     q, = fused_rows(64, 1, [4], d)
     q = (q.float() / 16).bfloat16()  # logits within 1 of their bias
     assert_small_rows(decode(ctx, p, q), *attention64(p, q, [1]), FEW)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("scale", [2, 5, 8, 30])
+@pytest.mark.parametrize("gap", [83, 85, 86.5])
+def test_a_block_of_zeros_has_the_maximum(ctx, d, scale, gap):  # noqa: F811
+    """Values of zero have the smallest scale, 2^-126; others 2^128 times that and more, whose weights
+    are among the smallest normal floats (e^-86.5 = 2^-124.8)."""
+    p = QuantPages(65, [240], 1, d, 16, beta=True)
+    for i, page in enumerate(blocks(p, 0)):
+        p.beta[page] = 0.0 if i % 4 == 0 else -gap
+        p.scales[1][page] = 2.0 ** (-126 if i % 4 == 0 else scale)
+        if i % 4 == 0:
+            p.codes[1].view(torch.uint8)[page] = 0
+    p.read()
+    q, = fused_rows(66, 1, [4], d)
+    q = (q.float() / 32).bfloat16()  # logits within 0.5 of their bias: no weight below 2^-126
+    assert_small_rows(decode(ctx, p, q), *attention64(p, q, [1]), FEW)
