@@ -473,10 +473,12 @@ __global__ void __launch_bounds__(kRowThreads, Rows<D, NB, kKind>::kMinCtas)
       float top[2];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {  // slot lg + 8 (e / 2), row 2 lj + e % 2
+        // (e4m3: factors first, as the product, up to 2^32, times a large scale may pass the largest
+        // float where the logit does not)
         const float be = e >> 1 ? b1 : b0;
         const bool ok = e0 + lg + 8 * (e >> 1) < see[k][e & 1] && be != -INFINITY;
         if constexpr (kE4m3)
-          c[k][e] = ok ? c[k][e] * kscale * fq[k][e & 1] + be : -INFINITY;
+          c[k][e] = ok ? c[k][e] * (kscale * fq[k][e & 1]) + be : -INFINITY;
         else
           c[k][e] = ok ? c[k][e] * p.scale + be : -INFINITY;
       }

@@ -79,3 +79,13 @@ def test_a_block_of_zeros_has_the_maximum(ctx, d, scale, gap):  # noqa: F811
     q, = fused_rows(66, 1, [4], d)
     q = (q.float() / 32).bfloat16()  # logits within 0.5 of their bias: no weight below 2^-126
     assert_small_rows(decode(ctx, p, q), *attention64(p, q, [1]), FEW)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_keys_whose_logits_are_large(ctx, d):  # noqa: F811
+    """Logits up to 2^120 or so: finite, so that one slot has all the weight."""
+    p = QuantPages(67, [240], 1, d, 16)
+    p.scales[0].mul_(2.0 ** 112)
+    p.read()
+    q, = fused_rows(68, 1, [4], d)
+    assert_rows(decode(ctx, p, q), *attention64(p, q, [1]), FEW)
