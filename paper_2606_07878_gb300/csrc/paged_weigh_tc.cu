@@ -684,9 +684,10 @@ __global__ void __launch_bounds__(kWtThreads, 1)
             if (!__any_sync(0xffffffffu, moves)) break;
           }
         } else {
-          // columns [lo, hi) are rows that see the first slot
+          // columns [lo, hi) are rows that see the first slot (of old slots, which all rows see, lo is
+          // held back: times g it may pass 32 bits)
           const int token0 = tile * f.tile_tokens;
-          const int lo = (slot0 - past - token0) * g - c0;
+          const int lo = max(slot0 - past - token0, -kWtHeld) * g - c0;
           const int hi = min(f.tile_tokens, it.count - token0) * g - c0;
           uint64_t s0[2] = {0ull, 0ull}, s1[2] = {0ull, 0ull};
           if (!odd && hi + c0 == tile_rows &&
