@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(kWeighThreads)
     for (int i = 0; i < g; ++i) {  // (what lies past the sequence's end is not used)
       const float4 y = *reinterpret_cast<const float4*>(x + ((int64_t)i << a.page_shift));
       const float2 e = row[i];
-      if (e.y > 0.f) {
+      if (e.y != 0.f) {  // (NaN: so is what the row gives)
         sum[0] += exp2f((y.x - e.x) * kLog2e) * e.y;
         sum[1] += exp2f((y.y - e.x) * kLog2e) * e.y;
         sum[2] += exp2f((y.z - e.x) * kLog2e) * e.y;
@@ -71,8 +71,14 @@ __global__ void __launch_bounds__(kWeighThreads)
       }
     }
 #pragma unroll
-    for (int i = 0; i < kWeighSlots; ++i)
-      if (j + i < s.len) w[i] = before[i] + sum[i];
+    for (int i = 0; i < kWeighSlots; ++i) {
+      if (j + i >= s.len) continue;
+      // of a masked slot a row of NaN makes e^-inf NaN
+      if (sum[i] != sum[i] && a.beta != nullptr &&
+          a.beta[(head << a.page_shift) + (j & mask) + i] == -INFINITY)
+        sum[i] = 0.f;
+      w[i] = before[i] + sum[i];
+    }
   }
 }
 
@@ -140,7 +146,7 @@ __global__ void __launch_bounds__(kWeighThreads)
           continue;
         const float2 m = p.ml[(int64_t)(s.first + row / g) * p.Hq + h * g + row % g];
         const float logit = (c[e] + c2[e]) * p.scale + be[e >> 1];
-        if (m.y > 0.f) sum[e >> 1] += exp2f((logit - m.x) * kLog2e) * m.y;
+        if (m.y != 0.f) sum[e >> 1] += exp2f((logit - m.x) * kLog2e) * m.y;
       }
     }
 #pragma unroll

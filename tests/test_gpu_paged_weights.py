@@ -6,7 +6,8 @@ import pytest
 import torch
 
 from paper_2606_07878_gb300 import still
-from test_gpu_paged import DEV, NAN, Pages, batch_of, ctx, fused_rows, i32  # noqa: F401
+from test_gpu_paged import (DEV, NAN, WEIGHTS, Pages, assert_rows, attention64, batch_of, ctx,  # noqa: F401
+                            fused_rows, i32)
 from test_gpu_paged_evict import OFF, scratch_of, slots, weights_of
 
 pytestmark = pytest.mark.gpu
@@ -35,3 +36,74 @@ def test_weights_of_very_long_sequences(ctx, g, page, n_slots):  # noqa: F811
         if j + step >= n_slots:
             want[-1] -= 2.0 ** -26  # the new token's own begins at 0
         assert ((got[j:j + step].double() - want).abs() <= OFF * want).all(), j
+
+
+def row_of_nan(q, kind):
+    q = q.clone()
+    q[..., 5] = NAN if kind == "nan" else math.inf
+    return q
+
+
+@pytest.mark.parametrize("kind", ["nan", "inf"])
+@pytest.mark.parametrize("d,new", [(64, 1), (128, 2), (256, 3), (64, 9), (128, 70)])
+def test_rows_of_nan(ctx, d, new, kind):  # noqa: F811
+    """What a row's weights are, slots that it sees become, whichever kernel adds them up: NaN, but 0
+    for those that are masked; other slots, KV-heads and sequences stay as they were."""
+    past = 100
+    p = Pages(73, [past + new, 70], 2, d, 16, beta=True)
+    masked = [3, 40, 64, past - 1]
+    for j in masked:
+        p.beta[int(p.table[0, j // 16]), :, j % 16] = -math.inf
+    q, = fused_rows(74, 2 * new, [4], d)
+    q = q.clone()
+    bad = (new - 1) // 2  # a token in the middle, a query head of KV-head 0
+    before = weights_of(p, 75)
+
+    def weigh(q):
+        w = before.clone()
+        still.still_paged_weigh(ctx, p.cache(), batch_of(p, [new] * 2), q, w, scratch_of(p, 2 * new, 4))
+        return w
+    clean = weigh(q)
+    q[bad, 1] = row_of_nan(q[bad, 1], kind)
+    w = weigh(q)
+    got, ref = slots(p, w, 0), slots(p, clean, 0)
+    seen = torch.arange(past + new, device=DEV) <= past + bad
+    seen[masked] = False
+    assert torch.isnan(got[seen, 0]).all()
+    # (the other rows' shares of an unseen or masked slot are what they were)
+    assert torch.equal(got[~seen, 0], ref[~seen, 0]) and torch.isfinite(ref).all()
+    assert torch.equal(got[:, 1], ref[:, 1]) and torch.equal(slots(p, w, 1), slots(p, clean, 1))
+
+
+@pytest.mark.parametrize("kind", ["nan", "inf"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("beta", [False, True])
+def test_rows_of_nan_beside_a_decode(ctx, d, beta, kind):  # noqa: F811
+    p = Pages(76, [300, 70], 2, d, 32, beta=beta)
+    masked = [3, 40, 64, 298] if beta else []
+    for j in masked:
+        p.beta[int(p.table[0, j // 32]), :, j % 32] = -math.inf
+    q, = fused_rows(77, 2, [6], d)
+    q = q.clone()
+    before = weights_of(p, 78)
+
+    def weigh(q):
+        w, out = before.clone(), torch.empty_like(q)
+        still.still_paged_decode_weigh(ctx, p.cache(), batch_of(p), q, out, w, scratch_of(p, 2, 6))
+        return w, out
+    clean, o0 = weigh(q)
+    q[0, 4] = row_of_nan(q[0, 4], kind)  # KV-head 1
+    w, o1 = weigh(q)
+    got, ref = slots(p, w, 0), slots(p, clean, 0)
+    seen = torch.ones(300, dtype=torch.bool, device=DEV)
+    seen[masked] = False
+    assert torch.isnan(got[seen, 1]).all() and torch.isnan(o1[0, 4]).all()
+    assert torch.equal(got[~seen, 1], ref[~seen, 1]) and torch.isfinite(ref).all()
+    assert torch.equal(got[:, 0], ref[:, 0]) and torch.equal(slots(p, w, 1), slots(p, clean, 1))
+    assert torch.equal(o0[0, :3], o1[0, :3]) and torch.equal(o0[1], o1[1])
+    # (the other rows of the group are formed again with weights in bf16, for the infinite values
+    # that a NaN may come from)
+    q[0, 4] = 0
+    ref, size = attention64(p, q, [1, 1])
+    for i in (3, 5):
+        assert_rows(o1[0, i], ref[0, i], size[0, i], WEIGHTS)
