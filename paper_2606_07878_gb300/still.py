@@ -134,6 +134,8 @@ def lib():
         P, I32, I64, D = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double
         PI64, PD, PI32 = ctypes.POINTER(I64), ctypes.POINTER(D), ctypes.POINTER(I32)
         PSEG = ctypes.POINTER(PosSegment)
+        # (typed: a cache in 8 bits is no cache in 16, nor the other way round)
+        PC16, PC8, PB = (ctypes.POINTER(x) for x in (_PagedCache, _PagedCacheQuant, _PagedBatch))
         sig = {
             "still_create": ([ctypes.c_int, ctypes.POINTER(P)], ctypes.c_int),
             "still_destroy": ([P], ctypes.c_int),
@@ -189,23 +191,23 @@ def lib():
                                            ctypes.POINTER(P), I64, ctypes.POINTER(P),
                                            ctypes.POINTER(P), I64, I32, I32, ctypes.c_float,
                                            ctypes.POINTER(P), P], ctypes.c_int),
-            "still_paged_append": ([P, P, P, I32, P, I64, P, I64, P, I64, I32, P, D, P, P],
+            "still_paged_append": ([P, PC16, PB, I32, P, I64, P, I64, P, I64, I32, P, D, P, P],
                                    ctypes.c_int),
-            "still_paged_decode": ([P, P, P, P, I64, I32, ctypes.c_float, P, P], ctypes.c_int),
-            "still_paged_prefill": ([P, P, P, I32, P, I64, I32, ctypes.c_float, P, P],
+            "still_paged_decode": ([P, PC16, PB, P, I64, I32, ctypes.c_float, P, P], ctypes.c_int),
+            "still_paged_prefill": ([P, PC16, PB, I32, P, I64, I32, ctypes.c_float, P, P],
                                     ctypes.c_int),
-            "still_paged_append_quant": ([P, P, P, I32, P, I64, P, I64, P, I64, I32, P, D, P, P],
+            "still_paged_append_quant": ([P, PC8, PB, I32, P, I64, P, I64, P, I64, I32, P, D, P, P],
                                          ctypes.c_int),
-            "still_paged_decode_quant": ([P, P, P, P, I64, I32, ctypes.c_float, P, P],
+            "still_paged_decode_quant": ([P, PC8, PB, P, I64, I32, ctypes.c_float, P, P],
                                          ctypes.c_int),
-            "still_paged_prefill_quant": ([P, P, P, I32, P, I64, I32, ctypes.c_float, P, P],
+            "still_paged_prefill_quant": ([P, PC8, PB, I32, P, I64, I32, ctypes.c_float, P, P],
                                           ctypes.c_int),
-            "still_paged_weigh_scratch": ([P, I32, I32], I64),
-            "still_paged_decode_weigh": ([P, P, P, P, I64, I32, ctypes.c_float, P, P,
+            "still_paged_weigh_scratch": ([PC16, I32, I32], I64),
+            "still_paged_decode_weigh": ([P, PC16, PB, P, I64, I32, ctypes.c_float, P, P,
                                           ctypes.c_float, P, I64, P], ctypes.c_int),
-            "still_paged_weigh": ([P, P, P, I32, P, I64, I32, ctypes.c_float, P, ctypes.c_float,
+            "still_paged_weigh": ([P, PC16, PB, I32, P, I64, I32, ctypes.c_float, P, ctypes.c_float,
                                    P, I64, P], ctypes.c_int),
-            "still_paged_evict": ([P, P, P, P, I32, I32, I32, P, P, I64, I32, P, P, P, P, P],
+            "still_paged_evict": ([P, PC16, PB, P, I32, I32, I32, PC16, P, I64, I32, P, P, P, P, P],
                                   ctypes.c_int),
             "still_lookahead_pass_info": ([I64, I64, I32, ctypes.POINTER(LookaheadPass)],
                                           ctypes.c_int),
