@@ -366,9 +366,10 @@ typedef struct {
  * power of two by which the call's new rows of the block stay within 448, the largest code, or the
  * scale it has already, if that is larger and slots of the sequence lie in the block before the new
  * ones; their codes are brought to the new scale (exact but where they become subnormal). A value is
- * off by at most 2^-4 of itself or 2^-18 of its block's largest, whichever is more, once, and older
- * ones of a block by half a code step more where the scale grew. NaN stays NaN; an infinity becomes
- * the largest code of the block.
+ * off by at most 2^-4 of itself or 2^-10 of the scale, whichever is more (2^-10 of a scale that is
+ * above its minimum, 2^-126, and was not inherited is less than 2^-17 of the block's largest value),
+ * and older ones of a block by 2^-10 of the new scale more where it grew. NaN stays NaN; an infinity
+ * becomes the largest code of the block.
  * No two sequences of a call may have new tokens in one block. Scales need no initial values. */
 still_status still_paged_append_quant(still_ctx* ctx, const still_paged_cache_quant* cache,
                                       const still_paged_batch* batch, int32_t n, const void* k,

@@ -14,9 +14,9 @@ namespace {
 // block of 16 slots then takes the smallest power of two s with max |x| <= 448 s over its new rows,
 // or the scale that it has already where that is larger and the block is partly filled; its codes
 // are x / s, rounded to nearest even. Powers of two cost no precision (e4m3 has the same 4 bits at
-// any size; the block's largest value is at least 224 s, so only what lies 2^14 below it meets the
-// subnormal codes) and let a block change its scale without rounding its older codes again, but for
-// those that become subnormal.
+// any size; the block's largest value is above 224 s, so only what lies 2^13.8 below it meets the
+// subnormal codes, off by 2^-10 s at most) and let a block change its scale without rounding its
+// older codes again, but for those that become subnormal.
 //
 // A warp takes the K or the V rows of a block and KV-head, at most 16 of them: it holds them in
 // registers between their maximum and their codes. The first token of a block (or of a sequence's

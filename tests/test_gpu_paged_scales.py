@@ -89,3 +89,34 @@ def test_keys_whose_logits_are_large(ctx, d):  # noqa: F811
     p.read()
     q, = fused_rows(68, 1, [4], d)
     assert_rows(decode(ctx, p, q), *attention64(p, q, [1]), FEW)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_what_a_code_is_off_by(ctx, d):  # noqa: F811
+    """2^-4 of a value or 2^-10 of the scale, whichever is more, and 2^-10 of the new scale more where
+    a block's scale grew: both are met by what lies halfway between two subnormal codes."""
+    p = QuantPages(69, [0], 1, d, 16, spare=40)
+    p.table = torch.arange(40, dtype=torch.int32, device=DEV)[None]
+    g = torch.Generator(device=DEV).manual_seed(70)
+    n = 40 * 16 - 1  # the last block is filled up behind it
+    x = torch.randn(n + 1, 1, d, generator=g, device=DEV)
+    x *= torch.exp2(20 * torch.rand(n + 1, 1, d, generator=g, device=DEV) - 20)
+    x[::16, :, 0], x[::16, :, 1] = 225.0, 2.0 ** -10  # 225 is 1 as a scale, 2^-10 half a step
+    x[n] = 0
+    x[n, :, 0] = 900.0  # 4
+    x = x.bfloat16()
+    half = torch.maximum(2.0 ** -4 * x.double().abs(), torch.tensor(2.0 ** -10))
+
+    def append(lo, hi):
+        p.lens = [hi]
+        still.still_paged_append_quant(ctx, p.cache(), batch_of(p, [hi - lo]), x[lo:hi], x[lo:hi])
+        p.read()
+        return [(p.rows(y, 0) - x[:hi].double()).abs() for y in (p.K, p.V)]
+    for off in append(0, n):
+        assert (off <= half[:n]).all() and (off[::16, :, 1] == 2.0 ** -10).all()
+    assert (p.scales[0] == 1).all() and (p.scales[1] == 1).all()
+    last = slice(n - 15, n)
+    for scales, off in zip(p.scales, append(n, n + 1)):
+        assert scales[-1] == 4 and (scales[:-1] == 1).all()
+        assert (off[:n - 15] <= half[:n - 15]).all() and (off[n] == 900 - 896).any()
+        assert (off[last] <= half[last] + 2.0 ** -8).all() and (off[last] > half[last]).any()
