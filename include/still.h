@@ -333,10 +333,11 @@ still_status still_paged_append(still_ctx* ctx, const still_paged_cache* cache,
  * out must not overlap q or the pools. Device-side argument faults are recorded as by
  * still_paged_append; rows that would read a page outside the pool come out as anything, those of
  * tokens that no sequence owns stay as they were.
- * Partial results lie in a workspace of these two calls alone (41 MB on 152 SMs). The context's
- * first call of either allocates it for every size, so that call belongs before a capture; it stays
- * where it is until still_destroy, so that captured calls stay valid whatever else the context is
- * used for. Calls that share a context must be ordered on one stream or otherwise serialised. */
+ * Partial results lie in a workspace (41 MB on 152 SMs) of these two calls and those below that
+ * attend or weigh: still_paged_decode_quant, still_paged_prefill_quant, still_paged_decode_weigh and
+ * still_paged_weigh. The context's first call of any of them allocates it for every size and all of
+ * them, so that call belongs before a capture; it stays where it is until still_destroy, so that
+ * captured calls stay valid whatever else the context is used for. Calls that share a context must be ordered on one stream or otherwise serialised. */
 still_status still_paged_decode(still_ctx* ctx, const still_paged_cache* cache,
                                 const still_paged_batch* batch, const void* q, int64_t q_stride,
                                 int32_t Hq, float scale, void* out, void* stream);
@@ -381,8 +382,9 @@ still_status still_paged_append_quant(still_ctx* ctx, const still_paged_cache_qu
  * status as there. Scales of blocks that hold a visible slot are positive and finite; what the
  * others hold does not matter, and neither do the codes of masked slots. Queries and weights are
  * not held in 8 bits. Where a call has few rows (still_paged_decode; without cu_new up to twice as
- * many) logits are sums in fp32 of exact products, and weights enter the product with V with an error
- * below 2^-21 of the largest of their row times its block's scale. In every other call with at most
+ * many) logits are sums in fp32 of exact products, and weights enter the product with V so that each,
+ * times its block's scale, is off by less than 2^-21 of the row's largest such product; weights below
+ * 2^-126 of the row's largest may count as 0. In every other call with at most
  * 128 query heads to a KV-head weights enter it as bf16 (2^-8), and so do values, exact where scales
  * are powers of two and rounded otherwise. */
 still_status still_paged_decode_quant(still_ctx* ctx, const still_paged_cache_quant* cache,
@@ -408,11 +410,15 @@ still_status still_paged_prefill_quant(still_ctx* ctx, const still_paged_cache_q
  * every token of a sequence has been weighed when it was new. decay in [0, 1]; with 0 nothing of the
  * old weight remains, whatever it was: the call's tokens alone count (an observation window at the
  * end of a prompt). A sequence without new tokens in the call, or a token that sees nothing, changes
- * nothing but by the decay of sequences that have new tokens.
+ * nothing but by the decay of sequences that have new tokens. A row that is NaN, or has an infinite
+ * logit, makes the slots that it sees NaN; masked ones get 0 from every row.
  * The sums are fp32 of logits that are fp32 sums of exact products; they do not depend on the order
  * in which blocks run.
- *   scratch  still_paged_weigh_scratch bytes of device memory (16-byte aligned) for as long as the
- *            call runs, too few: STILL_ERR_SHAPE. Calls that may run at once need their own.
+ *   scratch  device memory (16-byte aligned) for as long as the call runs, too little:
+ *            STILL_ERR_SHAPE. still_paged_decode_weigh needs still_paged_weigh_scratch bytes, which
+ *            hold the logits, 4 Hq bytes for every slot of the pool; still_paged_weigh alone what
+ *            lies before them, 8 n Hq rounded up to a multiple of 256. Calls that may run at once
+ *            need their own.
  * No two sequences of a call may share a page: their weights would be written at once.
  * still_paged_decode_weigh: still_paged_decode, and the weights beside it, at the cost of the
  * logits' way through memory. still_paged_weigh: the weights alone, any number of tokens, causal

@@ -602,7 +602,8 @@ def still_paged_prefill_quant(ctx, cache, batch, q, out, scale=0.0, stream=None)
 
 
 def still_paged_weigh_scratch(cache, n, Hq):
-    """Bytes of scratch for still_paged_decode_weigh and still_paged_weigh with n new tokens."""
+    """Bytes of scratch for still_paged_decode_weigh and still_paged_weigh with n new tokens; the
+    latter alone needs 8 n Hq of them, rounded up to a multiple of 256."""
     return lib().still_paged_weigh_scratch(cache.ref, n, Hq)
 
 
@@ -628,7 +629,7 @@ def still_paged_decode_weigh(ctx, cache, batch, q, out, weight, scratch, decay=1
 
 def still_paged_weigh(ctx, cache, batch, q, weight, scratch, decay=1.0, scale=0.0, stream=None):
     """Weights of the packed new tokens q [n, Hq, d] (heads contiguous, any token pitch); weight
-    and scratch as still_paged_decode_weigh's."""
+    as still_paged_decode_weigh's, of its scratch 8 n Hq bytes, rounded up to a multiple of 256."""
     n, Hq, d = q.shape
     qp, qs = _rows(q, Hq, cache.struct.head_dim)
     assert weight is not None

@@ -107,3 +107,33 @@ def test_rows_of_nan_beside_a_decode(ctx, d, beta, kind):  # noqa: F811
     ref, size = attention64(p, q, [1, 1])
     for i in (3, 5):
         assert_rows(o1[0, i], ref[0, i], size[0, i], WEIGHTS)
+
+
+@pytest.mark.parametrize("d,new", [(64, 1), (128, 2), (64, 40), (256, 70)])
+def test_scratch_of_weights_alone(ctx, d, new):  # noqa: F811
+    """still_paged_weigh needs 8 bytes for every token and query head, rounded up to 256, and uses no
+    more; a decode needs what still_paged_weigh_scratch gives."""
+    p = Pages(79, [new + 90, new], 2, d, 16)
+    Hq = 6
+    q, = fused_rows(80, 2 * new, [Hq], d)
+    before = weights_of(p, 81)
+    least = -(-2 * new * Hq * 8 // 256) * 256
+    pool = p.K.shape[0] * 16 * Hq * 4
+    assert still.still_paged_weigh_scratch(p.cache(), 2 * new, Hq) == least + pool
+
+    def weigh(scratch):
+        w = before.clone()
+        still.still_paged_weigh(ctx, p.cache(), batch_of(p, [new] * 2), q, w, scratch)
+        return w
+    scratch = torch.full((least + 4096,), 0x5a, dtype=torch.uint8, device=DEV)
+    w = weigh(scratch[:least])
+    assert (scratch[least:] == 0x5a).all()
+    assert torch.equal(w.view(torch.int32), weigh(scratch_of(p, 2 * new, Hq)).view(torch.int32))
+    for size in (0, least - 1):
+        with pytest.raises(still.StillError, match="SHAPE|INVALID_ARG"):
+            weigh(scratch[:size])
+    one = q[:2].contiguous()
+    small = torch.empty(255 + pool, dtype=torch.uint8, device=DEV)
+    with pytest.raises(still.StillError, match="SHAPE"):
+        still.still_paged_decode_weigh(ctx, p.cache(), batch_of(p), one, torch.empty_like(one),
+                                       before.clone(), small)
