@@ -10,7 +10,7 @@
 // The second one moves: 16 bytes a thread, rows of K and V.
 //
 // 131,072 slots of 8 KV-heads of 128 channels to 16,384 take 49 us, 24 to choose and 22 to move
-// (134 MB, 6.2 TB/s); 32 sequences of 700 to 1,500 slots of 2 heads to 164 take 14. What is left of
+// (134 MB, 6.2 TB/s); 32 sequences of 700 to 1,500 slots of 2 heads to 164 take 13 to 15. What is left of
 // the choice is latency: the reads of pages and weights (4.8 us; 16 slots a thread, four reads on
 // their way; one slot at a time took 40 us for the choice) and three rounds of histograms (count,
 // wait for the cluster, read eight histograms, 3 to 4 us each). Sums over warps and CTAs by a lane

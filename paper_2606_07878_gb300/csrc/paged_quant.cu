@@ -23,7 +23,8 @@ namespace {
 // new tokens) leads it; a CTA looks at a window of tokens for leaders. Other CTAs rotate queries.
 //
 // Memory and the latency of its reads bound it: 8,192 tokens of 32 query and 8 KV-heads of 128
-// channels are 185 MB, 43 us (4.3 TB/s). One grid for both, a window's queries before its keys and
+// channels are 185 MB, 43 us (4.3 TB/s); 16 query and 8 KV-heads of 256 channels 235 MB, 64 us (3.7).
+// Three CTAs an SM (256 channels: two) cost 44 (108) bytes of spills a thread. One grid for both, a window's queries before its keys and
 // values, took 57; keys and values behind the queries 49 (a CTA of theirs takes longer: the grid's
 // end waits for it).
 constexpr int kQuantThreads = 256;

@@ -40,10 +40,12 @@ namespace {
 //
 // In 8 bits 16 slots are half the bytes for the same instructions and more: codes become fp16 (two
 // an instruction), weights fp16 hi + lo of weight x scale / rho, a number that follows the row's
-// largest. The 24 sequences take 129 us (0.5 GB, 4.1 TB/s). They took 145 where a warp issued 545
-// instructions a batch, 250 of them in the integer and conversion pipe, with an address product for
-// every row, a division and two exponentials more; 153 with two batches on their way at a time, 132
-// with a fourth CTA on an SM (both spill).
+// largest. The 24 sequences take 130 us (0.5 GB, 3.9 TB/s; one of 131,072 slots with 256 channels
+// 130, 4.1): memory is busy 50% and issue slots 44%, and what bounds it is latency, as a warp has one
+// batch on its way, 4 KB in 8 bits, so that an SM has half of what it has in bf16. They took 145
+// where a warp issued 545 instructions a batch, 250 of them in the integer and conversion pipe, with
+// an address product for every row, a division and two exponentials more; 153 with two batches on
+// their way at a time, 132 with a fourth CTA on an SM (both spill).
 //
 // Memory bounds the large calls: the 24 sequences are 1.0 GB, 5.95 TB/s and 0.88 of a copy, with
 // the mma.sync pipe at 12%, so the tensor cores of tcgen05 would have nothing to gain. Small calls

@@ -23,7 +23,7 @@ STILL_DEV float weighed_before(const float* at, bool old, float decay) {
 // The second pass of a decode: the first one (paged_rows.cuh) leaves the logits, 4 bytes a row and
 // slot beside 4 d of K and V, so that K is not read again. A thread takes four slots of a page:
 // what it costs is one dependent read after another (lengths, page, logits). 9 us for 8 sequences of
-// 5,000 to 9,001 slots with 4 x 8 heads, 13 with a slot a thread (the call 53.8 and 57.8).
+// 5,000 to 9,001 slots with 4 x 8 heads, 13 with a slot a thread (the call 54 to 56, and 58).
 constexpr int kWeighSlots = 4;
 __global__ void __launch_bounds__(kWeighThreads)
     paged_weigh_logits_kernel(const __grid_constant__ PagedArgs a, const float* logits,
