@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
   const Seq s = paged_seq(a, b);
   const int count = min(s.len, f.keep);
   int32_t* kept = f.kept + ((int64_t)b * a.H + h) * f.keep;
-  for (int r = count + (int)rank * kChooseThreads + threadIdx.x; r < f.keep;
+  for (int64_t r = (int64_t)count + rank * kChooseThreads + threadIdx.x; r < f.keep;
        r += kCluster * kChooseThreads)
     kept[r] = -1;
   if (h == 0 && rank == 0 && threadIdx.x == 0) {
@@ -79,17 +79,19 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
       f.to_offset[b] = (a.pos_offset != nullptr ? a.pos_offset[b] : 0) + s.len - count;
   }
   if (s.len <= f.keep) {  // (of the whole cluster)
-    for (int r = (int)rank * kChooseThreads + threadIdx.x; r < count;
+    for (int64_t r = rank * kChooseThreads + threadIdx.x; r < count;
          r += kCluster * kChooseThreads)
-      kept[r] = r;
+      kept[r] = (int)r;
     return;
   }
   const int32_t* table = a.table + (int64_t)b * a.s_table;
-  // slots [j0, j1) of this CTA
-  const int per = ((s.len + kCluster - 1) / kCluster + 31) & ~31;
-  const int j0 = min(s.len, (int)rank * per), j1 = min(s.len, j0 + per);
+  // slots [j0, j1) of this CTA (unsigned, as loops step past an end that may be 2^31 - 256)
+  using Slot = uint32_t;
+  const Slot len = s.len;
+  const Slot per = ((len + kCluster - 1) / kCluster + 31) & ~31u;
+  const Slot j0 = min(len, rank * per), j1 = min(len, j0 + per);
   // Keys of four slots from j (a multiple of 4) on: they lie in one page.
-  auto read = [&](int j) {
+  auto read = [&](Slot j) {
     uint32_t k[4] = {0, 0, 0, 0};
     const int pg = paged_page(a, table, j);
     const float* at = f.weight + ((((int64_t)max(pg, 0) * a.H + h) << a.page_shift) +
@@ -97,14 +99,14 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if (j + e >= j1) continue;
-      const bool stays = j + e < f.sinks || j + e >= s.len - f.recent;
+      const bool stays = j + e < (Slot)f.sinks || j + e >= len - f.recent;
       k[e] = stays ? 0xffffffffu : pg < 0 ? 0 : key_of(at[e]);
     }
     return make_uint4(k[0], k[1], k[2], k[3]);
   };
-  const bool held = j1 - j0 <= in_smem;
+  const bool held = j1 - j0 <= (Slot)in_smem;
   uint4* const keys4 = reinterpret_cast<uint4*>(keys);
-  auto four = [&](int j) { return held ? keys4[(j - j0) / 4] : read(j); };
+  auto four = [&](Slot j) { return held ? keys4[(j - j0) / 4] : read(j); };
   for (int i = threadIdx.x; i < kDigits; i += kChooseThreads) hist[0][i] = 0;
   __syncthreads();
   uint32_t prefix = 0;       // the digits found so far, in place
@@ -115,7 +117,7 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
     const uint32_t digits = step == 2 ? 1024 : 2048;
     const uint32_t above = step == 0 ? 0u : ~0u << (step == 1 ? 21 : 10);
     uint32_t* const mine = hist[step & 1];
-    auto count = [&](int j, const uint4& k) {
+    auto count = [&](Slot j, const uint4& k) {
       const uint32_t x[4] = {k.x, k.y, k.z, k.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -124,23 +126,23 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
     };
     if (step == 0) {  // several reads on their way at a time: page, weight
       constexpr int kAtOnce = 4;
-      for (int j = j0 + 4 * threadIdx.x; j < j1; j += 4 * kAtOnce * kChooseThreads) {
+      for (Slot j = j0 + 4 * threadIdx.x; j < j1; j += 4 * kAtOnce * kChooseThreads) {
         uint4 k[kAtOnce];
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
-          const int x = j + 4 * i * kChooseThreads;
+          const Slot x = j + 4 * i * kChooseThreads;
           if (x < j1) k[i] = read(x);
         }
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
-          const int x = j + 4 * i * kChooseThreads;
+          const Slot x = j + 4 * i * kChooseThreads;
           if (x >= j1) break;
           if (held) keys4[(x - j0) / 4] = k[i];
           count(x, k[i]);
         }
       }
     } else {
-      for (int j = j0 + 4 * threadIdx.x; j < j1; j += 4 * kChooseThreads) count(j, four(j));
+      for (Slot j = j0 + 4 * threadIdx.x; j < j1; j += 4 * kChooseThreads) count(j, four(j));
     }
     if constexpr (kCluster > 1)
       cluster_sync();
@@ -185,9 +187,9 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
   }
   // ---- the kept slots, in order: keys above `prefix`, and the first `need` that equal it
   // (counts of both in one word, 16 bits each: a warp has 128 slots at a time)
-  const int each = ((j1 - j0 + kChooseWarps - 1) / kChooseWarps + 127) & ~127;
-  const int w0 = min(j1, j0 + warp * each), w1 = min(j1, w0 + each);
-  auto tally = [&](int j, const uint4& k) {
+  const Slot each = ((j1 - j0 + kChooseWarps - 1) / kChooseWarps + 127) & ~127u;
+  const Slot w0 = min(j1, j0 + warp * each), w1 = min(j1, w0 + each);
+  auto tally = [&](Slot j, const uint4& k) {
     uint32_t n = 0;
     const uint32_t x[4] = {k.x, k.y, k.z, k.w};
 #pragma unroll
@@ -196,7 +198,7 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
     return n;
   };
   uint32_t more = 0, equal = 0;
-  for (int j = w0 + 4 * lane; j < w1; j += 128) {
+  for (Slot j = w0 + 4 * lane; j < w1; j += 128) {
     const uint32_t n = tally(j, four(j));
     more += n & 0xffffu;
     equal += n >> 16;
@@ -226,8 +228,8 @@ __global__ void __launch_bounds__(kChooseThreads, 1)
     ctas = ld_cluster_u32x2(cluster_map(smem_u32(counts), lane));
   more = __reduce_add_sync(0xffffffffu, ctas.x) + sum_before(warp_sum, warp);
   equal = __reduce_add_sync(0xffffffffu, ctas.y) + sum_before(warp_equal, warp);
-  for (int j0w = w0; j0w < w1; j0w += 128) {
-    const int j = j0w + 4 * lane;
+  for (Slot j0w = w0; j0w < w1; j0w += 128) {
+    const Slot j = j0w + 4 * lane;
     const uint4 k = j < w1 ? four(j) : make_uint4(0, 0, 0, 0);
     const uint32_t n = tally(j, k);
     uint32_t upto = n;
