@@ -383,10 +383,10 @@ still_status still_paged_append_quant(still_ctx* ctx, const still_paged_cache_qu
  * others hold does not matter, and neither do the codes of masked slots. Queries and weights are
  * not held in 8 bits. Where a call has few rows (still_paged_decode; without cu_new up to twice as
  * many) logits are sums in fp32 of exact products, and weights enter the product with V so that each,
- * times its block's scale, is off by less than 2^-21 of the row's largest such product; weights below
- * 2^-126 of the row's largest may count as 0. In every other call with at most
- * 128 query heads to a KV-head weights enter it as bf16 (2^-8), and so do values, exact where scales
- * are powers of two and rounded otherwise. */
+ * times its block's scale, is off by less than 2^-21 of the row's largest such product. In every
+ * other call with at most 128 query heads to a KV-head weights enter it as bf16 (2^-8), and so do
+ * values, exact where scales are powers of two and rounded otherwise. In either, weights below 2^-126
+ * of their row's largest may count as 0. */
 still_status still_paged_decode_quant(still_ctx* ctx, const still_paged_cache_quant* cache,
                                       const still_paged_batch* batch, const void* q,
                                       int64_t q_stride, int32_t Hq, float scale, void* out,
