@@ -1,7 +1,5 @@
 """The paged cache in 8 bits where its scales are far apart: values before and behind a maximum that
 jumps, blocks of zeros."""
-import math
-
 import pytest
 import torch
 
